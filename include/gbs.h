@@ -318,6 +318,135 @@ int gbs_quantized_matmul(const gbs_plan_t* plan_x, const void* codes_x, const fl
                          void* out, int out_dtype, int64_t out_row_stride, void* cuda_stream);
 
 /*
+ * ------------------------------------------------------------------------------------------------------------------
+ * Paged KV cache in four bits, and attention over it (Section 5: the cache holds rotated, quantized rows; Section 2.3.1: a
+ * rotation that both sides of a product share leaves it unchanged, so keys and values stay rotated and only the query and
+ * the result are turned).  The paper has no counterpart of the paging.
+ *
+ * Plans: bits 4, d' = 128 (m = 1), group 0 or 128, d a multiple of 8, symmetric or asymmetric; other plans return
+ * GBS_ERR_UNSUPPORTED.  d is the width of a head; narrower heads are zero-padded to 128 coordinates (Section 4.2).
+ *
+ * Pool: `pages` holds n_pages pages of gbs_kv_page_bytes bytes.  A page holds, for each KV head in turn, a block of
+ * page_size tokens: key codes [page_size][64 bytes], value codes [page_size][64 bytes], key scales and value scales
+ * [page_size] floats each (Delta), or [page_size][2] for an asymmetric plan (Delta, lo).  Codes are packed as everywhere.
+ * page_table [n_seqs][max_pages] lists the pages of each sequence in order; only the first ceil(lengths[s] / page_size) entries
+ * of a row are read, the others are left as they are.  lengths [n_seqs]: tokens of each sequence.  refs [n_pages]: how many
+ * sequences hold a page; 0 = free.  A page that is not full belongs to one sequence alone.  A new pool has lengths
+ * and refs 0; no other preparation is needed.  All five arrays are device memory and belong to the caller.
+ *
+ * A call's items are sequences: item i is sequence seqs[i], or i where seqs is NULL (device int32).  Its tokens are rows
+ * cu_tokens[i] .. cu_tokens[i + 1] - 1 of the call's row tensors (device int32, n_items + 1 values that do not fall, from 0), or row i
+ * alone where cu_tokens is NULL.  They are the LAST tokens of the sequence as lengths[] has it: a step extends the
+ * sequences first, then appends and attends.  Rows behind cu_tokens[n_items] are neither read nor written.
+ * Numbers that only the device knows are checked there: an item whose sequence is out of range, a token whose position is
+ * below 0 or whose page is not one of the pool's is left out (a row that would be written from it becomes 0).
+ *
+ * Calls are enqueued on `cuda_stream` and may be captured.  Calls that change a pool and calls that use it have to be ordered
+ * by the caller, as any use of one buffer from two streams.
+ */
+#define GBS_KV_MAX_ITEMS 8192
+
+typedef struct gbs_kv_cache {
+    void* pages;            /* 16-byte aligned */
+    int64_t n_pages;        /* 1 .. 2^31 - 1 */
+    int n_kv_heads;         /* 1 .. 1024 */
+    int page_size;          /* 16, 32, 64 or 128 tokens */
+    int32_t* page_table;
+    int32_t* lengths;
+    int32_t* refs;
+    int n_seqs, max_pages;  /* n_seqs * max_pages entries; max_pages * page_size < 2^31 */
+} gbs_kv_cache_t;
+
+/* what became of an item of gbs_kv_extend and gbs_kv_fork (device int32) */
+#define GBS_KV_DONE 0
+#define GBS_KV_BAD_INDEX 1    /* a sequence out of range, or a negative count */
+#define GBS_KV_NOT_EMPTY 2    /* the target of a fork holds tokens */
+#define GBS_KV_NO_PAGES 3     /* not enough free pages for this item and those before it */
+#define GBS_KV_TOO_LONG 4     /* the sequence would not fit its row of the table */
+#define GBS_KV_DUPLICATE 5    /* an earlier item of the call names the same sequence (the same target) */
+
+/* Bytes of one page: n_kv_heads * page_size * (128 + 8 * scale floats of a row).  Host only. */
+int gbs_kv_page_bytes(const gbs_plan_t* plan, int n_kv_heads, int page_size, int64_t* out);
+
+/*
+ * Room for counts[i] more tokens in sequence seqs[i]: lengths grow, and free pages enter the table, the lowest free ones first,
+ * to the items in their order.  An item that is refused (status_out[i] != GBS_KV_DONE) changes nothing; from the first one that the
+ * free pages do not suffice for, every item that needs a page is refused.
+ *   seqs, counts   device int32 [n_items], n_items 0 .. GBS_KV_MAX_ITEMS; seqs NULL: sequence i; counts NULL: one token each
+ *   status_out     device int32 [n_items]
+ */
+int gbs_kv_extend(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* counts, int n_items,
+                  int32_t* status_out, void* cuda_stream);
+
+/*
+ * Sequence dst[i], which has to be empty, becomes a copy of sequence src[i]: full pages are shared (refs + 1), the tokens of a last
+ * page that is not full are copied into a page of its own, taken as by gbs_kv_extend.  All pairs see the
+ * sequences as they were before the call; one source may have any number of targets.
+ *   src, dst, status_out   device int32 [n_items], n_items 0 .. GBS_KV_MAX_ITEMS
+ */
+int gbs_kv_fork(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* src, const int32_t* dst, int n_items,
+                int32_t* status_out, void* cuda_stream);
+
+/*
+ * The sequences end: their lengths become 0, refs of their pages fall by 1, and pages at 0 are free.  A sequence out of range
+ * is left out; one that is named twice ends once.  Page contents and table entries stay.
+ */
+int gbs_kv_free(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, int n_items, void* cuda_stream);
+
+/*
+ * Move the pages in use (refs > 0) of `cache` into pages 0, 1, .. of `into`, in the order of their numbers, and write `into`'s table
+ * (entries behind a sequence's last page become -1), lengths and refs.  `into` is another pool of the same n_kv_heads,
+ * page_size, n_seqs and max_pages with any number of pages, none of its arrays shared with `cache`; what it held is lost.
+ *   page_map    device int32 [cache->n_pages], receives each page's new number, -1 for a free one
+ *   n_live      device int32, receives the number of pages in use.  If it exceeds into->n_pages, the pages beyond that are not
+ *               moved and stand as -1 in page_map and in the table: such an `into` is not to be used.
+ */
+int gbs_kv_compact(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const gbs_kv_cache_t* into, int32_t* page_map,
+                   int32_t* n_live, void* cuda_stream);
+
+/*
+ * gbs_rotate_quantize of key and value rows, written into the pages of their tokens.
+ *   k, v              device bf16 [n_tokens][n_kv_heads][d], rows 16-byte aligned: token t, head h starts at element
+ *                     t * token_stride + h * head_stride, strides multiples of 8 (k and v have the same)
+ *   n_tokens          rows that k and v hold; cu_tokens NULL: n_tokens = n_items
+ */
+int gbs_kv_append(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                  int64_t n_tokens, const void* k, const void* v, int64_t token_stride, int64_t head_stride, void* cuda_stream);
+
+/*
+ * The rows that the cache stands for, back in their own basis: gbs_dequantize with GBS_INVERSE_ROTATE of the items' tokens.
+ *   k_out, v_out      device bf16 [n_tokens][n_kv_heads][d], contiguous, 16-byte aligned
+ */
+int gbs_kv_read(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                int64_t n_tokens, void* k_out, void* v_out, void* cuda_stream);
+
+/* gbs_kv_attention flags */
+#define GBS_KV_CAUSAL 1       /* a token sees the cache up to its own position; without it, all of its sequence */
+
+/*
+ * Attention of the items' query tokens over the cache: with khat, vhat the rows that the cache stands for,
+ *     out[t][h] = sum_j p_j vhat_j,   p = softmax over the visible j of (scale * q[t][h] . khat_j),
+ * KV head h / (n_heads / n_kv_heads) serving query head h.  Token t at position p of its sequence sees positions j <= p (causal) and,
+ * with window > 0, j > p - window.  A row that sees nothing becomes 0.
+ *   q, out            device bf16, [n_tokens][n_heads][d] with strides in elements as in gbs_kv_append; out's own strides
+ *   n_heads           a multiple of n_kv_heads, at most 1024 query heads per KV head
+ *   max_tokens        no item has more tokens (1 where cu_tokens is NULL); an item's tokens beyond it become 0
+ *   max_len           no sequence of the call is longer (0: the table's width); one that is longer is read up to max_len only.
+ *                     It bounds how far the work is split, not what is read.
+ *   scale             0: 1 / sqrt(d)
+ *   workspace         device, gbs_kv_attention_workspace bytes, 16-byte aligned; overwritten, needs no preparation, and one call at
+ *                     a time may use it
+ * Query rows are rounded to 22 bits of their largest coordinate (up to 16 rows a KV head and item) or 11 (more rows), probabilities
+ * to 16 or 11 bits of themselves; sums and softmax statistics are fp32.
+ */
+int gbs_kv_attention_workspace(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, int n_heads, int64_t n_tokens, int max_tokens,
+                               int64_t* bytes_out);
+int gbs_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                     int64_t n_tokens, int max_tokens, int max_len, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                     int n_heads, float scale, int window, int flags, void* out, int64_t out_token_stride, int64_t out_head_stride,
+                     void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/*
  * State of one projection's search (Algorithm 1), a handful of numbers: plain data that may be copied, stored
  * and handed back later to resume the search where it stopped (gbs_search_state_init gives the algorithm's
  * start a = 0, b = 1, m = 1/2).

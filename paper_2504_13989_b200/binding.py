@@ -31,11 +31,16 @@ GBS_MAX_D_PAD = 32768
 GBS_MAX_CANDIDATES = 64
 
 GBS_PLAN_ASYMMETRIC = 1
+
+GBS_KV_MAX_ITEMS = 8192
+GBS_KV_CAUSAL = 1
+GBS_KV_DONE, GBS_KV_BAD_INDEX, GBS_KV_NOT_EMPTY, GBS_KV_NO_PAGES, GBS_KV_TOO_LONG, GBS_KV_DUPLICATE = range(6)
 EXPORTS = ("gbs_plan_create", "gbs_plan_create_ex", "gbs_plan_destroy", "gbs_plan_info", "gbs_plan_device_status", "gbs_rotate_quantize",
            "gbs_rotate_quantize_static", "gbs_static_device_status", "gbs_dequantize", "gbs_clip_error",
            "gbs_search_clip_ratio", "gbs_search_state_init", "gbs_search_clip_ratio_fn", "gbs_search_clip_ratio_batch",
            "gbs_hadamard_m", "gbs_status_string", "gbs_selftest_wait_expiry", "gbs_weight_rotate_quantize",
-           "gbs_quantized_matmul")
+           "gbs_quantized_matmul", "gbs_kv_page_bytes", "gbs_kv_extend", "gbs_kv_fork", "gbs_kv_free", "gbs_kv_compact",
+           "gbs_kv_append", "gbs_kv_read", "gbs_kv_attention_workspace", "gbs_kv_attention")
 GBS_STATIC_MAX_D_PAD = 4096
 
 
@@ -69,6 +74,13 @@ class SearchState(ctypes.Structure):
 class SearchTask(ctypes.Structure):
     _fields_ = [("plan", ctypes.c_void_p), ("x", ctypes.c_void_p), ("x_dtype", ctypes.c_int),
                 ("n_rows", ctypes.c_int64), ("x_row_stride", ctypes.c_int64)]
+
+
+class KVCacheStruct(ctypes.Structure):
+    """gbs_kv_cache_t: the arrays and sizes of a pool."""
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("n_kv_heads", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("page_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int), ("max_pages", ctypes.c_int)]
 
 
 OBJECTIVE_FN = ctypes.CFUNCTYPE(ctypes.c_double, ctypes.c_float, ctypes.c_void_p)
@@ -122,6 +134,19 @@ def lib() -> ctypes.CDLL:
         L.gbs_weight_rotate_quantize.restype = i32
         L.gbs_quantized_matmul.argtypes = [vp, vp, vp, i64, vp, vp, vp, i64, vp, i32, i64, vp]
         L.gbs_quantized_matmul.restype = i32
+        kv = ctypes.POINTER(KVCacheStruct)
+        L.gbs_kv_page_bytes.argtypes = [vp, i32, i32, ctypes.POINTER(i64)]
+        L.gbs_kv_extend.argtypes = [vp, kv, vp, vp, i32, vp, vp]
+        L.gbs_kv_fork.argtypes = [vp, kv, vp, vp, i32, vp, vp]
+        L.gbs_kv_free.argtypes = [vp, kv, vp, i32, vp]
+        L.gbs_kv_compact.argtypes = [vp, kv, kv, vp, vp, vp]
+        L.gbs_kv_append.argtypes = [vp, kv, vp, vp, i32, i64, vp, vp, i64, i64, vp]
+        L.gbs_kv_read.argtypes = [vp, kv, vp, vp, i32, i64, vp, vp, vp]
+        L.gbs_kv_attention_workspace.argtypes = [vp, kv, i32, i64, i32, ctypes.POINTER(i64)]
+        L.gbs_kv_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, i32, vp, i64, i64,
+                                       vp, i64, vp]
+        for name in EXPORTS[-9:]:
+            getattr(L, name).restype = i32
         L.gbs_hadamard_m.argtypes = [i32, vp]
         L.gbs_hadamard_m.restype = i32
         L.gbs_status_string.argtypes = [i32]
@@ -363,7 +388,8 @@ def gbs_quantized_matmul(plan_x: int, codes_x: torch.Tensor, scales_x: torch.Ten
     _check(lib().gbs_quantized_matmul(ctypes.c_void_p(plan_x), codes_x.data_ptr(), scales_x.data_ptr(), n_tok,
                                       ctypes.c_void_p(plan_w), codes_w.data_ptr(), scales_w.data_ptr(), n_out,
                                       out.data_ptr(), _dtype_code(out), out.stride(0), _stream_ptr(stream)),
-           "gbs_quantized_matmul")
+           "gbs_quantized_matmul", "gbs_kv_page_bytes", "gbs_kv_extend", "gbs_kv_fork", "gbs_kv_free", "gbs_kv_compact",
+           "gbs_kv_append", "gbs_kv_read", "gbs_kv_attention_workspace", "gbs_kv_attention")
 
 
 def gbs_search_state_init() -> SearchState:
@@ -509,6 +535,180 @@ class Plan:
             scales_host.copy_(scales, non_blocking=True)
         s.synchronize()
         return codes_host, scales_host
+
+
+# ----------------------------------------------------------------------------------------------
+# paged KV cache in four bits
+# ----------------------------------------------------------------------------------------------
+def gbs_kv_page_bytes(plan: int, n_kv_heads: int, page_size: int) -> int:
+    """Bytes of one page of a pool (host only)."""
+    out = ctypes.c_int64(0)
+    _check(lib().gbs_kv_page_bytes(ctypes.c_void_p(plan), n_kv_heads, page_size, ctypes.byref(out)), "gbs_kv_page_bytes")
+    return out.value
+
+
+class KVCache:
+    """A pool of pages that holds rotated, quantized keys and values, and the calls on it (gbs_kv_* in include/gbs.h).
+
+    The tensors belong to the caller and are used in place: pages [n_pages, gbs_kv_page_bytes] uint8, page_table
+    [n_seqs, max_pages], lengths [n_seqs] and refs [n_pages] int32.  KVCache.create makes them, empty.  Items of a call are
+    sequences: `seqs` (int32, None: 0, 1, ..), with `cu_tokens` (int32, [items + 1]) where an item has other than one token; their
+    tokens are the last ones of the sequences.  Nothing here waits for the device: what became of the items of extend and fork
+    stands in the tensors these return.
+    """
+
+    def __init__(self, plan: Plan, pages: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor,
+                 n_kv_heads: int, page_size: int):
+        self.page_bytes = gbs_kv_page_bytes(plan.handle, n_kv_heads, page_size)
+        for what, t, dtype, shape in (("pages", pages, torch.uint8, (pages.shape[0], self.page_bytes)),
+                                      ("page_table", page_table, torch.int32, tuple(page_table.shape[:2])),
+                                      ("lengths", lengths, torch.int32, tuple(page_table.shape[:1])),
+                                      ("refs", refs, torch.int32, tuple(pages.shape[:1]))):
+            _check_buffer(what, t, pages, dtype, 1)
+            if tuple(t.shape) != shape:
+                raise ValueError("gbs: %s must have shape %s, got %s" % (what, shape, tuple(t.shape)))
+        if page_table.dim() != 2:
+            raise ValueError("gbs: page_table must be [sequences, pages]")
+        self.plan, self.n_kv_heads, self.page_size = plan, n_kv_heads, page_size
+        self.pages, self.page_table, self.lengths, self.refs = pages, page_table, lengths, refs
+        self._c = KVCacheStruct(pages.data_ptr(), pages.shape[0], n_kv_heads, page_size, page_table.data_ptr(), lengths.data_ptr(),
+                                refs.data_ptr(), page_table.shape[0], page_table.shape[1])
+
+    @classmethod
+    def create(cls, plan: Plan, n_pages: int, n_kv_heads: int, page_size: int, n_seqs: int, max_pages: int, device="cuda:0"):
+        """An empty pool."""
+        pages = torch.empty((n_pages, gbs_kv_page_bytes(plan.handle, n_kv_heads, page_size)), dtype=torch.uint8, device=device)
+        table = torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device)
+        return cls(plan, pages, table, torch.zeros(n_seqs, dtype=torch.int32, device=device),
+                   torch.zeros(n_pages, dtype=torch.int32, device=device), n_kv_heads, page_size)
+
+    def _stream(self, stream, *scratch):
+        """The call's stream, which scratch memory of the call is given to."""
+        if stream is None:
+            return int(torch.cuda.current_stream(self.pages.device).cuda_stream)
+        for t in scratch:
+            t.record_stream(stream)
+        return int(stream.cuda_stream)
+
+    def _ints(self, what: str, t, n: int):
+        """Pointer of a row of n int32 (None: null)."""
+        if t is None:
+            return None
+        _check_buffer(what, t, self.pages, torch.int32, 0)
+        if t.dim() != 1 or t.shape[0] != n:
+            raise ValueError("gbs: %s must be one row of %d numbers, got shape %s" % (what, n, tuple(t.shape)))
+        return t.data_ptr()
+
+    def _items(self, seqs, cu_tokens, n_tokens: int):
+        """(pointer of seqs, pointer of cu_tokens, number of items)"""
+        n = seqs.shape[0] if seqs is not None else (cu_tokens.shape[0] - 1 if cu_tokens is not None else n_tokens)
+        return self._ints("seqs", seqs, n), self._ints("cu_tokens", cu_tokens, n + 1), n
+
+    def _rows(self, what: str, x: torch.Tensor, heads: int):
+        if not isinstance(x, torch.Tensor) or not x.is_cuda or x.device != self.pages.device:
+            raise ValueError("gbs: %s must be a tensor on %s" % (what, self.pages.device))
+        if x.dtype != torch.bfloat16:
+            raise TypeError("gbs: %s must be bfloat16, got %s" % (what, x.dtype))
+        d = self.plan.info.d
+        if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != d or x.stride(2) != 1:
+            raise ValueError("gbs: %s must be [tokens, %d, %d] with contiguous rows, got shape %s, strides %s" %
+                             (what, heads, d, tuple(x.shape), x.stride()))
+
+    def _strides(self, x: torch.Tensor):
+        # a stride that no element depends on may be anything
+        d = self.plan.info.d
+        return (x.stride(0) if x.shape[0] > 1 else d), (x.stride(1) if x.shape[1] > 1 else d)
+
+    def extend(self, seqs=None, counts=None, stream=None) -> torch.Tensor:
+        """Room for counts[i] (None: one) more tokens in each sequence; returns the items' status (GBS_KV_*)."""
+        n = next((t.shape[0] for t in (seqs, counts) if t is not None), self.page_table.shape[0])
+        status = torch.empty(n, dtype=torch.int32, device=self.pages.device)
+        _check(lib().gbs_kv_extend(self.plan.handle, ctypes.byref(self._c), self._ints("seqs", seqs, n), self._ints("counts", counts, n), n,
+                                   status.data_ptr(), self._stream(stream, status)), "gbs_kv_extend")
+        return status
+
+    def fork(self, src: torch.Tensor, dst: torch.Tensor, stream=None) -> torch.Tensor:
+        """Empty sequences dst[i] become copies of src[i] that share its full pages; returns the pairs' status (GBS_KV_*)."""
+        n = src.shape[0]
+        status = torch.empty(n, dtype=torch.int32, device=self.pages.device)
+        _check(lib().gbs_kv_fork(self.plan.handle, ctypes.byref(self._c), self._ints("src", src, n), self._ints("dst", dst, n), n,
+                                 status.data_ptr(), self._stream(stream, status)), "gbs_kv_fork")
+        return status
+
+    def free(self, seqs: torch.Tensor, stream=None) -> None:
+        """The sequences end; pages that no other sequence holds are free."""
+        _check(lib().gbs_kv_free(self.plan.handle, ctypes.byref(self._c), self._ints("seqs", seqs, seqs.shape[0]), seqs.shape[0],
+                                 self._stream(stream)), "gbs_kv_free")
+
+    def compact(self, into: "KVCache", page_map: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """Move the pages in use into the pool `into`, in order; returns their number (one int32 on the device)."""
+        if page_map is None:
+            page_map = torch.empty(self.pages.shape[0], dtype=torch.int32, device=self.pages.device)
+        live = torch.empty(1, dtype=torch.int32, device=self.pages.device)
+        if into.pages.device != self.pages.device or into.plan.info.asymmetric != self.plan.info.asymmetric:
+            raise ValueError("gbs: both pools must be on one device and of one kind of quantizer")
+        _check(lib().gbs_kv_compact(self.plan.handle, ctypes.byref(self._c), ctypes.byref(into._c),
+                                    self._ints("page_map", page_map, self.pages.shape[0]), live.data_ptr(),
+                                    self._stream(stream, page_map, live)), "gbs_kv_compact")
+        return live
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, seqs=None, cu_tokens=None, stream=None) -> None:
+        """Rotate and quantize key and value rows [tokens, n_kv_heads, d] (bf16) into the pages of their tokens."""
+        self._rows("k", k, self.n_kv_heads)
+        self._rows("v", v, self.n_kv_heads)
+        if v.shape[0] != k.shape[0]:
+            raise ValueError("gbs: k has %d tokens, v %d" % (k.shape[0], v.shape[0]))
+        if self._strides(v) != self._strides(k):
+            raise ValueError("gbs: k and v must have the same strides, got %s and %s" % (k.stride(), v.stride()))
+        s, cu, n = self._items(seqs, cu_tokens, k.shape[0])
+        _check(lib().gbs_kv_append(self.plan.handle, ctypes.byref(self._c), s, cu, n, k.shape[0], k.data_ptr(), v.data_ptr(),
+                                   *self._strides(k), self._stream(stream)), "gbs_kv_append")
+
+    def read(self, seqs=None, cu_tokens=None, n_tokens: int | None = None, out=None, stream=None):
+        """The rows that the cache stands for, [n_tokens, n_kv_heads, d] bf16 keys and values, in their own basis."""
+        if out is None:
+            if n_tokens is None:
+                if cu_tokens is not None:
+                    raise ValueError("gbs: n_tokens says how many rows cu_tokens (on the device) asks for")
+                n_tokens = seqs.shape[0] if seqs is not None else self.page_table.shape[0]
+            shape = (n_tokens, self.n_kv_heads, self.plan.info.d)
+            out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=self.pages.device) for _ in range(2))
+            scratch = out
+        else:
+            scratch = ()
+        k, v = out
+        for what, x in (("k_out", k), ("v_out", v)):
+            self._rows(what, x, self.n_kv_heads)
+            _check_buffer(what, x, self.pages, torch.bfloat16, k.numel())
+        s, cu, n = self._items(seqs, cu_tokens, k.shape[0])
+        _check(lib().gbs_kv_read(self.plan.handle, ctypes.byref(self._c), s, cu, n, k.shape[0], k.data_ptr(), v.data_ptr(),
+                                 self._stream(stream, *scratch)), "gbs_kv_read")
+        return k, v
+
+    def attention(self, q: torch.Tensor, seqs=None, cu_tokens=None, max_tokens: int = 1, causal: bool = True, window: int = 0,
+                  scale: float = 0.0, max_len: int = 0, out=None, stream=None) -> torch.Tensor:
+        """Attention of query tokens q [tokens, heads, d] (bf16) over the cache; the same shape comes back.  max_tokens: no item has
+        more tokens; max_len: no sequence of the call is longer (0: the table's width); scale 0: 1 / sqrt(d)."""
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            raise ValueError("gbs: q must be [tokens, heads, d]")
+        self._rows("q", q, q.shape[1])
+        scratch = []
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+            scratch.append(out)
+        self._rows("out", out, q.shape[1])
+        if out.shape[0] != q.shape[0]:
+            raise ValueError("gbs: q has %d tokens, out %d" % (q.shape[0], out.shape[0]))
+        s, cu, n = self._items(seqs, cu_tokens, q.shape[0])
+        need = ctypes.c_int64(0)
+        _check(lib().gbs_kv_attention_workspace(self.plan.handle, ctypes.byref(self._c), q.shape[1], q.shape[0], max_tokens, ctypes.byref(need)),
+               "gbs_kv_attention_workspace")
+        work = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        _check(lib().gbs_kv_attention(self.plan.handle, ctypes.byref(self._c), s, cu, n, q.shape[0], max_tokens, max_len, q.data_ptr(),
+                                      *self._strides(q), q.shape[1], float(scale), window, GBS_KV_CAUSAL if causal else 0, out.data_ptr(),
+                                      *self._strides(out), work.data_ptr(), need.value, self._stream(stream, work, *scratch)),
+               "gbs_kv_attention")
+        return out
 
 
 # the methods that _native.so has a regular call for

@@ -169,3 +169,58 @@ int gbs_tc_row_rotate_quantize(const gbs_plan* p, const void* x, int64_t n_rows,
                                float* scales, float* y_opt, cudaStream_t stream);
 int gbs_tc_uv_rotate_quantize(const gbs_plan* p, const void* x, int64_t n_rows, int64_t stride, void* codes,
                               float* scales, float* y_opt, cudaStream_t stream);
+
+// ---- paged KV cache (gbs_kv_host.cu checks, the others launch) ----
+struct gbs_kv_view {
+    unsigned char* pages;
+    int* page_table;
+    int* lengths;
+    int* refs;
+    int n_pages, heads, page_log;       // page_size = 1 << page_log
+    int n_seqs, max_pages;
+    int block_bytes;                    // one KV head of a page: page_size * (128 + 8 * scale floats of a row)
+    long long page_bytes;
+};
+
+int gbs_kv_append_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, const int* cu, int n_items, int64_t n_tokens, const void* k,
+                         const void* v, int64_t token_stride, int64_t head_stride, cudaStream_t stream);
+int gbs_kv_read_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, const int* cu, int n_items, int64_t n_tokens, void* k_out,
+                       void* v_out, cudaStream_t stream);
+int gbs_kv_extend_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, const int* counts, int n_items, int* status, cudaStream_t stream);
+int gbs_kv_fork_launch(const gbs_plan* p, const gbs_kv_view& c, const int* src, const int* dst, int n_items, int* status, cudaStream_t stream);
+int gbs_kv_free_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, cudaStream_t stream);
+int gbs_kv_compact_launch(const gbs_plan* p, const gbs_kv_view& c, const gbs_kv_view& into, int* page_map, int* n_live, cudaStream_t stream);
+
+// the arguments of an attention call, checked
+struct gbs_kv_attn {
+    gbs_kv_view c;
+    const int *seqs, *cu;
+    int n_items, max_tokens, max_len, window, causal;
+    int n_heads, group, d;              // group: query heads of a KV head
+    float scale;
+    long long n_tokens;
+    const void* q;
+    void* out;
+    long long q_token, q_head, out_token, out_head;
+};
+int64_t gbs_kv_attn_workspace(const gbs_plan* p, int group, int max_tokens);
+int gbs_kv_attn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, cudaStream_t stream);
+
+#ifdef __CUDACC__
+// Launch on `stream`, its set-up overlapping the end of the launch before it (kernels wait before they touch memory).
+template <typename K, typename... Args>
+int gbs_kv_launch(const gbs_plan* p, K kernel, dim3 grid, int threads, size_t smem, cudaStream_t stream, const Args&... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p->pdl ? 1 : 0;
+    return (int)cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+#endif

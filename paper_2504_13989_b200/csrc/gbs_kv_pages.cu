@@ -1,0 +1,336 @@
+// Bookkeeping of the paged KV cache (gbs_kv_extend, gbs_kv_fork, gbs_kv_free, gbs_kv_compact).
+//
+// refs[] is the whole truth about the pool: a page is free when its count is 0, and free pages are taken lowest first.  So the
+// outcome of a call does not depend on the order in which threads run, and nothing has to be kept next to it.  Who gets which page
+// follows from two prefix sums (pages wanted by the items before, free pages below), which one block computes: the items are at most
+// a few thousand and the counters of a pool that fills the GPU a few megabytes.  What is large, the pages' contents and the tables'
+// rows, is left to a second launch over all SMs.
+#include "gbs_kv.cuh"
+
+namespace {
+
+constexpr int ONE = 1024;                        // threads of the one block that allocates
+constexpr int COPY = 256;                        // threads of a block that copies
+
+// Exclusive prefix sum over the block; `total` is the sum.  Two barriers; `part` holds 32 ints.
+__device__ __forceinline__ int block_prefix(int v, int* part, int& total)
+{
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    int s = v;
+#pragma unroll
+    for (int h = 1; h < 32; h <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, s, h);
+        if (lane >= h) s += o;
+    }
+    __syncthreads();                             // the last round's values have been read
+    if (lane == 31) part[w] = s;
+    __syncthreads();
+    int below = lane < w ? part[lane] : 0, all = part[lane];
+#pragma unroll
+    for (int h = 16; h; h >>= 1) {
+        below += __shfl_xor_sync(0xffffffffu, below, h);
+        all += __shfl_xor_sync(0xffffffffu, all, h);
+    }
+    total = all;
+    return below + s - v;
+}
+
+// First item that names a sequence: a table in shared memory, keys and the lowest item of each.
+struct FirstOf {
+    int *key, *item;
+    unsigned mask;
+    __device__ __forceinline__ unsigned slot(int seq) const
+    {
+        unsigned h = ((unsigned)seq * 2654435761u) >> 7 & mask;
+        for (;;) {                               // the table has room for twice the items
+            const int was = atomicCAS(&key[h], -1, seq);
+            if (was == -1 || was == seq) return h;
+            h = (h + 1) & mask;
+        }
+    }
+};
+
+struct AllocArgs {
+    gbs_kv_view c;
+    const int *seqs, *other;                     // extend: sequences and counts; fork: targets and sources
+    int n_items;
+    int* status;
+    unsigned mask;
+};
+
+// What an item asks for: its status, the tokens it will have, its first new page and how many.
+struct Wish {
+    int status, seq, length, first, need;
+};
+template <bool FORK>
+__device__ __forceinline__ Wish wish_of(const AllocArgs& A, const FirstOf& f, int i)
+{
+    Wish w = {GBS_KV_BAD_INDEX, -1, 0, 0, 0};
+    w.seq = kv_sequence(A.c, A.seqs, i);
+    if (w.seq < 0) return w;
+    if (f.item[f.slot(w.seq)] != i) {
+        w.status = GBS_KV_DUPLICATE;
+        return w;
+    }
+    const int ps = 1 << A.c.page_log, have = kv_length(A.c, w.seq);
+    if (FORK) {
+        const int src = kv_sequence(A.c, A.other, i);
+        if (src < 0) return w;
+        if (have != 0) {
+            w.status = GBS_KV_NOT_EMPTY;
+            return w;
+        }
+        w.length = kv_length(A.c, src);
+        w.first = w.length >> A.c.page_log;
+        w.need = (w.length & (ps - 1)) != 0;
+    } else {
+        const int count = A.other ? A.other[i] : 1;
+        if (count < 0) return w;
+        if (count > (A.c.max_pages << A.c.page_log) - have) {
+            w.status = GBS_KV_TOO_LONG;
+            return w;
+        }
+        w.length = have + count;
+        w.first = (int)(((unsigned)have + ps - 1) >> A.c.page_log);
+        w.need = (int)(((unsigned)w.length + ps - 1) >> A.c.page_log) - w.first;
+    }
+    w.status = GBS_KV_DONE;
+    return w;
+}
+
+// Shared memory: FirstOf's two arrays of mask + 1, then for each item the pages wanted before it (and, at the end, its new length).
+template <bool FORK>
+__global__ __launch_bounds__(ONE) void k_kv_allocate(const __grid_constant__ AllocArgs A)
+{
+    extern __shared__ int sm[];
+    __shared__ int part[32];
+    FirstOf f = {sm, sm + A.mask + 1, A.mask};
+    int* before = sm + 2 * (A.mask + 1);
+    const int tid = threadIdx.x, n = A.n_items;
+    for (unsigned i = tid; i <= A.mask; i += ONE) {
+        f.key[i] = -1;
+        f.item[i] = 0x7fffffff;
+    }
+    kv_wait_before();
+    kv_let_next();
+    __syncthreads();
+    for (int i = tid; i < n; i += ONE) {
+        const int seq = kv_sequence(A.c, A.seqs, i);
+        if (seq >= 0) atomicMin(&f.item[f.slot(seq)], i);
+    }
+    __syncthreads();
+
+    // pages wanted before each item; more than the pool has need not be told apart
+    int wanted = 0;
+    for (int i0 = 0; i0 < n; i0 += ONE) {
+        const int i = i0 + tid;
+        const int need = i < n ? min(wish_of<FORK>(A, f, i).need, 1 << 20) : 0;
+        int total;
+        const int at = wanted + block_prefix(need, part, total);
+        if (i < n) before[i] = at;
+        wanted = min(wanted + total, 0x3fffffff);
+    }
+    __syncthreads();
+
+    // free pages, lowest first, go to the items in their order; what an item that is refused below has taken is given back there
+    int found = 0;
+    for (int p0 = 0; p0 < A.c.n_pages && found < wanted; p0 += 4 * ONE) {
+        const int p = p0 + 4 * tid;
+        int free_bits = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (p + k < A.c.n_pages && A.c.refs[p + k] == 0) free_bits |= 1 << k;
+        int total, r = found + block_prefix(__popc(free_bits), part, total);
+        for (; free_bits && r < wanted; free_bits &= free_bits - 1, ++r) {
+            const int page = p + __ffs(free_bits) - 1;
+            int lo = 0, hi = n - 1;              // the last item with before[] <= r
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (before[mid] <= r) lo = mid;
+                else hi = mid - 1;
+            }
+            const Wish w = wish_of<FORK>(A, f, lo);
+            A.c.page_table[(long long)w.seq * A.c.max_pages + w.first + (r - before[lo])] = page;
+            A.c.refs[page] = 1;
+        }
+        found += total;
+    }
+    __syncthreads();
+
+    // all wishes are read before a length changes: a fork's source may be another's target
+    for (int i = tid; i < n; i += ONE) {
+        Wish w = wish_of<FORK>(A, f, i);
+        if (w.status == GBS_KV_DONE && w.need > 0 && (long long)before[i] + w.need > found) {
+            w.status = GBS_KV_NO_PAGES;
+            for (int j = 0; j < w.need && before[i] + j < found; ++j)
+                A.c.refs[A.c.page_table[(long long)w.seq * A.c.max_pages + w.first + j]] = 0;
+        }
+        A.status[i] = w.status;
+        before[i] = w.status == GBS_KV_DONE ? w.length : -1;
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += ONE)
+        if (before[i] >= 0) A.c.lengths[kv_sequence(A.c, A.seqs, i)] = before[i];
+}
+
+__device__ __forceinline__ void copy_words(unsigned char* to, const unsigned char* from, int bytes)
+{
+    for (int i = 4 * threadIdx.x; i < bytes; i += 4 * COPY)
+        *reinterpret_cast<unsigned*>(to + i) = *reinterpret_cast<const unsigned*>(from + i);
+}
+__device__ __forceinline__ void copy_16(unsigned char* to, const unsigned char* from, int bytes)
+{
+    for (int i = 16 * threadIdx.x; i < bytes; i += 16 * COPY)
+        *reinterpret_cast<uint4*>(to + i) = *reinterpret_cast<const uint4*>(from + i);
+}
+
+// One block per pair and KV head: its part of the last page's tokens; head 0 also shares the full pages.  The target's length is the
+// one that the source had before the call.
+__global__ __launch_bounds__(COPY) void k_kv_share(const __grid_constant__ AllocArgs A)
+{
+    kv_wait_before();
+    kv_let_next();
+    const int i = blockIdx.x, head = blockIdx.y;
+    if (A.status[i] != GBS_KV_DONE) return;
+    const int dst = kv_sequence(A.c, A.seqs, i), src = kv_sequence(A.c, A.other, i);
+    const int length = kv_length(A.c, dst), full = length >> A.c.page_log, ps = 1 << A.c.page_log, tail = length & (ps - 1);
+    if (length == 0) return;
+    if (head == 0) {
+        const int* from = A.c.page_table + (long long)src * A.c.max_pages;
+        int* to = A.c.page_table + (long long)dst * A.c.max_pages;
+        for (int j = threadIdx.x; j < full; j += COPY) {
+            const int page = from[j];
+            to[j] = page;
+            if ((unsigned)page < (unsigned)A.c.n_pages) atomicAdd(&A.c.refs[page], 1);
+        }
+    }
+    if (tail == 0) return;
+    const int a = kv_page(A.c, src, length), b = kv_page(A.c, dst, length);
+    if (a < 0 || b < 0) return;
+    const unsigned char* from = kv_block(A.c, a, head);
+    unsigned char* to = kv_block(A.c, b, head);
+    const int scale_bytes = A.c.block_bytes / ps - 2 * KV_ROW;                   // both scales of a token
+    copy_16(to, from, tail * KV_ROW);
+    copy_16(to + ps * KV_ROW, from + ps * KV_ROW, tail * KV_ROW);
+    to += 2 * ps * KV_ROW;
+    from += 2 * ps * KV_ROW;
+    copy_words(to, from, tail * scale_bytes / 2);
+    copy_words(to + ps * scale_bytes / 2, from + ps * scale_bytes / 2, tail * scale_bytes / 2);
+}
+
+// One block per item; the exchange lets one of two blocks that name a sequence end it.
+__global__ __launch_bounds__(COPY) void k_kv_free(const __grid_constant__ AllocArgs A)
+{
+    __shared__ int length;
+    kv_wait_before();
+    kv_let_next();
+    const int seq = kv_sequence(A.c, A.seqs, blockIdx.x);
+    if (seq < 0) return;
+    if (threadIdx.x == 0) length = min(max(atomicExch(&A.c.lengths[seq], 0), 0), A.c.max_pages << A.c.page_log);
+    __syncthreads();
+    const int held = (int)(((unsigned)length + (1u << A.c.page_log) - 1) >> A.c.page_log);
+    const int* row = A.c.page_table + (long long)seq * A.c.max_pages;
+    for (int j = threadIdx.x; j < held; j += COPY) {
+        const int page = row[j];
+        if ((unsigned)page < (unsigned)A.c.n_pages) atomicSub(&A.c.refs[page], 1);
+    }
+}
+
+struct CompactArgs {
+    gbs_kv_view c, into;
+    int *map, *n_live;
+};
+
+// new numbers of the pages in use
+__global__ __launch_bounds__(ONE) void k_kv_number(const __grid_constant__ CompactArgs A)
+{
+    __shared__ int part[32];
+    kv_wait_before();
+    kv_let_next();
+    int live = 0;
+    for (int p0 = 0; p0 < A.c.n_pages; p0 += 4 * ONE) {
+        const int p = p0 + 4 * threadIdx.x;
+        int refs[4], used = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            refs[k] = p + k < A.c.n_pages ? A.c.refs[p + k] : 0;
+            used += refs[k] > 0;
+        }
+        int total, r = live + block_prefix(used, part, total);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (p + k < A.c.n_pages) {
+                const bool moved = refs[k] > 0 && r < A.into.n_pages;
+                A.map[p + k] = moved ? r : -1;
+                if (moved) A.into.refs[r] = refs[k];
+                r += refs[k] > 0;
+            }
+        live += total;
+    }
+    for (int p = live + threadIdx.x; p < A.into.n_pages; p += ONE) A.into.refs[p] = 0;
+    if (threadIdx.x == 0) *A.n_live = live;
+}
+
+__global__ __launch_bounds__(COPY) void k_kv_move(const __grid_constant__ CompactArgs A)
+{
+    kv_wait_before();
+    kv_let_next();
+    const int ps = 1 << A.c.page_log;
+    const long long entries = (long long)A.c.n_seqs * A.c.max_pages;
+    for (long long e = (long long)blockIdx.x * COPY + threadIdx.x; e < entries; e += (long long)gridDim.x * COPY) {
+        const int seq = (int)(e / A.c.max_pages), j = (int)(e - (long long)seq * A.c.max_pages);
+        const int page = j < (int)(((unsigned)kv_length(A.c, seq) + ps - 1) >> A.c.page_log) ? A.c.page_table[e] : -1;
+        A.into.page_table[e] = (unsigned)page < (unsigned)A.c.n_pages ? A.map[page] : -1;
+    }
+    for (int s = blockIdx.x * COPY + threadIdx.x; s < A.c.n_seqs; s += gridDim.x * COPY) A.into.lengths[s] = A.c.lengths[s];
+    for (int p = blockIdx.x; p < A.c.n_pages; p += gridDim.x) {
+        const int to = A.map[p];
+        if (to < 0) continue;
+        const uint4* from = reinterpret_cast<const uint4*>(A.c.pages + (long long)p * A.c.page_bytes);
+        uint4* at = reinterpret_cast<uint4*>(A.into.pages + (long long)to * A.c.page_bytes);
+        for (int i = threadIdx.x; i < (int)(A.c.page_bytes / 16); i += COPY) at[i] = from[i];
+    }
+}
+
+int allocate(const gbs_plan* p, bool fork, const AllocArgs& A0, cudaStream_t stream)
+{
+    AllocArgs A = A0;
+    A.mask = 63;
+    while (A.mask + 1 < 2u * (unsigned)A.n_items) A.mask = 2 * A.mask + 1;
+    const size_t smem = (2 * ((size_t)A.mask + 1) + (size_t)A.n_items) * sizeof(int);
+    const void* f = fork ? (const void*)k_kv_allocate<true> : (const void*)k_kv_allocate<false>;
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return (int)e;
+    }
+    return gbs_kv_launch(p, fork ? k_kv_allocate<true> : k_kv_allocate<false>, dim3(1), ONE, smem, stream, A);
+}
+
+}  // namespace
+
+int gbs_kv_extend_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, const int* counts, int n_items, int* status, cudaStream_t stream)
+{
+    return allocate(p, false, {c, seqs, counts, n_items, status, 0}, stream);
+}
+
+int gbs_kv_fork_launch(const gbs_plan* p, const gbs_kv_view& c, const int* src, const int* dst, int n_items, int* status, cudaStream_t stream)
+{
+    const AllocArgs A = {c, dst, src, n_items, status, 0};
+    const int e = allocate(p, true, A, stream);
+    if (e != 0) return e;
+    return gbs_kv_launch(p, k_kv_share, dim3((unsigned)n_items, (unsigned)c.heads), COPY, 0, stream, A);
+}
+
+int gbs_kv_free_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, cudaStream_t stream)
+{
+    const AllocArgs A = {c, seqs, nullptr, n_items, nullptr, 0};
+    return gbs_kv_launch(p, k_kv_free, dim3((unsigned)n_items), COPY, 0, stream, A);
+}
+
+int gbs_kv_compact_launch(const gbs_plan* p, const gbs_kv_view& c, const gbs_kv_view& into, int* page_map, int* n_live, cudaStream_t stream)
+{
+    const CompactArgs A = {c, into, page_map, n_live};
+    const int e = gbs_kv_launch(p, k_kv_number, dim3(1), ONE, 0, stream, A);
+    if (e != 0) return e;
+    return gbs_kv_launch(p, k_kv_move, dim3((unsigned)(p->sm_count * 8)), COPY, 0, stream, A);
+}
