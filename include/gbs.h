@@ -430,7 +430,8 @@ int gbs_kv_read(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32
  * with window > 0, j > p - window.  A row that sees nothing becomes 0.
  *   q, out            device bf16, [n_tokens][n_heads][d] with strides in elements as in gbs_kv_append; out's own strides
  *   n_heads           a multiple of n_kv_heads, at most 1024 query heads per KV head
- *   max_tokens        no item has more tokens (1 where cu_tokens is NULL); an item's tokens beyond it become 0
+ *   max_tokens        no item has more tokens (1 where cu_tokens is NULL); what is beyond it is left as it is.
+ *                     n_items * max_tokens * query heads of a KV head: at most 2^28
  *   max_len           no sequence of the call is longer (0: the table's width); one that is longer is read up to max_len only.
  *                     It bounds how far the work is split, not what is read.
  *   scale             0: 1 / sqrt(d)

@@ -173,7 +173,7 @@ int check_heads(const gbs_kv_view& c, int n_heads, int max_tokens, bool ragged)
 {
     if (n_heads < 1 || n_heads % c.heads != 0 || n_heads / c.heads > 1024) return GBS_ERR_INVALID_ARG;
     if (max_tokens < 1 || (!ragged && max_tokens != 1)) return GBS_ERR_INVALID_ARG;
-    return (int64_t)max_tokens * (n_heads / c.heads) < 1ll << 30 ? GBS_OK : GBS_ERR_INVALID_ARG;
+    return (int64_t)max_tokens * (n_heads / c.heads) <= 1ll << 28 ? GBS_OK : GBS_ERR_INVALID_ARG;
 }
 
 }  // namespace
@@ -202,7 +202,7 @@ extern "C" int gbs_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache
     if (rc == GBS_OK) rc = check_heads(A.c, n_heads, max_tokens, cu_tokens != nullptr);
     if (rc != GBS_OK) return rc;
     if ((flags & ~GBS_KV_CAUSAL) || window < 0 || max_len < 0 || !isfinite(scale)) return GBS_ERR_INVALID_ARG;
-    if (n_tokens * n_heads >= 1ll << 31) return GBS_ERR_INVALID_ARG;
+    if (n_tokens * n_heads >= 1ll << 31 || (int64_t)n_items * max_tokens * (n_heads / A.c.heads) > 1ll << 28) return GBS_ERR_INVALID_ARG;
     if (empty) return GBS_OK;
     if (!q || !out || !workspace || workspace_bytes < gbs_kv_attn_workspace(p, n_heads / A.c.heads, max_tokens)) return GBS_ERR_INVALID_ARG;
     rc = check_strides(p, q_token_stride, q_head_stride);
