@@ -4,15 +4,18 @@
 // (+ sum_j p_j lo_j): the codes go into the matrix unit as they are, exactly, and the rotation is applied to eight query rows and
 // eight results instead of to every cached row.
 //
-// What bounds it is the cache, 136 or 144 bytes a token and KV head, read once.  The matrix unit takes 16 rows at a time; there are at
-// most eight here, so each is given as a sum of two, q = hi + lo 2^-11 in fp16 and p Delta_v = hi + lo in bf16: 22 and 16 bits at no cost, and
-// both halves of a row land in the same thread.  Layouts are chosen so that codes go from shared memory to the operand registers
-// without being moved between threads: the order of the 128 coordinates of a score, of a group's 8 tokens and of the 128 columns of the
-// result is free, as long as both operands have the same.  A nibble becomes a number by or-ing it into the low mantissa bits of 1024
-// (fp16) or 128 (bf16) and subtracting that, exactly.
+// What bounds it is the cache, 136 or 144 bytes a token and KV head, read once, and next to it the conversion of 256 codes a token.
+// The codes are the tall operand of both products (16 tokens, then 16 coordinates, by 8 query rows), so no row of the matrix unit is idle, and
+// each number of the other operand is given as a sum of two fp16 numbers, 22 bits: q = hi + lo and w = p Delta_v = hi + lo.  Layouts are
+// chosen so that codes go from shared memory to the operand registers without being moved between threads: the order of the 128
+// coordinates of a score, of a group's 16 tokens and of the 128 rows of the result is free, as long as both operands have the same.  Only the weights are
+// transposed on the way (movmatrix).  A nibble becomes a number by putting it into the mantissa of 1024 and subtracting that, exactly.
+//
+// Two running maxima: m of the scores z (log2), as in any softmax, and M of z + log2 Delta_v, which keeps w inside fp16 whatever the
+// sizes of the values: w = 2^(z - m) Delta_v 2^(m - M).  They are moved only when a score exceeds m by 8 or w its range, which is rare.
 //
 // A warp works alone: it fetches units of 32 tokens (bulk copies into a ring of its own), keeps sums for its tokens in registers, and
-// meets the block's other warps where a segment ends.  The running maximum is moved only when a score exceeds it by 2^8.
+// meets the block's other warps where a segment ends.
 #include <cuda_fp16.h>
 
 #include "gbs_kv_sched.cuh"
@@ -22,9 +25,11 @@ namespace {
 
 constexpr int ROWS = 8, UNIT = 32;
 constexpr int WARPS = 6, THREADS = 32 * WARPS, STAGES = 3;
-constexpr int PART = ROWS * 128 + 3 * ROWS;          // floats of a partial result: sums, maximum, total, sum of p lo
+constexpr int PART = ROWS * 128 + 4 * ROWS;          // floats of a partial result: sums, m, total, sum of p lo, M
 constexpr int BLOCKS_PER_SM = 2;
-constexpr float MOVE = 8.f;                          // the maximum moves when a score is so much (log2) above it
+constexpr float MOVE = 8.f;                          // m moves when a score is so much (log2) above it
+constexpr float NONE = -1e30f;                       // maximum of no scores
+constexpr float W_UP = 64.f, W_MOST = 32768.f;       // w is 64 at M; M moves when one is beyond the other
 
 template <bool ASYM>
 struct Stage {
@@ -36,10 +41,11 @@ struct Stage {
 template <bool ASYM>
 struct Smem {
     Stage<ASYM> ring[WARPS][STAGES];
-    float part[WARPS][ROWS * 128];                   // 16-byte pieces in the order piece ^ (lane & 7) of each thread's eight
-    float m[WARPS][ROWS], l[WARPS][ROWS], add[WARPS][ROWS];
+    float part[WARPS][ROWS * 128];                   // 16-byte pieces c of each 64 bytes of rows 2 t, 2 t + 1 at c ^ t
+    float m[WARPS][ROWS], l[WARPS][ROWS], add[WARPS][ROWS], mw[WARPS][ROWS];
     __half qh[ROWS][128], ql[ROWS][128];             // coordinates in the order of the operand, see place()
     float factor[ROWS], qsum[ROWS];
+    int row_lo[ROWS], row_hi[ROWS], all_lo, all_hi;  // tokens that a row sees, and that every row sees
     unsigned long long full[WARPS][STAGES];
     unsigned valid[WARPS][STAGES];                   // bit h: tokens 16 h .. of the unit have a page
     KvSeg ahead[WARPS];                              // the segment of the next unit to fetch
@@ -55,21 +61,21 @@ struct Args {
     int* status;
 };
 
-__device__ __forceinline__ void mma_f16(float c[4], const unsigned a[4], unsigned b0, unsigned b1)
+__device__ __forceinline__ void mma_f16(float c[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, const unsigned b[2])
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
 }
-__device__ __forceinline__ void mma_bf16(float c[4], const unsigned a[4], unsigned b0, unsigned b1)
+// 8 x 8 16-bit numbers, a row in four lanes: rows become columns
+__device__ __forceinline__ unsigned transposed(unsigned x)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    unsigned y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 
 __device__ __forceinline__ unsigned as_u(__half2 x) { return *reinterpret_cast<unsigned*>(&x); }
-__device__ __forceinline__ unsigned as_u(__nv_bfloat162 x) { return *reinterpret_cast<unsigned*>(&x); }
 __device__ __forceinline__ __half2 as_h(unsigned x) { return *reinterpret_cast<__half2*>(&x); }
-__device__ __forceinline__ __nv_bfloat162 as_b(unsigned x) { return *reinterpret_cast<__nv_bfloat162*>(&x); }
 
 __device__ __forceinline__ float ex2(float x)
 {
@@ -78,26 +84,24 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// Eight codes of a word -> pairs (0, 4), (1, 5), (2, 6), (3, 7) in fp16.  A symmetric code c is kept as c ^ 8 = c + 8 of four bits.
+// (x & mask) ^ with, one operation
+__device__ __forceinline__ unsigned and_xor(unsigned x, unsigned mask, unsigned with)
+{
+    unsigned y;
+    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(y) : "r"(x), "r"(mask), "r"(with));
+    return y;
+}
+// Nibbles (i, i + 4) of a word, i = 0 .. 3, as pairs in fp16.  A symmetric code c is taken as c ^ 8 = c + 8 of four bits.
 template <bool ASYM>
 __device__ __forceinline__ void codes_f16(unsigned w, unsigned out[4])
 {
     constexpr unsigned LOW = ASYM ? 0x64006400u : 0x64086408u, HIGH = ASYM ? 0x64006400u : 0x64806480u;
     const __half2 off = __float2half2_rn(ASYM ? 1024.f : 1032.f), off16 = __float2half2_rn(ASYM ? -64.f : -72.f), by = __float2half2_rn(0.0625f);
     const unsigned w8 = w >> 8;
-    out[0] = as_u(__hsub2(as_h((w & 0x000f000fu) ^ LOW), off));
-    out[1] = as_u(__hfma2(as_h((w & 0x00f000f0u) ^ HIGH), by, off16));
-    out[2] = as_u(__hsub2(as_h((w8 & 0x000f000fu) ^ LOW), off));
-    out[3] = as_u(__hfma2(as_h((w8 & 0x00f000f0u) ^ HIGH), by, off16));
-}
-// Four codes of token a (low half) and of token b (high half) -> four pairs (a_i, b_i) in bf16.
-template <bool ASYM>
-__device__ __forceinline__ void codes_bf16(unsigned w, unsigned out[4])
-{
-    constexpr unsigned LOW = ASYM ? 0x43004300u : 0x43084308u;
-    const __nv_bfloat162 off = __float2bfloat162_rn(ASYM ? 128.f : 136.f);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = as_u(__hsub2(as_b(((w >> (4 * i)) & 0x000f000fu) ^ LOW), off));
+    out[0] = as_u(__hsub2(as_h(and_xor(w, 0x000f000fu, LOW)), off));
+    out[1] = as_u(__hfma2(as_h(and_xor(w, 0x00f000f0u, HIGH)), by, off16));
+    out[2] = as_u(__hsub2(as_h(and_xor(w8, 0x000f000fu, LOW)), off));
+    out[3] = as_u(__hfma2(as_h(and_xor(w8, 0x00f000f0u, HIGH)), by, off16));
 }
 
 // where coordinate 32 t + 8 w + n stands in a query row: operand register (w, n & 3) of thread t holds n and n + 4
@@ -113,6 +117,17 @@ __device__ __forceinline__ void store_row(__half* row, int l8, const __half h[16
         u.w = as_u(__halves2half2(x[3], x[7]));
         *reinterpret_cast<uint4*>(row + 64 * half + 8 * l8) = u;
     }
+}
+
+// sums of w c, of p and of p lo -> the result: sum / 64 2^(M - m) / total + extra / total, turned back
+__device__ __forceinline__ void finish(float y[16], int l8, float top, float top_w, float total, float extra)
+{
+    const float by = total == 0.f ? 0.f : 1.f / total;
+    const float by_w = by * (KV_NORM / W_UP) * ex2(top_w - top);
+    kv_hadamard(y, l8);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = total != total ? total : y[i] * by_w;
+    if (l8 == 0) y[0] = fmaf(extra * by, 128.f * KV_NORM, y[0]);             // the transform of a row of ones is 128 in its first place
 }
 
 // row of a tile -> token of the item and query head
@@ -150,39 +165,42 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
     const int in_block = piece < 2 ? piece * (KV_ROW << ps_log) : (2 * KV_ROW << ps_log) + (piece - 2) * ((ASYM ? 8 : 4) << ps_log);
     const int in_slot = piece < 2 ? KV_ROW : (ASYM ? 8 : 4);
     const int in_stage = (piece < 2 ? piece * UNIT * KV_ROW : 2 * UNIT * KV_ROW + (piece - 2) * Stage<ASYM>::SCALE) + half * (int)piece_bytes;
-    int fetch = w, fetch_page = -1, fetch_tok = 0, fetched = 0;             // the next unit, this lane's page and token of it
-    // (a lane below `pieces` copies one piece)
+    // the next unit to fetch: its place in the line, its first token (this lane's half of it), the end of its segment in the line and in
+    // tokens, this lane's page of it; the segment itself is kept in shared memory
+    int fetch = w, fetch_tok = 0, fetch_end = 0, fetch_hi = 0, fetch_page = -1, lane_off = 0, fetch_st = 0;
+    const int* fetch_row = nullptr;
     auto look = [&]() {
-        KvSeg* a = &S.ahead[w];
-        if (fetch >= units) return;
-        if (fetch >= a->at + a->e.units) {
-            KvSeg s = *a;
+        if (fetch >= fetch_end) {
+            if (fetch >= units) return;
+            KvSeg s = S.ahead[w];
             while (fetch >= s.at + s.e.units) kv_next(A, s, P.line.entries, P.line.tiles, ROWS, UNIT);
             __syncwarp();
-            if (lane == 0) *a = s;
+            if (lane == 0) S.ahead[w] = s;
             __syncwarp();
+            fetch_end = min(units, s.at + s.e.units);
+            fetch_hi = s.e.hi;
+            fetch_tok = (s.e.lo / UNIT + fetch - s.at) * UNIT + half * 16;
+            fetch_row = A.c.page_table + (long long)s.e.seq * A.c.max_pages;
+            lane_off = s.head * A.c.block_bytes + in_block;
         }
-        fetch_tok = (a->e.lo / UNIT + fetch - a->at) * UNIT + half * 16;
-        fetch_page = -1;
-        if (lane < pieces && fetch_tok < a->e.hi) fetch_page = kv_page(A.c, a->e.seq, fetch_tok);
+        fetch_page = lane < pieces && fetch_tok < fetch_hi ? fetch_row[fetch_tok >> ps_log] : -1;
     };
     auto issue = [&]() {
         if (fetch >= units) return;
-        const int st = fetched % STAGES;
-        const bool ok = fetch_page >= 0;
+        const bool ok = (unsigned)fetch_page < (unsigned)A.c.n_pages;
         const unsigned who = __ballot_sync(0xffffffffu, ok);
-        const unsigned valid = T == UNIT ? ((who & 1) ? 3u : 0u) : (who & 1) | ((who >> 4) & 1) << 1;
-        const int head = S.ahead[w].head;
         if (lane == 0) {
-            S.valid[w][st] = valid;
-            mbar_arrive_expect_tx(&S.full[w][st], (unsigned)(((who & 1) + ((who >> 4) & 1)) * T * (2 * KV_ROW + (ASYM ? 16 : 8))));
+            S.valid[w][fetch_st] = T == UNIT ? ((who & 1) ? 3u : 0u) : (who & 1) | ((who >> 4) & 1) << 1;
+            mbar_arrive_expect_tx(&S.full[w][fetch_st], ((who & 1) + ((who >> 4) & 1)) * (unsigned)(T * (2 * KV_ROW + (ASYM ? 16 : 8))));
         }
         __syncwarp();
         if (ok)
-            bulk_load(reinterpret_cast<unsigned char*>(&S.ring[w][st]) + in_stage,
-                      kv_block(A.c, fetch_page, head) + in_block + (fetch_tok & ((1 << ps_log) - 1)) * in_slot, piece_bytes, &S.full[w][st]);
-        ++fetched;
+            bulk_load(reinterpret_cast<unsigned char*>(&S.ring[w][fetch_st]) + in_stage,
+                      A.c.pages + ((long long)fetch_page * A.c.page_bytes + lane_off + (fetch_tok & ((1 << ps_log) - 1)) * in_slot), piece_bytes,
+                      &S.full[w][fetch_st]);
+        if (++fetch_st == STAGES) fetch_st = 0;
         fetch += WARPS;
+        fetch_tok += WARPS * UNIT;
         look();
     };
     if (lane == 0) S.ahead[w] = seg;
@@ -192,7 +210,8 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
     for (int i = 0; i < STAGES; ++i) issue();
 
     // ---- the segments ----
-    int mine = w, done = 0;                              // this warp's next unit of the line, units it has worked on
+    int mine = w, st = 0;                                // this warp's next unit of the line, and its stage
+    unsigned phase = 0;
     bool dead = false;
     for (;;) {
         // query rows: four of them per warp, rotated, halved
@@ -216,15 +235,16 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
 #pragma unroll
             for (int h = 1; h < 8; h <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, h));
             const int e = min(max((int)(__float_as_uint(m) >> 23), 1), 252);
-            const float down = __uint_as_float((unsigned)(253 - e) << 23), up = __uint_as_float((unsigned)(e + 1) << 23);     // 2^(126-e), its inverse
+            // 2^(139 - e) and its inverse: the largest coordinate is just below 2^13, what is left of it above 2^-24
+            const float down = __uint_as_float((unsigned)(266 - max(e, 13)) << 23), up = __uint_as_float((unsigned)(max(e, 13) - 12) << 23);
             __half hi[16], lo[16];
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float v = y[i] * down;
                 hi[i] = __float2half_rn(v);
-                lo[i] = __float2half_rn((v - __half2float(hi[i])) * 2048.f);
-                sum += __half2float(hi[i]) + __half2float(lo[i]) * (1.f / 2048.f);
+                lo[i] = __float2half_rn(v - __half2float(hi[i]));
+                sum += __half2float(hi[i]) + __half2float(lo[i]);
             }
 #pragma unroll
             for (int h = 1; h < 8; h <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, h);
@@ -232,188 +252,216 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             store_row(S.ql[row], l8, lo);
             if (l8 == 0) {
                 S.factor[row] = up * (A.scale * (KV_NORM * 1.4426950408889634f));
-                S.qsum[row] = sum;
+                S.qsum[row] = sum * S.factor[row];
+                const int token = min(seg.e.row0 + row, seg.e.rows - 1) / A.group;
+                S.row_lo[row] = kv_row_lo(A, seg.e, token);
+                S.row_hi[row] = kv_row_hi(A, seg.e, token);
+                if (row == 0) {                          // the last row sees the latest window, the first the shortest past
+                    S.all_lo = kv_row_lo(A, seg.e, (min(seg.e.rows, seg.e.row0 + ROWS) - 1) / A.group);
+                    S.all_hi = S.row_hi[0];
+                }
             }
         }
         __syncthreads();
-        unsigned qa[8][4];
+        unsigned qh[8][2], ql[8][2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint4 h = *reinterpret_cast<const uint4*>(&S.qh[g][32 * t + 8 * i]), l = *reinterpret_cast<const uint4*>(&S.ql[g][32 * t + 8 * i]);
-            qa[2 * i][0] = h.x; qa[2 * i][2] = h.y; qa[2 * i + 1][0] = h.z; qa[2 * i + 1][2] = h.w;
-            qa[2 * i][1] = l.x; qa[2 * i][3] = l.y; qa[2 * i + 1][1] = l.z; qa[2 * i + 1][3] = l.w;
+            qh[2 * i][0] = h.x; qh[2 * i][1] = h.y; qh[2 * i + 1][0] = h.z; qh[2 * i + 1][1] = h.w;
+            ql[2 * i][0] = l.x; ql[2 * i][1] = l.y; ql[2 * i + 1][0] = l.z; ql[2 * i + 1][1] = l.w;
         }
-        const float factor = S.factor[g], qsum = S.qsum[g] * factor;
-        const int my_token = min(seg.e.row0 + g, seg.e.rows - 1) / A.group;
-        const int row_lo = kv_row_lo(A, seg.e, my_token), row_hi = kv_row_hi(A, seg.e, my_token);
-        // tokens that all rows of the tile see need no mask
-        const int all_lo = kv_row_lo(A, seg.e, (min(seg.e.rows, seg.e.row0 + ROWS) - 1) / A.group), all_hi = kv_row_hi(A, seg.e, seg.e.row0 / A.group);
-
-        float o[16][4];
+        // this thread's scores and results are of rows 2 t and 2 t + 1
+        const float2 factor = *reinterpret_cast<const float2*>(&S.factor[2 * t]), qsum = *reinterpret_cast<const float2*>(&S.qsum[2 * t]);
+        float o[8][4];                                   // (coordinate 16 g + 2 j, rows 2 t, 2 t + 1), (coordinate 16 g + 2 j + 1, the same)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-        float m = -INFINITY, l = 0.f, add = 0.f;
-        const unsigned order = (t & 1) ? 0x1032u : 0x3210u;
+        for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+        float m0 = NONE, m1 = NONE, mw0 = NONE, mw1 = NONE, up0 = 0.f, up1 = 0.f, l0 = 0.f, l1 = 0.f, add0 = 0.f, add1 = 0.f;     // up = 64 2^(m - M)
 
-        const int stop = min(units, seg.at + seg.e.units);
+        const int stop = min(units, seg.at + seg.e.units), tok_at = (seg.e.lo / UNIT - seg.at) * UNIT;
         for (; mine < stop; mine += WARPS) {
-            const int st = done % STAGES;
-            if (!dead && !mbar_wait_warp(&S.abort, &S.full[w][st], (unsigned)(done / STAGES) & 1u, P.status, 61)) dead = true;
+            if (!dead && !mbar_wait_warp(&S.abort, &S.full[w][st], phase, P.status, 61)) dead = true;
             const Stage<ASYM>& X = S.ring[w][st];
             const unsigned valid = S.valid[w][st];
-            const int tok0 = (seg.e.lo / UNIT + mine - seg.at) * UNIT;
-            const bool plain = valid == 3u && tok0 >= all_lo && tok0 + UNIT <= all_hi;
-#pragma unroll
+            const int tok0 = tok_at + mine * UNIT;
+            const bool plain = valid == 3u && tok0 >= S.all_lo && tok0 + UNIT <= S.all_hi;
+#pragma unroll 1
             for (int h = 0; h < 2; ++h) {                // sixteen tokens at a time
-                float s[2][4];
+                // row g of an operand is token g ^ ((g >> 1) & 1), row g + 8 the one 8 further: see the values
+                const int tg = 16 * h + (g ^ ((g >> 1) & 1));
+                const uint4 ka = *reinterpret_cast<const uint4*>(X.k + tg * KV_ROW + 16 * t), kb = *reinterpret_cast<const uint4*>(X.k + (tg + 8) * KV_ROW + 16 * t);
+                const unsigned wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+                float s[4] = {0.f, 0.f, 0.f, 0.f}, r[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
-                    const uint4 kw = *reinterpret_cast<const uint4*>(X.k + (16 * h + 8 * b + g) * KV_ROW + 16 * t);
-                    const unsigned word[4] = {kw.x, kw.y, kw.z, kw.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        unsigned c[4];
-                        codes_f16<ASYM>(word[i], c);
-                        mma_f16(s[b], qa[2 * i], c[0], c[1]);
-                        mma_f16(s[b], qa[2 * i + 1], c[2], c[3]);
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    unsigned a[4], b[4];
+                    codes_f16<ASYM>(wa[i], a);
+                    codes_f16<ASYM>(wb[i], b);
+                    mma_f16(s, a[0], b[0], a[1], b[1], qh[2 * i]);
+                    mma_f16(r, a[0], b[0], a[1], b[1], ql[2 * i]);
+                    mma_f16(s, a[2], b[2], a[3], b[3], qh[2 * i + 1]);
+                    mma_f16(r, a[2], b[2], a[3], b[3], ql[2 * i + 1]);
                 }
-                // scores of this thread's row for tokens 2 t, 2 t + 1 of both groups of 8
-                float z[4], vs[4], vl[4];
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int at = 16 * h + 8 * b + 2 * t;
-                    float k0, k1, l0 = 0.f, l1 = 0.f;
-                    if (ASYM) {
-                        const float4 kk = *reinterpret_cast<const float4*>(X.ks + 8 * at), vv = *reinterpret_cast<const float4*>(X.vs + 8 * at);
-                        k0 = kk.x; l0 = kk.y; k1 = kk.z; l1 = kk.w;
-                        vs[2 * b] = vv.x; vl[2 * b] = vv.y; vs[2 * b + 1] = vv.z; vl[2 * b + 1] = vv.w;
-                    } else {
-                        const float2 kk = *reinterpret_cast<const float2*>(X.ks + 4 * at), vv = *reinterpret_cast<const float2*>(X.vs + 4 * at);
-                        k0 = kk.x; k1 = kk.y;
-                        vs[2 * b] = vv.x; vs[2 * b + 1] = vv.y;
-                        vl[2 * b] = vl[2 * b + 1] = 0.f;
-                    }
-                    const float d0 = fmaf(s[b][2], 1.f / 2048.f, s[b][0]), d1 = fmaf(s[b][3], 1.f / 2048.f, s[b][1]);
-                    z[2 * b] = d0 * (k0 * factor);
-                    z[2 * b + 1] = d1 * (k1 * factor);
-                    if (ASYM) {
-                        z[2 * b] = fmaf(l0, qsum, z[2 * b]);
-                        z[2 * b + 1] = fmaf(l1, qsum, z[2 * b + 1]);
-                    }
+                float va, vb, la = 0.f, lb = 0.f, z[4];  // (token, row 2 t), (token, row 2 t + 1), (token + 8, the same)
+                if (ASYM) {
+                    const float2 sa = *reinterpret_cast<const float2*>(X.ks + 8 * tg), sb = *reinterpret_cast<const float2*>(X.ks + 8 * (tg + 8));
+                    const float2 ua = *reinterpret_cast<const float2*>(X.vs + 8 * tg), ub = *reinterpret_cast<const float2*>(X.vs + 8 * (tg + 8));
+                    z[0] = fmaf(s[0] + r[0], sa.x * factor.x, sa.y * qsum.x);
+                    z[1] = fmaf(s[1] + r[1], sa.x * factor.y, sa.y * qsum.y);
+                    z[2] = fmaf(s[2] + r[2], sb.x * factor.x, sb.y * qsum.x);
+                    z[3] = fmaf(s[3] + r[3], sb.x * factor.y, sb.y * qsum.y);
+                    va = ua.x; la = ua.y; vb = ub.x; lb = ub.y;
+                } else {
+                    const float sa = *reinterpret_cast<const float*>(X.ks + 4 * tg), sb = *reinterpret_cast<const float*>(X.ks + 4 * (tg + 8));
+                    va = *reinterpret_cast<const float*>(X.vs + 4 * tg);
+                    vb = *reinterpret_cast<const float*>(X.vs + 4 * (tg + 8));
+                    z[0] = (s[0] + r[0]) * (sa * factor.x);
+                    z[1] = (s[1] + r[1]) * (sa * factor.y);
+                    z[2] = (s[2] + r[2]) * (sb * factor.x);
+                    z[3] = (s[3] + r[3]) * (sb * factor.y);
                 }
                 if (!plain) {
                     const bool page = (valid >> h) & 1;
+                    const int2 lo = *reinterpret_cast<const int2*>(&S.row_lo[2 * t]), hi = *reinterpret_cast<const int2*>(&S.row_hi[2 * t]);
+                    const int ta = tok0 + tg, tb = ta + 8;
+                    if (!page || ta < lo.x || ta >= hi.x) z[0] = -INFINITY;
+                    if (!page || ta < lo.y || ta >= hi.y) z[1] = -INFINITY;
+                    if (!page || tb < lo.x || tb >= hi.x) z[2] = -INFINITY;
+                    if (!page || tb < lo.y || tb >= hi.y) z[3] = -INFINITY;
+                    // scales of tokens that no row of this thread sees may be anything
+                    if (z[0] == -INFINITY && z[1] == -INFINITY) va = la = 0.f;
+                    if (z[2] == -INFINITY && z[3] == -INFINITY) vb = lb = 0.f;
+                }
+                float p[4], x[4];
+                auto weigh = [&]() {
+                    p[0] = ex2(z[0] - m0);
+                    p[1] = ex2(z[1] - m1);
+                    p[2] = ex2(z[2] - m0);
+                    p[3] = ex2(z[3] - m1);
+                    x[0] = p[0] * (va * up0);
+                    x[1] = p[1] * (va * up1);
+                    x[2] = p[2] * (vb * up0);
+                    x[3] = p[3] * (vb * up1);
+                };
+                weigh();
+                if (__any_sync(0xffffffffu, fmaxf(z[0], z[2]) > m0 + MOVE || fmaxf(z[1], z[3]) > m1 + MOVE || fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) > W_MOST)) {
+                    const float ga = __log2f(va), gb = __log2f(vb);
+                    float t0 = fmaxf(z[0], z[2]), t1 = fmaxf(z[1], z[3]), u0 = fmaxf(z[0] + ga, z[2] + gb), u1 = fmaxf(z[1] + ga, z[3] + gb);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int tok = tok0 + 16 * h + 8 * (i >> 1) + 2 * t + (i & 1);
-                        if (!page || tok < row_lo || tok >= row_hi) {
-                            z[i] = -INFINITY;
-                            vs[i] = vl[i] = 0.f;
-                        }
+                    for (int k = 4; k < 32; k <<= 1) {
+                        t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, k));
+                        t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, k));
+                        u0 = fmaxf(u0, __shfl_xor_sync(0xffffffffu, u0, k));
+                        u1 = fmaxf(u1, __shfl_xor_sync(0xffffffffu, u1, k));
                     }
-                }
-                const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
-                if (__any_sync(0xffffffffu, top > m + MOVE)) {
-                    float mx = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                    mx = fmaxf(mx, m);
-                    const float keep = mx == -INFINITY ? 1.f : ex2(m - mx);
-                    m = mx;
-                    l *= keep;
-                    add *= keep;
+                    t0 = fmaxf(t0, m0);
+                    t1 = fmaxf(t1, m1);
+                    u0 = fmaxf(u0, mw0);
+                    u1 = fmaxf(u1, mw1);
+                    const float k0 = ex2(m0 - t0), k1 = ex2(m1 - t1), y0 = ex2(mw0 - u0), y1 = ex2(mw1 - u1);
+                    m0 = t0; m1 = t1; mw0 = u0; mw1 = u1;
+                    up0 = W_UP * ex2(fminf(m0 - mw0, 100.f));                // no values but zeros: M stays where it was
+                    up1 = W_UP * ex2(fminf(m1 - mw1, 100.f));
+                    l0 *= k0; l1 *= k1; add0 *= k0; add1 *= k1;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        o[i][0] *= keep; o[i][1] *= keep; o[i][2] *= keep; o[i][3] *= keep;
+                    for (int i = 0; i < 8; ++i) {
+                        o[i][0] *= y0; o[i][1] *= y1; o[i][2] *= y0; o[i][3] *= y1;
                     }
+                    weigh();
                 }
-                const float base = m == -INFINITY ? 0.f : m;
-                unsigned pa[4];
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const float p0 = ex2(z[2 * b] - base), p1 = ex2(z[2 * b + 1] - base);
-                    l += p0 + p1;
-                    if (ASYM) add = fmaf(p0, vl[2 * b], fmaf(p1, vl[2 * b + 1], add));
-                    const float w0 = p0 * vs[2 * b], w1 = p1 * vs[2 * b + 1];
-                    const __nv_bfloat162 hi = __floats2bfloat162_rn(w0, w1);
-                    const float2 back = __bfloat1622float2(hi);
-                    pa[2 * b] = __byte_perm(as_u(hi), 0, order);
-                    pa[2 * b + 1] = __byte_perm(as_u(__floats2bfloat162_rn(w0 - back.x, w1 - back.y)), 0, order);
+                l0 += p[0] + p[2];
+                l1 += p[1] + p[3];
+                if (ASYM) {
+                    add0 = fmaf(p[0], la, fmaf(p[2], lb, add0));
+                    add1 = fmaf(p[1], la, fmaf(p[3], lb, add1));
                 }
-                // values: coordinates 16 g .. of tokens 2 t, 2 t + 1 of both groups, the second one first where t is odd: a load then
-                // takes two even and two odd rows, which lie in different halves of the banks
+                unsigned bh[2], bl[2];
+                {
+                    const __half2 ha = __floats2half2_rn(x[0], x[1]), hb = __floats2half2_rn(x[2], x[3]);
+                    const float2 ra = __half22float2(ha), rb = __half22float2(hb);
+                    bh[0] = transposed(as_u(ha));
+                    bh[1] = transposed(as_u(hb));
+                    bl[0] = transposed(as_u(__floats2half2_rn(x[0] - ra.x, x[1] - ra.y)));
+                    bl[1] = transposed(as_u(__floats2half2_rn(x[2] - rb.x, x[3] - rb.y)));
+                }
+                // values: coordinates 16 g .. of the tokens that rows 2 t, 2 t + 1 (and 8 further) stand for, in their order: a load
+                // takes two even and two odd tokens, which lie in different halves of the banks
                 const unsigned char* vp = X.v + (16 * h + 2 * t) * KV_ROW + 8 * g;
                 const uint2 v0 = *reinterpret_cast<const uint2*>(vp + (t & 1) * KV_ROW), v1 = *reinterpret_cast<const uint2*>(vp + (~t & 1) * KV_ROW);
                 const uint2 v2 = *reinterpret_cast<const uint2*>(vp + (8 + (t & 1)) * KV_ROW), v3 = *reinterpret_cast<const uint2*>(vp + (8 + (~t & 1)) * KV_ROW);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const unsigned sel = (i & 1) ? 0x7632u : 0x5410u;
-                    unsigned c0[4], c1[4];
-                    codes_bf16<ASYM>(__byte_perm(i < 2 ? v0.x : v0.y, i < 2 ? v1.x : v1.y, sel), c0);
-                    codes_bf16<ASYM>(__byte_perm(i < 2 ? v2.x : v2.y, i < 2 ? v3.x : v3.y, sel), c1);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) mma_bf16(o[4 * i + j], pa, c0[j], c1[j]);
+                    unsigned a[4], b[4];
+                    codes_f16<ASYM>(__byte_perm(i < 2 ? v0.x : v0.y, i < 2 ? v1.x : v1.y, sel), a);
+                    codes_f16<ASYM>(__byte_perm(i < 2 ? v2.x : v2.y, i < 2 ? v3.x : v3.y, sel), b);
+                    mma_f16(o[2 * i], a[0], a[1], b[0], b[1], bh);
+                    mma_f16(o[2 * i + 1], a[2], a[3], b[2], b[3], bh);
+                    mma_f16(o[2 * i], a[0], a[1], b[0], b[1], bl);
+                    mma_f16(o[2 * i + 1], a[2], a[3], b[2], b[3], bl);
                 }
             }
-            ++done;
+            if (++st == STAGES) {
+                st = 0;
+                phase ^= 1u;
+            }
             __syncwarp();
             if (!dead) issue();
         }
 
         // ---- the warps' sums ----
 #pragma unroll
-        for (int h = 1; h < 4; h <<= 1) {
-            l += __shfl_xor_sync(0xffffffffu, l, h);
-            add += __shfl_xor_sync(0xffffffffu, add, h);
+        for (int k = 4; k < 32; k <<= 1) {
+            l0 += __shfl_xor_sync(0xffffffffu, l0, k);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, k);
+            add0 += __shfl_xor_sync(0xffffffffu, add0, k);
+            add1 += __shfl_xor_sync(0xffffffffu, add1, k);
         }
-        if (t == 0) {
-            S.m[w][g] = m;
-            S.l[w][g] = l;
-            S.add[w][g] = add;
+        if (g == 0) {
+            *reinterpret_cast<float2*>(&S.m[w][2 * t]) = make_float2(m0, m1);
+            *reinterpret_cast<float2*>(&S.l[w][2 * t]) = make_float2(l0, l1);
+            *reinterpret_cast<float2*>(&S.add[w][2 * t]) = make_float2(add0, add1);
+            *reinterpret_cast<float2*>(&S.mw[w][2 * t]) = make_float2(mw0, mw1);
         }
-        // thread (g, t): row g, coordinates 32 t .. 32 t + 31
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const int i = 4 * (c & 3), k = c >> 2;
-            const float4 x = make_float4(o[i][k] + o[i][k + 2], o[i + 1][k] + o[i + 1][k + 2], o[i + 2][k] + o[i + 2][k + 2], o[i + 3][k] + o[i + 3][k + 2]);
-            *reinterpret_cast<float4*>(&S.part[w][g * 128 + 32 * t + 4 * (c ^ (lane & 7))]) = x;
+        for (int c = 0; c < 4; ++c) {
+            float* to = &S.part[w][2 * t * 128 + 16 * g + 4 * (c ^ t)];
+            *reinterpret_cast<float4*>(to) = make_float4(o[2 * c][0], o[2 * c][2], o[2 * c + 1][0], o[2 * c + 1][2]);
+            *reinterpret_cast<float4*>(to + 128) = make_float4(o[2 * c][1], o[2 * c][3], o[2 * c + 1][1], o[2 * c + 1][3]);
         }
         __syncthreads();
         const bool starts = seg.at >= 0, ends = seg.at + seg.e.units <= units;
         if (w < 2) {
             const int row = 4 * w + (lane >> 3), l8 = lane & 7;
-            float top = S.m[0][row];
+            float top = S.m[0][row], top_w = S.mw[0][row];
 #pragma unroll
-            for (int i = 1; i < WARPS; ++i) top = fmaxf(top, S.m[i][row]);
+            for (int i = 1; i < WARPS; ++i) {
+                top = fmaxf(top, S.m[i][row]);
+                top_w = fmaxf(top_w, S.mw[i][row]);
+            }
             float y[16], total = 0.f, extra = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) y[i] = 0.f;
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) {
-                const float keep = S.m[i][row] == -INFINITY && top == -INFINITY ? 1.f : ex2(S.m[i][row] - top);
+                const float keep = ex2(S.m[i][row] - top), keep_w = ex2(S.mw[i][row] - top_w);
                 total = fmaf(S.l[i][row], keep, total);
                 extra = fmaf(S.add[i][row], keep, extra);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {            // coordinates 64 (q >> 1) + 8 l8 + 4 (q & 1) ..
-                    const int at = 64 * (q >> 1) + 8 * l8 + 4 * (q & 1), who = 4 * row + (at >> 5);
-                    const float4 x = *reinterpret_cast<const float4*>(&S.part[i][row * 128 + (at & ~31) + 4 * (((at & 31) >> 2) ^ (who & 7))]);
-                    y[4 * q] = fmaf(x.x, keep, y[4 * q]);
-                    y[4 * q + 1] = fmaf(x.y, keep, y[4 * q + 1]);
-                    y[4 * q + 2] = fmaf(x.z, keep, y[4 * q + 2]);
-                    y[4 * q + 3] = fmaf(x.w, keep, y[4 * q + 3]);
+                    const int at = 64 * (q >> 1) + 8 * l8 + 4 * (q & 1);
+                    const float4 x = *reinterpret_cast<const float4*>(&S.part[i][row * 128 + (at & ~15) + 4 * (((at >> 2) & 3) ^ (row >> 1))]);
+                    y[4 * q] = fmaf(x.x, keep_w, y[4 * q]);
+                    y[4 * q + 1] = fmaf(x.y, keep_w, y[4 * q + 1]);
+                    y[4 * q + 2] = fmaf(x.z, keep_w, y[4 * q + 2]);
+                    y[4 * q + 3] = fmaf(x.w, keep_w, y[4 * q + 3]);
                 }
             }
             if (starts && ends) {
-                const float by = total == 0.f ? 0.f : 1.f / total;
-                kv_hadamard(y, l8);
-                if (l8 == 0) y[0] = fmaf(extra, 128.f, y[0]);                // the transform of a row of `extra`
+                finish(y, l8, top, top_w, total, extra);
                 if (seg.e.row0 + row < seg.e.rows) {
                     int token, head;
                     row_of(A, seg, row, token, head);
                     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (seg.e.first + token) * A.out_token + head * A.out_head;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) y[i] *= by * KV_NORM;
                     if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
                     if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
                 }
@@ -426,6 +474,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                     part[ROWS * 128 + row] = top;
                     part[ROWS * 128 + ROWS + row] = total;
                     part[ROWS * 128 + 2 * ROWS + row] = extra;
+                    part[ROWS * 128 + 3 * ROWS + row] = top_w;
                 }
                 if (threadIdx.x == 0 && starts) {
                     const int beyond = seg.at + seg.e.units - units;
@@ -436,7 +485,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
         if (seg.at + seg.e.units >= units) break;
         kv_next(A, seg, P.line.entries, P.line.tiles, ROWS, UNIT);
     }
-    if (dead) drain_copies(S.full[w], STAGES, fetched);
+    if (dead) drain_copies(S.full[w], STAGES, (fetch - w) / WARPS);
 }
 
 // The segments that several blocks share: block b joins the one that starts in block b, eight lanes a row.
@@ -452,34 +501,31 @@ __global__ __launch_bounds__(64) void k_kv_attn_join(const __grid_constant__ Arg
     s.head = j.head;
     s.e = kv_entry(A, j.index, P.line.tiles, ROWS, UNIT);
     const int row = threadIdx.x >> 3, l8 = threadIdx.x & 7;
-    float top = -INFINITY, total = 0.f, extra = 0.f, y[16];
+    float top = NONE, top_w = NONE, total = 0.f, extra = 0.f, y[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = 0.f;
     for (int b = 0; b < j.blocks; ++b) {
         const float* part = P.parts + ((long long)(blockIdx.x + b) * 2 + (b == 0 ? 1 : 0)) * PART;
-        const float m = part[ROWS * 128 + row], mx = fmaxf(m, top);
-        const float keep = mx == -INFINITY ? 1.f : ex2(top - mx), more = mx == -INFINITY ? 1.f : ex2(m - mx);
+        const float m = part[ROWS * 128 + row], mx = fmaxf(m, top), mw = part[ROWS * 128 + 3 * ROWS + row], mxw = fmaxf(mw, top_w);
+        const float keep = ex2(top - mx), more = ex2(m - mx), keep_w = ex2(top_w - mxw), more_w = ex2(mw - mxw);
         top = mx;
+        top_w = mxw;
         total = total * keep + part[ROWS * 128 + ROWS + row] * more;
         extra = extra * keep + part[ROWS * 128 + 2 * ROWS + row] * more;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const float4 x = *reinterpret_cast<const float4*>(part + row * 128 + 64 * (q >> 1) + 8 * l8 + 4 * (q & 1));
-            y[4 * q] = fmaf(x.x, more, y[4 * q] * keep);
-            y[4 * q + 1] = fmaf(x.y, more, y[4 * q + 1] * keep);
-            y[4 * q + 2] = fmaf(x.z, more, y[4 * q + 2] * keep);
-            y[4 * q + 3] = fmaf(x.w, more, y[4 * q + 3] * keep);
+            y[4 * q] = fmaf(x.x, more_w, y[4 * q] * keep_w);
+            y[4 * q + 1] = fmaf(x.y, more_w, y[4 * q + 1] * keep_w);
+            y[4 * q + 2] = fmaf(x.z, more_w, y[4 * q + 2] * keep_w);
+            y[4 * q + 3] = fmaf(x.w, more_w, y[4 * q + 3] * keep_w);
         }
     }
-    const float by = total == 0.f ? 0.f : 1.f / total;
-    kv_hadamard(y, l8);
-    if (l8 == 0) y[0] = fmaf(extra, 128.f, y[0]);
+    finish(y, l8, top, top_w, total, extra);
     if (s.e.row0 + row >= s.e.rows) return;
     int token, head;
     row_of(A, s, row, token, head);
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (s.e.first + token) * A.out_token + head * A.out_head;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] *= by * KV_NORM;
     if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
     if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
 }
