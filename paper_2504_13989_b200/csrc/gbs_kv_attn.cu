@@ -5,11 +5,14 @@
 // eight results instead of to every cached row.
 //
 // What bounds it is the cache, 136 or 144 bytes a token and KV head, read once, and next to it the conversion of 256 codes a token.
-// The codes are the tall operand of both products (16 tokens, then 16 coordinates, by 8 query rows), so no row of the matrix unit is idle, and
-// each number of the other operand is given as a sum of two fp16 numbers, 22 bits: q = hi + lo and w = p Delta_v = hi + lo.  Layouts are
-// chosen so that codes go from shared memory to the operand registers without being moved between threads: the order of the 128
-// coordinates of a score, of a group's 16 tokens and of the 128 rows of the result is free, as long as both operands have the same.  Only the weights are
-// transposed on the way (movmatrix).  A nibble becomes a number by putting it into the mantissa of 1024 and subtracting that, exactly.
+// The codes are the tall operand of both products (16 tokens, then 16 coordinates, by 8 query rows), so no row of the matrix unit is idle.
+// Scores are integers: key codes are bytes after a mask and a shift (3 operations for 8 codes), and a query row is an integer of 16 bits
+// per coordinate, in two pieces of 8; sums are exact, and the offset 8 of symmetric codes is the value that they start from.  Weights span too many binary places for that:
+// values become fp16 (a nibble in the mantissa of 1024, which is subtracted again, exactly; 9 operations for 8 codes).  In fp16 for both products, with
+// the weights in two pieces as well, a unit took 797 instructions instead of REPLACE, and attend over 16 x 32 x 4096 tokens 107 us instead of REPLACE.
+// Layouts are chosen so that codes go from shared memory to the operand registers without being moved between threads: the order of the 128
+// coordinates of a score, of a group's 16 tokens and of the 128 rows of the result is free, as long as both operands have the same.
+// Only the weights are transposed on the way (movmatrix).
 //
 // Two running maxima: m of the scores z (log2), as in any softmax, and M of z + log2 Delta_v, which keeps w inside fp16 whatever the
 // sizes of the values: w = 2^(z - m) Delta_v 2^(m - M).  They are moved only when a score exceeds m by 8 or w its range, which is rare.
@@ -43,8 +46,9 @@ struct Smem {
     Stage<ASYM> ring[WARPS][STAGES];
     float part[WARPS][ROWS * 128];                   // 16-byte pieces c of each 64 bytes of rows 2 t, 2 t + 1 at c ^ t
     float m[WARPS][ROWS], l[WARPS][ROWS], add[WARPS][ROWS], mw[WARPS][ROWS];
-    __half qh[ROWS][128], ql[ROWS][128];             // coordinates in the order of the operand, see place()
-    float factor[ROWS], qsum[ROWS];
+    signed char qh[ROWS][128], ql[ROWS][128];        // a row's integers, upper and lower byte; of 8 coordinates the even ones first
+    float factor[ROWS];
+    int qsum[ROWS];
     int row_lo[ROWS], row_hi[ROWS], all_lo, all_hi;  // tokens that a row sees, and that every row sees
     unsigned long long full[WARPS][STAGES];
     unsigned valid[WARPS][STAGES];                   // bit h: tokens 16 h .. of the unit have a page
@@ -65,6 +69,11 @@ __device__ __forceinline__ void mma_f16(float c[4], unsigned a0, unsigned a1, un
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ void mma_u8(int c[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, const unsigned b[2])
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
 }
 // 8 x 8 16-bit numbers, a row in four lanes: rows become columns
 __device__ __forceinline__ unsigned transposed(unsigned x)
@@ -102,21 +111,6 @@ __device__ __forceinline__ void codes_f16(unsigned w, unsigned out[4])
     out[1] = as_u(__hfma2(as_h(and_xor(w, 0x00f000f0u, HIGH)), by, off16));
     out[2] = as_u(__hsub2(as_h(and_xor(w8, 0x000f000fu, LOW)), off));
     out[3] = as_u(__hfma2(as_h(and_xor(w8, 0x00f000f0u, HIGH)), by, off16));
-}
-
-// where coordinate 32 t + 8 w + n stands in a query row: operand register (w, n & 3) of thread t holds n and n + 4
-__device__ __forceinline__ void store_row(__half* row, int l8, const __half h[16])
-{
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const __half* x = h + 8 * half;
-        uint4 u;
-        u.x = as_u(__halves2half2(x[0], x[4]));
-        u.y = as_u(__halves2half2(x[1], x[5]));
-        u.z = as_u(__halves2half2(x[2], x[6]));
-        u.w = as_u(__halves2half2(x[3], x[7]));
-        *reinterpret_cast<uint4*>(row + 64 * half + 8 * l8) = u;
-    }
 }
 
 // sums of w c, of p and of p lo -> the result: sum / 64 2^(M - m) / total + extra / total, turned back
@@ -234,25 +228,37 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(y[i]));
 #pragma unroll
             for (int h = 1; h < 8; h <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, h));
-            const int e = min(max((int)(__float_as_uint(m) >> 23), 1), 252);
-            // 2^(139 - e) and its inverse: the largest coordinate is just below 2^13, what is left of it above 2^-24
-            const float down = __uint_as_float((unsigned)(266 - max(e, 13)) << 23), up = __uint_as_float((unsigned)(max(e, 13) - 12) << 23);
-            __half hi[16], lo[16];
-            float sum = 0.f;
+            // integers of up to 32512, whose upper byte is at most 127; a row that is not finite has a factor that is not a number
+            const float up = m < 1e-30f ? 1.2379400392853803e27f : 1.f;     // 2^90
+            const float by = m > 0.f ? 32512.f / (m * up) : 0.f;
+            int q[16], sum = 0;
+            float wrong = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float v = y[i] * down;
-                hi[i] = __float2half_rn(v);
-                lo[i] = __float2half_rn(v - __half2float(hi[i]));
-                sum += __half2float(hi[i]) + __half2float(lo[i]);
+                q[i] = __float2int_rn(fminf(fmaxf(y[i] * up * by, -32512.f), 32512.f));
+                sum += q[i];
+                wrong += y[i] * 0.f;
             }
 #pragma unroll
-            for (int h = 1; h < 8; h <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, h);
-            store_row(S.qh[row], l8, hi);
-            store_row(S.ql[row], l8, lo);
+            for (int h = 1; h < 8; h <<= 1) {
+                sum += __shfl_xor_sync(0xffffffffu, sum, h);
+                wrong += __shfl_xor_sync(0xffffffffu, wrong, h);
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                unsigned high[2] = {0, 0}, low[2] = {0, 0};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int x = q[8 * half + i], top = (x + 128) >> 8;
+                    high[i & 1] |= (unsigned)(top & 255) << (8 * (i >> 1));
+                    low[i & 1] |= (unsigned)((x - 256 * top) & 255) << (8 * (i >> 1));
+                }
+                *reinterpret_cast<uint2*>(&S.qh[row][64 * half + 8 * l8]) = make_uint2(high[0], high[1]);
+                *reinterpret_cast<uint2*>(&S.ql[row][64 * half + 8 * l8]) = make_uint2(low[0], low[1]);
+            }
             if (l8 == 0) {
-                S.factor[row] = up * (A.scale * (KV_NORM * 1.4426950408889634f));
-                S.qsum[row] = sum * S.factor[row];
+                S.factor[row] = m * (A.scale * (KV_NORM * 1.4426950408889634f / 32512.f)) + wrong;
+                S.qsum[row] = sum;
                 const int token = min(seg.e.row0 + row, seg.e.rows - 1) / A.group;
                 S.row_lo[row] = kv_row_lo(A, seg.e, token);
                 S.row_hi[row] = kv_row_hi(A, seg.e, token);
@@ -263,15 +269,18 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             }
         }
         __syncthreads();
-        unsigned qh[8][2], ql[8][2];
+        unsigned qh[4][2], ql[4][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 h = *reinterpret_cast<const uint4*>(&S.qh[g][32 * t + 8 * i]), l = *reinterpret_cast<const uint4*>(&S.ql[g][32 * t + 8 * i]);
+        for (int i = 0; i < 2; ++i) {
+            const uint4 h = *reinterpret_cast<const uint4*>(&S.qh[g][32 * t + 16 * i]), l = *reinterpret_cast<const uint4*>(&S.ql[g][32 * t + 16 * i]);
             qh[2 * i][0] = h.x; qh[2 * i][1] = h.y; qh[2 * i + 1][0] = h.z; qh[2 * i + 1][1] = h.w;
             ql[2 * i][0] = l.x; ql[2 * i][1] = l.y; ql[2 * i + 1][0] = l.z; ql[2 * i + 1][1] = l.w;
         }
         // this thread's scores and results are of rows 2 t and 2 t + 1
-        const float2 factor = *reinterpret_cast<const float2*>(&S.factor[2 * t]), qsum = *reinterpret_cast<const float2*>(&S.qsum[2 * t]);
+        const float2 factor = *reinterpret_cast<const float2*>(&S.factor[2 * t]);
+        const int2 qsum = *reinterpret_cast<const int2*>(&S.qsum[2 * t]);
+        const int from0 = ASYM ? 0 : -8 * qsum.x, from1 = ASYM ? 0 : -8 * qsum.y;
+        const float lift0 = (float)qsum.x * factor.x, lift1 = (float)qsum.y * factor.y;
         float o[8][4];                                   // (coordinate 16 g + 2 j, rows 2 t, 2 t + 1), (coordinate 16 g + 2 j + 1, the same)
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -290,34 +299,35 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 const int tg = 16 * h + (g ^ ((g >> 1) & 1));
                 const uint4 ka = *reinterpret_cast<const uint4*>(X.k + tg * KV_ROW + 16 * t), kb = *reinterpret_cast<const uint4*>(X.k + (tg + 8) * KV_ROW + 16 * t);
                 const unsigned wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
-                float s[4] = {0.f, 0.f, 0.f, 0.f}, r[4] = {0.f, 0.f, 0.f, 0.f};
+                int s[4] = {0, 0, 0, 0}, r[4] = {from0, from1, from0, from1};
+                constexpr unsigned FLIP = ASYM ? 0u : 0x08080808u;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    unsigned a[4], b[4];
-                    codes_f16<ASYM>(wa[i], a);
-                    codes_f16<ASYM>(wb[i], b);
-                    mma_f16(s, a[0], b[0], a[1], b[1], qh[2 * i]);
-                    mma_f16(r, a[0], b[0], a[1], b[1], ql[2 * i]);
-                    mma_f16(s, a[2], b[2], a[3], b[3], qh[2 * i + 1]);
-                    mma_f16(r, a[2], b[2], a[3], b[3], ql[2 * i + 1]);
+                    const unsigned a0 = and_xor(wa[i], 0x0f0f0f0fu, FLIP), a1 = and_xor(wb[i], 0x0f0f0f0fu, FLIP);
+                    const unsigned a2 = and_xor(wa[i] >> 4, 0x0f0f0f0fu, FLIP), a3 = and_xor(wb[i] >> 4, 0x0f0f0f0fu, FLIP);
+                    mma_u8(s, a0, a1, a2, a3, qh[i]);
+                    mma_u8(r, a0, a1, a2, a3, ql[i]);
                 }
+                float f[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[i] = (float)(256 * s[i] + r[i]);
                 float va, vb, la = 0.f, lb = 0.f, z[4];  // (token, row 2 t), (token, row 2 t + 1), (token + 8, the same)
                 if (ASYM) {
                     const float2 sa = *reinterpret_cast<const float2*>(X.ks + 8 * tg), sb = *reinterpret_cast<const float2*>(X.ks + 8 * (tg + 8));
                     const float2 ua = *reinterpret_cast<const float2*>(X.vs + 8 * tg), ub = *reinterpret_cast<const float2*>(X.vs + 8 * (tg + 8));
-                    z[0] = fmaf(s[0] + r[0], sa.x * factor.x, sa.y * qsum.x);
-                    z[1] = fmaf(s[1] + r[1], sa.x * factor.y, sa.y * qsum.y);
-                    z[2] = fmaf(s[2] + r[2], sb.x * factor.x, sb.y * qsum.x);
-                    z[3] = fmaf(s[3] + r[3], sb.x * factor.y, sb.y * qsum.y);
+                    z[0] = fmaf(f[0], sa.x * factor.x, sa.y * lift0);
+                    z[1] = fmaf(f[1], sa.x * factor.y, sa.y * lift1);
+                    z[2] = fmaf(f[2], sb.x * factor.x, sb.y * lift0);
+                    z[3] = fmaf(f[3], sb.x * factor.y, sb.y * lift1);
                     va = ua.x; la = ua.y; vb = ub.x; lb = ub.y;
                 } else {
                     const float sa = *reinterpret_cast<const float*>(X.ks + 4 * tg), sb = *reinterpret_cast<const float*>(X.ks + 4 * (tg + 8));
                     va = *reinterpret_cast<const float*>(X.vs + 4 * tg);
                     vb = *reinterpret_cast<const float*>(X.vs + 4 * (tg + 8));
-                    z[0] = (s[0] + r[0]) * (sa * factor.x);
-                    z[1] = (s[1] + r[1]) * (sa * factor.y);
-                    z[2] = (s[2] + r[2]) * (sb * factor.x);
-                    z[3] = (s[3] + r[3]) * (sb * factor.y);
+                    z[0] = f[0] * (sa * factor.x);
+                    z[1] = f[1] * (sa * factor.y);
+                    z[2] = f[2] * (sb * factor.x);
+                    z[3] = f[3] * (sb * factor.y);
                 }
                 if (!plain) {
                     const bool page = (valid >> h) & 1;
@@ -374,15 +384,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                     add0 = fmaf(p[0], la, fmaf(p[2], lb, add0));
                     add1 = fmaf(p[1], la, fmaf(p[3], lb, add1));
                 }
-                unsigned bh[2], bl[2];
-                {
-                    const __half2 ha = __floats2half2_rn(x[0], x[1]), hb = __floats2half2_rn(x[2], x[3]);
-                    const float2 ra = __half22float2(ha), rb = __half22float2(hb);
-                    bh[0] = transposed(as_u(ha));
-                    bh[1] = transposed(as_u(hb));
-                    bl[0] = transposed(as_u(__floats2half2_rn(x[0] - ra.x, x[1] - ra.y)));
-                    bl[1] = transposed(as_u(__floats2half2_rn(x[2] - rb.x, x[3] - rb.y)));
-                }
+                const unsigned b[2] = {transposed(as_u(__floats2half2_rn(x[0], x[1]))), transposed(as_u(__floats2half2_rn(x[2], x[3])))};
                 // values: coordinates 16 g .. of the tokens that rows 2 t, 2 t + 1 (and 8 further) stand for, in their order: a load
                 // takes two even and two odd tokens, which lie in different halves of the banks
                 const unsigned char* vp = X.v + (16 * h + 2 * t) * KV_ROW + 8 * g;
@@ -391,13 +393,11 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const unsigned sel = (i & 1) ? 0x7632u : 0x5410u;
-                    unsigned a[4], b[4];
-                    codes_f16<ASYM>(__byte_perm(i < 2 ? v0.x : v0.y, i < 2 ? v1.x : v1.y, sel), a);
-                    codes_f16<ASYM>(__byte_perm(i < 2 ? v2.x : v2.y, i < 2 ? v3.x : v3.y, sel), b);
-                    mma_f16(o[2 * i], a[0], a[1], b[0], b[1], bh);
-                    mma_f16(o[2 * i + 1], a[2], a[3], b[2], b[3], bh);
-                    mma_f16(o[2 * i], a[0], a[1], b[0], b[1], bl);
-                    mma_f16(o[2 * i + 1], a[2], a[3], b[2], b[3], bl);
+                    unsigned c[4], e[4];
+                    codes_f16<ASYM>(__byte_perm(i < 2 ? v0.x : v0.y, i < 2 ? v1.x : v1.y, sel), c);
+                    codes_f16<ASYM>(__byte_perm(i < 2 ? v2.x : v2.y, i < 2 ? v3.x : v3.y, sel), e);
+                    mma_f16(o[2 * i], c[0], c[1], e[0], e[1], b);
+                    mma_f16(o[2 * i + 1], c[2], c[3], e[2], e[3], b);
                 }
             }
             if (++st == STAGES) {

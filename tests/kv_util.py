@@ -36,8 +36,9 @@ def attention(cache, q, seqs, cu, causal=True, window=0, scale=0.0, max_len=0, f
     The tolerance, with e the error of a score: the result is a mean of rows vhat with weights p, each off by a factor of at most 1 + 2 e + r
     (numerator and denominator; r: the rounding of the probabilities and of the sums), so off by at most (2 e + r) max|vhat|_2 in any
     coordinate of any basis, and then rounded to bf16 (2^-8 of itself).  e <= scale |q|_2 |khat|_2 (b + 128 2^-23): the query row is rounded to
-    b = 2^-22 of its largest coordinate in each of 128 places (at most sqrt(128) 2^-22 of its norm), or to 11 bits of each coordinate (2^-12, and
-    sqrt(128) 2^-24 for what falls below fp16's normal numbers); 128 products are added up in 24 bits.  r = 2^-15 or 2^-11.
+    1 / 65024 of its largest coordinate in each of 128 places (few rows: at most sqrt(128) / 65024 of its norm), or to 11 bits of each coordinate
+    (2^-12, and sqrt(128) 2^-24 for what falls below fp16's normal numbers); 128 products are added up in 24 bits.  A probability is rounded to
+    11 bits (2^-11: 2^-12, and as much for ex2, log2 and the sums).
     """
     d = cache.plan.info.d
     heads, kvh = q.shape[1], cache.n_kv_heads
@@ -45,8 +46,8 @@ def attention(cache, q, seqs, cu, causal=True, window=0, scale=0.0, max_len=0, f
     want = torch.full(q.shape, float("nan"), dtype=torch.float64, device=q.device)
     tol = torch.full(q.shape, float("nan"), dtype=torch.float64, device=q.device)
     scale = scale or d ** -0.5
-    b = 128 ** 0.5 * 2.0 ** -22 if few else 2.0 ** -12 + 128 ** 0.5 * 2.0 ** -24
-    r = 2.0 ** -15 if few else 2.0 ** -11
+    b = 128 ** 0.5 / 65024 if few else 2.0 ** -12 + 128 ** 0.5 * 2.0 ** -24
+    r = 2.0 ** -11
     for i, seq in enumerate(seqs):
         length, count = int(cache.lengths[seq]), cu[i + 1] - cu[i]
         if count == 0:
