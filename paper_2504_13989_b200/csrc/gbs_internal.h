@@ -203,8 +203,13 @@ struct gbs_kv_attn {
     void* out;
     long long q_token, q_head, out_token, out_head;
 };
-int64_t gbs_kv_attn_workspace(const gbs_plan* p, int group, int max_tokens);
-int gbs_kv_attn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, cudaStream_t stream);
+// gbs_kv_attn.cu : up to GBS_KV_FEW_ROWS query rows of an item and KV head
+#define GBS_KV_FEW_ROWS 16
+int64_t gbs_kv_few_workspace(const gbs_plan* p);
+int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, cudaStream_t stream);
+// gbs_tc_kvattn.cu : more rows
+int64_t gbs_tc_kvattn_workspace(const gbs_plan* p);
+int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, cudaStream_t stream);
 
 #ifdef __CUDACC__
 // Launch on `stream`, its set-up overlapping the end of the launch before it (kernels wait before they touch memory).

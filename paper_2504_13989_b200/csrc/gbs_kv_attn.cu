@@ -17,22 +17,20 @@
 // Two running maxima: m of the scores z (log2), as in any softmax, and M of z + log2 Delta_v, which keeps w inside fp16 whatever the
 // sizes of the values: w = 2^(z - m) Delta_v 2^(m - M).  They are moved only when a score exceeds m by 8 or w its range, which is rare.
 //
-// A warp works alone: it fetches units of 32 tokens (bulk copies into a ring of its own), keeps sums for its tokens in registers, and
-// meets the block's other warps where a segment ends.
-#include <cuda_fp16.h>
-
-#include "gbs_kv_sched.cuh"
+// One warp of a block fetches units of 32 tokens (bulk copies into a ring), four at a time, eight lanes for the up to eight pieces of one.  The
+// others take them in turn, keep sums for their tokens in registers, and meet where a segment ends.
+#include "gbs_kv_attn.cuh"
 #include "gbs_tc_common.cuh"
 
 namespace {
 
 constexpr int ROWS = 8, UNIT = 32;
-constexpr int WARPS = 6, THREADS = 32 * WARPS, STAGES = 3;
-constexpr int PART = ROWS * 128 + 4 * ROWS;          // floats of a partial result: sums, m, total, sum of p lo, M
-constexpr int BLOCKS_PER_SM = 2;
+constexpr int WARPS = 4, THREADS = 32 * WARPS + 32;  // warps that compute, and the one that fetches
+constexpr int STAGES = 3 * WARPS;                    // unit i of a block's line is worked on by warp i % WARPS, from stage i % STAGES
+constexpr int PART = KV_PART<ROWS>;
+constexpr int BLOCKS_PER_SM = 3;
 constexpr float MOVE = 8.f;                          // m moves when a score is so much (log2) above it
-constexpr float NONE = -1e30f;                       // maximum of no scores
-constexpr float W_UP = 64.f, W_MOST = 32768.f;       // w is 64 at M; M moves when one is beyond the other
+constexpr float W_MOST = 32768.f;                    // M moves when a w is beyond that
 
 template <bool ASYM>
 struct Stage {
@@ -43,26 +41,18 @@ struct Stage {
 
 template <bool ASYM>
 struct Smem {
-    Stage<ASYM> ring[WARPS][STAGES];
+    Stage<ASYM> ring[STAGES];
     float part[WARPS][ROWS * 128];                   // 16-byte pieces c of each 64 bytes of rows 2 t, 2 t + 1 at c ^ t
     float m[WARPS][ROWS], l[WARPS][ROWS], add[WARPS][ROWS], mw[WARPS][ROWS];
     signed char qh[ROWS][128], ql[ROWS][128];        // a row's integers, upper and lower byte; of 8 coordinates the even ones first
     float factor[ROWS];
     int qsum[ROWS];
     int row_lo[ROWS], row_hi[ROWS], all_lo, all_hi;  // tokens that a row sees, and that every row sees
-    unsigned long long full[WARPS][STAGES];
-    unsigned valid[WARPS][STAGES];                   // bit h: tokens 16 h .. of the unit have a page
-    KvSeg ahead[WARPS];                              // the segment of the next unit to fetch
-    long long share[WARPS + 3];
+    unsigned long long full[STAGES], empty[STAGES];
+    unsigned valid[STAGES];                          // bit h: tokens 16 h .. of the unit have a page
+    KvSeg seg[2];                                    // the segment that the block works on, and the next one
+    long long share[WARPS + 1 + 3];
     int abort;
-};
-
-struct Args {
-    gbs_kv_attn a;
-    KvLine line;
-    float* parts;                                    // [blocks][2][PART]
-    KvJoin* joins;                                   // [blocks]
-    int* status;
 };
 
 __device__ __forceinline__ void mma_f16(float c[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, const unsigned b[2])
@@ -83,64 +73,21 @@ __device__ __forceinline__ unsigned transposed(unsigned x)
     return y;
 }
 
-__device__ __forceinline__ unsigned as_u(__half2 x) { return *reinterpret_cast<unsigned*>(&x); }
-__device__ __forceinline__ __half2 as_h(unsigned x) { return *reinterpret_cast<__half2*>(&x); }
-
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// (x & mask) ^ with, one operation
-__device__ __forceinline__ unsigned and_xor(unsigned x, unsigned mask, unsigned with)
-{
-    unsigned y;
-    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(y) : "r"(x), "r"(mask), "r"(with));
-    return y;
-}
-// Nibbles (i, i + 4) of a word, i = 0 .. 3, as pairs in fp16.  A symmetric code c is taken as c ^ 8 = c + 8 of four bits.
-template <bool ASYM>
-__device__ __forceinline__ void codes_f16(unsigned w, unsigned out[4])
-{
-    constexpr unsigned LOW = ASYM ? 0x64006400u : 0x64086408u, HIGH = ASYM ? 0x64006400u : 0x64806480u;
-    const __half2 off = __float2half2_rn(ASYM ? 1024.f : 1032.f), off16 = __float2half2_rn(ASYM ? -64.f : -72.f), by = __float2half2_rn(0.0625f);
-    const unsigned w8 = w >> 8;
-    out[0] = as_u(__hsub2(as_h(and_xor(w, 0x000f000fu, LOW)), off));
-    out[1] = as_u(__hfma2(as_h(and_xor(w, 0x00f000f0u, HIGH)), by, off16));
-    out[2] = as_u(__hsub2(as_h(and_xor(w8, 0x000f000fu, LOW)), off));
-    out[3] = as_u(__hfma2(as_h(and_xor(w8, 0x00f000f0u, HIGH)), by, off16));
-}
-
-// sums of w c, of p and of p lo -> the result: sum / 64 2^(M - m) / total + extra / total, turned back
-__device__ __forceinline__ void finish(float y[16], int l8, float top, float top_w, float total, float extra)
-{
-    const float by = total == 0.f ? 0.f : 1.f / total;
-    const float by_w = by * (KV_NORM / W_UP) * ex2(top_w - top);
-    kv_hadamard(y, l8);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] = total != total ? total : y[i] * by_w;
-    if (l8 == 0) y[0] = fmaf(extra * by, 128.f * KV_NORM, y[0]);             // the transform of a row of ones is 128 in its first place
-}
-
-// row of a tile -> token of the item and query head
-__device__ __forceinline__ void row_of(const gbs_kv_attn& A, const KvSeg& s, int row, int& token, int& head)
-{
-    const int r = s.e.row0 + row;
-    token = r / A.group;
-    head = s.head * A.group + (r - token * A.group);
-}
+// the warps that compute
+__device__ __forceinline__ void meet() { asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory"); }
 
 template <bool ASYM>
-__global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __grid_constant__ Args P)
+__global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __grid_constant__ KvAttnArgs P)
 {
     extern __shared__ __align__(128) unsigned char smem_raw[];
     Smem<ASYM>& S = *reinterpret_cast<Smem<ASYM>*>(smem_raw);
     const gbs_kv_attn& A = P.a;
     const int lane = threadIdx.x & 31, w = warp_index(), g = lane >> 2, t = lane & 3;
     if (threadIdx.x == 0) S.abort = 0;
-    if (lane < STAGES) mbar_init(&S.full[w][lane], 1);
+    if (threadIdx.x < STAGES) {
+        mbar_init(&S.full[threadIdx.x], 1);
+        mbar_init(&S.empty[threadIdx.x], 1);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
@@ -152,69 +99,64 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
     if (threadIdx.x == 0) P.joins[blockIdx.x] = KvJoin{0, 0, 0, 0};
     if (units == 0) return;
 
-    // ---- fetching: units w, w + WARPS, .. of the block's line ----
-    const int ps_log = A.c.page_log, T = min(UNIT, 1 << ps_log);
-    const int pieces = T == UNIT ? 4 : 8, half = lane >> 2, piece = lane & 3;
-    const unsigned piece_bytes = piece < 2 ? T * KV_ROW : T * (ASYM ? 8 : 4);
-    const int in_block = piece < 2 ? piece * (KV_ROW << ps_log) : (2 * KV_ROW << ps_log) + (piece - 2) * ((ASYM ? 8 : 4) << ps_log);
-    const int in_slot = piece < 2 ? KV_ROW : (ASYM ? 8 : 4);
-    const int in_stage = (piece < 2 ? piece * UNIT * KV_ROW : 2 * UNIT * KV_ROW + (piece - 2) * Stage<ASYM>::SCALE) + half * (int)piece_bytes;
-    // the next unit to fetch: its place in the line, its first token (this lane's half of it), the end of its segment in the line and in
-    // tokens, this lane's page of it; the segment itself is kept in shared memory
-    int fetch = w, fetch_tok = 0, fetch_end = 0, fetch_hi = 0, fetch_page = -1, lane_off = 0, fetch_st = 0;
-    const int* fetch_row = nullptr;
-    auto look = [&]() {
-        if (fetch >= fetch_end) {
-            if (fetch >= units) return;
-            KvSeg s = S.ahead[w];
-            while (fetch >= s.at + s.e.units) kv_next(A, s, P.line.entries, P.line.tiles, ROWS, UNIT);
-            __syncwarp();
-            if (lane == 0) S.ahead[w] = s;
-            __syncwarp();
-            fetch_end = min(units, s.at + s.e.units);
-            fetch_hi = s.e.hi;
-            fetch_tok = (s.e.lo / UNIT + fetch - s.at) * UNIT + half * 16;
-            fetch_row = A.c.page_table + (long long)s.e.seq * A.c.max_pages;
-            lane_off = s.head * A.c.block_bytes + in_block;
+    if (w == WARPS) {
+        // ---- fetching ----
+        const int ps_log = A.c.page_log, T = min(UNIT, 1 << ps_log);
+        const int mine = lane >> 3, half = (lane >> 2) & 1, piece = lane & 3;
+        const bool part = T < UNIT || half == 0;             // this lane copies a piece
+        const unsigned piece_bytes = piece < 2 ? T * KV_ROW : T * (ASYM ? 8 : 4);
+        const int in_block = piece < 2 ? piece * (KV_ROW << ps_log) : (2 * KV_ROW << ps_log) + (piece - 2) * ((ASYM ? 8 : 4) << ps_log);
+        const int in_slot = piece < 2 ? KV_ROW : (ASYM ? 8 : 4);
+        const int in_stage = (piece < 2 ? piece * UNIT * KV_ROW : 2 * UNIT * KV_ROW + (piece - 2) * Stage<ASYM>::SCALE) + half * (int)piece_bytes;
+        bool dead = false;
+        int at = 0;
+        for (; at < units && !dead;) {
+            const int stop = min(units, seg.at + seg.e.units);
+            const int* row = A.c.page_table + (long long)seg.e.seq * A.c.max_pages;
+            const int off = seg.head * A.c.block_bytes + in_block;
+            int tok = (seg.e.lo / UNIT - seg.at + at + mine) * UNIT + half * 16;
+            int page = part && tok < seg.e.hi ? row[tok >> ps_log] : -1;
+            for (; at < stop; at += 4) {
+                const int u = at + mine, st = u % STAGES, use = u / STAGES;
+                const int next_tok = tok + 4 * UNIT, next = part && at + 4 < stop && next_tok < seg.e.hi ? row[next_tok >> ps_log] : -1;
+                if (u < stop && use > 0 && !mbar_wait(&S.abort, &S.empty[st], (unsigned)(use - 1) & 1u, P.status, 62)) dead = true;
+                if (__any_sync(0xffffffffu, dead)) { dead = true; break; }
+                const bool ok = u < stop && (unsigned)page < (unsigned)A.c.n_pages;
+                const unsigned who = __ballot_sync(0xffffffffu, ok) >> (8 * mine), first = who & 1, second = (who >> 4) & 1;
+                if (u < stop && (lane & 7) == 0) {
+                    S.valid[st] = T == UNIT ? 3u * first : first | second << 1;
+                    mbar_arrive_expect_tx(&S.full[st], (first + second) * (unsigned)(T * (2 * KV_ROW + (ASYM ? 16 : 8))));
+                }
+                __syncwarp();
+                if (ok)
+                    bulk_load(reinterpret_cast<unsigned char*>(&S.ring[st]) + in_stage,
+                              A.c.pages + ((long long)page * A.c.page_bytes + off + (tok & ((1 << ps_log) - 1)) * in_slot), piece_bytes, &S.full[st]);
+                tok = next_tok;
+                page = next;
+            }
+            at = min(at, stop);
+            if (at < units) kv_next(A, seg, P.line.entries, P.line.tiles, ROWS, UNIT);
         }
-        fetch_page = lane < pieces && fetch_tok < fetch_hi ? fetch_row[fetch_tok >> ps_log] : -1;
-    };
-    auto issue = [&]() {
-        if (fetch >= units) return;
-        const bool ok = (unsigned)fetch_page < (unsigned)A.c.n_pages;
-        const unsigned who = __ballot_sync(0xffffffffu, ok);
-        if (lane == 0) {
-            S.valid[w][fetch_st] = T == UNIT ? ((who & 1) ? 3u : 0u) : (who & 1) | ((who >> 4) & 1) << 1;
-            mbar_arrive_expect_tx(&S.full[w][fetch_st], ((who & 1) + ((who >> 4) & 1)) * (unsigned)(T * (2 * KV_ROW + (ASYM ? 16 : 8))));
-        }
-        __syncwarp();
-        if (ok)
-            bulk_load(reinterpret_cast<unsigned char*>(&S.ring[w][fetch_st]) + in_stage,
-                      A.c.pages + ((long long)fetch_page * A.c.page_bytes + lane_off + (fetch_tok & ((1 << ps_log) - 1)) * in_slot), piece_bytes,
-                      &S.full[w][fetch_st]);
-        if (++fetch_st == STAGES) fetch_st = 0;
-        fetch += WARPS;
-        fetch_tok += WARPS * UNIT;
-        look();
-    };
-    if (lane == 0) S.ahead[w] = seg;
-    __syncwarp();
-    look();
-#pragma unroll 1
-    for (int i = 0; i < STAGES; ++i) issue();
+        if (dead) drain_copies(S.full, STAGES, at);
+        return;
+    }
 
     // ---- the segments ----
-    int mine = w, st = 0;                                // this warp's next unit of the line, and its stage
+    int mine = w, st = w;                                    // this warp's next unit of the line, and its stage
     unsigned phase = 0;
     bool dead = false;
-    for (;;) {
+    if (threadIdx.x == 0) S.seg[0] = seg;
+    meet();
+    for (int round = 0;; ++round) {
+        // read where it is needed, not kept in registers
+        const KvSeg& seg = S.seg[round & 1];
         // query rows: four of them per warp, rotated, halved
         if (w < 2) {
             const int row = 4 * w + (lane >> 3), l8 = lane & 7;
             uint4 a = make_uint4(0, 0, 0, 0), b = a;
             if (seg.e.row0 + row < seg.e.rows) {
                 int token, head;
-                row_of(A, seg, row, token, head);
+                kv_row_of(A, seg, row, token, head);
                 const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(A.q) + (seg.e.first + token) * A.q_token + head * A.q_head;
                 if (8 * l8 < A.d) a = *reinterpret_cast<const uint4*>(x + 8 * l8);
                 if (64 + 8 * l8 < A.d) b = *reinterpret_cast<const uint4*>(x + 64 + 8 * l8);
@@ -268,7 +210,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 }
             }
         }
-        __syncthreads();
+        meet();
         unsigned qh[4][2], ql[4][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -288,12 +230,12 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
 
         const int stop = min(units, seg.at + seg.e.units), tok_at = (seg.e.lo / UNIT - seg.at) * UNIT;
         for (; mine < stop; mine += WARPS) {
-            if (!dead && !mbar_wait_warp(&S.abort, &S.full[w][st], phase, P.status, 61)) dead = true;
-            const Stage<ASYM>& X = S.ring[w][st];
-            const unsigned valid = S.valid[w][st];
+            if (!dead && !mbar_wait_warp(&S.abort, &S.full[st], phase, P.status, 61)) dead = true;
+            const Stage<ASYM>& X = S.ring[st];
+            const unsigned valid = S.valid[st];
             const int tok0 = tok_at + mine * UNIT;
             const bool plain = valid == 3u && tok0 >= S.all_lo && tok0 + UNIT <= S.all_hi;
-#pragma unroll 1
+#pragma unroll
             for (int h = 0; h < 2; ++h) {                // sixteen tokens at a time
                 // row g of an operand is token g ^ ((g >> 1) & 1), row g + 8 the one 8 further: see the values
                 const int tg = 16 * h + (g ^ ((g >> 1) & 1));
@@ -303,8 +245,8 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 constexpr unsigned FLIP = ASYM ? 0u : 0x08080808u;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const unsigned a0 = and_xor(wa[i], 0x0f0f0f0fu, FLIP), a1 = and_xor(wb[i], 0x0f0f0f0fu, FLIP);
-                    const unsigned a2 = and_xor(wa[i] >> 4, 0x0f0f0f0fu, FLIP), a3 = and_xor(wb[i] >> 4, 0x0f0f0f0fu, FLIP);
+                    const unsigned a0 = kv_and_xor(wa[i], 0x0f0f0f0fu, FLIP), a1 = kv_and_xor(wb[i], 0x0f0f0f0fu, FLIP);
+                    const unsigned a2 = kv_and_xor(wa[i] >> 4, 0x0f0f0f0fu, FLIP), a3 = kv_and_xor(wb[i] >> 4, 0x0f0f0f0fu, FLIP);
                     mma_u8(s, a0, a1, a2, a3, qh[i]);
                     mma_u8(r, a0, a1, a2, a3, ql[i]);
                 }
@@ -337,16 +279,24 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                     if (!page || ta < lo.y || ta >= hi.y) z[1] = -INFINITY;
                     if (!page || tb < lo.x || tb >= hi.x) z[2] = -INFINITY;
                     if (!page || tb < lo.y || tb >= hi.y) z[3] = -INFINITY;
-                    // scales of tokens that no row of this thread sees may be anything
-                    if (z[0] == -INFINITY && z[1] == -INFINITY) va = la = 0.f;
-                    if (z[2] == -INFINITY && z[3] == -INFINITY) vb = lb = 0.f;
+                    // scales that are no numbers make the scores of the rows that see them none, and those of tokens that no row sees may be anything
+                    if ((z[0] == -INFINITY && z[1] == -INFINITY) || !(fabsf(va) < INFINITY) || !(fabsf(la) < INFINITY)) {
+                        if (z[0] != -INFINITY) z[0] = NAN;
+                        if (z[1] != -INFINITY) z[1] = NAN;
+                        va = la = 0.f;
+                    }
+                    if ((z[2] == -INFINITY && z[3] == -INFINITY) || !(fabsf(vb) < INFINITY) || !(fabsf(lb) < INFINITY)) {
+                        if (z[2] != -INFINITY) z[2] = NAN;
+                        if (z[3] != -INFINITY) z[3] = NAN;
+                        vb = lb = 0.f;
+                    }
                 }
                 float p[4], x[4];
                 auto weigh = [&]() {
-                    p[0] = ex2(z[0] - m0);
-                    p[1] = ex2(z[1] - m1);
-                    p[2] = ex2(z[2] - m0);
-                    p[3] = ex2(z[3] - m1);
+                    p[0] = kv_ex2(z[0] - m0);
+                    p[1] = kv_ex2(z[1] - m1);
+                    p[2] = kv_ex2(z[2] - m0);
+                    p[3] = kv_ex2(z[3] - m1);
                     x[0] = p[0] * (va * up0);
                     x[1] = p[1] * (va * up1);
                     x[2] = p[2] * (vb * up0);
@@ -367,10 +317,10 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                     t1 = fmaxf(t1, m1);
                     u0 = fmaxf(u0, mw0);
                     u1 = fmaxf(u1, mw1);
-                    const float k0 = ex2(m0 - t0), k1 = ex2(m1 - t1), y0 = ex2(mw0 - u0), y1 = ex2(mw1 - u1);
+                    const float k0 = kv_ex2(m0 - t0), k1 = kv_ex2(m1 - t1), y0 = kv_ex2(mw0 - u0), y1 = kv_ex2(mw1 - u1);
                     m0 = t0; m1 = t1; mw0 = u0; mw1 = u1;
-                    up0 = W_UP * ex2(fminf(m0 - mw0, 100.f));                // no values but zeros: M stays where it was
-                    up1 = W_UP * ex2(fminf(m1 - mw1, 100.f));
+                    up0 = W_UP * kv_ex2(fminf(m0 - mw0, 100.f));                // no values but zeros: M stays where it was
+                    up1 = W_UP * kv_ex2(fminf(m1 - mw1, 100.f));
                     l0 *= k0; l1 *= k1; add0 *= k0; add1 *= k1;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -394,18 +344,18 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 for (int i = 0; i < 4; ++i) {
                     const unsigned sel = (i & 1) ? 0x7632u : 0x5410u;
                     unsigned c[4], e[4];
-                    codes_f16<ASYM>(__byte_perm(i < 2 ? v0.x : v0.y, i < 2 ? v1.x : v1.y, sel), c);
-                    codes_f16<ASYM>(__byte_perm(i < 2 ? v2.x : v2.y, i < 2 ? v3.x : v3.y, sel), e);
+                    kv_codes_f16<ASYM>(__byte_perm(i < 2 ? v0.x : v0.y, i < 2 ? v1.x : v1.y, sel), c);
+                    kv_codes_f16<ASYM>(__byte_perm(i < 2 ? v2.x : v2.y, i < 2 ? v3.x : v3.y, sel), e);
                     mma_f16(o[2 * i], c[0], c[1], e[0], e[1], b);
                     mma_f16(o[2 * i + 1], c[2], c[3], e[2], e[3], b);
                 }
             }
-            if (++st == STAGES) {
-                st = 0;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&S.empty[st]);
+            if ((st += WARPS) >= STAGES) {
+                st = w;
                 phase ^= 1u;
             }
-            __syncwarp();
-            if (!dead) issue();
         }
 
         // ---- the warps' sums ----
@@ -428,7 +378,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             *reinterpret_cast<float4*>(to) = make_float4(o[2 * c][0], o[2 * c][2], o[2 * c + 1][0], o[2 * c + 1][2]);
             *reinterpret_cast<float4*>(to + 128) = make_float4(o[2 * c][1], o[2 * c][3], o[2 * c + 1][1], o[2 * c + 1][3]);
         }
-        __syncthreads();
+        meet();
         const bool starts = seg.at >= 0, ends = seg.at + seg.e.units <= units;
         if (w < 2) {
             const int row = 4 * w + (lane >> 3), l8 = lane & 7;
@@ -443,7 +393,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             for (int i = 0; i < 16; ++i) y[i] = 0.f;
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) {
-                const float keep = ex2(S.m[i][row] - top), keep_w = ex2(S.mw[i][row] - top_w);
+                const float keep = kv_ex2(S.m[i][row] - top), keep_w = kv_ex2(S.mw[i][row] - top_w);
                 total = fmaf(S.l[i][row], keep, total);
                 extra = fmaf(S.add[i][row], keep, extra);
 #pragma unroll
@@ -457,10 +407,10 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 }
             }
             if (starts && ends) {
-                finish(y, l8, top, top_w, total, extra);
+                kv_finish(y, l8, top, top_w, total, extra);
                 if (seg.e.row0 + row < seg.e.rows) {
                     int token, head;
-                    row_of(A, seg, row, token, head);
+                    kv_row_of(A, seg, row, token, head);
                     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (seg.e.first + token) * A.out_token + head * A.out_head;
                     if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
                     if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
@@ -483,71 +433,33 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             }
         }
         if (seg.at + seg.e.units >= units) break;
-        kv_next(A, seg, P.line.entries, P.line.tiles, ROWS, UNIT);
-    }
-    if (dead) drain_copies(S.full[w], STAGES, (fetch - w) / WARPS);
-}
-
-// The segments that several blocks share: block b joins the one that starts in block b, eight lanes a row.
-__global__ __launch_bounds__(64) void k_kv_attn_join(const __grid_constant__ Args P)
-{
-    kv_wait_before();
-    kv_let_next();
-    const KvJoin j = P.joins[blockIdx.x];
-    if (j.blocks == 0) return;
-    const gbs_kv_attn& A = P.a;
-    KvSeg s;
-    s.index = j.index;
-    s.head = j.head;
-    s.e = kv_entry(A, j.index, P.line.tiles, ROWS, UNIT);
-    const int row = threadIdx.x >> 3, l8 = threadIdx.x & 7;
-    float top = NONE, top_w = NONE, total = 0.f, extra = 0.f, y[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] = 0.f;
-    for (int b = 0; b < j.blocks; ++b) {
-        const float* part = P.parts + ((long long)(blockIdx.x + b) * 2 + (b == 0 ? 1 : 0)) * PART;
-        const float m = part[ROWS * 128 + row], mx = fmaxf(m, top), mw = part[ROWS * 128 + 3 * ROWS + row], mxw = fmaxf(mw, top_w);
-        const float keep = ex2(top - mx), more = ex2(m - mx), keep_w = ex2(top_w - mxw), more_w = ex2(mw - mxw);
-        top = mx;
-        top_w = mxw;
-        total = total * keep + part[ROWS * 128 + ROWS + row] * more;
-        extra = extra * keep + part[ROWS * 128 + 2 * ROWS + row] * more;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float4 x = *reinterpret_cast<const float4*>(part + row * 128 + 64 * (q >> 1) + 8 * l8 + 4 * (q & 1));
-            y[4 * q] = fmaf(x.x, more_w, y[4 * q] * keep_w);
-            y[4 * q + 1] = fmaf(x.y, more_w, y[4 * q + 1] * keep_w);
-            y[4 * q + 2] = fmaf(x.z, more_w, y[4 * q + 2] * keep_w);
-            y[4 * q + 3] = fmaf(x.w, more_w, y[4 * q + 3] * keep_w);
+        if (w == 0) {
+            KvSeg next = seg;
+            kv_next(A, next, P.line.entries, P.line.tiles, ROWS, UNIT);
+            if (lane == 0) S.seg[(round + 1) & 1] = next;
         }
+        meet();
     }
-    finish(y, l8, top, top_w, total, extra);
-    if (s.e.row0 + row >= s.e.rows) return;
-    int token, head;
-    row_of(A, s, row, token, head);
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (s.e.first + token) * A.out_token + head * A.out_head;
-    if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
-    if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
 }
 
 int blocks_of(const gbs_plan* p) { return p->sm_count * BLOCKS_PER_SM; }
 
 }  // namespace
 
-int64_t gbs_kv_attn_workspace(const gbs_plan* p, int, int)
+int64_t gbs_kv_few_workspace(const gbs_plan* p)
 {
     return (int64_t)blocks_of(p) * (2 * PART * sizeof(float) + sizeof(KvJoin)) + 16;
 }
 
-int gbs_kv_attn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, cudaStream_t stream)
+int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, cudaStream_t stream)
 {
-    Args P = {};
+    KvAttnArgs P = {};
     P.a = A;
     P.line.tile_rows = ROWS;
     P.line.unit = UNIT;
     P.line.tiles = (int)(((int64_t)A.max_tokens * A.group + ROWS - 1) / ROWS);
     P.line.entries = A.n_items * P.line.tiles;
-    P.line.least = 2 * WARPS;
+    P.line.least = 12;
     const int blocks = blocks_of(p);
     P.joins = static_cast<KvJoin*>(workspace);
     P.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + blocks * sizeof(KvJoin));
@@ -558,5 +470,5 @@ int gbs_kv_attn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace,
     if (e != cudaSuccess) return (int)e;
     const int rc = gbs_kv_launch(p, p->asym ? k_kv_attn_few<true> : k_kv_attn_few<false>, dim3((unsigned)blocks), THREADS, smem, stream, P);
     if (rc != 0) return rc;
-    return gbs_kv_launch(p, k_kv_attn_join, dim3((unsigned)blocks), 64, 0, stream, P);
+    return gbs_kv_launch(p, k_kv_attn_join<ROWS, UNIT>, dim3((unsigned)blocks), 256, 0, stream, P);
 }

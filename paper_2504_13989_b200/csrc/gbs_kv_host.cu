@@ -169,6 +169,14 @@ extern "C" int gbs_kv_read(const gbs_plan_t* p, const gbs_kv_cache_t* cache, con
 
 namespace {
 
+// tiles of 8 rows up to here, of 128 beyond
+bool few_rows(int group, int max_tokens) { return (int64_t)max_tokens * group <= GBS_KV_FEW_ROWS; }
+
+int64_t workspace_bytes_of(const gbs_plan* p, int group, int max_tokens)
+{
+    return few_rows(group, max_tokens) ? gbs_kv_few_workspace(p) : gbs_tc_kvattn_workspace(p);
+}
+
 int check_heads(const gbs_kv_view& c, int n_heads, int max_tokens, bool ragged)
 {
     if (n_heads < 1 || n_heads % c.heads != 0 || n_heads / c.heads > 1024) return GBS_ERR_INVALID_ARG;
@@ -186,7 +194,7 @@ extern "C" int gbs_kv_attention_workspace(const gbs_plan_t* p, const gbs_kv_cach
     if (rc == GBS_OK) rc = check_heads(c, n_heads, max_tokens, true);
     if (rc != GBS_OK) return rc;
     if (!bytes_out || n_tokens < 0) return GBS_ERR_INVALID_ARG;
-    *bytes_out = gbs_kv_attn_workspace(p, n_heads / c.heads, max_tokens);
+    *bytes_out = workspace_bytes_of(p, n_heads / c.heads, max_tokens);
     return GBS_OK;
 }
 
@@ -204,7 +212,7 @@ extern "C" int gbs_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache
     if ((flags & ~GBS_KV_CAUSAL) || window < 0 || max_len < 0 || !isfinite(scale)) return GBS_ERR_INVALID_ARG;
     if (n_tokens * n_heads >= 1ll << 31 || (int64_t)n_items * max_tokens * (n_heads / A.c.heads) > 1ll << 28) return GBS_ERR_INVALID_ARG;
     if (empty) return GBS_OK;
-    if (!q || !out || !workspace || workspace_bytes < gbs_kv_attn_workspace(p, n_heads / A.c.heads, max_tokens)) return GBS_ERR_INVALID_ARG;
+    if (!q || !out || !workspace || workspace_bytes < workspace_bytes_of(p, n_heads / A.c.heads, max_tokens)) return GBS_ERR_INVALID_ARG;
     rc = check_strides(p, q_token_stride, q_head_stride);
     if (rc == GBS_OK) rc = check_strides(p, out_token_stride, out_head_stride);
     if (rc != GBS_OK) return rc;
@@ -227,5 +235,8 @@ extern "C" int gbs_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache
     A.q_head = q_head_stride;
     A.out_token = out_token_stride;
     A.out_head = out_head_stride;
-    return on_device(p, [&] { return gbs_kv_attn_launch(p, A, workspace, static_cast<cudaStream_t>(stream)); });
+    return on_device(p, [&] {
+        return few_rows(A.group, max_tokens) ? gbs_kv_few_launch(p, A, workspace, static_cast<cudaStream_t>(stream))
+                                             : gbs_tc_kvattn_launch(p, A, workspace, static_cast<cudaStream_t>(stream));
+    });
 }

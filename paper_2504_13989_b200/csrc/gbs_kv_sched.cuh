@@ -38,21 +38,21 @@ __device__ __forceinline__ KvEntry kv_entry(const gbs_kv_attn& A, int index, int
     KvEntry e;
     const int item = index / tiles, tile = index - item * tiles;
     e.first = item;
+    e.seq = A.seqs ? A.seqs[item] : item;
     int count = 1;
     if (A.cu) {
         e.first = A.cu[item];
         count = A.cu[item + 1] - e.first;
     }
+    if ((unsigned)e.seq >= (unsigned)A.c.n_seqs) e.seq = -1;
+    const int length = e.seq < 0 ? 0 : kv_length(A.c, e.seq);
     // no item has more rows than the call, nor a row outside it, whatever cu holds
     if (e.first < 0 || e.first > (int)A.n_tokens) count = 0;
     else count = min(count, (int)A.n_tokens - e.first);
     e.row0 = tile * tile_rows;
     e.rows = max(0, min(count, A.max_tokens)) * A.group;
-    e.seq = -1;
     e.before = e.length = e.lo = e.hi = e.units = 0;
     if (e.row0 >= e.rows) return e;
-    e.seq = kv_sequence(A.c, A.seqs, item);
-    const int length = e.seq < 0 ? 0 : kv_length(A.c, e.seq);
     e.before = length - count;
     e.length = min(length, A.max_len);
     const int last = min(e.rows, e.row0 + tile_rows) - 1;
