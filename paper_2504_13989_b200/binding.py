@@ -170,6 +170,9 @@ def native():
         for name, f in _PYTHON_METHODS.items():
             if Plan.__dict__.get(name) is f:                      # a method that was replaced stays
                 setattr(Plan, name, _native.method(name, f, Plan.alloc_outputs if name == "rotate_quantize" else None))
+        for name, f in _PYTHON_KV_METHODS.items():
+            if KVCache.__dict__.get(name) is f:
+                setattr(KVCache, name, _native.method(name, f, None))
         _native_module = _native
     return _native_module
 
@@ -573,6 +576,7 @@ class KVCache:
         self.pages, self.page_table, self.lengths, self.refs = pages, page_table, lengths, refs
         self._c = KVCacheStruct(pages.data_ptr(), pages.shape[0], n_kv_heads, page_size, page_table.data_ptr(), lengths.data_ptr(),
                                 refs.data_ptr(), page_table.shape[0], page_table.shape[1])
+        self._calls = native().Pool(plan._calls, pages, page_table, lengths, refs, n_kv_heads, page_size)
 
     @classmethod
     def create(cls, plan: Plan, n_pages: int, n_kv_heads: int, page_size: int, n_seqs: int, max_pages: int, device="cuda:0"):
@@ -712,6 +716,7 @@ class KVCache:
 
 
 # the methods that _native.so has a regular call for
+_PYTHON_KV_METHODS = {name: KVCache.__dict__[name] for name in ("extend", "fork", "free", "append", "read", "attention")}
 _PYTHON_METHODS = {name: Plan.__dict__[name] for name in ("rotate_quantize", "dequantize", "quantized_matmul", "clip_error")}
 
 

@@ -321,13 +321,228 @@ PyObject* calls_clear(PyObject* self, PyObject*)
     Py_RETURN_NONE;
 }
 
-// A method: the names of its arguments in Plan's order, how many must be given, and what to do with them.
+// ---- Pool(calls, pages, page_table, lengths, refs, n_kv_heads, page_size): what the native methods know of a KVCache
+struct Pool {
+    PyObject_HEAD
+    PyObject* calls;          // the plan's Calls: says when the plan is closed
+    gbs_kv_cache_t cache;     // the KVCache keeps the tensors
+    int device;
+};
+PyTypeObject* pool_type = nullptr;
+
+int pool_init(PyObject* self, PyObject* args, PyObject*)
+{
+    Pool* p = reinterpret_cast<Pool*>(self);
+    PyObject *calls, *o[4];
+    int heads, page;
+    if (!PyArg_ParseTuple(args, "OOOOOii", &calls, &o[0], &o[1], &o[2], &o[3], &heads, &page)) return -1;
+    const at::Tensor* t[4];
+    for (int i = 0; i < 4; ++i) t[i] = cuda_tensor(o[i]);
+    if (Py_TYPE(calls) != calls_type || !t[0] || !t[1] || !t[2] || !t[3] || t[1]->dim() != 2) {
+        PyErr_SetString(PyExc_ValueError, "gbs: not a plan's calls and a pool's tensors");
+        return -1;
+    }
+    try {
+        p->cache = {t[0]->data_ptr(), t[0]->size(0), heads, page, static_cast<int32_t*>(t[1]->data_ptr()), static_cast<int32_t*>(t[2]->data_ptr()),
+                    static_cast<int32_t*>(t[3]->data_ptr()), static_cast<int>(t[1]->size(0)), static_cast<int>(t[1]->size(1))};
+        p->device = t[0]->device().index();
+    } catch (...) {
+        PyErr_SetString(PyExc_ValueError, "gbs: a pool's tensor has no memory");
+        return -1;
+    }
+    Py_XSETREF(p->calls, Py_NewRef(calls));
+    return 0;
+}
+void pool_dealloc(PyObject* self)
+{
+    PyTypeObject* type = Py_TYPE(self);
+    Py_CLEAR(reinterpret_cast<Pool*>(self)->calls);
+    type->tp_free(self);
+    Py_DECREF(type);
+}
+
+// the plan of a pool, null once it is closed
+const PlanRef* plan_ref(const Pool& p)
+{
+    const Calls* c = reinterpret_cast<const Calls*>(p.calls);
+    return c && c->ref.plan ? &c->ref : nullptr;
+}
+
+// a row of n int32 on the pool's device; null stays null
+bool ints_of(const Pool& p, PyObject* o, int64_t n, const int32_t** out)
+{
+    *out = nullptr;
+    if (!o || o == Py_None) return true;
+    const at::Tensor* t = cuda_tensor(o);
+    if (!t || t->scalar_type() != at::kInt || t->dim() != 1 || t->size(0) != n || !t->is_contiguous() || t->device().index() != p.device) return false;
+    *out = static_cast<const int32_t*>(t->data_ptr());
+    return true;
+}
+int64_t length_of(PyObject* o)
+{
+    if (!o || !THPVariable_Check(o)) return -1;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.dim() == 1 ? t.size(0) : -1;
+}
+
+struct Rows {
+    const at::Tensor* t;
+    void* ptr;
+    int64_t n, heads, token, head;
+};
+// [tokens, heads, d] in bf16 with contiguous rows
+bool rows3_of(const Pool& p, PyObject* o, int d, Rows* r)
+{
+    const at::Tensor* t = cuda_tensor(o);
+    if (!t || t->scalar_type() != at::kBFloat16 || t->dim() != 3 || t->size(2) != d || t->stride(2) != 1 || t->device().index() != p.device) return false;
+    *r = {t, t->data_ptr(), t->size(0), t->size(1), t->size(0) > 1 ? t->stride(0) : d, t->size(1) > 1 ? t->stride(1) : d};
+    return true;
+}
+
+struct Items {
+    const int32_t *seqs, *cu;
+    int64_t n;
+};
+bool items_of(const Pool& p, PyObject* seqs, PyObject* cu, int64_t tokens, Items* it)
+{
+    const bool has_seqs = seqs && seqs != Py_None, has_cu = cu && cu != Py_None;
+    it->n = has_seqs ? length_of(seqs) : has_cu ? length_of(cu) - 1 : tokens;
+    return it->n >= 0 && it->n <= GBS_KV_MAX_ITEMS && ints_of(p, seqs, it->n, &it->seqs) && ints_of(p, cu, it->n + 1, &it->cu);
+}
+
+bool none(PyObject* o) { return !o || o == Py_None; }
+
+// an int argument; absent: `standard`
+bool int_of(PyObject* o, int standard, int* out)
+{
+    *out = standard;
+    if (!o) return true;
+    const long v = PyLong_Check(o) ? PyLong_AsLong(o) : -1;
+    if (!PyLong_Check(o) || PyErr_Occurred() || v < 0 || v > 0x7fffffff) { PyErr_Clear(); return false; }
+    *out = static_cast<int>(v);
+    return true;
+}
+
+void* stream_on(const Pool& p) { return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(p.device)).stream(); }
+at::Device device_of(const Pool& p) { return at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(p.device)); }
+at::Tensor ints(const Pool& p, int64_t n) { return at::detail::empty_cuda({n}, at::kInt, device_of(p), std::nullopt); }
+
+// The regular calls on a pool: on the current stream of its device.
+PyObject* do_kv_extend(const Pool& p, const PlanRef& ref, PyObject* const* g)        // seqs, counts, stream
+{
+    GBS_BEGIN
+    if (!none(g[2])) Py_RETURN_NONE;
+    const int64_t n = !none(g[0]) ? length_of(g[0]) : !none(g[1]) ? length_of(g[1]) : p.cache.n_seqs;
+    const int32_t *seqs, *counts;
+    if (n < 0 || n > GBS_KV_MAX_ITEMS || !ints_of(p, g[0], n, &seqs) || !ints_of(p, g[1], n, &counts)) Py_RETURN_NONE;
+    at::Tensor status = ints(p, n);
+    int32_t* sp = static_cast<int32_t*>(status.data_ptr());
+    if (gbs_kv_extend(ref.plan, &p.cache, seqs, counts, static_cast<int>(n), sp, stream_on(p)) != GBS_OK) Py_RETURN_NONE;
+    return THPVariable_Wrap(std::move(status));
+    GBS_END
+}
+PyObject* do_kv_fork(const Pool& p, const PlanRef& ref, PyObject* const* g)          // src, dst, stream
+{
+    GBS_BEGIN
+    const int64_t n = length_of(g[0]);
+    const int32_t *src, *dst;
+    if (!none(g[2]) || n < 0 || n > GBS_KV_MAX_ITEMS || none(g[1]) || !ints_of(p, g[0], n, &src) || !ints_of(p, g[1], n, &dst)) Py_RETURN_NONE;
+    at::Tensor status = ints(p, n);
+    int32_t* sp = static_cast<int32_t*>(status.data_ptr());
+    if (gbs_kv_fork(ref.plan, &p.cache, src, dst, static_cast<int>(n), sp, stream_on(p)) != GBS_OK) Py_RETURN_NONE;
+    return THPVariable_Wrap(std::move(status));
+    GBS_END
+}
+// Calls that return None answer True: None says that the call was not made.
+PyObject* do_kv_free(const Pool& p, const PlanRef& ref, PyObject* const* g)          // seqs, stream
+{
+    GBS_BEGIN
+    const int64_t n = length_of(g[0]);
+    const int32_t* seqs;
+    if (!none(g[1]) || n < 0 || n > GBS_KV_MAX_ITEMS || !ints_of(p, g[0], n, &seqs)) Py_RETURN_NONE;
+    if (gbs_kv_free(ref.plan, &p.cache, seqs, static_cast<int>(n), stream_on(p)) != GBS_OK) Py_RETURN_NONE;
+    Py_RETURN_TRUE;
+    GBS_END
+}
+PyObject* do_kv_append(const Pool& p, const PlanRef& ref, PyObject* const* g)        // k, v, seqs, cu_tokens, stream
+{
+    GBS_BEGIN
+    Rows k, v;
+    Items it;
+    if (!none(g[4]) || !rows3_of(p, g[0], ref.info.d, &k) || !rows3_of(p, g[1], ref.info.d, &v)) Py_RETURN_NONE;
+    if (k.n != v.n || k.token != v.token || k.head != v.head || k.heads != p.cache.n_kv_heads || v.heads != k.heads) Py_RETURN_NONE;
+    if (!items_of(p, g[2], g[3], k.n, &it)) Py_RETURN_NONE;
+    if (gbs_kv_append(ref.plan, &p.cache, it.seqs, it.cu, static_cast<int>(it.n), k.n, k.ptr, v.ptr, k.token, k.head, stream_on(p)) != GBS_OK)
+        Py_RETURN_NONE;
+    Py_RETURN_TRUE;
+    GBS_END
+}
+PyObject* do_kv_read(const Pool& p, const PlanRef& ref, PyObject* const* g)          // seqs, cu_tokens, n_tokens, out, stream
+{
+    GBS_BEGIN
+    int n;
+    Items it;
+    if (!none(g[3]) || !none(g[4]) || none(g[2]) || !int_of(g[2], 0, &n) || !items_of(p, g[0], g[1], n, &it)) Py_RETURN_NONE;
+    at::Tensor out[2];
+    void* ptr[2];
+    for (int i = 0; i < 2; ++i) {
+        out[i] = at::detail::empty_cuda({n, p.cache.n_kv_heads, ref.info.d}, at::kBFloat16, device_of(p), std::nullopt);
+        ptr[i] = out[i].data_ptr();
+    }
+    if (gbs_kv_read(ref.plan, &p.cache, it.seqs, it.cu, static_cast<int>(it.n), n, ptr[0], ptr[1], stream_on(p)) != GBS_OK) Py_RETURN_NONE;
+    PyObject* t = PyTuple_New(2);
+    if (!t) return nullptr;
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(t, i, THPVariable_Wrap(std::move(out[i])));
+    return t;
+    GBS_END
+}
+// q, seqs, cu_tokens, max_tokens, causal, window, scale, max_len, out, stream
+PyObject* do_kv_attention(const Pool& p, const PlanRef& ref, PyObject* const* g)
+{
+    GBS_BEGIN
+    Rows q, o;
+    Items it;
+    int most, window, longest;
+    if (!none(g[9]) || !rows3_of(p, g[0], ref.info.d, &q) || !items_of(p, g[1], g[2], q.n, &it)) Py_RETURN_NONE;
+    if (!int_of(g[3], 1, &most) || !int_of(g[5], 0, &window) || !int_of(g[7], 0, &longest)) Py_RETURN_NONE;
+    const int causal = g[4] ? PyObject_IsTrue(g[4]) : 1;
+    const double scale = g[6] ? PyFloat_AsDouble(g[6]) : 0.0;
+    if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+    int64_t need;
+    if (q.heads > 0x7fffffff || gbs_kv_attention_workspace(ref.plan, &p.cache, static_cast<int>(q.heads), q.n, most, &need) != GBS_OK) Py_RETURN_NONE;
+    at::Tensor out;
+    if (none(g[8])) {
+        out = at::detail::empty_cuda(q.t->sizes(), at::kBFloat16, device_of(p), std::nullopt);
+        o = {&out, out.data_ptr(), q.n, q.heads, q.heads * ref.info.d, ref.info.d};
+    } else if (!rows3_of(p, g[8], ref.info.d, &o) || o.n != q.n || o.heads != q.heads) Py_RETURN_NONE;
+    at::Tensor work = at::detail::empty_cuda({need}, at::kByte, device_of(p), std::nullopt);
+    void* wp = work.data_ptr();
+    if (gbs_kv_attention(ref.plan, &p.cache, it.seqs, it.cu, static_cast<int>(it.n), q.n, most, longest, q.ptr, q.token, q.head,
+                         static_cast<int>(q.heads), static_cast<float>(scale), window, causal ? GBS_KV_CAUSAL : 0, o.ptr, o.token, o.head, wp,
+                         need, stream_on(p)) != GBS_OK)
+        Py_RETURN_NONE;
+    if (!none(g[8])) return Py_NewRef(g[8]);
+    return THPVariable_Wrap(std::move(out));
+    GBS_END
+}
+
+// A method: the names of its arguments in the class's order, how many must be given, and what to do with them; `on_pool` is for KVCache.
+constexpr int MOST_ARGS = 10;
 struct Method {
     const char* name;
     int count, required;
-    const char* args[8];
+    const char* args[MOST_ARGS];
     PyObject* (*call)(const PlanRef&, PyObject* const* given);
+    PyObject* (*on_pool)(const Pool&, const PlanRef&, PyObject* const* given) = nullptr;
+    bool returns_none = false;
 };
+constexpr Method KV_EXTEND = {"extend", 3, 0, {"seqs", "counts", "stream"}, nullptr, do_kv_extend};
+constexpr Method KV_FORK = {"fork", 3, 2, {"src", "dst", "stream"}, nullptr, do_kv_fork};
+constexpr Method KV_FREE = {"free", 2, 1, {"seqs", "stream"}, nullptr, do_kv_free, true};
+constexpr Method KV_APPEND = {"append", 5, 2, {"k", "v", "seqs", "cu_tokens", "stream"}, nullptr, do_kv_append, true};
+constexpr Method KV_READ = {"read", 5, 0, {"seqs", "cu_tokens", "n_tokens", "out", "stream"}, nullptr, do_kv_read};
+constexpr Method KV_ATTENTION = {"attention", 10, 1, {"q", "seqs", "cu_tokens", "max_tokens", "causal", "window", "scale", "max_len", "out", "stream"},
+                                 nullptr, do_kv_attention};
 
 PyObject* or_none(PyObject* o) { return o ? o : Py_None; }
 
@@ -381,8 +596,11 @@ PyObject* method_call(PyObject* self, PyObject* const* args, size_t nargsf, PyOb
     const Py_ssize_t n = PyVectorcall_NARGS(nargsf) - 1, nk = kwnames ? PyTuple_GET_SIZE(kwnames) : 0;
     PyObject* calls = n >= 0 ? PyObject_GetAttr(args[0], name_calls) : nullptr;
     if (!calls) PyErr_Clear();
-    PyObject* given[8] = {nullptr};
-    bool regular = calls && Py_TYPE(calls) == calls_type && reinterpret_cast<Calls*>(calls)->ref.plan && n <= M.count;
+    PyObject* given[MOST_ARGS] = {nullptr};
+    const PlanRef* plan = nullptr;
+    if (calls && Py_TYPE(calls) == (M.on_pool ? pool_type : calls_type))
+        plan = M.on_pool ? plan_ref(*reinterpret_cast<Pool*>(calls)) : &reinterpret_cast<Calls*>(calls)->ref;
+    bool regular = plan && plan->plan && n <= M.count;
     for (Py_ssize_t i = 0; regular && i < n; ++i) given[i] = args[1 + i];
     for (Py_ssize_t k = 0; regular && k < nk; ++k) {
         int at = -1;
@@ -395,9 +613,10 @@ PyObject* method_call(PyObject* self, PyObject* const* args, size_t nargsf, PyOb
     if (regular && o->alloc) regular = own_alloc(args[0], o->alloc);
     PyObject* out = nullptr;
     if (regular) {
-        const PlanRef ref = reinterpret_cast<Calls*>(calls)->ref;      // the caller's argument keeps the plan
-        out = M.call(ref, given);
+        const PlanRef ref = *plan;                                     // the caller's argument keeps the plan
+        out = M.on_pool ? M.on_pool(*reinterpret_cast<Pool*>(calls), ref, given) : M.call(ref, given);
         if (out == Py_None) { Py_DECREF(out); regular = false; }
+        else if (out && M.returns_none) { Py_DECREF(out); out = Py_NewRef(Py_None); }
     }
     Py_XDECREF(calls);
     return regular ? out : PyObject_Vectorcall(o->wrapped, args, nargsf, kwnames);
@@ -438,7 +657,7 @@ void method_dealloc(PyObject* self)
     Py_DECREF(type);
 }
 PyTypeObject* method_type = nullptr;
-const Method* const METHODS[] = {&ROTATE, &DEQUANTIZE, &MATMUL, &CLIP};
+const Method* const METHODS[] = {&ROTATE, &DEQUANTIZE, &MATMUL, &CLIP, &KV_EXTEND, &KV_FORK, &KV_FREE, &KV_APPEND, &KV_READ, &KV_ATTENTION};
 
 PyObject* make_method(PyObject*, PyObject* args)
 {
@@ -465,6 +684,10 @@ PyType_Slot calls_slots[] = {{Py_tp_init, reinterpret_cast<void*>(calls_init)}, 
                              {Py_tp_new, reinterpret_cast<void*>(PyType_GenericNew)}, {Py_tp_methods, calls_methods}, {0, nullptr}};
 PyType_Spec calls_spec = {"paper_2504_13989_b200._native.Calls", sizeof(Calls), 0, Py_TPFLAGS_DEFAULT, calls_slots};
 
+PyType_Slot pool_slots[] = {{Py_tp_init, reinterpret_cast<void*>(pool_init)}, {Py_tp_dealloc, reinterpret_cast<void*>(pool_dealloc)},
+                            {Py_tp_new, reinterpret_cast<void*>(PyType_GenericNew)}, {0, nullptr}};
+PyType_Spec pool_spec = {"paper_2504_13989_b200._native.Pool", sizeof(Pool), 0, Py_TPFLAGS_DEFAULT, pool_slots};
+
 PyMemberDef method_members[] = {{"__vectorcalloffset__", Py_T_PYSSIZET, offsetof(MethodObject, vectorcall), Py_READONLY, nullptr},
                                 {nullptr, 0, 0, 0, nullptr}};
 PyType_Slot method_slots[] = {{Py_tp_dealloc, reinterpret_cast<void*>(method_dealloc)}, {Py_tp_traverse, reinterpret_cast<void*>(method_traverse)},
@@ -490,10 +713,12 @@ PyMODINIT_FUNC PyInit__native(void)
     name_calls = PyUnicode_InternFromString("_calls");
     name_alloc = PyUnicode_InternFromString("alloc_outputs");
     calls_type = reinterpret_cast<PyTypeObject*>(PyType_FromSpec(&calls_spec));
+    pool_type = reinterpret_cast<PyTypeObject*>(PyType_FromSpec(&pool_spec));
     method_type = reinterpret_cast<PyTypeObject*>(PyType_FromSpec(&method_spec));
     PyObject* m = PyModule_Create(&module);
-    if (!name_calls || !name_alloc || !calls_type || !method_type || !m ||
-        PyModule_AddObjectRef(m, "Calls", reinterpret_cast<PyObject*>(calls_type)) < 0) {
+    if (!name_calls || !name_alloc || !calls_type || !pool_type || !method_type || !m ||
+        PyModule_AddObjectRef(m, "Calls", reinterpret_cast<PyObject*>(calls_type)) < 0 ||
+        PyModule_AddObjectRef(m, "Pool", reinterpret_cast<PyObject*>(pool_type)) < 0) {
         Py_XDECREF(m);
         return nullptr;
     }

@@ -478,3 +478,44 @@ def test_a_serving_loop():
             want, tol = kv_util.attention(into, q, [1, 3, 5], [0, 1, 2, 3])
             assert bool(((got.double() - want).abs() <= tol).all())
         assert into.lengths[[1, 3, 5]].tolist() == (cache.lengths[[1, 3, 5]] + 18).tolist()
+
+
+def test_native_and_python_paths_agree():
+    """The regular calls of _native.so against the functions that they stand in front of; calls after the plan is closed are refused."""
+    def python(name):
+        return getattr(KVCache, name).__wrapped__
+    # tokens that were given room and not written hold what the pool held: numbers that are none, where one is seen
+    same = lambda x, y: torch.allclose(x, y, rtol=0, atol=0, equal_nan=True)  # noqa: E731
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(6)
+    plan = plan_of(96)
+    a, b = (filled(plan, [40, 3, 0, 100], 2, 16, seed=2, spare=40) for _ in range(2))
+    seqs, counts = ints([3, 2, 0]), ints([2, 5, 1])
+    cu = ints([0, 2, 7, 8])
+    for s, c in ((seqs, counts), (None, None), (seqs, None)):
+        assert torch.equal(a.extend(s, c), python("extend")(b, s, c))
+    a.free(seqs=ints([1])), python("free")(b, ints([1]))
+    assert torch.equal(a.fork(ints([3]), dst=ints([1])), python("fork")(b, ints([3]), ints([1])))
+    k, v = (torch.randn((8, 2, 96), generator=gen, device=DEV).to(torch.bfloat16) for _ in range(2))
+    assert a.append(k, v, seqs, cu_tokens=cu) is None
+    python("append")(b, k, v, seqs, cu)
+    for x in ("pages", "page_table", "lengths", "refs"):
+        x, y = getattr(a, x), getattr(b, x)
+        assert torch.equal(x, y)
+    for x, y in zip(a.read(seqs, cu, 8), python("read")(b, seqs, cu, 8)):
+        assert torch.equal(x, y)
+    q = torch.randn((8, 6, 96), generator=gen, device=DEV).to(torch.bfloat16)
+    want = python("attention")(b, q, seqs, cu, 5, causal=False, window=30, scale=0.1, max_len=64)
+    assert same(a.attention(q, seqs, cu, 5, causal=False, window=30, scale=0.1, max_len=64), want)
+    out = torch.empty_like(q)
+    assert a.attention(q, seqs, cu, 5, False, 30, 0.1, 64, out) is out and same(out, want)
+    wide = torch.zeros((8, 12, 96), dtype=torch.bfloat16, device=DEV)
+    wide[:, :6] = q
+    assert same(a.attention(wide[:, :6], seqs, cu, 5, causal=False, window=30, scale=0.1, max_len=64), want)
+    with pytest.raises(GbsError):
+        a.attention(q, seqs, cu, 0)
+    plan.close()
+    with pytest.raises(GbsError):
+        a.attention(q, seqs, cu, 5)
+    with pytest.raises(GbsError):
+        a.extend()
