@@ -191,12 +191,27 @@ int gbs_kv_fork_launch(const gbs_plan* p, const gbs_kv_view& c, const int* src, 
 int gbs_kv_free_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, cudaStream_t stream);
 int gbs_kv_compact_launch(const gbs_plan* p, const gbs_kv_view& c, const gbs_kv_view& into, int* page_map, int* n_live, cudaStream_t stream);
 
+// x / d for x < 2^28, d <= 2^28, as a product
+struct gbs_kv_div {
+    unsigned magic;                     // ceil(2^shift / d) <= 2^30
+    int shift;
+    void set(unsigned d)
+    {
+        for (shift = 29; (1ull << (shift - 29)) < d;) ++shift;
+        magic = (unsigned)(((1ull << shift) + d - 1) / d);
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int operator()(int x) const { return (int)((unsigned long long)(unsigned)x * magic >> shift); }
+#endif
+};
+
 // the arguments of an attention call, checked
 struct gbs_kv_attn {
     gbs_kv_view c;
     const int *seqs, *cu;
     int n_items, max_tokens, max_len, window, causal;
     int n_heads, group, d;              // group: query heads of a KV head
+    gbs_kv_div by_group;
     float scale;
     long long n_tokens;
     const void* q;

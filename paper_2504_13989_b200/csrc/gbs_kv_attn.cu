@@ -19,6 +19,10 @@
 //
 // One warp of a block fetches units of 32 tokens (bulk copies into a ring), four at a time, eight lanes for the up to eight pieces of one.  The
 // others take them in turn, keep sums for their tokens in registers, and meet where a segment ends.
+#include <stddef.h>
+
+#include <algorithm>
+
 #include "gbs_kv_attn.cuh"
 #include "gbs_tc_common.cuh"
 
@@ -26,8 +30,9 @@ namespace {
 
 constexpr int ROWS = 8, UNIT = 32;
 constexpr int WARPS = 4, THREADS = 32 * WARPS + 32;  // warps that compute, and the one that fetches
-constexpr int STAGES = 3 * WARPS;                    // unit i of a block's line is worked on by warp i % WARPS, from stage i % STAGES
+constexpr int STAGES = 11;                           // unit i of a block's is worked on by warp i % WARPS, from stage i % STAGES
 constexpr int PART = KV_PART<ROWS>;
+static_assert(2 * WARPS == ROWS, "each warp finishes two rows");
 constexpr int BLOCKS_PER_SM = 3;
 constexpr float MOVE = 8.f;                          // m moves when a score is so much (log2) above it
 constexpr float W_MOST = 32768.f;                    // M moves when a w is beyond that
@@ -44,16 +49,28 @@ struct Smem {
     Stage<ASYM> ring[STAGES];
     float part[WARPS][ROWS * 128];                   // 16-byte pieces c of each 64 bytes of rows 2 t, 2 t + 1 at c ^ t
     float m[WARPS][ROWS], l[WARPS][ROWS], add[WARPS][ROWS], mw[WARPS][ROWS];
-    signed char qh[ROWS][128], ql[ROWS][128];        // a row's integers, upper and lower byte; of 8 coordinates the even ones first
-    float factor[ROWS];
-    int qsum[ROWS];
-    int row_lo[ROWS], row_hi[ROWS], all_lo, all_hi;  // tokens that a row sees, and that every row sees
-    unsigned long long full[STAGES], empty[STAGES];
+    // of two segments in turn: the rows' integers (upper and lower byte; of 8 coordinates the even ones first), their factors and sums, what
+    // each row sees and what all of them see, the segment and the block's piece of it
+    struct alignas(16) Query {
+        signed char h[ROWS][128], l[ROWS][128];
+        float factor[ROWS];
+        int sum[ROWS], lo[ROWS], hi[ROWS];
+        int all_lo, all_hi;
+        KvSeg seg;
+        KvPiece piece;
+        bool last;
+    } query[2];
+    unsigned long long full[STAGES], empty[STAGES], qfull[2], qempty[2];
     unsigned valid[STAGES];                          // bit h: tokens 16 h .. of the unit have a page
-    KvSeg seg[2];                                    // the segment that the block works on, and the next one
-    long long share[WARPS + 1 + 3];
+    KvSeg seg;                                       // the block's first segment
+    long long share[WARPS + 1];
+    bool bad[WARPS];
     int abort;
 };
+
+static_assert(offsetof(Smem<true>, query) % 16 == 0 && offsetof(Smem<false>, query) % 16 == 0 && sizeof(Smem<true>::Query) % 16 == 0, "read 16 bytes at a time");
+static_assert(sizeof(Smem<true>) + 1024 <= 228 * 1024 / BLOCKS_PER_SM, "so many blocks have room on an SM");
+static_assert(sizeof(Stage<true>) % 128 == 0 && sizeof(Stage<false>) % 128 == 0, "copied and read 16 bytes at a time");
 
 __device__ __forceinline__ void mma_f16(float c[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, const unsigned b[2])
 {
@@ -73,6 +90,78 @@ __device__ __forceinline__ unsigned transposed(unsigned x)
     return y;
 }
 
+// The query rows of a segment by one warp, eight lanes a row: rotated, and made integers.
+template <bool ASYM>
+__device__ __forceinline__ void prepare(const gbs_kv_attn& A, const KvSeg& seg, typename Smem<ASYM>::Query& Q, int lane)
+{
+    const int l8 = lane & 7;
+    uint4 raw[2][2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = 4 * r + (lane >> 3);
+        raw[r][0] = raw[r][1] = make_uint4(0, 0, 0, 0);
+        if (seg.e.row0 + row < seg.e.rows) {
+            int token, head;
+            kv_row_of(A, seg, row, token, head);
+            const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(A.q) + (seg.e.first + token) * A.q_token + head * A.q_head;
+            if (8 * l8 < A.d) raw[r][0] = *reinterpret_cast<const uint4*>(x + 8 * l8);
+            if (64 + 8 * l8 < A.d) raw[r][1] = *reinterpret_cast<const uint4*>(x + 64 + 8 * l8);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = 4 * r + (lane >> 3);
+                    float y[16];
+                    kv_unpack_bf16(raw[r][0], y);
+                    kv_unpack_bf16(raw[r][1], y + 8);
+                    kv_hadamard(y, l8);
+                    float m = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(y[i]));
+#pragma unroll
+                    for (int h = 1; h < 8; h <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, h));
+                    // integers of up to 32512, whose upper byte is at most 127; a row that is not finite has a factor that is not a number
+                    const float up = m < 1e-30f ? 1.2379400392853803e27f : 1.f;     // 2^90
+                    const float by = m > 0.f ? 32512.f / (m * up) : 0.f;
+                    int q[16], sum = 0;
+                    float wrong = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        q[i] = __float2int_rn(fminf(fmaxf(y[i] * up * by, -32512.f), 32512.f));
+                        sum += q[i];
+                        wrong += y[i] * 0.f;
+                    }
+#pragma unroll
+                    for (int h = 1; h < 8; h <<= 1) {
+                        sum += __shfl_xor_sync(0xffffffffu, sum, h);
+                        wrong += __shfl_xor_sync(0xffffffffu, wrong, h);
+                    }
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        unsigned high[2] = {0, 0}, low[2] = {0, 0};
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int x = q[8 * half + i], top = (x + 128) >> 8;
+                            high[i & 1] |= (unsigned)(top & 255) << (8 * (i >> 1));
+                            low[i & 1] |= (unsigned)((x - 256 * top) & 255) << (8 * (i >> 1));
+                        }
+                        *reinterpret_cast<uint2*>(&Q.h[row][64 * half + 8 * l8]) = make_uint2(high[0], high[1]);
+                        *reinterpret_cast<uint2*>(&Q.l[row][64 * half + 8 * l8]) = make_uint2(low[0], low[1]);
+                    }
+                    if (l8 == 0) {
+                        Q.factor[row] = m * (A.scale * (KV_NORM * 1.4426950408889634f / 32512.f)) + wrong;
+                        Q.sum[row] = sum;
+                        const int token = A.by_group(min(seg.e.row0 + row, seg.e.rows - 1));
+                        Q.lo[row] = kv_row_lo(A, seg.e, token);
+                        Q.hi[row] = kv_row_hi(A, seg.e, token);
+                        if (row == 0) {                          // the last row sees the latest window, the first the shortest past
+                            Q.all_lo = kv_row_lo(A, seg.e, A.by_group(min(seg.e.rows, seg.e.row0 + ROWS) - 1));
+                            Q.all_hi = Q.hi[0];
+                        }
+                    }
+    }
+}
+
 // the warps that compute
 __device__ __forceinline__ void meet() { asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory"); }
 
@@ -88,42 +177,48 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
         mbar_init(&S.full[threadIdx.x], 1);
         mbar_init(&S.empty[threadIdx.x], 1);
     }
+    if (threadIdx.x < 2) {
+        mbar_init(&S.qfull[threadIdx.x], 1);
+        mbar_init(&S.qempty[threadIdx.x], WARPS);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
     kv_wait_before();
     kv_let_next();
 
-    KvSeg seg;
-    const int units = kv_share<THREADS>(A, P.line, seg, S.share);
-    if (threadIdx.x == 0) P.joins[blockIdx.x] = KvJoin{0, 0, 0, 0};
-    if (units == 0) return;
+    const int places = kv_share<THREADS>(A, P.line, &S.seg, S.share);
+    if (threadIdx.x == 0 && P.line.pad >= 0) P.joins[blockIdx.x] = KvJoin{0, 0, 0, 0};
+    if (places == 0) return;
 
     if (w == WARPS) {
         // ---- fetching ----
         const int ps_log = A.c.page_log, T = min(UNIT, 1 << ps_log);
         const int mine = lane >> 3, half = (lane >> 2) & 1, piece = lane & 3;
-        const bool part = T < UNIT || half == 0;             // this lane copies a piece
+        const bool copies = T < UNIT || half == 0;           // this lane copies a piece
         const unsigned piece_bytes = piece < 2 ? T * KV_ROW : T * (ASYM ? 8 : 4);
         const int in_block = piece < 2 ? piece * (KV_ROW << ps_log) : (2 * KV_ROW << ps_log) + (piece - 2) * ((ASYM ? 8 : 4) << ps_log);
         const int in_slot = piece < 2 ? KV_ROW : (ASYM ? 8 : 4);
         const int in_stage = (piece < 2 ? piece * UNIT * KV_ROW : 2 * UNIT * KV_ROW + (piece - 2) * Stage<ASYM>::SCALE) + half * (int)piece_bytes;
-        bool dead = false;
-        int at = 0;
-        for (; at < units && !dead;) {
-            const int stop = min(units, seg.at + seg.e.units);
+        bool dead = false, more = true;
+        int at = 0;                                          // units of the block so far
+        KvSeg seg = S.seg;
+        for (int round = 0; more && !dead; ++round) {
+            const KvPiece part = kv_piece(P.line, seg, places);
+            more = kv_more(P.line, seg, places);
             const int* row = A.c.page_table + (long long)seg.e.seq * A.c.max_pages;
             const int off = seg.head * A.c.block_bytes + in_block;
-            int tok = (seg.e.lo / UNIT - seg.at + at + mine) * UNIT + half * 16;
-            int page = part && tok < seg.e.hi ? row[tok >> ps_log] : -1;
-            for (; at < stop; at += 4) {
-                const int u = at + mine, st = u % STAGES, use = u / STAGES;
-                const int next_tok = tok + 4 * UNIT, next = part && at + 4 < stop && next_tok < seg.e.hi ? row[next_tok >> ps_log] : -1;
-                if (u < stop && use > 0 && !mbar_wait(&S.abort, &S.empty[st], (unsigned)(use - 1) & 1u, P.status, 62)) dead = true;
+            int tok = ((seg.e.lo >> 5) + part.skip + mine) * UNIT + half * 16;
+            int page = copies && mine < part.n && tok < seg.e.hi ? row[tok >> ps_log] : -1;
+            for (int i = 0; i < part.n || i == 0; i += 4) {
+                const int u = at + i + mine, st = u % STAGES, use = u / STAGES;
+                const bool have = i + mine < part.n;
+                const int next_tok = tok + 4 * UNIT, next = copies && i + 4 + mine < part.n && next_tok < seg.e.hi ? row[next_tok >> ps_log] : -1;
+                if (have && use > 0 && !mbar_wait(&S.abort, &S.empty[st], (unsigned)(use - 1) & 1u, P.status, 62)) dead = true;
                 if (__any_sync(0xffffffffu, dead)) { dead = true; break; }
-                const bool ok = u < stop && (unsigned)page < (unsigned)A.c.n_pages;
+                const bool ok = have && (unsigned)page < (unsigned)A.c.n_pages;
                 const unsigned who = __ballot_sync(0xffffffffu, ok) >> (8 * mine), first = who & 1, second = (who >> 4) & 1;
-                if (u < stop && (lane & 7) == 0) {
+                if (have && (lane & 7) == 0) {
                     S.valid[st] = T == UNIT ? 3u * first : first | second << 1;
                     mbar_arrive_expect_tx(&S.full[st], (first + second) * (unsigned)(T * (2 * KV_ROW + (ASYM ? 16 : 8))));
                 }
@@ -133,94 +228,42 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                               A.c.pages + ((long long)page * A.c.page_bytes + off + (tok & ((1 << ps_log) - 1)) * in_slot), piece_bytes, &S.full[st]);
                 tok = next_tok;
                 page = next;
+                if (i > 0) continue;
+                // with the first units under way: the segment's query rows, eight lanes a row, rotated and made integers
+                if (round > 1 && !mbar_wait_warp(&S.abort, &S.qempty[round & 1], (unsigned)(round / 2 - 1) & 1u, P.status, 63)) { dead = true; break; }
+                prepare<ASYM>(A, seg, S.query[round & 1], lane);
+                if (lane == 0) {
+                    S.query[round & 1].seg = seg;
+                    S.query[round & 1].piece = part;
+                    S.query[round & 1].last = !more;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&S.qfull[round & 1]);
             }
-            at = min(at, stop);
-            if (at < units) kv_next(A, seg, P.line.entries, P.line.tiles, ROWS, UNIT);
+            at += max(part.n, 0);
+            if (more) kv_next(A, P.line, seg);
         }
         if (dead) drain_copies(S.full, STAGES, at);
         return;
     }
 
     // ---- the segments ----
-    int mine = w, st = w;                                    // this warp's next unit of the line, and its stage
+    int mine = w, st = w, done = 0;                          // this warp's next unit of the block's, and its stage; units of the segments before
     unsigned phase = 0;
     bool dead = false;
-    if (threadIdx.x == 0) S.seg[0] = seg;
-    meet();
     for (int round = 0;; ++round) {
-        // read where it is needed, not kept in registers
-        const KvSeg& seg = S.seg[round & 1];
-        // query rows: four of them per warp, rotated, halved
-        if (w < 2) {
-            const int row = 4 * w + (lane >> 3), l8 = lane & 7;
-            uint4 a = make_uint4(0, 0, 0, 0), b = a;
-            if (seg.e.row0 + row < seg.e.rows) {
-                int token, head;
-                kv_row_of(A, seg, row, token, head);
-                const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(A.q) + (seg.e.first + token) * A.q_token + head * A.q_head;
-                if (8 * l8 < A.d) a = *reinterpret_cast<const uint4*>(x + 8 * l8);
-                if (64 + 8 * l8 < A.d) b = *reinterpret_cast<const uint4*>(x + 64 + 8 * l8);
-            }
-            float y[16];
-            kv_unpack_bf16(a, y);
-            kv_unpack_bf16(b, y + 8);
-            kv_hadamard(y, l8);
-            float m = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(y[i]));
-#pragma unroll
-            for (int h = 1; h < 8; h <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, h));
-            // integers of up to 32512, whose upper byte is at most 127; a row that is not finite has a factor that is not a number
-            const float up = m < 1e-30f ? 1.2379400392853803e27f : 1.f;     // 2^90
-            const float by = m > 0.f ? 32512.f / (m * up) : 0.f;
-            int q[16], sum = 0;
-            float wrong = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                q[i] = __float2int_rn(fminf(fmaxf(y[i] * up * by, -32512.f), 32512.f));
-                sum += q[i];
-                wrong += y[i] * 0.f;
-            }
-#pragma unroll
-            for (int h = 1; h < 8; h <<= 1) {
-                sum += __shfl_xor_sync(0xffffffffu, sum, h);
-                wrong += __shfl_xor_sync(0xffffffffu, wrong, h);
-            }
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                unsigned high[2] = {0, 0}, low[2] = {0, 0};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int x = q[8 * half + i], top = (x + 128) >> 8;
-                    high[i & 1] |= (unsigned)(top & 255) << (8 * (i >> 1));
-                    low[i & 1] |= (unsigned)((x - 256 * top) & 255) << (8 * (i >> 1));
-                }
-                *reinterpret_cast<uint2*>(&S.qh[row][64 * half + 8 * l8]) = make_uint2(high[0], high[1]);
-                *reinterpret_cast<uint2*>(&S.ql[row][64 * half + 8 * l8]) = make_uint2(low[0], low[1]);
-            }
-            if (l8 == 0) {
-                S.factor[row] = m * (A.scale * (KV_NORM * 1.4426950408889634f / 32512.f)) + wrong;
-                S.qsum[row] = sum;
-                const int token = min(seg.e.row0 + row, seg.e.rows - 1) / A.group;
-                S.row_lo[row] = kv_row_lo(A, seg.e, token);
-                S.row_hi[row] = kv_row_hi(A, seg.e, token);
-                if (row == 0) {                          // the last row sees the latest window, the first the shortest past
-                    S.all_lo = kv_row_lo(A, seg.e, (min(seg.e.rows, seg.e.row0 + ROWS) - 1) / A.group);
-                    S.all_hi = S.row_hi[0];
-                }
-            }
-        }
-        meet();
+        const auto& Q = S.query[round & 1];
+        if (!dead && !mbar_wait_warp(&S.abort, &S.qfull[round & 1], (unsigned)(round / 2) & 1u, P.status, 64)) dead = true;
         unsigned qh[4][2], ql[4][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const uint4 h = *reinterpret_cast<const uint4*>(&S.qh[g][32 * t + 16 * i]), l = *reinterpret_cast<const uint4*>(&S.ql[g][32 * t + 16 * i]);
+            const uint4 h = *reinterpret_cast<const uint4*>(&Q.h[g][32 * t + 16 * i]), l = *reinterpret_cast<const uint4*>(&Q.l[g][32 * t + 16 * i]);
             qh[2 * i][0] = h.x; qh[2 * i][1] = h.y; qh[2 * i + 1][0] = h.z; qh[2 * i + 1][1] = h.w;
             ql[2 * i][0] = l.x; ql[2 * i][1] = l.y; ql[2 * i + 1][0] = l.z; ql[2 * i + 1][1] = l.w;
         }
         // this thread's scores and results are of rows 2 t and 2 t + 1
-        const float2 factor = *reinterpret_cast<const float2*>(&S.factor[2 * t]);
-        const int2 qsum = *reinterpret_cast<const int2*>(&S.qsum[2 * t]);
+        const float2 factor = *reinterpret_cast<const float2*>(&Q.factor[2 * t]);
+        const int2 qsum = *reinterpret_cast<const int2*>(&Q.sum[2 * t]);
         const int from0 = ASYM ? 0 : -8 * qsum.x, from1 = ASYM ? 0 : -8 * qsum.y;
         const float lift0 = (float)qsum.x * factor.x, lift1 = (float)qsum.y * factor.y;
         float o[8][4];                                   // (coordinate 16 g + 2 j, rows 2 t, 2 t + 1), (coordinate 16 g + 2 j + 1, the same)
@@ -228,13 +271,13 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
         for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
         float m0 = NONE, m1 = NONE, mw0 = NONE, mw1 = NONE, up0 = 0.f, up1 = 0.f, l0 = 0.f, l1 = 0.f, add0 = 0.f, add1 = 0.f;     // up = 64 2^(m - M)
 
-        const int stop = min(units, seg.at + seg.e.units), tok_at = (seg.e.lo / UNIT - seg.at) * UNIT;
+        const int stop = done + max(Q.piece.n, 0), tok_at = ((Q.seg.e.lo >> 5) + Q.piece.skip - done) * UNIT;
         for (; mine < stop; mine += WARPS) {
             if (!dead && !mbar_wait_warp(&S.abort, &S.full[st], phase, P.status, 61)) dead = true;
             const Stage<ASYM>& X = S.ring[st];
             const unsigned valid = S.valid[st];
             const int tok0 = tok_at + mine * UNIT;
-            const bool plain = valid == 3u && tok0 >= S.all_lo && tok0 + UNIT <= S.all_hi;
+            const bool plain = valid == 3u && tok0 >= Q.all_lo && tok0 + UNIT <= Q.all_hi;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {                // sixteen tokens at a time
                 // row g of an operand is token g ^ ((g >> 1) & 1), row g + 8 the one 8 further: see the values
@@ -273,7 +316,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 }
                 if (!plain) {
                     const bool page = (valid >> h) & 1;
-                    const int2 lo = *reinterpret_cast<const int2*>(&S.row_lo[2 * t]), hi = *reinterpret_cast<const int2*>(&S.row_hi[2 * t]);
+                    const int2 lo = *reinterpret_cast<const int2*>(&Q.lo[2 * t]), hi = *reinterpret_cast<const int2*>(&Q.hi[2 * t]);
                     const int ta = tok0 + tg, tb = ta + 8;
                     if (!page || ta < lo.x || ta >= hi.x) z[0] = -INFINITY;
                     if (!page || ta < lo.y || ta >= hi.y) z[1] = -INFINITY;
@@ -353,11 +396,12 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             __syncwarp();
             if (lane == 0) mbar_arrive(&S.empty[st]);
             if ((st += WARPS) >= STAGES) {
-                st = w;
+                st -= STAGES;
                 phase ^= 1u;
             }
         }
 
+        done = stop;
         // ---- the warps' sums ----
 #pragma unroll
         for (int k = 4; k < 32; k <<= 1) {
@@ -366,6 +410,11 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             add0 += __shfl_xor_sync(0xffffffffu, add0, k);
             add1 += __shfl_xor_sync(0xffffffffu, add1, k);
         }
+        const KvSeg seg = Q.seg;
+        const KvPiece piece = Q.piece;
+        const bool last = Q.last;
+        meet();                                              // the sums before these have been read
+        if (lane == 0) mbar_arrive(&S.qempty[round & 1]);
         if (g == 0) {
             *reinterpret_cast<float2*>(&S.m[w][2 * t]) = make_float2(m0, m1);
             *reinterpret_cast<float2*>(&S.l[w][2 * t]) = make_float2(l0, l1);
@@ -378,13 +427,14 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             *reinterpret_cast<float4*>(to) = make_float4(o[2 * c][0], o[2 * c][2], o[2 * c + 1][0], o[2 * c + 1][2]);
             *reinterpret_cast<float4*>(to + 128) = make_float4(o[2 * c][1], o[2 * c][3], o[2 * c + 1][1], o[2 * c + 1][3]);
         }
+        if (lane == 0) S.bad[w] = dead;
         meet();
-        const bool starts = seg.at >= 0, ends = seg.at + seg.e.units <= units;
-        if (w < 2) {
-            const int row = 4 * w + (lane >> 3), l8 = lane & 7;
-            float top = S.m[0][row], top_w = S.mw[0][row];
+        // two rows a warp, eight lanes a row (the upper half of the warp does the same and writes nothing)
+        if (piece.n > 0) {
+            const int row = 2 * w + ((lane >> 3) & 1), l8 = lane & 7;
+            float top = NONE, top_w = NONE;
 #pragma unroll
-            for (int i = 1; i < WARPS; ++i) {
+            for (int i = 0; i < WARPS; ++i) {
                 top = fmaxf(top, S.m[i][row]);
                 top_w = fmaxf(top_w, S.mw[i][row]);
             }
@@ -406,17 +456,17 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                     y[4 * q + 3] = fmaf(x.w, keep_w, y[4 * q + 3]);
                 }
             }
-            if (starts && ends) {
+            if (piece.starts && piece.ends) {
                 kv_finish(y, l8, top, top_w, total, extra);
-                if (seg.e.row0 + row < seg.e.rows) {
+                if (seg.e.row0 + row < seg.e.rows && lane < 16) {
                     int token, head;
                     kv_row_of(A, seg, row, token, head);
                     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (seg.e.first + token) * A.out_token + head * A.out_head;
                     if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
                     if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
                 }
-            } else {
-                float* part = P.parts + ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * PART;
+            } else if (lane < 16) {
+                float* part = P.parts + ((long long)blockIdx.x * 2 + (piece.starts ? 1 : 0)) * PART;
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     *reinterpret_cast<float4*>(part + row * 128 + 64 * (q >> 1) + 8 * l8 + 4 * (q & 1)) = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
@@ -426,19 +476,14 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                     part[ROWS * 128 + 2 * ROWS + row] = extra;
                     part[ROWS * 128 + 3 * ROWS + row] = top_w;
                 }
-                if (threadIdx.x == 0 && starts) {
-                    const int beyond = seg.at + seg.e.units - units;
-                    P.joins[blockIdx.x] = KvJoin{seg.index, seg.head, 1 + (beyond + units - 1) / units, 0};   // the blocks behind have as many units, or their rest
-                }
+                if (threadIdx.x == 0 && piece.starts) P.joins[blockIdx.x] = kv_join(P.line, seg, places);
             }
         }
-        if (seg.at + seg.e.units >= units) break;
-        if (w == 0) {
-            KvSeg next = seg;
-            kv_next(A, next, P.line.entries, P.line.tiles, ROWS, UNIT);
-            if (lane == 0) S.seg[(round + 1) & 1] = next;
-        }
-        meet();
+        // a wait that ran out ends all of them together
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) bad |= S.bad[i];
+        if (last || bad) break;
     }
 }
 
@@ -456,11 +501,14 @@ int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, 
     KvAttnArgs P = {};
     P.a = A;
     P.line.tile_rows = ROWS;
-    P.line.unit = UNIT;
+    P.line.unit_log = 5;
     P.line.tiles = (int)(((int64_t)A.max_tokens * A.group + ROWS - 1) / ROWS);
+    P.line.by_tiles.set((unsigned)P.line.tiles);
     P.line.entries = A.n_items * P.line.tiles;
-    P.line.least = 12;
-    const int blocks = blocks_of(p);
+    // a short sequence is not worth dividing: the join's launch takes as long as a block needs for 16 units
+    P.line.pad = A.max_len <= 16 * UNIT ? -1 : 7;
+    P.line.least = P.line.pad < 0 ? 1 : 12;
+    const int blocks = P.line.pad < 0 ? (int)std::min<int64_t>((int64_t)P.line.entries * A.c.heads, blocks_of(p)) : blocks_of(p);
     P.joins = static_cast<KvJoin*>(workspace);
     P.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + blocks * sizeof(KvJoin));
     P.status = p->d_status;
@@ -469,6 +517,6 @@ int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, 
     const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return (int)e;
     const int rc = gbs_kv_launch(p, p->asym ? k_kv_attn_few<true> : k_kv_attn_few<false>, dim3((unsigned)blocks), THREADS, smem, stream, P);
-    if (rc != 0) return rc;
-    return gbs_kv_launch(p, k_kv_attn_join<ROWS, UNIT>, dim3((unsigned)blocks), 256, 0, stream, P);
+    if (rc != 0 || P.line.pad < 0) return rc;
+    return gbs_kv_launch(p, k_kv_attn_join<ROWS>, dim3((unsigned)blocks), 256, 0, stream, P);
 }

@@ -67,14 +67,14 @@ __device__ __forceinline__ void kv_finish(float y[16], int l8, float top, float 
 __device__ __forceinline__ void kv_row_of(const gbs_kv_attn& A, const KvSeg& s, int row, int& token, int& head)
 {
     const int r = s.e.row0 + row;
-    token = r / A.group;
+    token = A.by_group(r);
     head = s.head * A.group + (r - token * A.group);
 }
 
 // The segments that several blocks share: block b joins the one that starts in block b, a warp a row, eight
 // rows a block of this kernel.  The pieces' weights come first, a
 // lane a piece, so that their sums can be fetched many at a time: up to a few dozen pieces of a long sequence are as many trips to memory otherwise.
-template <int ROWS, int UNIT>
+template <int ROWS>
 __global__ __launch_bounds__(256) void k_kv_attn_join(const __grid_constant__ KvAttnArgs P)
 {
     constexpr int PART = KV_PART<ROWS>;
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(const __grid_constant__ Kv
     KvSeg s;
     s.index = j.index;
     s.head = j.head;
-    s.e = kv_entry(A, j.index, P.line.tiles, ROWS, UNIT);
+    s.e = kv_entry(A, P.line, j.index);
     const int l8 = lane & 7;                             // the four groups of eight lanes do the same; the first one writes
     float y[16];
 #pragma unroll

@@ -2,6 +2,8 @@
 // anything is launched; what only the device knows (lengths, page numbers) the kernels check.
 #include <math.h>
 
+#include <algorithm>
+
 #include "gbs_internal.h"
 
 namespace {
@@ -220,12 +222,13 @@ extern "C" int gbs_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache
     A.seqs = seqs;
     A.cu = cu_tokens;
     A.n_items = n_items;
-    A.max_tokens = max_tokens;
+    A.max_tokens = (int)std::min<int64_t>(max_tokens, n_tokens);
     A.max_len = max_len > 0 ? max_len : A.c.max_pages << A.c.page_log;
     A.window = window;
     A.causal = flags & GBS_KV_CAUSAL;
     A.n_heads = n_heads;
     A.group = n_heads / A.c.heads;
+    A.by_group.set((unsigned)A.group);
     A.d = p->d;
     A.scale = scale == 0.f ? (float)(1.0 / sqrt((double)p->d)) : scale;
     A.n_tokens = n_tokens;

@@ -2,10 +2,12 @@
 //
 // Rows of an item are numbered token-major, (token, query head of the KV head); a tile is `rows` of them of one KV head, a segment is a
 // tile with the part of the cache that any of its rows sees, cut into units of `unit` tokens.  The segments, in the order (item, tile, KV
-// head), make one line of units, which the blocks share evenly: block b takes units b q .. (b + 1) q - 1, whatever segments they
-// belong to.  So a batch of very different lengths is balanced without the host knowing one of them.  A segment that lies in one block is
+// head), make one line, which the blocks share evenly: block b takes places b q .. (b + 1) q - 1, whatever segments they
+// belong to.  So a batch of very different lengths is balanced without the host knowing one of them.  A segment takes as many places as it has
+// units and `pad` more at its front, for what a segment costs apart from its units.  A segment whose units lie in one block is
 // finished there; of one that several blocks share each leaves its sums in its workspace, and the join adds them up.  A
 // block has at most two such segments: its first (slot 0) and its last (slot 1).
+// Where no sequence is long, segments are not divided at all (pad < 0): each takes one place, and there is nothing to join.
 #pragma once
 
 #include "gbs_kv.cuh"
@@ -33,10 +35,19 @@ __device__ __forceinline__ int kv_row_lo(const gbs_kv_attn& A, const KvEntry& e,
     return A.window > 0 ? max(0, e.before + token - A.window + 1) : 0;
 }
 
-__device__ __forceinline__ KvEntry kv_entry(const gbs_kv_attn& A, int index, int tiles, int tile_rows, int unit)
+struct KvLine {
+    int entries, tiles, tile_rows;
+    int unit_log;
+    int pad;               // places of a segment before its units; -1: segments are not divided
+    int least;             // a block takes at least so many places
+    gbs_kv_div by_tiles;
+    __device__ __forceinline__ int places(int units) const { return pad < 0 ? units != 0 : units != 0 ? units + pad : 0; }
+};
+
+__device__ __forceinline__ KvEntry kv_entry(const gbs_kv_attn& A, const KvLine& L, int index)
 {
     KvEntry e;
-    const int item = index / tiles, tile = index - item * tiles;
+    const int item = L.by_tiles(index), tile = index - item * L.tiles;
     e.first = item;
     e.seq = A.seqs ? A.seqs[item] : item;
     int count = 1;
@@ -49,54 +60,67 @@ __device__ __forceinline__ KvEntry kv_entry(const gbs_kv_attn& A, int index, int
     // no item has more rows than the call, nor a row outside it, whatever cu holds
     if (e.first < 0 || e.first > (int)A.n_tokens) count = 0;
     else count = min(count, (int)A.n_tokens - e.first);
-    e.row0 = tile * tile_rows;
+    e.row0 = tile * L.tile_rows;
     e.rows = max(0, min(count, A.max_tokens)) * A.group;
     e.before = e.length = e.lo = e.hi = e.units = 0;
     if (e.row0 >= e.rows) return e;
     e.before = length - count;
     e.length = min(length, A.max_len);
-    const int last = min(e.rows, e.row0 + tile_rows) - 1;
-    e.hi = kv_row_hi(A, e, last / A.group);
-    e.lo = kv_row_lo(A, e, e.row0 / A.group);
+    const int last = min(e.rows, e.row0 + L.tile_rows) - 1;
+    e.hi = kv_row_hi(A, e, A.by_group(last));
+    e.lo = kv_row_lo(A, e, A.by_group(e.row0));
     // a tile that sees nothing is one unit too: its rows become 0
     e.units = 1;
-    if (e.hi > e.lo) e.units = (e.hi - 1) / unit - e.lo / unit + 1;
+    if (e.hi > e.lo) e.units = ((e.hi - 1) >> L.unit_log) - (e.lo >> L.unit_log) + 1;
     return e;
 }
 
-// A segment in a block's line: units 0 .. end of the line are the block's.
+// A segment in a block's line.
 struct KvSeg {
     int index, head;       // entry, KV head
-    int at;                // where its first unit lies; below 0 where the block before has its start
+    int at;                // its first place; below 0 where the block before has it
     KvEntry e;
 };
 
-__device__ __forceinline__ void kv_next(const gbs_kv_attn& A, KvSeg& s, int entries, int tiles, int tile_rows, int unit)
+// What of a segment is a block's: units skip .. skip + n - 1 of it.
+struct KvPiece {
+    int skip, n;
+    bool starts, ends;     // it has the segment's first unit, its last one
+};
+__device__ __forceinline__ KvPiece kv_piece(const KvLine& L, const KvSeg& s, int places)
 {
-    s.at += s.e.units;
+    if (L.pad < 0) return KvPiece{0, s.e.units, true, true};
+    const int first = s.at + L.pad, end = first + s.e.units;
+    return KvPiece{max(0, -first), min(places, end) - max(first, 0), first >= 0, end <= places};
+}
+// whether the block has places behind this segment
+__device__ __forceinline__ bool kv_more(const KvLine& L, const KvSeg& s, int places) { return s.at + L.places(s.e.units) < places; }
+
+__device__ __forceinline__ void kv_next(const gbs_kv_attn& A, const KvLine& L, KvSeg& s)
+{
+    s.at += L.places(s.e.units);
     if (++s.head < A.c.heads) return;
     s.head = 0;
     do {
-        if (++s.index >= entries) { s.e.units = 0x3fffffff; return; }       // behind the last: never reached by a block's units
-        s.e = kv_entry(A, s.index, tiles, tile_rows, unit);
+        if (++s.index >= L.entries) { s.e.units = 0x3fffffff; return; }     // behind the last: a block has no places there
+        s.e = kv_entry(A, L, s.index);
     } while (s.e.units == 0);
 }
 
-struct KvLine {
-    int entries, tiles, tile_rows, unit;
-    int least;             // a block takes at least so many units; 0: whole segments, one after another
-};
-
-// The block's share: how many units, and the segment of the first one.  All threads of the block call it; `sh` holds 3 + 3 * warps ints.
-// Units are counted in 64 bits: sums over all entries and heads.
+// The block's share: how many places, and in S the segment of the first one.  All threads of the block call it; `sh` is shared memory for
+// one number a warp.  Places are counted in 64 bits: sums over all entries and heads.
 template <int THREADS>
-__device__ __forceinline__ int kv_share(const gbs_kv_attn& A, const KvLine& L, KvSeg& s, long long* sh)
+__device__ __forceinline__ int kv_share(const gbs_kv_attn& A, const KvLine& L, KvSeg* found, long long* sh)
 {
     constexpr int WARPS = THREADS / 32;
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const int per = (L.entries + THREADS - 1) / THREADS, e0 = min(tid * per, L.entries), e1 = min(e0 + per, L.entries);
     long long mine = 0;
-    for (int i = e0; i < e1; ++i) mine += kv_entry(A, i, L.tiles, L.tile_rows, L.unit).units;
+    KvEntry e = {};
+    for (int i = e0; i < e1; ++i) {
+        e = kv_entry(A, L, i);
+        mine += L.places(e.units);
+    }
     long long sum = mine;
 #pragma unroll
     for (int h = 1; h < 32; h <<= 1) {
@@ -116,34 +140,34 @@ __device__ __forceinline__ int kv_share(const gbs_kv_attn& A, const KvLine& L, K
     if (quota < L.least) quota = L.least;
     const long long from = quota * blockIdx.x;
     long long here = (below + sum - mine) * A.c.heads;                      // where this thread's first entry lies
-    int* found = reinterpret_cast<int*>(sh + WARPS);
-    __syncthreads();
     if (from < total && here <= from && from < here + mine * A.c.heads) {
         int i = e0;
-        long long n;
         for (;; ++i) {
-            n = kv_entry(A, i, L.tiles, L.tile_rows, L.unit).units;
-            if (from < here + n * A.c.heads) break;
-            here += n * A.c.heads;
+            if (per > 1) e = kv_entry(A, L, i);
+            const long long n = (long long)L.places(e.units) * A.c.heads;
+            if (from < here + n) break;
+            here += n;
         }
-        const int head = (int)((from - here) / n);
-        found[0] = i;
-        found[1] = head;
-        found[2] = (int)(here + head * n - from);                           // 0 or below
+        const int n = L.places(e.units), head = (int)((from - here) / n);
+        found->index = i;
+        found->head = head;
+        found->at = (int)(here + (long long)head * n - from);               // 0 or below
+        found->e = e;
     }
     __syncthreads();
-    if (from >= total) return 0;
-    s.index = found[0];
-    s.head = found[1];
-    s.at = found[2];
-    s.e = kv_entry(A, s.index, L.tiles, L.tile_rows, L.unit);
-    return (int)min(quota, total - from);
+    return from >= total ? 0 : (int)min(quota, total - from);
 }
 
-// What a block leaves for the join about the segment that starts in it and ends in another block; blocks = 0: no such segment.
+// What a block leaves for the join about the segment whose first unit it has and that ends in another block; blocks = 0: no such segment.
 struct KvJoin {
     int index, head, blocks;
     int pad;
 };
+// the blocks behind have as many places each, or their rest
+__device__ __forceinline__ KvJoin kv_join(const KvLine& L, const KvSeg& s, int places)
+{
+    const int beyond = s.at + L.pad + s.e.units - places;
+    return KvJoin{s.index, s.head, 1 + (beyond + places - 1) / places, 0};
+}
 
 }  // namespace

@@ -30,7 +30,8 @@ struct Smem {
     float factor[ROWS], qsum[ROWS];
     float m[ROWS], l[ROWS], add[ROWS];
     unsigned long long kfull, kfree, vfull, vfree, sfull, pfull;
-    long long share[THREADS / 32 + 3];
+    KvSeg seg;
+    long long share[THREADS / 32];
     unsigned tmem;
     int abort;
 };
@@ -139,15 +140,16 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
     kv_wait_before();
     kv_let_next();
 
-    KvSeg seg;
-    const int units = kv_share<THREADS>(A, P.line, seg, S.share);
+    const int places = kv_share<THREADS>(A, P.line, &S.seg, S.share);
+    KvSeg seg = S.seg;
     if (tid == 0) P.joins[blockIdx.x] = KvJoin{0, 0, 0, 0};
 
     const int ps_log = A.c.page_log, ps = 1 << ps_log;
     unsigned it = 0;                                         // tiles so far, by which the barriers' phases go
-    for (bool more = units > 0; more;) {
-        const int skip = max(0, -seg.at), n = min(units, seg.at + seg.e.units) - max(seg.at, 0);
-        const int tok0 = (seg.e.lo / UNIT + skip) * UNIT;
+    for (bool more = places > 0; more;) {
+        const KvPiece piece = kv_piece(P.line, seg, places);
+        const int n = piece.n, tok0 = (seg.e.lo / UNIT + piece.skip) * UNIT;
+        if (n <= 0) break;                                   // the block's last places are in front of a segment's units
 
         // ---- query rows: eight lanes a row, 32 rows at a time ----
         Token x;
@@ -162,20 +164,26 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
             page = tok + UNIT < seg.e.hi ? row[(tok + UNIT) >> ps_log] : -1;
         }
         {
-#pragma unroll 1
-            for (int r0 = 0; r0 < ROWS; r0 += 32) {
-                const int row = r0 + (tid >> 3), l8 = tid & 7;
-                uint4 a = make_uint4(0, 0, 0, 0), b = a;
+            const int l8 = tid & 7;
+            uint4 raw[4][2];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = 32 * r + (tid >> 3);
+                raw[r][0] = raw[r][1] = make_uint4(0, 0, 0, 0);
                 if (seg.e.row0 + row < seg.e.rows) {
                     int token, head;
                     kv_row_of(A, seg, row, token, head);
                     const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(A.q) + (seg.e.first + token) * A.q_token + head * A.q_head;
-                    if (8 * l8 < A.d) a = *reinterpret_cast<const uint4*>(q + 8 * l8);
-                    if (64 + 8 * l8 < A.d) b = *reinterpret_cast<const uint4*>(q + 64 + 8 * l8);
+                    if (8 * l8 < A.d) raw[r][0] = *reinterpret_cast<const uint4*>(q + 8 * l8);
+                    if (64 + 8 * l8 < A.d) raw[r][1] = *reinterpret_cast<const uint4*>(q + 64 + 8 * l8);
                 }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = 32 * r + (tid >> 3);
                 float y[16];
-                kv_unpack_bf16(a, y);
-                kv_unpack_bf16(b, y + 8);
+                kv_unpack_bf16(raw[r][0], y);
+                kv_unpack_bf16(raw[r][1], y + 8);
                 kv_hadamard(y, l8);
                 float m = 0.f;
 #pragma unroll
@@ -290,10 +298,10 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
             // ---- softmax: a thread a row ----
             const unsigned lanes = tmem + ((unsigned)w << 21);
             const bool here = seg.e.row0 + tid < seg.e.rows;
-            const int my_token = (min(seg.e.row0 + tid, seg.e.rows - 1)) / A.group;
+            const int my_token = A.by_group(min(seg.e.row0 + tid, seg.e.rows - 1));
             const int row_lo = kv_row_lo(A, seg.e, my_token), row_hi = here ? kv_row_hi(A, seg.e, my_token) : 0;
             // tokens that every row of the tile sees need no mask
-            const int all_lo = kv_row_lo(A, seg.e, (min(seg.e.rows, seg.e.row0 + ROWS) - 1) / A.group), all_hi = kv_row_hi(A, seg.e, seg.e.row0 / A.group);
+            const int all_lo = kv_row_lo(A, seg.e, A.by_group(min(seg.e.rows, seg.e.row0 + ROWS) - 1)), all_hi = kv_row_hi(A, seg.e, A.by_group(seg.e.row0));
             const float f = S.factor[tid], qs = S.qsum[tid];
             const f32x2 f2 = both(f), qs2 = both(qs);
             float M = NONE;
@@ -433,7 +441,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
         it += n;
         __syncthreads();
         tc_fence_after();
-        const bool starts = seg.at >= 0, ends = seg.at + seg.e.units <= units;
+        const bool starts = piece.starts, ends = piece.ends;
         if (S.abort) break;
         {
             float* part = P.parts + ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * PART;
@@ -470,10 +478,10 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
                 }
             }
             if (tid == 0 && starts && !ends)
-                P.joins[blockIdx.x] = KvJoin{seg.index, seg.head, 1 + (seg.at + seg.e.units - 1) / units, 0};
+                P.joins[blockIdx.x] = kv_join(P.line, seg, places);
         }
-        more = seg.at + seg.e.units < units;
-        if (more) kv_next(A, seg, P.line.entries, P.line.tiles, ROWS, UNIT);
+        more = kv_more(P.line, seg, places);
+        if (more) kv_next(A, P.line, seg);
         __syncthreads();                                     // shared memory is free for the next segment
     }
     tc_fence_before();
@@ -498,8 +506,10 @@ int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspac
     KvAttnArgs P = {};
     P.a = A;
     P.line.tile_rows = ROWS;
-    P.line.unit = UNIT;
+    P.line.unit_log = 7;
+    P.line.pad = 3;
     P.line.tiles = (int)(((int64_t)A.max_tokens * A.group + ROWS - 1) / ROWS);
+    P.line.by_tiles.set((unsigned)P.line.tiles);
     P.line.entries = A.n_items * P.line.tiles;
     P.line.least = 1;
     const int blocks = blocks_of(p);
@@ -512,5 +522,5 @@ int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspac
     if (e != cudaSuccess) return (int)e;
     const int rc = gbs_kv_launch(p, p->asym ? k_tc_kvattn<true> : k_tc_kvattn<false>, dim3((unsigned)blocks), THREADS, smem, stream, P);
     if (rc != 0) return rc;
-    return gbs_kv_launch(p, k_kv_attn_join<ROWS, UNIT>, dim3((unsigned)blocks, ROWS / 8), 256, 0, stream, P);
+    return gbs_kv_launch(p, k_kv_attn_join<ROWS>, dim3((unsigned)blocks, ROWS / 8), 256, 0, stream, P);
 }
