@@ -6,8 +6,9 @@
 // With log2 Delta_v inside the exponent one running maximum M (of z) serves both the weights' range in fp16 and the softmax; a row with zero
 // values alone has codes 0, and takes the largest scale next to it.  f is the row's factor (its power of two, the softmax scale).
 //
-// Warps 0-3: softmax, a thread a row.  Warps 4-7: codes to fp16, a thread a cached token; they fetch the next tile's codes into
-// registers while this one's are worked on.  Warp 4 also issues the MMAs: a ninth warp would cost all of them 32 registers each.  Scores and weights share 128 columns of tensor memory (a thread's
+// All eight warps do the same in turn: the softmax of 16 rows (a thread has two of them and every fourth pair of columns, so that a tile's per-token
+// numbers are read once for 16 rows), then half a row of key codes and half a row of value codes of the next tile to fp16, fetched
+// into registers a tile ahead.  Warp 0 also issues the MMAs.  Scores and weights share 128 columns of tensor memory (a warp's
 // fp16 weights overwrite scores it has read), the sums take 128 more, so two blocks run on an SM and fill each other's gaps.
 // The work per tile and SM: 2 x 512 cycles of MMA, 1024 of ex2; what bounds it is REPLACE.
 #include "gbs_kv_attn.cuh"
@@ -28,8 +29,9 @@ struct Smem {
     unsigned char v[UNIT * 256];                     // N-major for the second product: the same bytes
     float ks[2][UNIT], lv[2][UNIT], rv[2][UNIT], kl[2][UNIT], vl[2][UNIT];       // of tile i in [i & 1]: Delta_k, log2 Delta_v, 1 / Delta_v, lo
     float factor[ROWS], qsum[ROWS];
+    int lo[ROWS], hi[ROWS];                          // tokens that a row sees
     float m[ROWS], l[ROWS], add[ROWS];
-    unsigned long long kfull, kfree, vfull, vfree, sfull, pfull;
+    unsigned long long kfull, vfull, vfree, sfull, pfull;
     KvSeg seg;
     long long share[THREADS / 32];
     unsigned tmem;
@@ -43,11 +45,46 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
     return d;
 }
 __device__ __forceinline__ f32x2 both(float x) { return pk(__float_as_uint(x), __float_as_uint(x)); }
-__device__ __forceinline__ void tmem_ld_wait16(unsigned r[16])
+// 16 lanes: thread T has rows T / 4 and T / 4 + 8; of each 8 columns 2 (T % 4) and the next one (registers 4 i, 4 i + 1 of the upper row,
+// 4 i + 2, 4 i + 3 of the lower), of each 4 columns T % 4 (registers 2 i and 2 i + 1)
+__device__ __forceinline__ void tmem_ld64(unsigned taddr, unsigned r[32])
 {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-        : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-          "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st64(unsigned taddr, const unsigned r[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.16x256b.x8.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32p(unsigned taddr, unsigned r[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x128b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32p(unsigned taddr, const unsigned r[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.16x128b.x8.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -59,9 +96,9 @@ __device__ __forceinline__ unsigned piece_at(int row, int piece)
 // byte of a 16-byte piece (4 coordinates) of a row of sums
 __device__ __forceinline__ unsigned sum_at(int row, int piece) { return (unsigned)row * 512 + (unsigned)((piece ^ (row & 31)) << 4); }
 
-// A cached token's codes and scales on their way through registers.
+// Half of a cached token's codes (64 coordinates) and its scales on their way through registers.
 struct Token {
-    uint4 k[4], v[4];
+    uint4 k[2], v[2];
     float ks, kl, vs, vl;
     bool ok;
 };
@@ -72,17 +109,15 @@ __device__ __forceinline__ const unsigned char* find(const gbs_kv_attn& A, const
     return kv_block(A.c, page, s.head);
 }
 template <bool ASYM>
-__device__ __forceinline__ void load_k(Token& x, const unsigned char* block, int slot, int ps)
+__device__ __forceinline__ void load_k(Token& x, const unsigned char* block, int slot, int ps, int half)
 {
     x.ok = block != nullptr;
-    x.ks = x.kl = x.vl = 0.f;
-    x.vs = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.k[i] = make_uint4(0, 0, 0, 0);
+    x.ks = x.kl = x.vs = x.vl = 0.f;
+    x.k[0] = x.k[1] = make_uint4(0, 0, 0, 0);
     if (!block) return;
-    const uint4* c = reinterpret_cast<const uint4*>(block + slot * KV_ROW);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.k[i] = c[i];
+    const uint4* c = reinterpret_cast<const uint4*>(block + slot * KV_ROW) + 2 * half;
+    x.k[0] = c[0];
+    x.k[1] = c[1];
     const float* sc = reinterpret_cast<const float*>(block + 2 * ps * KV_ROW);
     if (ASYM) {
         const float2 a = reinterpret_cast<const float2*>(sc)[slot], b = reinterpret_cast<const float2*>(sc)[ps + slot];
@@ -92,26 +127,25 @@ __device__ __forceinline__ void load_k(Token& x, const unsigned char* block, int
         x.vs = sc[ps + slot];
     }
 }
-__device__ __forceinline__ void load_v(Token& x, const unsigned char* block, int slot, int ps)
+__device__ __forceinline__ void load_v(Token& x, const unsigned char* block, int slot, int ps, int half)
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[i] = make_uint4(0, 0, 0, 0);
+    x.v[0] = x.v[1] = make_uint4(0, 0, 0, 0);
     if (!block) return;
-    const uint4* c = reinterpret_cast<const uint4*>(block + (ps + slot) * KV_ROW);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[i] = c[i];
+    const uint4* c = reinterpret_cast<const uint4*>(block + (ps + slot) * KV_ROW) + 2 * half;
+    x.v[0] = c[0];
+    x.v[1] = c[1];
 }
 // A word's 8 coordinates stand in the order 0, 4, 1, 5, 2, 6, 3, 7, in the queries as well; the results' columns are put back at the end.
 template <bool ASYM>
-__device__ __forceinline__ void store_codes(unsigned char* tile, int row, const uint4 c[4])
+__device__ __forceinline__ void store_codes(unsigned char* tile, int row, int half, const uint4 c[2])
 {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 8; ++i) {
         const uint4 q = c[i >> 2];
         const unsigned w = (i & 3) == 0 ? q.x : (i & 3) == 1 ? q.y : (i & 3) == 2 ? q.z : q.w;
         unsigned h[4];
         kv_codes_f16<ASYM>(w, h);
-        *reinterpret_cast<uint4*>(tile + piece_at(row, i)) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(tile + piece_at(row, 8 * half + i)) = make_uint4(h[0], h[1], h[2], h[3]);
     }
 }
 
@@ -121,18 +155,17 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
     extern __shared__ unsigned char smem_raw[];
     Smem& S = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const gbs_kv_attn& A = P.a;
-    const int tid = threadIdx.x, w = warp_index();
+    const int tid = threadIdx.x, lane = tid & 31, w = warp_index();
     if (tid == 0) {
         S.abort = 0;
-        mbar_init(&S.kfull, 128);
-        mbar_init(&S.kfree, 1);
-        mbar_init(&S.vfull, 128);
+        mbar_init(&S.kfull, 8);
+        mbar_init(&S.vfull, 8);
         mbar_init(&S.vfree, 1);
         mbar_init(&S.sfull, 1);
-        mbar_init(&S.pfull, 128);
+        mbar_init(&S.pfull, 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (w == 4) tmem_alloc(&S.tmem, TMEM_COLS);
+    if (w == 0) tmem_alloc(&S.tmem, TMEM_COLS);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -153,16 +186,13 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
 
         // ---- query rows: eight lanes a row, 32 rows at a time ----
         Token x;
-        const unsigned char* block = nullptr;
-        int page = -1;
-        if (w >= 4) {
-            const int tok = tok0 + tid - 128;
-            const int* row = A.c.page_table + (long long)seg.e.seq * A.c.max_pages;
-            block = find(A, seg, tok, tok < seg.e.hi ? row[tok >> ps_log] : -1);
-            load_k<ASYM>(x, block, tok & (ps - 1), ps);
-            load_v(x, block, tok & (ps - 1), ps);
-            page = tok + UNIT < seg.e.hi ? row[(tok + UNIT) >> ps_log] : -1;
-        }
+        const int me = tid & 127, part = tid >> 7;           // this thread's token of a tile, and which half of its row
+        const int* row_of_pages = A.c.page_table + (long long)seg.e.seq * A.c.max_pages;
+        const auto page_of = [&](int tok) { return tok < seg.e.hi ? row_of_pages[tok >> ps_log] : -1; };
+        const unsigned char* block = find(A, seg, tok0 + me, page_of(tok0 + me));
+        load_k<ASYM>(x, block, (tok0 + me) & (ps - 1), ps, part);
+        load_v(x, block, (tok0 + me) & (ps - 1), ps, part);
+        int page = page_of(tok0 + me + UNIT);
         {
             const int l8 = tid & 7;
             uint4 raw[4][2];
@@ -211,243 +241,261 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
                 if (l8 == 0) {
                     S.factor[row] = up * (A.scale * (KV_NORM * 1.4426950408889634f));
                     S.qsum[row] = sum;
+                    const int token = A.by_group(min(seg.e.row0 + row, seg.e.rows - 1));
+                    S.lo[row] = kv_row_lo(A, seg.e, token);
+                    S.hi[row] = seg.e.row0 + row < seg.e.rows ? kv_row_hi(A, seg.e, token) : 0;
                 }
             }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
 
-        if (w >= 4) {
-            // ---- codes to fp16; warp 4: the MMAs as well ----
-            constexpr unsigned ID_S = (1u << 4) | ((unsigned)(UNIT >> 3) << 17) | ((unsigned)(ROWS >> 4) << 24);             // fp16, both K-major
-            constexpr unsigned ID_O = ID_S | (1u << 16);                                                                    // B N-major
-            const unsigned long long qd = smem_desc(smem_u32(S.q), 16, 1024, 2), kd = smem_desc(smem_u32(S.k), 16, 1024, 2),
-                                     vd = smem_desc(smem_u32(S.v), 128 * 128, 1024, 2);
-            const int me = tid - 128;
-            const int* row = A.c.page_table + (long long)seg.e.seq * A.c.max_pages;
-            // the keys of tile i into shared memory, those of tile i + 1 on their way
-            auto keys = [&](int i) {
-                const unsigned now = it + i;
-                const int tok = tok0 + i * UNIT + me, b = now & 1;
-                // zero rows take the largest scale next to them; tokens that are not there weigh nothing, and scales that are no
-                // numbers make the scores of those that see them none
+        constexpr unsigned ID_S = (1u << 4) | ((unsigned)(UNIT >> 3) << 17) | ((unsigned)(ROWS >> 4) << 24);             // fp16, both K-major
+        constexpr unsigned ID_O = ID_S | (1u << 16);                                                                    // B N-major
+        // the keys of tile i into shared memory, those of tile i + 1 on their way.  The tile before has been read: its scores are there
+        const auto keys = [&](int i) {
+            const int tok = tok0 + i * UNIT + me, b = (it + i) & 1;
+            // zero rows take the largest scale next to them; tokens that are not there weigh nothing, and scales that are no
+            // numbers make the scores of those that see them none
+            if (part == 0) {
                 float vs = x.vs, near = x.vs;
 #pragma unroll
                 for (int h = 16; h; h >>= 1) near = fmaxf(near, __shfl_xor_sync(0xffffffffu, near, h));
                 const bool wrong = !(fabsf(vs) < INFINITY) || !(fabsf(x.vl) < INFINITY);
                 if (vs == 0.f) vs = near > 0.f ? near : 1.f;
                 vs = fmaxf(vs, 7.888609052210118e-31f);                          // 2^-100
-                const float lv = !x.ok ? -INFINITY : wrong ? NAN : __log2f(vs), rv = x.ok && !wrong ? 1.f / vs : 0.f;
-                if (now > 0 && !mbar_wait(&S.abort, &S.kfree, (now + 1) & 1u, P.status, 74)) return false;
+                S.lv[b][me] = !x.ok ? -INFINITY : wrong ? NAN : __log2f(vs);
+                S.rv[b][me] = x.ok && !wrong ? 1.f / vs : 0.f;
+                if (ASYM) S.vl[b][me] = wrong ? 0.f : x.vl;
+            } else {
                 S.ks[b][me] = x.ks;
-                S.lv[b][me] = lv;
-                S.rv[b][me] = rv;
-                if (ASYM) {
-                    S.kl[b][me] = x.kl;
-                    S.vl[b][me] = wrong ? 0.f : x.vl;
-                }
-                store_codes<ASYM>(S.k, me, x.k);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(&S.kfull);
-                const int next = tok + UNIT;
-                block = i + 1 < n ? find(A, seg, next, page) : nullptr;
-                page = next + UNIT < seg.e.hi ? row[(next + UNIT) >> ps_log] : -1;
-                load_k<ASYM>(x, block, next & (ps - 1), ps);
-                return true;
-            };
-            auto scores = [&](int i) {
-                if (w != 4) return true;
-                if (!mbar_wait_warp(&S.abort, &S.kfull, (it + i) & 1u, P.status, 71)) return false;
-                tc_fence_after();
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {                // sixteen coordinates: 32 bytes, four of them in a block of 64
-                    const unsigned long long off = (unsigned)((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
-                    umma_f16(tmem, qd + off, kd + off, ID_S, k > 0);
-                }
-                umma_commit(&S.sfull);
-                umma_commit(&S.kfree);
-                return true;
-            };
-            bool ok = __all_sync(0xffffffffu, keys(0));
-            if (ok) ok = scores(0);
-            for (int i = 0; i < n && __all_sync(0xffffffffu, ok); ++i) {
-                const unsigned now = it + i;
-                const int tok = tok0 + i * UNIT + me;
-                if (now > 0 && !mbar_wait(&S.abort, &S.vfree, (now + 1) & 1u, P.status, 75)) ok = false;
-                if (!__all_sync(0xffffffffu, ok)) break;
-                store_codes<ASYM>(S.v, me, x.v);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(&S.vfull);
-                if (i + 1 < n) {
-                    const unsigned char* ahead = block;
-                    load_v(x, ahead, (tok + UNIT) & (ps - 1), ps);
-                    ok = keys(i + 1);
-                }
-                if (w == 4) {
-                    if (!__all_sync(0xffffffffu, ok) || !mbar_wait_warp(&S.abort, &S.vfull, now & 1u, P.status, 72) ||
-                        !mbar_wait_warp(&S.abort, &S.pfull, now & 1u, P.status, 73)) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)              // sixteen tokens: two groups of eight rows
-                        umma_f16_ts(tmem + O_COL, tmem + 8 * k, vd + (unsigned)((k * 2048) >> 4), ID_O, i > 0 || k > 0);
-                    umma_commit(&S.vfree);
-                    if (i + 1 < n) ok = scores(i + 1);
-                }
+                if (ASYM) S.kl[b][me] = x.kl;
             }
-        } else {
-            // ---- softmax: a thread a row ----
-            const unsigned lanes = tmem + ((unsigned)w << 21);
-            const bool here = seg.e.row0 + tid < seg.e.rows;
-            const int my_token = A.by_group(min(seg.e.row0 + tid, seg.e.rows - 1));
-            const int row_lo = kv_row_lo(A, seg.e, my_token), row_hi = here ? kv_row_hi(A, seg.e, my_token) : 0;
-            // tokens that every row of the tile sees need no mask
-            const int all_lo = kv_row_lo(A, seg.e, A.by_group(min(seg.e.rows, seg.e.row0 + ROWS) - 1)), all_hi = kv_row_hi(A, seg.e, A.by_group(seg.e.row0));
-            const float f = S.factor[tid], qs = S.qsum[tid];
-            const f32x2 f2 = both(f), qs2 = both(qs);
-            float M = NONE;
-            f32x2 l2 = both(0.f), add2v = both(0.f);
-            bool ok = true;
-            for (int i = 0; i < n && ok; ++i) {
-                const unsigned now = it + i;
-                const int b = now & 1, tok = tok0 + i * UNIT;
-                const bool plain = tok >= all_lo && tok + UNIT <= all_hi;
-                if (!(ok = mbar_wait_warp(&S.abort, &S.sfull, now & 1u, P.status, 76))) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    unsigned r[32];
-                    tmem_ld32_issue(lanes + 32 * c, r);
-                    tmem_ld_wait(r);
-                    const ulonglong2* ks = reinterpret_cast<const ulonglong2*>(&S.ks[b][32 * c]);
-                    const ulonglong2* lv = reinterpret_cast<const ulonglong2*>(&S.lv[b][32 * c]);
-                    const ulonglong2* kl = reinterpret_cast<const ulonglong2*>(&S.kl[b][32 * c]);
-                    f32x2 z[16];
+            store_codes<ASYM>(S.k, me, part, x.k);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&S.kfull);
+            const int next = tok + UNIT;
+            block = i + 1 < n ? find(A, seg, next, page) : nullptr;
+            page = page_of(next + UNIT);
+            load_k<ASYM>(x, block, next & (ps - 1), ps, part);
+        };
+        const auto values = [&](int i, const unsigned char* next_block) {
+            store_codes<ASYM>(S.v, me, part, x.v);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&S.vfull);
+            load_v(x, next_block, (tok0 + (i + 1) * UNIT + me) & (ps - 1), ps, part);
+        };
+        const auto scores = [&](int i) {
+            if (!mbar_wait_warp(&S.abort, &S.kfull, (it + i) & 1u, P.status, 71)) return false;
+            tc_fence_after();
+            const unsigned long long qd = smem_desc(smem_u32(S.q), 16, 1024, 2), kd = smem_desc(smem_u32(S.k), 16, 1024, 2);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const ulonglong2 k2 = ks[j], v2 = lv[j];
-                        f32x2 a = mul2(pk(r[4 * j], r[4 * j + 1]), k2.x), d = mul2(pk(r[4 * j + 2], r[4 * j + 3]), k2.y);
-                        if (ASYM) {
-                            const ulonglong2 o2 = kl[j];
-                            a = fma2(o2.x, qs2, a);
-                            d = fma2(o2.y, qs2, d);
-                        }
-                        z[2 * j] = fma2(a, f2, v2.x);
-                        z[2 * j + 1] = fma2(d, f2, v2.y);
-                    }
-                    if (!plain) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            unsigned u0, u1;
-                            unpk(z[j], u0, u1);
-                            const int t = tok + 32 * c + 2 * j;
-                            if (t < row_lo || t >= row_hi) u0 = 0xff800000u;
-                            if (t + 1 < row_lo || t + 1 >= row_hi) u1 = 0xff800000u;
-                            z[j] = pk(u0, u1);
-                        }
-                    }
-                    float top = NONE;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        unsigned u0, u1;
-                        unpk(z[j], u0, u1);
-                        top = max3(__uint_as_float(u0), __uint_as_float(u1), top);
-                    }
-                    if (__any_sync(0xffffffffu, top > M + MOVE)) {
-                        const float mx = fmaxf(M, top), keep = kv_ex2(M - mx);
-                        M = mx;
-                        const f32x2 keep2 = both(keep);
-                        l2 = mul2(l2, keep2);
-                        add2v = mul2(add2v, keep2);
-                        tmem_st_wait();
-                        if (i > 0) {
-#pragma unroll 1
-                            for (int q = 0; q < 8; ++q) {
-                                unsigned o[16];
-                                uint4 st[4];
-                                tmem_ld16_issue(lanes + O_COL + 16 * q, o);
-                                tmem_ld_wait16(o);
-#pragma unroll
-                                for (int k = 0; k < 4; ++k)
-                                    st[k] = make_uint4(__float_as_uint(__uint_as_float(o[4 * k]) * keep), __float_as_uint(__uint_as_float(o[4 * k + 1]) * keep),
-                                                       __float_as_uint(__uint_as_float(o[4 * k + 2]) * keep), __float_as_uint(__uint_as_float(o[4 * k + 3]) * keep));
-                                tmem_st16(lanes + O_COL + 16 * q, st);
-                            }
-                        }
-                        const __half2 kh = __float2half2_rn(keep);
-#pragma unroll 1
-                        for (int q = 0; q < c; ++q) {
-                            unsigned o[16];
-                            uint4 st[4];
-                            tmem_ld16_issue(lanes + 16 * q, o);
-                            tmem_ld_wait16(o);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                st[k] = make_uint4(as_u(__hmul2(as_h(o[4 * k]), kh)), as_u(__hmul2(as_h(o[4 * k + 1]), kh)), as_u(__hmul2(as_h(o[4 * k + 2]), kh)),
-                                                   as_u(__hmul2(as_h(o[4 * k + 3]), kh)));
-                            tmem_st16(lanes + 16 * q, st);
-                        }
-                    }
-                    const ulonglong2* rv = reinterpret_cast<const ulonglong2*>(&S.rv[b][32 * c]);
-                    const ulonglong2* vl = reinterpret_cast<const ulonglong2*>(&S.vl[b][32 * c]);
-                    const f32x2 base = both(6.f - M);                            // weights are 64 at M
-                    uint4 st[4];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const ulonglong2 r2 = rv[j];
-                        unsigned h[2];
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            unsigned u0, u1;
-                            unpk(add2(z[2 * j + k], base), u0, u1);
-                            const float w0 = kv_ex2(__uint_as_float(u0)), w1 = kv_ex2(__uint_as_float(u1));
-                            const f32x2 p = mul2(pk(__float_as_uint(w0), __float_as_uint(w1)), k ? r2.y : r2.x);
-                            l2 = add2(l2, p);
-                            if (ASYM) {
-                                const ulonglong2 o2 = vl[j];
-                                add2v = fma2(p, k ? o2.y : o2.x, add2v);
-                            }
-                            h[k] = as_u(__floats2half2_rn(w0, w1));
-                        }
-                        if (j & 1) { st[j >> 1].z = h[0]; st[j >> 1].w = h[1]; }
-                        else { st[j >> 1].x = h[0]; st[j >> 1].y = h[1]; }
-                    }
-                    tmem_st16(lanes + 16 * c, st);
-                }
-                tmem_st_wait();
-                tc_fence_before();
-                mbar_arrive(&S.pfull);
+            for (int k = 0; k < 8; ++k) {                    // sixteen coordinates: 32 bytes, four of them in a block of 64
+                const unsigned long long off = (unsigned)((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
+                umma_f16(tmem, qd + off, kd + off, ID_S, k > 0);
             }
-            // ---- the rows' sums, by way of shared memory ----
-            if (ok && mbar_wait_warp(&S.abort, &S.vfree, (it + n - 1) & 1u, P.status, 77)) {
-                tc_fence_after();
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    unsigned r[32];
-                    tmem_ld32_issue(lanes + O_COL + 32 * c, r);
-                    tmem_ld_wait(r);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        *reinterpret_cast<uint4*>(S.k + sum_at(tid, 8 * c + j)) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
-                }
-            }
-            unsigned a, b;
-            unpk(l2, a, b);
-            S.l[tid] = __uint_as_float(a) + __uint_as_float(b);
-            unpk(add2v, a, b);
-            S.add[tid] = __uint_as_float(a) + __uint_as_float(b);
-            S.m[tid] = M;
-            tc_fence_before();
+            umma_commit(&S.sfull);
+            return true;
+        };
+
+        // this thread's rows: r0 and r0 + 8
+        const int r0 = 32 * (w & 3) + 16 * (w >> 2) + (lane >> 2), c0 = 2 * (lane & 3);
+        const unsigned lanes = tmem + ((unsigned)(32 * (w & 3) + 16 * (w >> 2)) << 16);
+        const f32x2 fa = both(S.factor[r0]), fb = both(S.factor[r0 + 8]);
+        const f32x2 qa = both(S.qsum[r0]), qb = both(S.qsum[r0 + 8]);
+        // tokens that every row of the tile sees need no mask
+        const int all_lo = kv_row_lo(A, seg.e, A.by_group(min(seg.e.rows, seg.e.row0 + ROWS) - 1)), all_hi = kv_row_hi(A, seg.e, A.by_group(seg.e.row0));
+        float Ma = NONE, Mb = NONE;
+        f32x2 la = both(0.f), lb = la, ea = la, eb = la;     // totals and sums of p lo, of even and odd columns
+        keys(0);
+        {
+            const unsigned char* ahead = block;
+            values(0, ahead);
         }
+        bool ok = w != 0 || scores(0);
+        for (int i = 0; i < n && ok; ++i) {
+            const unsigned now = it + i;
+            const int b = now & 1, tok = tok0 + i * UNIT;
+            const bool plain = tok >= all_lo && tok + UNIT <= all_hi;
+            if (!(ok = mbar_wait_warp(&S.abort, &S.sfull, now & 1u, P.status, 76))) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < 2; ++c) {                    // 64 columns at a time
+                unsigned r[32];
+                tmem_ld64(lanes + 64 * c, r);
+                tmem_ld_wait(r);
+                const int at = 64 * c + c0;
+                f32x2 z[16];                                 // of columns 8 j + c0, the next one: upper row, lower row
+                float ta = NONE, tb = NONE;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const f32x2 k2 = *reinterpret_cast<const f32x2*>(&S.ks[b][at + 8 * j]), v2 = *reinterpret_cast<const f32x2*>(&S.lv[b][at + 8 * j]);
+                    f32x2 u = mul2(pk(r[4 * j], r[4 * j + 1]), k2), d = mul2(pk(r[4 * j + 2], r[4 * j + 3]), k2);
+                    if (ASYM) {
+                        const f32x2 o2 = *reinterpret_cast<const f32x2*>(&S.kl[b][at + 8 * j]);
+                        u = fma2(o2, qa, u);
+                        d = fma2(o2, qb, d);
+                    }
+                    z[2 * j] = fma2(u, fa, v2);
+                    z[2 * j + 1] = fma2(d, fb, v2);
+                }
+                if (!plain) {
+                    const int loa = S.lo[r0], hia = S.hi[r0], lob = S.lo[r0 + 8], hib = S.hi[r0 + 8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        unsigned u0, u1;
+                        const int t = tok + at + 8 * j;
+                        unpk(z[2 * j], u0, u1);
+                        if (t < loa || t >= hia) u0 = 0xff800000u;
+                        if (t + 1 < loa || t + 1 >= hia) u1 = 0xff800000u;
+                        z[2 * j] = pk(u0, u1);
+                        unpk(z[2 * j + 1], u0, u1);
+                        if (t < lob || t >= hib) u0 = 0xff800000u;
+                        if (t + 1 < lob || t + 1 >= hib) u1 = 0xff800000u;
+                        z[2 * j + 1] = pk(u0, u1);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    unsigned u0, u1;
+                    unpk(z[2 * j], u0, u1);
+                    ta = max3(__uint_as_float(u0), __uint_as_float(u1), ta);
+                    unpk(z[2 * j + 1], u0, u1);
+                    tb = max3(__uint_as_float(u0), __uint_as_float(u1), tb);
+                }
+                if (__any_sync(0xffffffffu, ta > Ma + MOVE || tb > Mb + MOVE)) {
+                    // rare: a row's four threads agree on its maximum, and what has been added up by the old one shrinks
+#pragma unroll
+                    for (int h = 1; h < 4; h <<= 1) {
+                        ta = fmaxf(ta, __shfl_xor_sync(0xffffffffu, ta, h));
+                        tb = fmaxf(tb, __shfl_xor_sync(0xffffffffu, tb, h));
+                    }
+                    ta = fmaxf(ta, Ma);
+                    tb = fmaxf(tb, Mb);
+                    const float keep_a = kv_ex2(Ma - ta), keep_b = kv_ex2(Mb - tb);
+                    Ma = ta;
+                    Mb = tb;
+                    la = mul2(la, both(keep_a));
+                    lb = mul2(lb, both(keep_b));
+                    ea = mul2(ea, both(keep_a));
+                    eb = mul2(eb, both(keep_b));
+                    tmem_st_wait();
+                    if (i > 0) {
+#pragma unroll 1
+                        for (int q = 0; q < 2; ++q) {
+                            unsigned o[32];
+                            tmem_ld64(lanes + O_COL + 64 * q, o);
+                            tmem_ld_wait(o);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * ((k & 2) ? keep_b : keep_a));
+                            tmem_st64(lanes + O_COL + 64 * q, o);
+                        }
+                    }
+                    if (c > 0) {
+                        unsigned o[16];
+                        tmem_ld32p(lanes, o);
+                        const __half2 ha = __float2half2_rn(keep_a), hb = __float2half2_rn(keep_b);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[k] = as_u(__hmul2(as_h(o[k]), (k & 1) ? hb : ha));
+                        tmem_st32p(lanes, o);
+                    }
+                }
+                const f32x2 base_a = both(6.f - Ma), base_b = both(6.f - Mb);        // weights are 64 at M
+                unsigned st[16];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const f32x2 r2 = *reinterpret_cast<const f32x2*>(&S.rv[b][at + 8 * j]);
+                    unsigned u0, u1, d0, d1;
+                    unpk(add2(z[2 * j], base_a), u0, u1);
+                    unpk(add2(z[2 * j + 1], base_b), d0, d1);
+                    const float wa0 = kv_ex2(__uint_as_float(u0)), wa1 = kv_ex2(__uint_as_float(u1));
+                    const float wb0 = kv_ex2(__uint_as_float(d0)), wb1 = kv_ex2(__uint_as_float(d1));
+                    const f32x2 wa = pk(__float_as_uint(wa0), __float_as_uint(wa1)), wb = pk(__float_as_uint(wb0), __float_as_uint(wb1));
+                    if (ASYM) {
+                        const f32x2 o2 = *reinterpret_cast<const f32x2*>(&S.vl[b][at + 8 * j]);
+                        const f32x2 pa = mul2(wa, r2), pb = mul2(wb, r2);
+                        la = add2(la, pa);
+                        lb = add2(lb, pb);
+                        ea = fma2(pa, o2, ea);
+                        eb = fma2(pb, o2, eb);
+                    } else {
+                        la = fma2(wa, r2, la);
+                        lb = fma2(wb, r2, lb);
+                    }
+                    st[2 * j] = as_u(__floats2half2_rn(wa0, wa1));
+                    st[2 * j + 1] = as_u(__floats2half2_rn(wb0, wb1));
+                }
+                tmem_st32p(lanes + 32 * c, st);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&S.pfull);
+            if (w == 0) {
+                if (!(ok = mbar_wait_warp(&S.abort, &S.vfull, now & 1u, P.status, 72) && mbar_wait_warp(&S.abort, &S.pfull, now & 1u, P.status, 73))) break;
+                tc_fence_after();
+                const unsigned long long vd = smem_desc(smem_u32(S.v), 128 * 128, 1024, 2);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)                  // sixteen tokens: two groups of eight rows
+                    umma_f16_ts(tmem + O_COL, tmem + 8 * k, vd + (unsigned)((k * 2048) >> 4), ID_O, i > 0 || k > 0);
+                umma_commit(&S.vfree);
+            }
+            if (i + 1 < n) {
+                const unsigned char* ahead;
+                keys(i + 1);
+                ahead = block;
+                if (w == 0 && !(ok = scores(i + 1))) break;
+                if (!(ok = mbar_wait_warp(&S.abort, &S.vfree, now & 1u, P.status, 75))) break;
+                values(i + 1, ahead);
+            }
+        }
+        // ---- the rows' sums, by way of shared memory ----
+        if (ok && mbar_wait_warp(&S.abort, &S.vfree, (it + n - 1) & 1u, P.status, 77)) {
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < 2; ++c) {
+                unsigned r[32];
+                tmem_ld64(lanes + O_COL + 64 * c, r);
+                tmem_ld_wait(r);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int col = 64 * c + 8 * j + c0;
+                    *reinterpret_cast<uint2*>(S.k + sum_at(r0, col >> 2) + 4 * (col & 3)) = make_uint2(r[4 * j], r[4 * j + 1]);
+                    *reinterpret_cast<uint2*>(S.k + sum_at(r0 + 8, col >> 2) + 4 * (col & 3)) = make_uint2(r[4 * j + 2], r[4 * j + 3]);
+                }
+            }
+        }
+        {
+            const auto sum4 = [&](f32x2 v) {
+                unsigned u0, u1;
+                unpk(v, u0, u1);
+                float t = __uint_as_float(u0) + __uint_as_float(u1);
+                t += __shfl_xor_sync(0xffffffffu, t, 1);
+                return t + __shfl_xor_sync(0xffffffffu, t, 2);
+            };
+            const float ta = sum4(la), tb = sum4(lb), xa = sum4(ea), xb = sum4(eb);
+            if ((lane & 3) == 0) {
+                S.l[r0] = ta;
+                S.l[r0 + 8] = tb;
+                S.add[r0] = xa;
+                S.add[r0 + 8] = xb;
+                S.m[r0] = Ma;
+                S.m[r0 + 8] = Mb;
+            }
+        }
+        tc_fence_before();
         it += n;
         __syncthreads();
         tc_fence_after();
         const bool starts = piece.starts, ends = piece.ends;
         if (S.abort) break;
         {
-            float* part = P.parts + ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * PART;
+            float* sums = P.parts + ((long long)blockIdx.x * 2 + (starts ? 1 : 0)) * PART;
 #pragma unroll 1
-            for (int r0 = 0; r0 < ROWS; r0 += 32) {
-                const int row = r0 + (tid >> 3), l8 = tid & 7;
+            for (int q0 = 0; q0 < ROWS; q0 += 32) {
+                const int row = q0 + (tid >> 3), l8 = tid & 7;
                 float y[16];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {                // columns 64 (q >> 1) + 8 l8 + 4 (q & 1) .. hold coordinates 0, 4, 1, 5 (2, 6, 3, 7) of their eight
@@ -468,12 +516,12 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
                 } else {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        *reinterpret_cast<float4*>(part + row * 128 + 64 * (q >> 1) + 8 * l8 + 4 * (q & 1)) = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
+                        *reinterpret_cast<float4*>(sums + row * 128 + 64 * (q >> 1) + 8 * l8 + 4 * (q & 1)) = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
                     if (l8 == 0) {                           // the sums and the totals go by the same M: 64 times their size
-                        part[ROWS * 128 + row] = m;
-                        part[ROWS * 128 + ROWS + row] = total;
-                        part[ROWS * 128 + 2 * ROWS + row] = extra;
-                        part[ROWS * 128 + 3 * ROWS + row] = m + 6.f;
+                        sums[ROWS * 128 + row] = m;
+                        sums[ROWS * 128 + ROWS + row] = total;
+                        sums[ROWS * 128 + 2 * ROWS + row] = extra;
+                        sums[ROWS * 128 + 3 * ROWS + row] = m + 6.f;
                     }
                 }
             }
@@ -486,7 +534,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
     }
     tc_fence_before();
     __syncthreads();
-    if (w == 4) {
+    if (w == 0) {
         tc_fence_after();
         tmem_dealloc(tmem, TMEM_COLS);
     }
