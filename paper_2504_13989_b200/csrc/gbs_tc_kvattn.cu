@@ -103,18 +103,17 @@ struct Token {
     bool ok;
 };
 
-__device__ __forceinline__ const unsigned char* find(const gbs_kv_attn& A, const KvSeg& s, int tok, int page)
+// whether a token is there to be seen, and its block: some block of the pool where it is not, whose codes then weigh nothing
+__device__ __forceinline__ bool find(const gbs_kv_attn& A, const KvSeg& s, int tok, int page, const unsigned char*& block)
 {
-    if (tok < s.e.lo || tok >= s.e.hi || (unsigned)page >= (unsigned)A.c.n_pages) return nullptr;
-    return kv_block(A.c, page, s.head);
+    const bool ok = tok >= s.e.lo && tok < s.e.hi && (unsigned)page < (unsigned)A.c.n_pages;
+    block = kv_block(A.c, ok ? page : 0, s.head);
+    return ok;
 }
 template <bool ASYM>
 __device__ __forceinline__ void load_k(Token& x, const unsigned char* block, int slot, int ps, int half)
 {
-    x.ok = block != nullptr;
-    x.ks = x.kl = x.vs = x.vl = 0.f;
-    x.k[0] = x.k[1] = make_uint4(0, 0, 0, 0);
-    if (!block) return;
+    x.kl = x.vl = 0.f;
     const uint4* c = reinterpret_cast<const uint4*>(block + slot * KV_ROW) + 2 * half;
     x.k[0] = c[0];
     x.k[1] = c[1];
@@ -129,8 +128,6 @@ __device__ __forceinline__ void load_k(Token& x, const unsigned char* block, int
 }
 __device__ __forceinline__ void load_v(Token& x, const unsigned char* block, int slot, int ps, int half)
 {
-    x.v[0] = x.v[1] = make_uint4(0, 0, 0, 0);
-    if (!block) return;
     const uint4* c = reinterpret_cast<const uint4*>(block + (ps + slot) * KV_ROW) + 2 * half;
     x.v[0] = c[0];
     x.v[1] = c[1];
@@ -139,13 +136,39 @@ __device__ __forceinline__ void load_v(Token& x, const unsigned char* block, int
 template <bool ASYM>
 __device__ __forceinline__ void store_codes(unsigned char* tile, int row, int half, const uint4 c[2])
 {
+    const unsigned first = smem_u32(tile) + piece_at(row, 8 * half);     // a tile starts on 1024 bytes: the piece's number is exclusive-or'ed in
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint4 q = c[i >> 2];
         const unsigned w = (i & 3) == 0 ? q.x : (i & 3) == 1 ? q.y : (i & 3) == 2 ? q.z : q.w;
         unsigned h[4];
         kv_codes_f16<ASYM>(w, h);
-        *reinterpret_cast<uint4*>(tile + piece_at(row, 8 * half + i)) = make_uint4(h[0], h[1], h[2], h[3]);
+        st_shared_v4(first ^ (unsigned)(i << 4), make_uint4(h[0], h[1], h[2], h[3]));
+    }
+}
+
+// What a warp's 16 rows have added up, and the weights of the first half of the tile, times a factor of each row; rare.
+__device__ __forceinline__ void shrink(unsigned lanes, float keep_a, float keep_b, bool sums, bool weights)
+{
+    tmem_st_wait();
+    if (sums) {
+#pragma unroll 1
+        for (int q = 0; q < 2; ++q) {
+            unsigned o[32];
+            tmem_ld64(lanes + O_COL + 64 * q, o);
+            tmem_ld_wait(o);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * ((k & 2) ? keep_b : keep_a));
+            tmem_st64(lanes + O_COL + 64 * q, o);
+        }
+    }
+    if (weights) {
+        unsigned o[16];
+        tmem_ld32p(lanes, o);
+        const __half2 ha = __float2half2_rn(keep_a), hb = __float2half2_rn(keep_b);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) o[k] = as_u(__hmul2(as_h(o[k]), (k & 1) ? hb : ha));
+        tmem_st32p(lanes, o);
     }
 }
 
@@ -189,7 +212,8 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
         const int me = tid & 127, part = tid >> 7;           // this thread's token of a tile, and which half of its row
         const int* row_of_pages = A.c.page_table + (long long)seg.e.seq * A.c.max_pages;
         const auto page_of = [&](int tok) { return tok < seg.e.hi ? row_of_pages[tok >> ps_log] : -1; };
-        const unsigned char* block = find(A, seg, tok0 + me, page_of(tok0 + me));
+        const unsigned char* block;
+        x.ok = find(A, seg, tok0 + me, page_of(tok0 + me), block);
         load_k<ASYM>(x, block, (tok0 + me) & (ps - 1), ps, part);
         load_v(x, block, (tok0 + me) & (ps - 1), ps, part);
         int page = page_of(tok0 + me + UNIT);
@@ -258,25 +282,25 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
             // zero rows take the largest scale next to them; tokens that are not there weigh nothing, and scales that are no
             // numbers make the scores of those that see them none
             if (part == 0) {
-                float vs = x.vs, near = x.vs;
+                float vs = x.ok ? x.vs : 0.f, near = vs;
 #pragma unroll
                 for (int h = 16; h; h >>= 1) near = fmaxf(near, __shfl_xor_sync(0xffffffffu, near, h));
-                const bool wrong = !(fabsf(vs) < INFINITY) || !(fabsf(x.vl) < INFINITY);
+                const bool wrong = x.ok && (!(fabsf(vs) < INFINITY) || !(fabsf(x.vl) < INFINITY));
                 if (vs == 0.f) vs = near > 0.f ? near : 1.f;
                 vs = fmaxf(vs, 7.888609052210118e-31f);                          // 2^-100
                 S.lv[b][me] = !x.ok ? -INFINITY : wrong ? NAN : __log2f(vs);
                 S.rv[b][me] = x.ok && !wrong ? 1.f / vs : 0.f;
-                if (ASYM) S.vl[b][me] = wrong ? 0.f : x.vl;
+                if (ASYM) S.vl[b][me] = wrong || !x.ok ? 0.f : x.vl;
             } else {
-                S.ks[b][me] = x.ks;
-                if (ASYM) S.kl[b][me] = x.kl;
+                S.ks[b][me] = x.ok ? x.ks : 0.f;
+                if (ASYM) S.kl[b][me] = x.ok ? x.kl : 0.f;
             }
             store_codes<ASYM>(S.k, me, part, x.k);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(&S.kfull);
             const int next = tok + UNIT;
-            block = i + 1 < n ? find(A, seg, next, page) : nullptr;
+            x.ok = find(A, seg, next, i + 1 < n ? page : -1, block);
             page = page_of(next + UNIT);
             load_k<ASYM>(x, block, next & (ps - 1), ps, part);
         };
@@ -381,26 +405,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
                     lb = mul2(lb, both(keep_b));
                     ea = mul2(ea, both(keep_a));
                     eb = mul2(eb, both(keep_b));
-                    tmem_st_wait();
-                    if (i > 0) {
-#pragma unroll 1
-                        for (int q = 0; q < 2; ++q) {
-                            unsigned o[32];
-                            tmem_ld64(lanes + O_COL + 64 * q, o);
-                            tmem_ld_wait(o);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * ((k & 2) ? keep_b : keep_a));
-                            tmem_st64(lanes + O_COL + 64 * q, o);
-                        }
-                    }
-                    if (c > 0) {
-                        unsigned o[16];
-                        tmem_ld32p(lanes, o);
-                        const __half2 ha = __float2half2_rn(keep_a), hb = __float2half2_rn(keep_b);
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) o[k] = as_u(__hmul2(as_h(o[k]), (k & 1) ? hb : ha));
-                        tmem_st32p(lanes, o);
-                    }
+                    shrink(lanes, keep_a, keep_b, i > 0, c > 0);
                 }
                 const f32x2 base_a = both(6.f - Ma), base_b = both(6.f - Mb);        // weights are 64 at M
                 unsigned st[16];
