@@ -348,7 +348,7 @@ int gbs_quantized_matmul(const gbs_plan_t* plan_x, const void* codes_x, const fl
 
 typedef struct gbs_kv_cache {
     void* pages;            /* 16-byte aligned */
-    int64_t n_pages;        /* 1 .. 2^31 - 1 */
+    int64_t n_pages;        /* 1 .. 2^30 */
     int n_kv_heads;         /* 1 .. 1024 */
     int page_size;          /* 16, 32, 64 or 128 tokens */
     int32_t* page_table;

@@ -25,7 +25,7 @@ int view_of(const gbs_plan* p, const gbs_kv_cache_t* c, gbs_kv_view* out)
     if (!c) return GBS_ERR_INVALID_ARG;
     const int page_log = log2_page(c->page_size);
     if (page_log < 0 || c->n_kv_heads < 1 || c->n_kv_heads > 1024) return GBS_ERR_INVALID_ARG;
-    if (c->n_pages < 1 || c->n_pages > 0x7fffffffll || c->n_seqs < 1 || c->max_pages < 1) return GBS_ERR_INVALID_ARG;
+    if (c->n_pages < 1 || c->n_pages > 1ll << 30 || c->n_seqs < 1 || c->max_pages < 1) return GBS_ERR_INVALID_ARG;
     if ((int64_t)c->max_pages * c->page_size > 0x7fffffffll) return GBS_ERR_INVALID_ARG;
     if (!c->pages || !c->page_table || !c->lengths || !c->refs) return GBS_ERR_INVALID_ARG;
     if (!aligned(c->pages, 16) || !aligned(c->page_table, 4) || !aligned(c->lengths, 4) || !aligned(c->refs, 4)) return GBS_ERR_ALIGNMENT;

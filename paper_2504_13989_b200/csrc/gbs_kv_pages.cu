@@ -10,8 +10,11 @@
 namespace {
 
 constexpr int ONE = 1024;                        // threads of the one block that allocates
-constexpr int COPY = 256;                        // threads of a block that copies
+constexpr int COPY = 256;                        // threads of a block that copies pages
+constexpr int PART = 128;                        // threads of a block that copies part of a page, or ends a sequence
+constexpr int EACH = 4;                          // counters of a thread of the one block at a time (8 and 16: slower, 33 and 38 us for 30)
 
+static_assert(ONE == 32 * 32, "a warp adds up what 32 warps have");
 // Exclusive prefix sum over the block; `total` is the sum.  Two barriers; `part` holds 32 ints.
 __device__ __forceinline__ int block_prefix(int v, int* part, int& total)
 {
@@ -46,6 +49,24 @@ struct FirstOf {
             const int was = atomicCAS(&key[h], -1, seq);
             if (was == -1 || was == seq) return h;
             h = (h + 1) & mask;
+        }
+    }
+};
+
+// EACH counters from p on; behind the last page: `behind`.  On their way while the ones before are worked on.
+struct Counters {
+    int r[EACH];
+    __device__ __forceinline__ void load(const gbs_kv_view& c, int p, int behind)
+    {
+        if (p + EACH <= c.n_pages && (reinterpret_cast<uintptr_t>(c.refs) & 15) == 0) {
+#pragma unroll
+            for (int k = 0; k < EACH; k += 4) {
+                const int4 v = *reinterpret_cast<const int4*>(c.refs + p + k);
+                r[k] = v.x; r[k + 1] = v.y; r[k + 2] = v.z; r[k + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) r[k] = p + k < c.n_pages ? c.refs[p + k] : behind;
         }
     }
 };
@@ -98,60 +119,72 @@ __device__ __forceinline__ Wish wish_of(const AllocArgs& A, const FirstOf& f, in
     return w;
 }
 
-// Shared memory: FirstOf's two arrays of mask + 1, then for each item the pages wanted before it (and, at the end, its new length).
+// Shared memory: FirstOf's two arrays of mask + 1, then for each item where in the table page number 0 of the line of taken pages would be
+// entered for it, and how many pages the items before it want (at the end, its new length).
 template <bool FORK>
 __global__ __launch_bounds__(ONE) void k_kv_allocate(const __grid_constant__ AllocArgs A)
 {
-    extern __shared__ int sm[];
+    extern __shared__ __align__(8) int sm[];
     __shared__ int part[32];
     FirstOf f = {sm, sm + A.mask + 1, A.mask};
-    int* before = sm + 2 * (A.mask + 1);
     const int tid = threadIdx.x, n = A.n_items;
+    long long* entry = reinterpret_cast<long long*>(sm + 2 * (A.mask + 1));
+    int* before = reinterpret_cast<int*>(entry + n);
     for (unsigned i = tid; i <= A.mask; i += ONE) {
         f.key[i] = -1;
         f.item[i] = 0x7fffffff;
     }
     kv_wait_before();
     kv_let_next();
+    Counters now;
+    now.load(A.c, EACH * tid, 1);
     __syncthreads();
     for (int i = tid; i < n; i += ONE) {
         const int seq = kv_sequence(A.c, A.seqs, i);
         if (seq >= 0) atomicMin(&f.item[f.slot(seq)], i);
     }
     __syncthreads();
+    // nothing that a wish goes by changes before the end, so a thread's first one is kept
+    const Wish mine = wish_of<FORK>(A, f, min(tid, n - 1));
+    const auto wish = [&](int i) { return i == tid ? mine : wish_of<FORK>(A, f, i); };
 
     // pages wanted before each item; more than the pool has need not be told apart
     int wanted = 0;
     for (int i0 = 0; i0 < n; i0 += ONE) {
         const int i = i0 + tid;
-        const int need = i < n ? min(wish_of<FORK>(A, f, i).need, 1 << 20) : 0;
+        const Wish w = i < n ? wish(i) : Wish{0, 0, 0, 0, 0};
         int total;
-        const int at = wanted + block_prefix(need, part, total);
-        if (i < n) before[i] = at;
+        const int at = wanted + block_prefix(min(w.need, 1 << 20), part, total);
+        if (i < n) {
+            before[i] = at;
+            entry[i] = (long long)w.seq * A.c.max_pages + w.first - at;
+        }
         wanted = min(wanted + total, 0x3fffffff);
     }
     __syncthreads();
 
     // free pages, lowest first, go to the items in their order; what an item that is refused below has taken is given back there
     int found = 0;
-    for (int p0 = 0; p0 < A.c.n_pages && found < wanted; p0 += 4 * ONE) {
-        const int p = p0 + 4 * tid;
-        int free_bits = 0;
+    for (int p0 = 0; p0 < A.c.n_pages && found < wanted; p0 += EACH * ONE) {
+        const int p = p0 + EACH * tid;
+        unsigned free_bits = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (p + k < A.c.n_pages && A.c.refs[p + k] == 0) free_bits |= 1 << k;
+        for (int k = 0; k < EACH; ++k) free_bits |= (now.r[k] == 0 ? 1u : 0u) << k;
+        now.load(A.c, p + EACH * ONE, 1);
         int total, r = found + block_prefix(__popc(free_bits), part, total);
-        for (; free_bits && r < wanted; free_bits &= free_bits - 1, ++r) {
-            const int page = p + __ffs(free_bits) - 1;
+        if (free_bits && r < wanted) {
             int lo = 0, hi = n - 1;              // the last item with before[] <= r
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
                 if (before[mid] <= r) lo = mid;
                 else hi = mid - 1;
             }
-            const Wish w = wish_of<FORK>(A, f, lo);
-            A.c.page_table[(long long)w.seq * A.c.max_pages + w.first + (r - before[lo])] = page;
-            A.c.refs[page] = 1;
+            for (; free_bits && r < wanted; free_bits &= free_bits - 1, ++r) {
+                while (lo + 1 < n && before[lo + 1] <= r) ++lo;
+                const int page = p + __ffs(free_bits) - 1;
+                A.c.page_table[entry[lo] + r] = page;
+                A.c.refs[page] = 1;
+            }
         }
         found += total;
     }
@@ -159,7 +192,7 @@ __global__ __launch_bounds__(ONE) void k_kv_allocate(const __grid_constant__ All
 
     // all wishes are read before a length changes: a fork's source may be another's target
     for (int i = tid; i < n; i += ONE) {
-        Wish w = wish_of<FORK>(A, f, i);
+        Wish w = wish(i);
         if (w.status == GBS_KV_DONE && w.need > 0 && (long long)before[i] + w.need > found) {
             w.status = GBS_KV_NO_PAGES;
             for (int j = 0; j < w.need && before[i] + j < found; ++j)
@@ -170,23 +203,23 @@ __global__ __launch_bounds__(ONE) void k_kv_allocate(const __grid_constant__ All
     }
     __syncthreads();
     for (int i = tid; i < n; i += ONE)
-        if (before[i] >= 0) A.c.lengths[kv_sequence(A.c, A.seqs, i)] = before[i];
+        if (before[i] >= 0) A.c.lengths[i == tid ? mine.seq : kv_sequence(A.c, A.seqs, i)] = before[i];
 }
 
 __device__ __forceinline__ void copy_words(unsigned char* to, const unsigned char* from, int bytes)
 {
-    for (int i = 4 * threadIdx.x; i < bytes; i += 4 * COPY)
+    for (int i = 4 * threadIdx.x; i < bytes; i += 4 * PART)
         *reinterpret_cast<unsigned*>(to + i) = *reinterpret_cast<const unsigned*>(from + i);
 }
 __device__ __forceinline__ void copy_16(unsigned char* to, const unsigned char* from, int bytes)
 {
-    for (int i = 16 * threadIdx.x; i < bytes; i += 16 * COPY)
+    for (int i = 16 * threadIdx.x; i < bytes; i += 16 * PART)
         *reinterpret_cast<uint4*>(to + i) = *reinterpret_cast<const uint4*>(from + i);
 }
 
 // One block per pair and KV head: its part of the last page's tokens; head 0 also shares the full pages.  The target's length is the
 // one that the source had before the call.
-__global__ __launch_bounds__(COPY) void k_kv_share(const __grid_constant__ AllocArgs A)
+__global__ __launch_bounds__(PART) void k_kv_share(const __grid_constant__ AllocArgs A)
 {
     kv_wait_before();
     kv_let_next();
@@ -198,7 +231,7 @@ __global__ __launch_bounds__(COPY) void k_kv_share(const __grid_constant__ Alloc
     if (head == 0) {
         const int* from = A.c.page_table + (long long)src * A.c.max_pages;
         int* to = A.c.page_table + (long long)dst * A.c.max_pages;
-        for (int j = threadIdx.x; j < full; j += COPY) {
+        for (int j = threadIdx.x; j < full; j += PART) {
             const int page = from[j];
             to[j] = page;
             if ((unsigned)page < (unsigned)A.c.n_pages) atomicAdd(&A.c.refs[page], 1);
@@ -219,7 +252,7 @@ __global__ __launch_bounds__(COPY) void k_kv_share(const __grid_constant__ Alloc
 }
 
 // One block per item; the exchange lets one of two blocks that name a sequence end it.
-__global__ __launch_bounds__(COPY) void k_kv_free(const __grid_constant__ AllocArgs A)
+__global__ __launch_bounds__(PART) void k_kv_free(const __grid_constant__ AllocArgs A)
 {
     __shared__ int length;
     kv_wait_before();
@@ -230,7 +263,7 @@ __global__ __launch_bounds__(COPY) void k_kv_free(const __grid_constant__ AllocA
     __syncthreads();
     const int held = (int)(((unsigned)length + (1u << A.c.page_log) - 1) >> A.c.page_log);
     const int* row = A.c.page_table + (long long)seq * A.c.max_pages;
-    for (int j = threadIdx.x; j < held; j += COPY) {
+    for (int j = threadIdx.x; j < held; j += PART) {
         const int page = row[j];
         if ((unsigned)page < (unsigned)A.c.n_pages) atomicSub(&A.c.refs[page], 1);
     }
@@ -247,18 +280,21 @@ __global__ __launch_bounds__(ONE) void k_kv_number(const __grid_constant__ Compa
     __shared__ int part[32];
     kv_wait_before();
     kv_let_next();
+    Counters now;
+    now.load(A.c, EACH * threadIdx.x, 0);
     int live = 0;
-    for (int p0 = 0; p0 < A.c.n_pages; p0 += 4 * ONE) {
-        const int p = p0 + 4 * threadIdx.x;
-        int refs[4], used = 0;
+    for (int p0 = 0; p0 < A.c.n_pages; p0 += EACH * ONE) {
+        const int p = p0 + EACH * (int)threadIdx.x;
+        int refs[EACH], used = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            refs[k] = p + k < A.c.n_pages ? A.c.refs[p + k] : 0;
+        for (int k = 0; k < EACH; ++k) {
+            refs[k] = now.r[k];
             used += refs[k] > 0;
         }
+        now.load(A.c, p + EACH * ONE, 0);
         int total, r = live + block_prefix(used, part, total);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < EACH; ++k)
             if (p + k < A.c.n_pages) {
                 const bool moved = refs[k] > 0 && r < A.into.n_pages;
                 A.map[p + k] = moved ? r : -1;
@@ -297,7 +333,7 @@ int allocate(const gbs_plan* p, bool fork, const AllocArgs& A0, cudaStream_t str
     AllocArgs A = A0;
     A.mask = 63;
     while (A.mask + 1 < 2u * (unsigned)A.n_items) A.mask = 2 * A.mask + 1;
-    const size_t smem = (2 * ((size_t)A.mask + 1) + (size_t)A.n_items) * sizeof(int);
+    const size_t smem = (2 * ((size_t)A.mask + 1) + 3 * (size_t)A.n_items) * sizeof(int);
     const void* f = fork ? (const void*)k_kv_allocate<true> : (const void*)k_kv_allocate<false>;
     if (smem > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -318,13 +354,13 @@ int gbs_kv_fork_launch(const gbs_plan* p, const gbs_kv_view& c, const int* src, 
     const AllocArgs A = {c, dst, src, n_items, status, 0};
     const int e = allocate(p, true, A, stream);
     if (e != 0) return e;
-    return gbs_kv_launch(p, k_kv_share, dim3((unsigned)n_items, (unsigned)c.heads), COPY, 0, stream, A);
+    return gbs_kv_launch(p, k_kv_share, dim3((unsigned)n_items, (unsigned)c.heads), PART, 0, stream, A);
 }
 
 int gbs_kv_free_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, cudaStream_t stream)
 {
     const AllocArgs A = {c, seqs, nullptr, n_items, nullptr, 0};
-    return gbs_kv_launch(p, k_kv_free, dim3((unsigned)n_items), COPY, 0, stream, A);
+    return gbs_kv_launch(p, k_kv_free, dim3((unsigned)n_items), PART, 0, stream, A);
 }
 
 int gbs_kv_compact_launch(const gbs_plan* p, const gbs_kv_view& c, const gbs_kv_view& into, int* page_map, int* n_live, cudaStream_t stream)

@@ -32,7 +32,7 @@ def pool(**kw):
 
 BAD_POOLS = [
     (dict(pages=None), INVALID), (dict(page_table=None), INVALID), (dict(lengths=None), INVALID), (dict(refs=None), INVALID),
-    (dict(n_pages=0), INVALID), (dict(n_pages=1 << 31), INVALID), (dict(n_kv_heads=0), INVALID), (dict(n_kv_heads=1025), INVALID),
+    (dict(n_pages=0), INVALID), (dict(n_pages=(1 << 30) + 1), INVALID), (dict(n_kv_heads=0), INVALID), (dict(n_kv_heads=1025), INVALID),
     (dict(page_size=8), INVALID), (dict(page_size=48), INVALID), (dict(page_size=256), INVALID), (dict(n_seqs=0), INVALID),
     (dict(max_pages=0), INVALID), (dict(page_size=128, max_pages=1 << 24), INVALID),
     (dict(pages=(1 << 20) + 8), ALIGN), (dict(page_table=(1 << 21) + 2), ALIGN), (dict(lengths=(1 << 22) + 1), ALIGN), (dict(refs=(1 << 23) + 2), ALIGN),
