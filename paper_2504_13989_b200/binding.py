@@ -716,7 +716,7 @@ class KVCache:
 
 
 # the methods that _native.so has a regular call for
-_PYTHON_KV_METHODS = {name: KVCache.__dict__[name] for name in ("extend", "fork", "free", "append", "read", "attention")}
+_PYTHON_KV_METHODS = {name: KVCache.__dict__[name] for name in ("extend", "fork", "free", "compact", "append", "read", "attention")}
 _PYTHON_METHODS = {name: Plan.__dict__[name] for name in ("rotate_quantize", "dequantize", "quantized_matmul", "clip_error")}
 
 

@@ -319,12 +319,26 @@ __global__ __launch_bounds__(COPY) void k_kv_move(const __grid_constant__ Compac
         A.into.page_table[e] = (unsigned)page < (unsigned)A.c.n_pages ? A.map[page] : -1;
     }
     for (int s = blockIdx.x * COPY + threadIdx.x; s < A.c.n_seqs; s += gridDim.x * COPY) A.into.lengths[s] = A.c.lengths[s];
-    for (int p = blockIdx.x; p < A.c.n_pages; p += gridDim.x) {
-        const int to = A.map[p];
-        if (to < 0) continue;
-        const uint4* from = reinterpret_cast<const uint4*>(A.c.pages + (long long)p * A.c.page_bytes);
-        uint4* at = reinterpret_cast<uint4*>(A.into.pages + (long long)to * A.c.page_bytes);
-        for (int i = threadIdx.x; i < (int)(A.c.page_bytes / 16); i += COPY) at[i] = from[i];
+    // pages one after another, eight pieces of a thread on their way at once; the next page's number is asked for ahead
+    const int pieces = (int)(A.c.page_bytes / 16);
+    int p = blockIdx.x, to = p < A.c.n_pages ? A.map[p] : -1;
+    while (p < A.c.n_pages) {
+        const int next = p + gridDim.x, next_to = next < A.c.n_pages ? A.map[next] : -1;
+        if (to >= 0) {
+            const uint4* from = reinterpret_cast<const uint4*>(A.c.pages + (long long)p * A.c.page_bytes);
+            uint4* at = reinterpret_cast<uint4*>(A.into.pages + (long long)to * A.c.page_bytes);
+            for (int i = threadIdx.x; i < pieces; i += 8 * COPY) {
+                uint4 v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (i + k * COPY < pieces) v[k] = __ldcs(from + i + k * COPY);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (i + k * COPY < pieces) __stcs(at + i + k * COPY, v[k]);
+            }
+        }
+        p = next;
+        to = next_to;
     }
 }
 

@@ -329,6 +329,7 @@ struct Pool {
     int device;
 };
 PyTypeObject* pool_type = nullptr;
+PyObject* name_calls = nullptr;
 
 int pool_init(PyObject* self, PyObject* args, PyObject*)
 {
@@ -526,6 +527,26 @@ PyObject* do_kv_attention(const Pool& p, const PlanRef& ref, PyObject* const* g)
     GBS_END
 }
 
+PyObject* do_kv_compact(const Pool& p, const PlanRef& ref, PyObject* const* g)       // into, page_map, stream
+{
+    GBS_BEGIN
+    if (!none(g[2])) Py_RETURN_NONE;
+    PyObject* other = PyObject_GetAttr(g[0], name_calls);
+    if (!other) { PyErr_Clear(); Py_RETURN_NONE; }
+    const bool regular = Py_TYPE(other) == pool_type && reinterpret_cast<Pool*>(other)->device == p.device && plan_ref(*reinterpret_cast<Pool*>(other)) &&
+                         plan_ref(*reinterpret_cast<Pool*>(other))->info.asymmetric == ref.info.asymmetric;
+    const gbs_kv_cache_t into = regular ? reinterpret_cast<Pool*>(other)->cache : gbs_kv_cache_t{};      // the caller's argument keeps its tensors
+    Py_DECREF(other);
+    const int32_t* given;
+    if (!regular || !ints_of(p, g[1], p.cache.n_pages, &given)) Py_RETURN_NONE;
+    at::Tensor map, live = ints(p, 1);
+    if (!given) map = ints(p, p.cache.n_pages);
+    int32_t *mp = given ? const_cast<int32_t*>(given) : static_cast<int32_t*>(map.data_ptr()), *lp = static_cast<int32_t*>(live.data_ptr());
+    if (gbs_kv_compact(ref.plan, &p.cache, &into, mp, lp, stream_on(p)) != GBS_OK) Py_RETURN_NONE;
+    return THPVariable_Wrap(std::move(live));
+    GBS_END
+}
+
 // A method: the names of its arguments in the class's order, how many must be given, and what to do with them; `on_pool` is for KVCache.
 constexpr int MOST_ARGS = 10;
 struct Method {
@@ -539,6 +560,7 @@ struct Method {
 constexpr Method KV_EXTEND = {"extend", 3, 0, {"seqs", "counts", "stream"}, nullptr, do_kv_extend};
 constexpr Method KV_FORK = {"fork", 3, 2, {"src", "dst", "stream"}, nullptr, do_kv_fork};
 constexpr Method KV_FREE = {"free", 2, 1, {"seqs", "stream"}, nullptr, do_kv_free, true};
+constexpr Method KV_COMPACT = {"compact", 3, 1, {"into", "page_map", "stream"}, nullptr, do_kv_compact};
 constexpr Method KV_APPEND = {"append", 5, 2, {"k", "v", "seqs", "cu_tokens", "stream"}, nullptr, do_kv_append, true};
 constexpr Method KV_READ = {"read", 5, 0, {"seqs", "cu_tokens", "n_tokens", "out", "stream"}, nullptr, do_kv_read};
 constexpr Method KV_ATTENTION = {"attention", 10, 1, {"q", "seqs", "cu_tokens", "max_tokens", "causal", "window", "scale", "max_len", "out", "stream"},
@@ -577,7 +599,7 @@ struct MethodObject {
     PyObject* wrapped;
     PyObject* alloc;          // Plan.alloc_outputs, or null where the call allocates without it
 };
-PyObject *name_calls = nullptr, *name_alloc = nullptr;
+PyObject* name_alloc = nullptr;
 
 // whether the plan's outputs come from Plan's own alloc_outputs (a subclass or an instance may have another)
 bool own_alloc(PyObject* plan, PyObject* alloc)
@@ -657,7 +679,7 @@ void method_dealloc(PyObject* self)
     Py_DECREF(type);
 }
 PyTypeObject* method_type = nullptr;
-const Method* const METHODS[] = {&ROTATE, &DEQUANTIZE, &MATMUL, &CLIP, &KV_EXTEND, &KV_FORK, &KV_FREE, &KV_APPEND, &KV_READ, &KV_ATTENTION};
+const Method* const METHODS[] = {&ROTATE, &DEQUANTIZE, &MATMUL, &CLIP, &KV_EXTEND, &KV_FORK, &KV_FREE, &KV_COMPACT, &KV_APPEND, &KV_READ, &KV_ATTENTION};
 
 PyObject* make_method(PyObject*, PyObject* args)
 {

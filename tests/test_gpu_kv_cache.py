@@ -514,6 +514,12 @@ def test_native_and_python_paths_agree():
     assert same(a.attention(wide[:, :6], seqs, cu, 5, causal=False, window=30, scale=0.1, max_len=64), want)
     with pytest.raises(GbsError):
         a.attention(q, seqs, cu, 0)
+    into = [KVCache.create(plan, 60, 2, 16, 4, a.page_table.shape[1], DEV) for _ in range(2)]
+    maps = [torch.empty(a.pages.shape[0], dtype=torch.int32, device=DEV) for _ in range(2)]
+    assert torch.equal(a.compact(into[0], page_map=maps[0]), python("compact")(b, into[1], maps[1])) and torch.equal(maps[0], maps[1])
+    assert torch.equal(a.compact(into[0]), b.compact(into[1], maps[1])) and torch.equal(into[0].page_table, into[1].page_table)
+    with pytest.raises(GbsError):
+        a.compact(a)
     plan.close()
     with pytest.raises(GbsError):
         a.attention(q, seqs, cu, 5)
