@@ -31,6 +31,7 @@ struct Smem {
     float factor[ROWS], qsum[ROWS];
     int lo[ROWS], hi[ROWS];                          // tokens that a row sees
     float m[ROWS], l[ROWS], add[ROWS];
+    unsigned long long block[3][UNIT / 16];          // of tile i in [i % 3]: where the blocks of its pages are; bit 0: there is none
     unsigned long long kfull, vfull, vfree, sfull, pfull;
     KvSeg seg;
     long long share[THREADS / 32];
@@ -103,20 +104,20 @@ struct Token {
     bool ok;
 };
 
-// whether a token is there to be seen, and its block: some block of the pool where it is not, whose codes then weigh nothing
-__device__ __forceinline__ bool find(const gbs_kv_attn& A, const KvSeg& s, int tok, int page, const unsigned char*& block)
+// Where the block of a page is, bit 0 set for a page that is none: some block of the pool then, whose codes will weigh nothing.
+__device__ __forceinline__ unsigned long long block_of(const gbs_kv_attn& A, const KvSeg& s, int page)
 {
-    const bool ok = tok >= s.e.lo && tok < s.e.hi && (unsigned)page < (unsigned)A.c.n_pages;
-    block = kv_block(A.c, ok ? page : 0, s.head);
-    return ok;
+    const bool ok = (unsigned)page < (unsigned)A.c.n_pages;
+    return reinterpret_cast<unsigned long long>(kv_block(A.c, ok ? page : 0, s.head)) | (ok ? 0ull : 1ull);
 }
+// `at`: this thread's codes in a block
 template <bool ASYM>
-__device__ __forceinline__ void load_k(Token& x, const unsigned char* block, int slot, int ps, int half)
+__device__ __forceinline__ void load_k(Token& x, const unsigned char* block, int at, int slot, int ps)
 {
-    x.kl = x.vl = 0.f;
-    const uint4* c = reinterpret_cast<const uint4*>(block + slot * KV_ROW) + 2 * half;
+    const uint4* c = reinterpret_cast<const uint4*>(block + at);
     x.k[0] = c[0];
     x.k[1] = c[1];
+    x.kl = x.vl = 0.f;
     const float* sc = reinterpret_cast<const float*>(block + 2 * ps * KV_ROW);
     if (ASYM) {
         const float2 a = reinterpret_cast<const float2*>(sc)[slot], b = reinterpret_cast<const float2*>(sc)[ps + slot];
@@ -126,13 +127,12 @@ __device__ __forceinline__ void load_k(Token& x, const unsigned char* block, int
         x.vs = sc[ps + slot];
     }
 }
-__device__ __forceinline__ void load_v(Token& x, const unsigned char* block, int slot, int ps, int half)
+__device__ __forceinline__ void load_v(Token& x, const unsigned char* block, int at)
 {
-    const uint4* c = reinterpret_cast<const uint4*>(block + (ps + slot) * KV_ROW) + 2 * half;
+    const uint4* c = reinterpret_cast<const uint4*>(block + at);
     x.v[0] = c[0];
     x.v[1] = c[1];
 }
-// A word's 8 coordinates stand in the order 0, 4, 1, 5, 2, 6, 3, 7, in the queries as well; the results' columns are put back at the end.
 template <bool ASYM>
 __device__ __forceinline__ void store_codes(unsigned char* tile, int row, int half, const uint4 c[2])
 {
@@ -210,13 +210,21 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
         // ---- query rows: eight lanes a row, 32 rows at a time ----
         Token x;
         const int me = tid & 127, part = tid >> 7;           // this thread's token of a tile, and which half of its row
+        const int slot = me & (ps - 1), my_page = me >> ps_log, k_at = slot * KV_ROW + 32 * part, v_at = k_at + ps * KV_ROW;     // the same in every tile
         const int* row_of_pages = A.c.page_table + (long long)seg.e.seq * A.c.max_pages;
         const auto page_of = [&](int tok) { return tok < seg.e.hi ? row_of_pages[tok >> ps_log] : -1; };
-        const unsigned char* block;
-        x.ok = find(A, seg, tok0 + me, page_of(tok0 + me), block);
-        load_k<ASYM>(x, block, (tok0 + me) & (ps - 1), ps, part);
-        load_v(x, block, (tok0 + me) & (ps - 1), ps, part);
-        int page = page_of(tok0 + me + UNIT);
+        const auto seen = [&](unsigned long long b, int tok) { return !(b & 1) && tok >= seg.e.lo && tok < seg.e.hi; };
+        unsigned long long here = block_of(A, seg, page_of(tok0 + me));
+        const unsigned char* block = reinterpret_cast<const unsigned char*>(here & ~1ull);
+        x.ok = seen(here, tok0 + me);
+        load_k<ASYM>(x, block, k_at, slot, ps);
+        load_v(x, block, v_at);
+        // warp 7, a lane a page: the blocks of the tiles ahead
+        int page = -1;
+        if (w == 7 && lane < (UNIT >> ps_log)) {
+            S.block[1][lane] = block_of(A, seg, page_of(tok0 + UNIT + (lane << ps_log)));
+            page = page_of(tok0 + 2 * UNIT + (lane << ps_log));
+        }
         {
             const int l8 = tid & 7;
             uint4 raw[4][2];
@@ -282,34 +290,37 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_tc_kvattn(const __gr
             // zero rows take the largest scale next to them; tokens that are not there weigh nothing, and scales that are no
             // numbers make the scores of those that see them none
             if (part == 0) {
-                float vs = x.ok ? x.vs : 0.f, near = vs;
-#pragma unroll
-                for (int h = 16; h; h >>= 1) near = fmaxf(near, __shfl_xor_sync(0xffffffffu, near, h));
+                float vs = x.ok ? x.vs : 0.f;
+                const float near = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(vs) & 0x7fffffffu));
                 const bool wrong = x.ok && (!(fabsf(vs) < INFINITY) || !(fabsf(x.vl) < INFINITY));
-                if (vs == 0.f) vs = near > 0.f ? near : 1.f;
+                if (vs == 0.f) vs = near > 0.f && near < INFINITY ? near : 1.f;
                 vs = fmaxf(vs, 7.888609052210118e-31f);                          // 2^-100
                 S.lv[b][me] = !x.ok ? -INFINITY : wrong ? NAN : __log2f(vs);
-                S.rv[b][me] = x.ok && !wrong ? 1.f / vs : 0.f;
+                S.rv[b][me] = x.ok && !wrong ? __fdividef(1.f, vs) : 0.f;
                 if (ASYM) S.vl[b][me] = wrong || !x.ok ? 0.f : x.vl;
             } else {
                 S.ks[b][me] = x.ok ? x.ks : 0.f;
                 if (ASYM) S.kl[b][me] = x.ok ? x.kl : 0.f;
+                if (w == 7 && lane < (UNIT >> ps_log)) {
+                    S.block[(unsigned)(i + 2) % 3u][lane] = block_of(A, seg, page);
+                    page = page_of(tok0 + (i + 3) * UNIT + (lane << ps_log));
+                }
             }
             store_codes<ASYM>(S.k, me, part, x.k);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(&S.kfull);
-            const int next = tok + UNIT;
-            x.ok = find(A, seg, next, i + 1 < n ? page : -1, block);
-            page = page_of(next + UNIT);
-            load_k<ASYM>(x, block, next & (ps - 1), ps, part);
+            const unsigned long long e = S.block[(unsigned)(i + 1) % 3u][my_page];
+            block = reinterpret_cast<const unsigned char*>(e & ~1ull);
+            x.ok = seen(e, tok + UNIT);
+            load_k<ASYM>(x, block, k_at, slot, ps);
         };
         const auto values = [&](int i, const unsigned char* next_block) {
             store_codes<ASYM>(S.v, me, part, x.v);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(&S.vfull);
-            load_v(x, next_block, (tok0 + (i + 1) * UNIT + me) & (ps - 1), ps, part);
+            load_v(x, next_block, v_at);
         };
         const auto scores = [&](int i) {
             if (!mbar_wait_warp(&S.abort, &S.kfull, (it + i) & 1u, P.status, 71)) return false;
