@@ -6,8 +6,9 @@
 // g and g + 8, coordinates 8 (t + 4 j) .. + 7 for j = 0 .. 3, that is 16-byte pieces of 16-bit rows and 4-byte pieces of codes, four lanes next to each
 // other.  Bits 3 and 4 (t) lie across lanes and have to go to the matrix unit, with two of the three bits below; what is left, the third
 // one and j, is in registers.  The result has the layout of the operand, so no number moves between lanes.
-// Seven stages over eight lanes a row, three of them by shuffles, took 119 and 85 instructions a row and warp instead of REPLACE:
-// 14000 tokens x 8 heads written and read back in 54.7 us instead of REPLACE.
+// Seven stages over eight lanes a row, three of them by shuffles, took 119 and 85 instructions a row and warp (write and read) instead of 59 and 52:
+// 14000 tokens x 8 heads written and read back in 62.7 us instead of 42.7.
+// What bounds it then is the issue of instructions; the bytes (130 MB) would take 20 us.
 // Reading back, the codes go in as fp16, and everything up to the scale is exact.
 #include <cuda_fp16.h>
 
