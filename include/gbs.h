@@ -337,7 +337,8 @@ int gbs_quantized_matmul(const gbs_plan_t* plan_x, const void* codes_x, const fl
  * A call's items are sequences: item i is sequence seqs[i], or i where seqs is NULL (device int32).  Its tokens are rows
  * cu_tokens[i] .. cu_tokens[i + 1] - 1 of the call's row tensors (device int32, n_items + 1 values that do not fall, from 0), or row i
  * alone where cu_tokens is NULL.  They are the LAST tokens of the sequence as lengths[] has it: a step extends the
- * sequences first, then appends and attends.  Rows behind cu_tokens[n_items] are neither read nor written.
+ * sequences first, then appends and attends.  So an item that gbs_kv_extend refused must not be appended: its rows would replace the
+ * sequence's last ones.  Rows behind cu_tokens[n_items] count for nothing and are not written.
  * Numbers that only the device knows are checked there: an item whose sequence is out of range, a token whose position is
  * below 0 or whose page is not one of the pool's is left out (a row that would be written from it becomes 0).
  *
@@ -354,7 +355,7 @@ typedef struct gbs_kv_cache {
     int32_t* page_table;
     int32_t* lengths;
     int32_t* refs;
-    int n_seqs, max_pages;  /* n_seqs * max_pages entries; max_pages * page_size < 2^31 */
+    int n_seqs, max_pages;  /* n_seqs * max_pages entries; max_pages at most 2^20 */
 } gbs_kv_cache_t;
 
 /* what became of an item of gbs_kv_extend and gbs_kv_fork (device int32) */
@@ -370,8 +371,8 @@ int gbs_kv_page_bytes(const gbs_plan_t* plan, int n_kv_heads, int page_size, int
 
 /*
  * Room for counts[i] more tokens in sequence seqs[i]: lengths grow, and free pages enter the table, the lowest free ones first,
- * to the items in their order.  An item that is refused (status_out[i] != GBS_KV_DONE) changes nothing; from the first one that the
- * free pages do not suffice for, every item that needs a page is refused.
+ * to the items in their order.  An item that is refused (status_out[i] != GBS_KV_DONE) leaves its sequence and the pool's refs as they
+ * were; from the first one that the free pages do not suffice for, every item that needs a page is refused.
  *   seqs, counts   device int32 [n_items], n_items 0 .. GBS_KV_MAX_ITEMS; seqs NULL: sequence i; counts NULL: one token each
  *   status_out     device int32 [n_items]
  */
@@ -409,6 +410,7 @@ int gbs_kv_compact(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const gb
  *   k, v              device bf16 [n_tokens][n_kv_heads][d], rows 16-byte aligned: token t, head h starts at element
  *                     t * token_stride + h * head_stride, strides multiples of 8 (k and v have the same)
  *   n_tokens          rows that k and v hold; cu_tokens NULL: n_tokens = n_items
+ * Where two items name one sequence, both write its last tokens, and either's bytes may stay.
  */
 int gbs_kv_append(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
                   int64_t n_tokens, const void* k, const void* v, int64_t token_stride, int64_t head_stride, void* cuda_stream);
@@ -421,16 +423,18 @@ int gbs_kv_read(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32
                 int64_t n_tokens, void* k_out, void* v_out, void* cuda_stream);
 
 /* gbs_kv_attention flags */
-#define GBS_KV_CAUSAL 1       /* a token sees the cache up to its own position; without it, all of its sequence */
+#define GBS_KV_CAUSAL 1       /* a token sees the cache up to its own position; without it, all of its sequence, of which it need not be a part */
 
 /*
  * Attention of the items' query tokens over the cache: with khat, vhat the rows that the cache stands for,
  *     out[t][h] = sum_j p_j vhat_j,   p = softmax over the visible j of (scale * q[t][h] . khat_j),
  * KV head h / (n_heads / n_kv_heads) serving query head h.  Token t at position p of its sequence sees positions j <= p (causal) and,
  * with window > 0, j > p - window.  A row that sees nothing becomes 0.
- *   q, out            device bf16, [n_tokens][n_heads][d] with strides in elements as in gbs_kv_append; out's own strides
+ *   q, out            device bf16, [n_tokens][n_heads][d] with strides in elements as in gbs_kv_append; out's own strides.  No row of
+ *                     out overlaps another one or a row of q
  *   n_heads           a multiple of n_kv_heads, at most 1024 query heads per KV head
- *   max_tokens        no item has more tokens (1 where cu_tokens is NULL); what is beyond it is left as it is.
+ *   max_tokens        no item has more tokens (1 where cu_tokens is NULL); what is beyond it is left as it is.  It chooses the
+ *                     kernel and bounds what is looked through for work, so the closer the better.
  *                     n_items * max_tokens * query heads of a KV head: at most 2^28
  *   max_len           no sequence of the call is longer (0: the table's width); one that is longer is read up to max_len only.
  *                     It bounds how far the work is split, not what is read.

@@ -452,6 +452,7 @@ class Plan:
         calls = native().Calls
         self.handle = gbs_plan_create_ex(d, d_pad, m, bits, group, alpha, GBS_PLAN_ASYMMETRIC if asymmetric else 0)
         self.info = gbs_plan_info(self.handle)
+        self._device = torch.cuda.current_device()                 # the plan's, since the C call takes the current one
         self._calls = calls(self.handle)                           # what the native methods know of this plan
 
     def close(self):
@@ -543,8 +544,16 @@ class Plan:
 # ----------------------------------------------------------------------------------------------
 # paged KV cache in four bits
 # ----------------------------------------------------------------------------------------------
+def _int32(what: str, v: int) -> int:
+    """ctypes would cut a larger number to 32 bits."""
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError("gbs: %s does not fit 32 bits: %d" % (what, v))
+    return v
+
+
 def gbs_kv_page_bytes(plan: int, n_kv_heads: int, page_size: int) -> int:
     """Bytes of one page of a pool (host only)."""
+    _int32("n_kv_heads", n_kv_heads), _int32("page_size", page_size)
     out = ctypes.c_int64(0)
     _check(lib().gbs_kv_page_bytes(ctypes.c_void_p(plan), n_kv_heads, page_size, ctypes.byref(out)), "gbs_kv_page_bytes")
     return out.value
@@ -572,8 +581,11 @@ class KVCache:
                 raise ValueError("gbs: %s must have shape %s, got %s" % (what, shape, tuple(t.shape)))
         if page_table.dim() != 2:
             raise ValueError("gbs: page_table must be [sequences, pages]")
+        if pages.device.index != plan._device:
+            raise ValueError("gbs: the pool is on %s, its plan on cuda:%d" % (pages.device, plan._device))
         self.plan, self.n_kv_heads, self.page_size = plan, n_kv_heads, page_size
         self.pages, self.page_table, self.lengths, self.refs = pages, page_table, lengths, refs
+        self._kept = pages, page_table, lengths, refs              # the calls use these, whatever the names above are bound to later
         self._c = KVCacheStruct(pages.data_ptr(), pages.shape[0], n_kv_heads, page_size, page_table.data_ptr(), lengths.data_ptr(),
                                 refs.data_ptr(), page_table.shape[0], page_table.shape[1])
         self._calls = native().Pool(plan._calls, pages, page_table, lengths, refs, n_kv_heads, page_size)
@@ -692,10 +704,13 @@ class KVCache:
     def attention(self, q: torch.Tensor, seqs=None, cu_tokens=None, max_tokens: int = 1, causal: bool = True, window: int = 0,
                   scale: float = 0.0, max_len: int = 0, out=None, stream=None) -> torch.Tensor:
         """Attention of query tokens q [tokens, heads, d] (bf16) over the cache; the same shape comes back.  max_tokens: no item has
-        more tokens; max_len: no sequence of the call is longer (0: the table's width); scale 0: 1 / sqrt(d)."""
+        more tokens; max_len: no sequence of the call is longer (0: the table's width); scale 0: 1 / sqrt(d).  Rows behind the last item's, and
+        an item's beyond max_tokens, are left as they are in `out`, and undefined without one."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise ValueError("gbs: q must be [tokens, heads, d]")
         self._rows("q", q, q.shape[1])
+        for what, v in (("max_tokens", max_tokens), ("window", window), ("max_len", max_len)):
+            _int32(what, v)
         scratch = []
         if out is None:
             out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)

@@ -26,7 +26,7 @@ int view_of(const gbs_plan* p, const gbs_kv_cache_t* c, gbs_kv_view* out)
     const int page_log = log2_page(c->page_size);
     if (page_log < 0 || c->n_kv_heads < 1 || c->n_kv_heads > 1024) return GBS_ERR_INVALID_ARG;
     if (c->n_pages < 1 || c->n_pages > 1ll << 30 || c->n_seqs < 1 || c->max_pages < 1) return GBS_ERR_INVALID_ARG;
-    if ((int64_t)c->max_pages * c->page_size > 0x7fffffffll) return GBS_ERR_INVALID_ARG;
+    if (c->max_pages > 1 << 20) return GBS_ERR_INVALID_ARG;          // positions fit 27 bits, and the pages that 1024 items want 30
     if (!c->pages || !c->page_table || !c->lengths || !c->refs) return GBS_ERR_INVALID_ARG;
     if (!aligned(c->pages, 16) || !aligned(c->page_table, 4) || !aligned(c->lengths, 4) || !aligned(c->refs, 4)) return GBS_ERR_ALIGNMENT;
     out->pages = static_cast<unsigned char*>(c->pages);
@@ -219,12 +219,13 @@ extern "C" int gbs_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache
     if (rc == GBS_OK) rc = check_strides(p, out_token_stride, out_head_stride);
     if (rc != GBS_OK) return rc;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16)) return GBS_ERR_ALIGNMENT;
+    if (q == out) return GBS_ERR_INVALID_ARG;                        // rows are read after others have been written
     A.seqs = seqs;
     A.cu = cu_tokens;
     A.n_items = n_items;
     A.max_tokens = (int)std::min<int64_t>(max_tokens, n_tokens);
     A.max_len = max_len > 0 ? max_len : A.c.max_pages << A.c.page_log;
-    A.window = window;
+    A.window = std::min(window, 1 << 30);                            // beyond any position: position - window stays within 32 bits
     A.causal = flags & GBS_KV_CAUSAL;
     A.n_heads = n_heads;
     A.group = n_heads / A.c.heads;

@@ -65,6 +65,7 @@ __device__ __forceinline__ TokenPlace look_up(const RowArgs& A, int first, int l
     if (A.cu) {
         from = A.cu[item];
         count = A.cu[item + 1] - from;
+        if (token < from) return p;                      // before the first item
     }
     const int seq = kv_sequence(A.c, A.seqs, item);
     if (seq < 0) return p;

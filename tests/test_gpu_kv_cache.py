@@ -525,3 +525,115 @@ def test_native_and_python_paths_agree():
         a.attention(q, seqs, cu, 5)
     with pytest.raises(GbsError):
         a.extend()
+
+
+# ----------------------------------------------------------------------------------------------
+# calls at the edges of what is allowed
+# ----------------------------------------------------------------------------------------------
+def test_rows_before_the_first_item_are_not_written():
+    with plan_of(128) as plan:
+        cache = filled(plan, [20, 9], 2, 16)
+        before = cache.pages.clone()
+        x = torch.ones((6, 2, 128), dtype=torch.bfloat16, device=DEV)
+        cache.append(x, x, None, ints([6, 6, 6]))
+        assert torch.equal(cache.pages, before)
+        cache.append(x, x, None, ints([4, 6, 6]))                           # the last two tokens of sequence 0
+        assert torch.equal(kv_util.rows_of(cache, 0, 18)[0], kv_util.rows_of(KVCache(plan, before, cache.page_table, cache.lengths, cache.refs, 2, 16), 0, 18)[0])
+        assert not torch.equal(cache.pages, before)
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [3, 3], [40, 70]])
+def test_the_widest_window_and_items_with_more_tokens_than_their_sequence(counts):
+    with plan_of(128) as plan:
+        cache = filled(plan, [130, 33], 2, 32)
+        for window in (2 ** 31 - 1, 2 ** 30, 2 ** 27):
+            for causal in (True, False):
+                check_attention(cache, [0, 1], counts, 4, causal=causal, window=window)
+
+
+@pytest.mark.parametrize("counts", [[1, 1, 1], [30, 1, 64]])
+def test_one_sequence_read_by_several_items(counts):
+    with plan_of(80) as plan:
+        cache = filled(plan, [200, 90], 2, 16)
+        check_attention(cache, [0, 0, 1], counts, 8)
+
+
+def test_two_graphs_on_two_streams_and_calls_between_them():
+    """Two captured steps on one pool, replayed at the same time; each has a workspace of its own."""
+    with plan_of(128) as plan:
+        cache = filled(plan, [5000, 900, 40], 4, 64)
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(3)
+        work = []
+        for counts in ([1, 1, 1], [100, 33, 40]):
+            cu, most = ints(cu_of(counts)), max(counts)
+            q = torch.randn((sum(counts), 16, 128), generator=gen, device=DEV).to(torch.bfloat16)
+            want = cache.attention(q, None, cu, most)
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                out = cache.attention(q, None, cu, most)
+            work.append((g, out, want, torch.cuda.Stream(), q, cu, most))
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for g, out, _, s, _, _, _ in work:
+                out.zero_()
+            torch.cuda.synchronize()
+            for g, _, _, s, _, _, _ in work:
+                with torch.cuda.stream(s):
+                    g.replay()
+            eager = [cache.attention(q, None, cu, most) for _, _, _, _, q, cu, most in work]
+            torch.cuda.synchronize()
+            for (_, out, want, *_), e in zip(work, eager):
+                assert torch.equal(out, want) and torch.equal(e, want)
+        assert plan.device_status() == 0
+
+
+def test_a_whole_step_is_captured():
+    """extend, append and attention of a step in one graph: every replay adds a token to each sequence."""
+    with plan_of(128) as plan:
+        n, steps = 5, 40
+        a, b = (KVCache.create(plan, 40, 2, 16, n, 8, DEV) for _ in range(2))
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(9)
+        x = torch.randn((steps, 3, n, 8, 128), generator=gen, device=DEV).to(torch.bfloat16)
+        q, k, v = torch.zeros_like(x[0, 0]), torch.zeros_like(x[0, 0, :, :2]).contiguous(), torch.zeros_like(x[0, 0, :, :2]).contiguous()
+
+        def step(cache):
+            status = cache.extend()
+            cache.append(k, v)
+            return status, cache.attention(q)
+        step(a)                                                             # what a first call sets up
+        for t in (a.lengths, a.refs):
+            t.zero_()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            status, got = step(a)
+        for t in (a.lengths, a.refs):
+            t.zero_()
+        for i in range(steps):
+            q.copy_(x[i, 0]), k.copy_(x[i, 1, :, :2]), v.copy_(x[i, 2, :, :2])
+            g.replay()
+            want_status, want = step(b)
+            assert not status.any() and torch.equal(status, want_status) and torch.equal(got, want)
+            assert a.lengths.tolist() == [i + 1] * n == b.lengths.tolist()
+
+
+def test_more_refusals_of_the_binding():
+    with plan_of(128) as plan:
+        cache = filled(plan, [20], 2, 16)
+        q = torch.randn((1, 4, 128), device=DEV).to(torch.bfloat16)
+        with pytest.raises(GbsError):
+            cache.attention(q, out=q)
+        for name in ("max_tokens", "window", "max_len"):
+            with pytest.raises(ValueError):
+                cache.attention(q, **{name: 2 ** 32 + 1})
+            with pytest.raises(GbsError):
+                cache.attention(q, **{name: -1})
+        other = plan._device
+        plan._device = other + 1
+        with pytest.raises(ValueError):
+            KVCache(plan, cache.pages, cache.page_table, cache.lengths, cache.refs, 2, 16)
+        plan._device = other
+        want = cache.attention(q)
+        cache.lengths = torch.zeros_like(cache.lengths)                     # a name, not the pool's tensor
+        assert torch.equal(cache.attention(q), want)

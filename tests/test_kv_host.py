@@ -152,3 +152,20 @@ def test_attention(lib):
     assert lib.gbs_kv_attention_workspace(pl, r, 8, 3, 2, None) == INVALID
     assert lib.gbs_kv_attention_workspace(pl, r, 6, 3, 2, ctypes.byref(size)) == INVALID
     assert lib.gbs_kv_attention_workspace(pl, r, 8, -1, 2, ctypes.byref(size)) == INVALID
+
+
+def test_the_widest_table_and_one_beyond(lib):
+    assert set(calls(lib, plan(), pool(max_pages=1 << 20, page_size=128)).values()) == {OK}
+    assert set(calls(lib, plan(), pool(max_pages=(1 << 20) + 1)).values()) == {INVALID}
+
+
+def test_attention_in_place_is_refused(lib):
+    c = pool()
+    f = lambda q, out: lib.gbs_kv_attention(plan(), ctypes.byref(c), P, P, 2, 3, 2, 0, q, 1024, 128, 8, 0.0, 0, 1, out, 1024, 128, P, 1 << 40, None)  # noqa: E731
+    assert f(P, P) == INVALID
+
+
+def test_numbers_beyond_32_bits_are_not_cut(lib):
+    for heads, page in ((2 ** 32 + 2, 16), (2, 2 ** 32 + 16)):
+        with pytest.raises(ValueError):
+            binding.gbs_kv_page_bytes(ctypes.addressof(plan()), heads, page)
