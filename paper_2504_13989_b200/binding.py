@@ -391,8 +391,7 @@ def gbs_quantized_matmul(plan_x: int, codes_x: torch.Tensor, scales_x: torch.Ten
     _check(lib().gbs_quantized_matmul(ctypes.c_void_p(plan_x), codes_x.data_ptr(), scales_x.data_ptr(), n_tok,
                                       ctypes.c_void_p(plan_w), codes_w.data_ptr(), scales_w.data_ptr(), n_out,
                                       out.data_ptr(), _dtype_code(out), out.stride(0), _stream_ptr(stream)),
-           "gbs_quantized_matmul", "gbs_kv_page_bytes", "gbs_kv_extend", "gbs_kv_fork", "gbs_kv_free", "gbs_kv_compact",
-           "gbs_kv_append", "gbs_kv_read", "gbs_kv_attention_workspace", "gbs_kv_attention")
+           "gbs_quantized_matmul")
 
 
 def gbs_search_state_init() -> SearchState:
