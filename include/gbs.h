@@ -441,9 +441,10 @@ int gbs_kv_read(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32
  *   scale             0: 1 / sqrt(d)
  *   workspace         device, gbs_kv_attention_workspace bytes, 16-byte aligned; overwritten, needs no preparation, and one call at
  *                     a time may use it
- * Rotated query rows are rounded to 16 bits of their largest coordinate (up to 16 rows a KV head and item), or to 11 bits of each
- * coordinate (more rows), probabilities to 11 bits; sums and softmax statistics are fp32.  With more than 16 rows a KV head and item, value
- * rows more than 2^100 smaller than others that the same row sees may lose their share of the softmax's sum.
+ * Up to 16 rows a KV head and item, rotated query rows are rounded to 16 bits of their largest coordinate, and codes enter as they are; with more
+ * rows query coordinates, scales and the cached coordinates that they give are each rounded to 11 bits.  Probabilities are rounded to
+ * 11 bits; sums and softmax statistics are fp32.  With more than 16 rows, value rows more than 2^100 smaller than others that
+ * the same row sees may lose their share of the softmax's sum.
  */
 int gbs_kv_attention_workspace(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, int n_heads, int64_t n_tokens, int max_tokens,
                                int64_t* bytes_out);

@@ -11,14 +11,15 @@ def h128():
     return torch.from_numpy(H).to(DEV)
 
 
-def rows_of(cache, seq, count=None):
-    """Keys and values [heads, tokens, 128] (rotated domain, 64 bits) that the first `count` tokens of a sequence stand for."""
+def rows_of(cache, seq, count=None, middles=False):
+    """Keys and values [heads, tokens, 128] (rotated domain, 64 bits) that the first `count` tokens of a sequence stand for; with `middles`, behind
+    them |lo + 8 Delta| of their rows [heads, tokens] (0 for a symmetric plan)."""
     ps, asym = cache.page_size, bool(cache.plan.info.asymmetric)
     sf = 2 if asym else 1
     count = int(cache.lengths[seq]) if count is None else count
     ids = cache.page_table[seq, :-(-count // ps)].long()
     blocks = cache.pages[ids].view(len(ids), cache.n_kv_heads, -1)
-    out = []
+    out, mid = [], []
     for i in range(2):
         c = blocks[:, :, i * ps * 64:(i + 1) * ps * 64].reshape(len(ids), cache.n_kv_heads, ps, 64).to(torch.int16)
         q = torch.stack([c & 15, c >> 4], -1).flatten(-2)
@@ -27,7 +28,8 @@ def rows_of(cache, seq, count=None):
         q = q.double()
         y = q * s[..., :1] + s[..., 1:] if asym else (q - 16 * (q > 7)) * s
         out.append(y.transpose(0, 1).flatten(1, 2)[:, :count])
-    return out
+        mid.append(((s[..., 1] + 8 * s[..., 0]).abs() if asym else 0 * s[..., 0]).transpose(0, 1).flatten(1, 2)[:, :count])
+    return out + mid if middles else out
 
 
 def attention(cache, q, seqs, cu, causal=True, window=0, scale=0.0, max_len=0, few=True):
@@ -39,6 +41,10 @@ def attention(cache, q, seqs, cu, causal=True, window=0, scale=0.0, max_len=0, f
     1 / 65024 of its largest coordinate in each of 128 places (few rows: at most sqrt(128) / 65024 of its norm), or to 11 bits of each coordinate
     (2^-12, and sqrt(128) 2^-24 for what falls below fp16's normal numbers); 128 products are added up in 24 bits.  A probability is rounded to
     11 bits (2^-11: 2^-12, and as much for ex2, log2 and the sums).
+
+    With many rows cached rows are rounded too: a coordinate x = c Delta + mid, mid = lo + 8 Delta (symmetric: 0), has Delta, mid and then x itself
+    rounded to 11 bits, so it is off by at most 2^-12 (|x - mid| + |mid| + |x|) <= 2^-11 (|x| + |mid|), a row by 2^-11 (|x|_2 + sqrt(128) |mid|)
+    =: 2^-11 (|x|_2 + m).  That adds scale |q|_2 2^-11 (|khat|_2 + m) to e, and 2^-11 max(|vhat|_2 + m) to the result.
     """
     d = cache.plan.info.d
     heads, kvh = q.shape[1], cache.n_kv_heads
@@ -58,7 +64,7 @@ def attention(cache, q, seqs, cu, causal=True, window=0, scale=0.0, max_len=0, f
         if length == 0:
             want[cu[i]:cu[i + 1]], tol[cu[i]:cu[i + 1]] = 0, 0
             continue
-        k, v = rows_of(cache, seq)
+        k, v, km, vm = rows_of(cache, seq, middles=True)
         s = torch.einsum("qhgd,hkd->qhgk", x, k) * scale
         pos = (length - count + torch.arange(count, device=q.device))[:, None]
         t = torch.arange(length, device=q.device)
@@ -77,6 +83,9 @@ def attention(cache, q, seqs, cu, causal=True, window=0, scale=0.0, max_len=0, f
         vn = (v.norm(dim=-1)[None] * seen[:, None]).amax(-1)
         e = abs(scale) * x.norm(dim=-1) * kn[:, :, None] * (b + 128 * 2.0 ** -23)
         lim = 2.0 ** -8 * o.abs() + ((2 * e + r) * vn[:, :, None])[..., None]
+        if not few:
+            kr, vr = (2.0 ** -11 * ((y.norm(dim=-1) + 128 ** 0.5 * m)[None] * seen[:, None]).amax(-1) for y, m in ((k, km), (v, vm)))
+            lim = lim + (2 * abs(scale) * x.norm(dim=-1) * kr[:, :, None] * vn[:, :, None] + vr[:, :, None])[..., None]
         want[cu[i]:cu[i + 1]] = o.reshape(count, heads, d)
         tol[cu[i]:cu[i + 1]] = lim.reshape(count, heads, d)
     return want, tol
