@@ -85,7 +85,6 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(const __grid_constant__ Kv
     if (j.blocks == 0) return;
     const gbs_kv_attn& A = P.a;
     const int row = 8 * blockIdx.y + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (row >= j.rows) return;
     // piece b's sums: the first block's last segment, the others' first
     const float* first = P.parts + ((long long)blockIdx.x * 2 + 1) * PART;
     const auto piece = [&](int b) { return b == 0 ? first : first + (long long)(2 * b - 1) * PART; };
@@ -140,7 +139,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(const __grid_constant__ Kv
         y[8 + i] = full[row & 7][64 + 8 * l8 + i];
     }
     kv_finish(y, l8, top, top_w, total, extra);
-    if (lane >= 8) return;
+    if (s.e.row0 + row >= s.e.rows || lane >= 8) return;
     int token, head;
     kv_row_of(A, s, row, token, head);
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (s.e.first + token) * A.out_token + head * A.out_head;

@@ -7,7 +7,7 @@
 // other.  Bits 3 and 4 (t) lie across lanes and have to go to the matrix unit, with two of the three bits below; what is left, the third
 // one and j, is in registers.  The result has the layout of the operand, so no number moves between lanes.
 // Seven stages over eight lanes a row, three of them by shuffles, took 119 and 85 instructions a row and warp (write and read) instead of 59 and 52:
-// 14000 tokens x 8 heads written and read back in 62.7 us instead of 42.7.
+// 14000 tokens x 8 heads written and read back in 62.7 us instead of 44.
 // What bounds it then is the issue of instructions; the bytes (130 MB) would take 20 us.
 // Reading back, the codes go in as fp16, and everything up to the scale is exact.
 #include <cuda_fp16.h>

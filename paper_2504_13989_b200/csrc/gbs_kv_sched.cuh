@@ -161,13 +161,13 @@ __device__ __forceinline__ int kv_share(const gbs_kv_attn& A, const KvLine& L, K
 // What a block leaves for the join about the segment whose first unit it has and that ends in another block; blocks = 0: no such segment.
 struct KvJoin {
     int index, head, blocks;
-    int rows;                  // of the tile
+    int pad;
 };
 // the blocks behind have as many places each, or their rest
 __device__ __forceinline__ KvJoin kv_join(const KvLine& L, const KvSeg& s, int places)
 {
     const int beyond = s.at + L.pad + s.e.units - places;
-    return KvJoin{s.index, s.head, 1 + (beyond + places - 1) / places, s.e.rows - s.e.row0};
+    return KvJoin{s.index, s.head, 1 + (beyond + places - 1) / places, 0};
 }
 
 }  // namespace
