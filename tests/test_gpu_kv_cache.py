@@ -637,3 +637,59 @@ def test_more_refusals_of_the_binding():
         want = cache.attention(q)
         cache.lengths = torch.zeros_like(cache.lengths)                     # a name, not the pool's tensor
         assert torch.equal(cache.attention(q), want)
+
+
+@pytest.mark.parametrize("asym", [False, True])
+@pytest.mark.parametrize("count", [1, 3, 60, 150])
+def test_scales_that_are_no_numbers_reach_the_rows_that_see_them(count, asym):
+    with plan_of(128, asym) as plan:
+        for which, bad in ((0, float("nan")), (1, float("nan")), (1, float("inf"))):
+            cache = filled(plan, [200], 2, 32)
+            gen = torch.Generator(device=DEV)
+            gen.manual_seed(count)
+            q = torch.randn((count, 4, 128), generator=gen, device=DEV).to(torch.bfloat16)
+            cu, few = ints([0, count]), 2 * count <= 16
+            want, tol = kv_util.attention(cache, q, [0], [0, count], few=few)
+            at = max(180, 200 - count // 2)                                 # this token's scale, of KV head 1
+            sf = 2 if asym else 1
+            block = cache.pages[cache.page_table[0, at // 32].long()].view(2, -1)[1]
+            block[32 * 128:].view(torch.float32)[which * 32 * sf + (at % 32) * sf] = bad
+            got = cache.attention(q, ints([0]), cu, count).double()
+            sees = torch.zeros((count, 4), dtype=torch.bool, device=DEV)
+            sees[torch.arange(200 - count, 200, device=DEV) >= at, 2:] = True
+            assert bool(torch.isnan(got[sees]).all()) and bool(((got - want).abs() <= tol)[~sees].all())
+
+
+@pytest.mark.parametrize("counts", [[1], [3], [300]])
+def test_values_of_zero_and_of_many_sizes(counts):
+    """Zero values first, then ever larger ones; the rows of a long prompt see some of them each.  Groups of 32 tokens have one size."""
+    with plan_of(128, alpha=1.0) as plan:
+        cache = filled(plan, [300], 2, 16, scale=0.1)
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(21)
+        k = (torch.randn((300, 2, 128), generator=gen, device=DEV) * 0.1).to(torch.bfloat16)
+        size = torch.tensor([0.0, 0.0, 2.0 ** -40, 2.0 ** -38, 0.0, 2.0 ** -20, 1.0, 2.0 ** 6, 2.0 ** 30, 0.0], device=DEV).repeat_interleave(32)[:300]
+        v = (torch.randn((300, 2, 128), generator=gen, device=DEV) * size[:, None, None]).to(torch.bfloat16)
+        for _ in range(2):
+            cache.append(k, v, None, ints([0, 300]))
+            check_attention(cache, [0], counts, 6)
+            check_attention(cache, [0], counts, 6, window=40)
+            v = v.flip(0).contiguous()                                      # the largest first
+
+
+@pytest.mark.parametrize("asym", [False, True])
+def test_a_negative_scale_and_windows_at_every_offset(asym):
+    with plan_of(64, asym) as plan:
+        cache = filled(plan, [260], 1, 16)
+        for counts in ([2], [130]):
+            check_attention(cache, [0], counts, 3, scale=-0.2)
+            for window in (1, 2, 31, 32, 33, 64, 127, 128, 129):
+                check_attention(cache, [0], counts, 3, window=window)
+
+
+def test_prompts_of_every_length_around_a_tile():
+    """One KV head with three query heads: rows that fill one tile of 128, both, or a little of the next block's."""
+    with plan_of(128) as plan:
+        for count in (6, 42, 43, 44, 85, 86, 87, 128, 171, 172):
+            cache = filled(plan, [count, count + 1, count + 200], 1, 64, seed=count)
+            check_attention(cache, [0, 1, 2], [count] * 3, 3)
