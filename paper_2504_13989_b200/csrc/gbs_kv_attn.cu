@@ -112,54 +112,54 @@ __device__ __forceinline__ void prepare(const gbs_kv_attn& A, const KvSeg& seg, 
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int row = 4 * r + (lane >> 3);
-                    float y[16];
-                    kv_unpack_bf16(raw[r][0], y);
-                    kv_unpack_bf16(raw[r][1], y + 8);
-                    kv_hadamard(y, l8);
-                    float m = 0.f;
+        float y[16];
+        kv_unpack_bf16(raw[r][0], y);
+        kv_unpack_bf16(raw[r][1], y + 8);
+        kv_hadamard(y, l8);
+        float m = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(y[i]));
+        for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(y[i]));
 #pragma unroll
-                    for (int h = 1; h < 8; h <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, h));
-                    // integers of up to 32512, whose upper byte is at most 127; a row that is not finite has a factor that is not a number
-                    const float up = m < 1e-30f ? 1.2379400392853803e27f : 1.f;     // 2^90
-                    const float by = m > 0.f ? 32512.f / (m * up) : 0.f;
-                    int q[16], sum = 0;
-                    float wrong = 0.f;
+        for (int h = 1; h < 8; h <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, h));
+        // integers of up to 32512, whose upper byte is at most 127; a row that is not finite has a factor that is not a number
+        const float up = m < 1e-30f ? 1.2379400392853803e27f : 1.f;     // 2^90
+        const float by = m > 0.f ? 32512.f / (m * up) : 0.f;
+        int q[16], sum = 0;
+        float wrong = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        q[i] = __float2int_rn(fminf(fmaxf(y[i] * up * by, -32512.f), 32512.f));
-                        sum += q[i];
-                        wrong += y[i] * 0.f;
-                    }
+        for (int i = 0; i < 16; ++i) {
+            q[i] = __float2int_rn(fminf(fmaxf(y[i] * up * by, -32512.f), 32512.f));
+            sum += q[i];
+            wrong += y[i] * 0.f;
+        }
 #pragma unroll
-                    for (int h = 1; h < 8; h <<= 1) {
-                        sum += __shfl_xor_sync(0xffffffffu, sum, h);
-                        wrong += __shfl_xor_sync(0xffffffffu, wrong, h);
-                    }
+        for (int h = 1; h < 8; h <<= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, h);
+            wrong += __shfl_xor_sync(0xffffffffu, wrong, h);
+        }
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        unsigned high[2] = {0, 0}, low[2] = {0, 0};
+        for (int half = 0; half < 2; ++half) {
+            unsigned high[2] = {0, 0}, low[2] = {0, 0};
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int x = q[8 * half + i], top = (x + 128) >> 8;
-                            high[i & 1] |= (unsigned)(top & 255) << (8 * (i >> 1));
-                            low[i & 1] |= (unsigned)((x - 256 * top) & 255) << (8 * (i >> 1));
-                        }
-                        *reinterpret_cast<uint2*>(&Q.h[row][64 * half + 8 * l8]) = make_uint2(high[0], high[1]);
-                        *reinterpret_cast<uint2*>(&Q.l[row][64 * half + 8 * l8]) = make_uint2(low[0], low[1]);
-                    }
-                    if (l8 == 0) {
-                        Q.factor[row] = m * (A.scale * (KV_NORM * 1.4426950408889634f / 32512.f)) + wrong;
-                        Q.sum[row] = sum;
-                        const int token = A.by_group(min(seg.e.row0 + row, seg.e.rows - 1));
-                        Q.lo[row] = kv_row_lo(A, seg.e, token);
-                        Q.hi[row] = kv_row_hi(A, seg.e, token);
-                        if (row == 0) {                          // the last row sees the latest window, the first the shortest past
-                            Q.all_lo = kv_row_lo(A, seg.e, A.by_group(min(seg.e.rows, seg.e.row0 + ROWS) - 1));
-                            Q.all_hi = Q.hi[0];
-                        }
-                    }
+            for (int i = 0; i < 8; ++i) {
+                const int x = q[8 * half + i], top = (x + 128) >> 8;
+                high[i & 1] |= (unsigned)(top & 255) << (8 * (i >> 1));
+                low[i & 1] |= (unsigned)((x - 256 * top) & 255) << (8 * (i >> 1));
+            }
+            *reinterpret_cast<uint2*>(&Q.h[row][64 * half + 8 * l8]) = make_uint2(high[0], high[1]);
+            *reinterpret_cast<uint2*>(&Q.l[row][64 * half + 8 * l8]) = make_uint2(low[0], low[1]);
+        }
+        if (l8 == 0) {
+            Q.factor[row] = m * (A.scale * (KV_NORM * 1.4426950408889634f / 32512.f)) + wrong;
+            Q.sum[row] = sum;
+            const int token = A.by_group(min(seg.e.row0 + row, seg.e.rows - 1));
+            Q.lo[row] = kv_row_lo(A, seg.e, token);
+            Q.hi[row] = kv_row_hi(A, seg.e, token);
+            if (row == 0) {                          // the last row sees the latest window, the first the shortest past
+                Q.all_lo = kv_row_lo(A, seg.e, A.by_group(min(seg.e.rows, seg.e.row0 + ROWS) - 1));
+                Q.all_hi = Q.hi[0];
+            }
+        }
     }
 }
 
