@@ -700,14 +700,17 @@ class KVCache:
                                  self._stream(stream, *scratch)), "gbs_kv_read")
         return k, v
 
-    def attention(self, q: torch.Tensor, seqs=None, cu_tokens=None, max_tokens: int = 1, causal: bool = True, window: int = 0,
+    def attention(self, q: torch.Tensor, seqs=None, cu_tokens=None, max_tokens: int | None = None, causal: bool = True, window: int = 0,
                   scale: float = 0.0, max_len: int = 0, out=None, stream=None) -> torch.Tensor:
         """Attention of query tokens q [tokens, heads, d] (bf16) over the cache; the same shape comes back.  max_tokens: no item has
-        more tokens; max_len: no sequence of the call is longer (0: the table's width); scale 0: 1 / sqrt(d).  Rows behind the last item's, and
-        an item's beyond max_tokens, are left as they are in `out`, and undefined without one."""
+        more tokens (None: as many as q has, or 1 without cu_tokens; it chooses the kernel, so the closer the better); max_len: no
+        sequence of the call is longer (0: the table's width); scale 0: 1 / sqrt(d).  Rows behind the last item's, and an item's beyond
+        max_tokens, are left as they are in `out`, and undefined without one."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise ValueError("gbs: q must be [tokens, heads, d]")
         self._rows("q", q, q.shape[1])
+        if max_tokens is None:
+            max_tokens = max(1, q.shape[0]) if cu_tokens is not None else 1
         for what, v in (("max_tokens", max_tokens), ("window", window), ("max_len", max_len)):
             _int32(what, v)
         scratch = []

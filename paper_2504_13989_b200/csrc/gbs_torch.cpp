@@ -23,6 +23,9 @@
 #include <cuda_runtime_api.h>
 #include <stddef.h>
 #include <string.h>
+
+#include <algorithm>
+
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -505,7 +508,7 @@ PyObject* do_kv_attention(const Pool& p, const PlanRef& ref, PyObject* const* g)
     Items it;
     int most, window, longest;
     if (!none(g[9]) || !rows3_of(p, g[0], ref.info.d, &q) || !items_of(p, g[1], g[2], q.n, &it)) Py_RETURN_NONE;
-    if (!int_of(g[3], 1, &most) || !int_of(g[5], 0, &window) || !int_of(g[7], 0, &longest)) Py_RETURN_NONE;
+    if (q.n > 0x7fffffff || !int_of(none(g[3]) ? nullptr : g[3], none(g[2]) ? 1 : static_cast<int>(std::max<int64_t>(1, q.n)), &most) || !int_of(g[5], 0, &window) || !int_of(g[7], 0, &longest)) Py_RETURN_NONE;
     const int causal = g[4] ? PyObject_IsTrue(g[4]) : 1;
     const double scale = g[6] ? PyFloat_AsDouble(g[6]) : 0.0;
     if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }

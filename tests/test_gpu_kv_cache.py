@@ -618,6 +618,19 @@ def test_a_whole_step_is_captured():
             assert a.lengths.tolist() == [i + 1] * n == b.lengths.tolist()
 
 
+def test_without_max_tokens_every_row_is_answered():
+    with plan_of(128) as plan:
+        cache = filled(plan, [90, 50, 7], 2, 16)
+        for counts in ([1, 1, 1], [2, 0, 3], [40, 30, 1]):
+            q = torch.randn((sum(counts), 8, 128), device=DEV).to(torch.bfloat16)
+            cu = ints(cu_of(counts))
+            few = sum(counts) * 4 <= 16
+            want, tol = kv_util.attention(cache, q, [0, 1, 2], cu_of(counts), few=few)
+            python = binding._PYTHON_KV_METHODS["attention"](cache, q, None, cu)
+            for got in (cache.attention(q, None, cu), cache.attention(q, None, cu, None), python):
+                assert bool(((got.double() - want).abs() <= tol).all())
+
+
 def test_more_refusals_of_the_binding():
     with plan_of(128) as plan:
         cache = filled(plan, [20], 2, 16)
