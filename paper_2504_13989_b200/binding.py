@@ -565,7 +565,8 @@ class KVCache:
     [n_seqs, max_pages], lengths [n_seqs] and refs [n_pages] int32.  KVCache.create makes them, empty.  Items of a call are
     sequences: `seqs` (int32, None: 0, 1, ..), with `cu_tokens` (int32, [items + 1]) where an item has other than one token; their
     tokens are the last ones of the sequences.  Nothing here waits for the device: what became of the items of extend and fork
-    stands in the tensors these return.
+    stands in the tensors these return.  With `stream`, a call's results are
+    allocated on it; ordering it behind the work that its arguments come from is the caller's.
     """
 
     def __init__(self, plan: Plan, pages: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor,
@@ -597,12 +598,26 @@ class KVCache:
         return cls(plan, pages, table, torch.zeros(n_seqs, dtype=torch.int32, device=device),
                    torch.zeros(n_pages, dtype=torch.int32, device=device), n_kv_heads, page_size)
 
-    def _stream(self, stream, *scratch):
-        """The call's stream, which scratch memory of the call is given to."""
+    def _empty(self, stream, shape, dtype, handed_on=True):
+        """Memory for a call's results or its workspace, taken on the call's stream: a block that is free on another one may still be used by
+        work that waits there.  Results, which the caller's stream goes on with, are not taken again before that one is done with them."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.pages.device)
+        with torch.cuda.stream(stream):
+            t = torch.empty(shape, dtype=dtype, device=self.pages.device)
+        if handed_on:
+            t.record_stream(torch.cuda.current_stream(self.pages.device))
+        return t
+
+    def _stream(self, stream, *used):
+        """The call's stream; the tensors that it uses are kept until it is done with them, whichever stream they are freed on."""
         if stream is None:
             return int(torch.cuda.current_stream(self.pages.device).cuda_stream)
-        for t in scratch:
-            t.record_stream(stream)
+        if stream.device != self.pages.device:
+            raise ValueError("gbs: the pool is on %s, the stream on %s" % (self.pages.device, stream.device))
+        for t in self._kept + used:
+            if t is not None:
+                t.record_stream(stream)
         return int(stream.cuda_stream)
 
     def _ints(self, what: str, t, n: int):
@@ -637,34 +652,34 @@ class KVCache:
     def extend(self, seqs=None, counts=None, stream=None) -> torch.Tensor:
         """Room for counts[i] (None: one) more tokens in each sequence; returns the items' status (GBS_KV_*)."""
         n = next((t.shape[0] for t in (seqs, counts) if t is not None), self.page_table.shape[0])
-        status = torch.empty(n, dtype=torch.int32, device=self.pages.device)
+        status = self._empty(stream, n, torch.int32)
         _check(lib().gbs_kv_extend(self.plan.handle, ctypes.byref(self._c), self._ints("seqs", seqs, n), self._ints("counts", counts, n), n,
-                                   status.data_ptr(), self._stream(stream, status)), "gbs_kv_extend")
+                                   status.data_ptr(), self._stream(stream, seqs, counts)), "gbs_kv_extend")
         return status
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor, stream=None) -> torch.Tensor:
         """Empty sequences dst[i] become copies of src[i] that share its full pages; returns the pairs' status (GBS_KV_*)."""
         n = src.shape[0]
-        status = torch.empty(n, dtype=torch.int32, device=self.pages.device)
+        status = self._empty(stream, n, torch.int32)
         _check(lib().gbs_kv_fork(self.plan.handle, ctypes.byref(self._c), self._ints("src", src, n), self._ints("dst", dst, n), n,
-                                 status.data_ptr(), self._stream(stream, status)), "gbs_kv_fork")
+                                 status.data_ptr(), self._stream(stream, src, dst)), "gbs_kv_fork")
         return status
 
     def free(self, seqs: torch.Tensor, stream=None) -> None:
         """The sequences end; pages that no other sequence holds are free."""
         _check(lib().gbs_kv_free(self.plan.handle, ctypes.byref(self._c), self._ints("seqs", seqs, seqs.shape[0]), seqs.shape[0],
-                                 self._stream(stream)), "gbs_kv_free")
+                                 self._stream(stream, seqs)), "gbs_kv_free")
 
     def compact(self, into: "KVCache", page_map: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """Move the pages in use into the pool `into`, in order; returns their number (one int32 on the device)."""
         if page_map is None:
-            page_map = torch.empty(self.pages.shape[0], dtype=torch.int32, device=self.pages.device)
-        live = torch.empty(1, dtype=torch.int32, device=self.pages.device)
+            page_map = self._empty(stream, self.pages.shape[0], torch.int32, False)
+        live = self._empty(stream, 1, torch.int32)
         if into.pages.device != self.pages.device or into.plan.info.asymmetric != self.plan.info.asymmetric:
             raise ValueError("gbs: both pools must be on one device and of one kind of quantizer")
         _check(lib().gbs_kv_compact(self.plan.handle, ctypes.byref(self._c), ctypes.byref(into._c),
                                     self._ints("page_map", page_map, self.pages.shape[0]), live.data_ptr(),
-                                    self._stream(stream, page_map, live)), "gbs_kv_compact")
+                                    self._stream(stream, page_map, *into._kept)), "gbs_kv_compact")
         return live
 
     def append(self, k: torch.Tensor, v: torch.Tensor, seqs=None, cu_tokens=None, stream=None) -> None:
@@ -677,7 +692,7 @@ class KVCache:
             raise ValueError("gbs: k and v must have the same strides, got %s and %s" % (k.stride(), v.stride()))
         s, cu, n = self._items(seqs, cu_tokens, k.shape[0])
         _check(lib().gbs_kv_append(self.plan.handle, ctypes.byref(self._c), s, cu, n, k.shape[0], k.data_ptr(), v.data_ptr(),
-                                   *self._strides(k), self._stream(stream)), "gbs_kv_append")
+                                   *self._strides(k), self._stream(stream, k, v, seqs, cu_tokens)), "gbs_kv_append")
 
     def read(self, seqs=None, cu_tokens=None, n_tokens: int | None = None, out=None, stream=None):
         """The rows that the cache stands for, [n_tokens, n_kv_heads, d] bf16 keys and values, in their own basis."""
@@ -687,17 +702,14 @@ class KVCache:
                     raise ValueError("gbs: n_tokens says how many rows cu_tokens (on the device) asks for")
                 n_tokens = seqs.shape[0] if seqs is not None else self.page_table.shape[0]
             shape = (n_tokens, self.n_kv_heads, self.plan.info.d)
-            out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=self.pages.device) for _ in range(2))
-            scratch = out
-        else:
-            scratch = ()
+            out = tuple(self._empty(stream, shape, torch.bfloat16) for _ in range(2))
         k, v = out
         for what, x in (("k_out", k), ("v_out", v)):
             self._rows(what, x, self.n_kv_heads)
             _check_buffer(what, x, self.pages, torch.bfloat16, k.numel())
         s, cu, n = self._items(seqs, cu_tokens, k.shape[0])
         _check(lib().gbs_kv_read(self.plan.handle, ctypes.byref(self._c), s, cu, n, k.shape[0], k.data_ptr(), v.data_ptr(),
-                                 self._stream(stream, *scratch)), "gbs_kv_read")
+                                 self._stream(stream, k, v, seqs, cu_tokens)), "gbs_kv_read")
         return k, v
 
     def attention(self, q: torch.Tensor, seqs=None, cu_tokens=None, max_tokens: int | None = None, causal: bool = True, window: int = 0,
@@ -713,10 +725,8 @@ class KVCache:
             max_tokens = max(1, q.shape[0]) if cu_tokens is not None else 1
         for what, v in (("max_tokens", max_tokens), ("window", window), ("max_len", max_len)):
             _int32(what, v)
-        scratch = []
         if out is None:
-            out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-            scratch.append(out)
+            out = self._empty(stream, q.shape, torch.bfloat16)
         self._rows("out", out, q.shape[1])
         if out.shape[0] != q.shape[0]:
             raise ValueError("gbs: q has %d tokens, out %d" % (q.shape[0], out.shape[0]))
@@ -724,10 +734,10 @@ class KVCache:
         need = ctypes.c_int64(0)
         _check(lib().gbs_kv_attention_workspace(self.plan.handle, ctypes.byref(self._c), q.shape[1], q.shape[0], max_tokens, ctypes.byref(need)),
                "gbs_kv_attention_workspace")
-        work = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        work = self._empty(stream, need.value, torch.uint8, False)
         _check(lib().gbs_kv_attention(self.plan.handle, ctypes.byref(self._c), s, cu, n, q.shape[0], max_tokens, max_len, q.data_ptr(),
                                       *self._strides(q), q.shape[1], float(scale), window, GBS_KV_CAUSAL if causal else 0, out.data_ptr(),
-                                      *self._strides(out), work.data_ptr(), need.value, self._stream(stream, work, *scratch)),
+                                      *self._strides(out), work.data_ptr(), need.value, self._stream(stream, q, out, seqs, cu_tokens)),
                "gbs_kv_attention")
         return out
 
