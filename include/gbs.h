@@ -338,7 +338,7 @@ int gbs_quantized_matmul(const gbs_plan_t* plan_x, const void* codes_x, const fl
  * cu_tokens[i] .. cu_tokens[i + 1] - 1 of the call's row tensors (device int32, n_items + 1 values that do not fall, from 0), or row i
  * alone where cu_tokens is NULL.  They are the LAST tokens of the sequence as lengths[] has it: a step extends the
  * sequences first, then appends and attends.  So an item that gbs_kv_extend refused must not be appended: its rows would replace the
- * sequence's last ones.  Rows behind cu_tokens[n_items] count for nothing and are not written.
+ * sequence's last ones, which other sequences may share; gbs_kv_append_extended leaves such items out.  Rows behind cu_tokens[n_items] count for nothing and are not written.
  * Numbers that only the device knows are checked there: an item whose sequence is out of range, a token whose position is
  * below 0 or whose page is not one of the pool's is left out (a row that would be written from it becomes 0).
  *
@@ -411,9 +411,16 @@ int gbs_kv_compact(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const gb
  *                     t * token_stride + h * head_stride, strides multiples of 8 (k and v have the same)
  *   n_tokens          rows that k and v hold; cu_tokens NULL: n_tokens = n_items
  * Where two items name one sequence, both write its last tokens, and either's bytes may stay.
+ *
+ * gbs_kv_append_extended writes the rows of those items alone that gbs_kv_extend has served, so that a step which is enqueued as a whole,
+ * or captured, may run out of pages: rows of an item with status[i] != GBS_KV_DONE are left out.
+ *   status            device int32 [n_items], as gbs_kv_extend wrote it for the same items; NULL: all items are written
  */
 int gbs_kv_append(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
                   int64_t n_tokens, const void* k, const void* v, int64_t token_stride, int64_t head_stride, void* cuda_stream);
+int gbs_kv_append_extended(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                           int64_t n_tokens, const void* k, const void* v, int64_t token_stride, int64_t head_stride, const int32_t* status,
+                           void* cuda_stream);
 
 /*
  * The rows that the cache stands for, back in their own basis: gbs_dequantize with GBS_INVERSE_ROTATE of the items' tokens.

@@ -40,7 +40,7 @@ EXPORTS = ("gbs_plan_create", "gbs_plan_create_ex", "gbs_plan_destroy", "gbs_pla
            "gbs_search_clip_ratio", "gbs_search_state_init", "gbs_search_clip_ratio_fn", "gbs_search_clip_ratio_batch",
            "gbs_hadamard_m", "gbs_status_string", "gbs_selftest_wait_expiry", "gbs_weight_rotate_quantize",
            "gbs_quantized_matmul", "gbs_kv_page_bytes", "gbs_kv_extend", "gbs_kv_fork", "gbs_kv_free", "gbs_kv_compact",
-           "gbs_kv_append", "gbs_kv_read", "gbs_kv_attention_workspace", "gbs_kv_attention")
+           "gbs_kv_append", "gbs_kv_append_extended", "gbs_kv_read", "gbs_kv_attention_workspace", "gbs_kv_attention")
 GBS_STATIC_MAX_D_PAD = 4096
 
 
@@ -141,11 +141,12 @@ def lib() -> ctypes.CDLL:
         L.gbs_kv_free.argtypes = [vp, kv, vp, i32, vp]
         L.gbs_kv_compact.argtypes = [vp, kv, kv, vp, vp, vp]
         L.gbs_kv_append.argtypes = [vp, kv, vp, vp, i32, i64, vp, vp, i64, i64, vp]
+        L.gbs_kv_append_extended.argtypes = [vp, kv, vp, vp, i32, i64, vp, vp, i64, i64, vp, vp]
         L.gbs_kv_read.argtypes = [vp, kv, vp, vp, i32, i64, vp, vp, vp]
         L.gbs_kv_attention_workspace.argtypes = [vp, kv, i32, i64, i32, ctypes.POINTER(i64)]
         L.gbs_kv_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, i32, vp, i64, i64,
                                        vp, i64, vp]
-        for name in EXPORTS[-9:]:
+        for name in EXPORTS[-10:]:
             getattr(L, name).restype = i32
         L.gbs_hadamard_m.argtypes = [i32, vp]
         L.gbs_hadamard_m.restype = i32
@@ -682,8 +683,9 @@ class KVCache:
                                     self._stream(stream, page_map, *into._kept)), "gbs_kv_compact")
         return live
 
-    def append(self, k: torch.Tensor, v: torch.Tensor, seqs=None, cu_tokens=None, stream=None) -> None:
-        """Rotate and quantize key and value rows [tokens, n_kv_heads, d] (bf16) into the pages of their tokens."""
+    def append(self, k: torch.Tensor, v: torch.Tensor, seqs=None, cu_tokens=None, stream=None, status=None) -> None:
+        """Rotate and quantize key and value rows [tokens, n_kv_heads, d] (bf16) into the pages of their tokens.  status: what extend returned
+        for these items; those that it refused are left out (without it their rows replace the last ones of their sequences)."""
         self._rows("k", k, self.n_kv_heads)
         self._rows("v", v, self.n_kv_heads)
         if v.shape[0] != k.shape[0]:
@@ -691,8 +693,9 @@ class KVCache:
         if self._strides(v) != self._strides(k):
             raise ValueError("gbs: k and v must have the same strides, got %s and %s" % (k.stride(), v.stride()))
         s, cu, n = self._items(seqs, cu_tokens, k.shape[0])
-        _check(lib().gbs_kv_append(self.plan.handle, ctypes.byref(self._c), s, cu, n, k.shape[0], k.data_ptr(), v.data_ptr(),
-                                   *self._strides(k), self._stream(stream, k, v, seqs, cu_tokens)), "gbs_kv_append")
+        _check(lib().gbs_kv_append_extended(self.plan.handle, ctypes.byref(self._c), s, cu, n, k.shape[0], k.data_ptr(), v.data_ptr(),
+                                            *self._strides(k), self._ints("status", status, n),
+                                            self._stream(stream, k, v, seqs, cu_tokens, status)), "gbs_kv_append")
 
     def read(self, seqs=None, cu_tokens=None, n_tokens: int | None = None, out=None, stream=None):
         """The rows that the cache stands for, [n_tokens, n_kv_heads, d] bf16 keys and values, in their own basis."""

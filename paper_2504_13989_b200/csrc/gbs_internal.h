@@ -183,7 +183,7 @@ struct gbs_kv_view {
 };
 
 int gbs_kv_append_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, const int* cu, int n_items, int64_t n_tokens, const void* k,
-                         const void* v, int64_t token_stride, int64_t head_stride, cudaStream_t stream);
+                         const void* v, int64_t token_stride, int64_t head_stride, const int* status, cudaStream_t stream);
 int gbs_kv_read_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, const int* cu, int n_items, int64_t n_tokens, void* k_out,
                        void* v_out, cudaStream_t stream);
 int gbs_kv_extend_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, const int* counts, int n_items, int* status, cudaStream_t stream);

@@ -139,8 +139,9 @@ extern "C" int gbs_kv_compact(const gbs_plan_t* p, const gbs_kv_cache_t* cache, 
     return on_device(p, [&] { return gbs_kv_compact_launch(p, v, w, page_map, n_live, static_cast<cudaStream_t>(stream)); });
 }
 
-extern "C" int gbs_kv_append(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
-                             int64_t n_tokens, const void* k, const void* v, int64_t token_stride, int64_t head_stride, void* stream)
+extern "C" int gbs_kv_append_extended(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens,
+                                      int n_items, int64_t n_tokens, const void* k, const void* v, int64_t token_stride, int64_t head_stride,
+                                      const int32_t* status, void* stream)
 {
     gbs_kv_view c;
     bool empty = false;
@@ -150,10 +151,16 @@ extern "C" int gbs_kv_append(const gbs_plan_t* p, const gbs_kv_cache_t* cache, c
     if (!k || !v) return GBS_ERR_INVALID_ARG;
     rc = check_strides(p, token_stride, head_stride);
     if (rc != GBS_OK) return rc;
-    if (!aligned(k, 16) || !aligned(v, 16)) return GBS_ERR_ALIGNMENT;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(status, 4)) return GBS_ERR_ALIGNMENT;
     return on_device(p, [&] {
-        return gbs_kv_append_launch(p, c, seqs, cu_tokens, n_items, n_tokens, k, v, token_stride, head_stride, static_cast<cudaStream_t>(stream));
+        return gbs_kv_append_launch(p, c, seqs, cu_tokens, n_items, n_tokens, k, v, token_stride, head_stride, status, static_cast<cudaStream_t>(stream));
     });
+}
+
+extern "C" int gbs_kv_append(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                             int64_t n_tokens, const void* k, const void* v, int64_t token_stride, int64_t head_stride, void* stream)
+{
+    return gbs_kv_append_extended(p, cache, seqs, cu_tokens, n_items, n_tokens, k, v, token_stride, head_stride, nullptr, stream);
 }
 
 extern "C" int gbs_kv_read(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,

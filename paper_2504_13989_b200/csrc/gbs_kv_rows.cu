@@ -21,7 +21,7 @@ constexpr int THREADS = 128, ROWS = THREADS / 2;   // rows of a block
 
 struct RowArgs {
     gbs_kv_view c;
-    const int *seqs, *cu;
+    const int *seqs, *cu, *status;                 // status: of an extend; items that it refused have no place (null: all have)
     int n_items;
     unsigned n_rows, rows_per_token;               // rows: (token, head, key or value)
     int d;
@@ -68,7 +68,7 @@ __device__ __forceinline__ TokenPlace look_up(const RowArgs& A, int first, int l
         if (token < from) return p;                      // before the first item
     }
     const int seq = kv_sequence(A.c, A.seqs, item);
-    if (seq < 0) return p;
+    if (seq < 0 || (A.status && A.status[item] != GBS_KV_DONE)) return p;
     const int length = kv_length(A.c, seq), pos = length - count + (token - from);
     if (pos < 0 || pos >= length) return p;
     const int page = kv_page(A.c, seq, pos);
@@ -349,9 +349,10 @@ RowArgs row_args(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, const
 }  // namespace
 
 int gbs_kv_append_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, const int* cu, int n_items, int64_t n_tokens, const void* k,
-                         const void* v, int64_t token_stride, int64_t head_stride, cudaStream_t stream)
+                         const void* v, int64_t token_stride, int64_t head_stride, const int* status, cudaStream_t stream)
 {
     RowArgs A = row_args(p, c, seqs, cu, n_items, n_tokens);
+    A.status = status;
     A.k = static_cast<const __nv_bfloat16*>(k);
     A.v = static_cast<const __nv_bfloat16*>(v);
     A.token_stride = token_stride;

@@ -468,15 +468,17 @@ PyObject* do_kv_free(const Pool& p, const PlanRef& ref, PyObject* const* g)     
     Py_RETURN_TRUE;
     GBS_END
 }
-PyObject* do_kv_append(const Pool& p, const PlanRef& ref, PyObject* const* g)        // k, v, seqs, cu_tokens, stream
+PyObject* do_kv_append(const Pool& p, const PlanRef& ref, PyObject* const* g)        // k, v, seqs, cu_tokens, stream, status
 {
     GBS_BEGIN
     Rows k, v;
     Items it;
+    const int32_t* status;
     if (!none(g[4]) || !rows3_of(p, g[0], ref.info.d, &k) || !rows3_of(p, g[1], ref.info.d, &v)) Py_RETURN_NONE;
     if (k.n != v.n || k.token != v.token || k.head != v.head || k.heads != p.cache.n_kv_heads || v.heads != k.heads) Py_RETURN_NONE;
-    if (!items_of(p, g[2], g[3], k.n, &it)) Py_RETURN_NONE;
-    if (gbs_kv_append(ref.plan, &p.cache, it.seqs, it.cu, static_cast<int>(it.n), k.n, k.ptr, v.ptr, k.token, k.head, stream_on(p)) != GBS_OK)
+    if (!items_of(p, g[2], g[3], k.n, &it) || !ints_of(p, g[5], it.n, &status)) Py_RETURN_NONE;
+    if (gbs_kv_append_extended(ref.plan, &p.cache, it.seqs, it.cu, static_cast<int>(it.n), k.n, k.ptr, v.ptr, k.token, k.head, status,
+                               stream_on(p)) != GBS_OK)
         Py_RETURN_NONE;
     Py_RETURN_TRUE;
     GBS_END
@@ -564,7 +566,7 @@ constexpr Method KV_EXTEND = {"extend", 3, 0, {"seqs", "counts", "stream"}, null
 constexpr Method KV_FORK = {"fork", 3, 2, {"src", "dst", "stream"}, nullptr, do_kv_fork};
 constexpr Method KV_FREE = {"free", 2, 1, {"seqs", "stream"}, nullptr, do_kv_free, true};
 constexpr Method KV_COMPACT = {"compact", 3, 1, {"into", "page_map", "stream"}, nullptr, do_kv_compact};
-constexpr Method KV_APPEND = {"append", 5, 2, {"k", "v", "seqs", "cu_tokens", "stream"}, nullptr, do_kv_append, true};
+constexpr Method KV_APPEND = {"append", 6, 2, {"k", "v", "seqs", "cu_tokens", "stream", "status"}, nullptr, do_kv_append, true};
 constexpr Method KV_READ = {"read", 5, 0, {"seqs", "cu_tokens", "n_tokens", "out", "stream"}, nullptr, do_kv_read};
 constexpr Method KV_ATTENTION = {"attention", 10, 1, {"q", "seqs", "cu_tokens", "max_tokens", "causal", "window", "scale", "max_len", "out", "stream"},
                                  nullptr, do_kv_attention};

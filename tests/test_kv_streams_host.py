@@ -73,7 +73,7 @@ s, t, cu, page_map = ints(0, 1, 2), ints(1, 1, 1), ints(0, 1, 2, 3), ints(0, 0, 
 CALLS = [  # name, arguments, of which tensors, how many results, whether there is memory that no result is
     ("extend", dict(seqs=s, counts=t), (s, t), 1, 0), ("fork", dict(src=s, dst=t), (s, t), 1, 0), ("free", dict(seqs=s), (s,), 0, 0),
     ("compact", dict(), (), 1, 1), ("compact", dict(page_map=page_map), (page_map,), 1, 0),
-    ("append", dict(k=x, v=x, seqs=s, cu_tokens=cu), (x, s, cu), 0, 0), ("read", dict(seqs=s, cu_tokens=cu, n_tokens=3), (s, cu), 2, 0),
+    ("append", dict(k=x, v=x, seqs=s, cu_tokens=cu, status=t), (x, s, cu, t), 0, 0), ("read", dict(seqs=s, cu_tokens=cu, n_tokens=3), (s, cu), 2, 0),
     ("attention", dict(q=x, seqs=s, cu_tokens=cu), (x, s, cu), 1, 1),
 ]
 
@@ -90,7 +90,7 @@ def test_memory_comes_from_the_stream_of_the_call(name, kw, tensors, results, hi
         assert (g.data_ptr(), a.current) in a.recorded
     for i in tensors + a.cache._kept:                          # the caller may let go of these at once
         assert (i.data_ptr(), a.side) in a.recorded
-    assert a.calls[-1][0] == "gbs_kv_" + name and a.side.cuda_stream in a.calls[-1][1]
+    assert a.calls[-1][0] == "gbs_kv_" + name + "_extended" * (name == "append") and a.side.cuda_stream in a.calls[-1][1]
 
 
 @pytest.mark.parametrize("name,kw,tensors,results,hidden", CALLS)
