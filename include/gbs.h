@@ -411,6 +411,7 @@ int gbs_kv_compact(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const gb
  *                     t * token_stride + h * head_stride, strides multiples of 8 (k and v have the same)
  *   n_tokens          rows that k and v hold; cu_tokens NULL: n_tokens = n_items
  * Where two items name one sequence, both write its last tokens, and either's bytes may stay.
+ * A row that holds a NaN gets a scale that is one: attention over it, and what is read back, are NaN.
  *
  * gbs_kv_append_extended writes the rows of those items alone that gbs_kv_extend has served, so that a step which is enqueued as a whole,
  * or captured, may run out of pages: rows of an item with status[i] != GBS_KV_DONE are left out.

@@ -247,6 +247,8 @@ __global__ __launch_bounds__(THREADS) void k_kv_append(const __grid_constant__ R
             m = max4(m);
             if (m < TINY) up = UP;
             scale = A.c_scale * m;
+            // every coordinate of a row with a NaN is one, and the maximum passes over them
+            if (y[r][0] != y[r][0]) scale = y[r][0];
             a1 = m > 0.f ? A.c_half / (m * up) : 0.f;
         }
         if (up != 1.f) {
