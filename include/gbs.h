@@ -453,7 +453,8 @@ int gbs_kv_read(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32
  * rows query coordinates, scales and the cached coordinates that they give are each rounded to 11 bits.  Probabilities are rounded to
  * 11 bits; sums and softmax statistics are fp32.  With more than 16 rows, a row more than 2^21 smaller than another of the same 32 tokens
  * (positions 32 i .. 32 i + 31) has fewer bits, and value rows more than 2^100 smaller than others that
- * the same row sees may lose their share of the softmax's sum.
+ * the same row sees may lose their share of the softmax's sum.  A token with a scale that is infinite or a NaN makes the rows that see
+ * it NaN.
  */
 int gbs_kv_attention_workspace(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, int n_heads, int64_t n_tokens, int max_tokens,
                                int64_t* bytes_out);

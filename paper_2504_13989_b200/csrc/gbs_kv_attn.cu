@@ -163,6 +163,9 @@ __device__ __forceinline__ void prepare(const gbs_kv_attn& A, const KvSeg& seg, 
     }
 }
 
+// An infinite scale becomes NaN: a score of -infinity is a masked one.
+__device__ __forceinline__ float no_inf(float x) { return fmaf(x, 0.f, x); }
+
 // the warps that compute
 __device__ __forceinline__ void meet() { asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory"); }
 
@@ -301,13 +304,14 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 if (ASYM) {
                     const float2 sa = *reinterpret_cast<const float2*>(X.ks + 8 * tg), sb = *reinterpret_cast<const float2*>(X.ks + 8 * (tg + 8));
                     const float2 ua = *reinterpret_cast<const float2*>(X.vs + 8 * tg), ub = *reinterpret_cast<const float2*>(X.vs + 8 * (tg + 8));
-                    z[0] = fmaf(f[0], sa.x * factor.x, sa.y * lift0);
-                    z[1] = fmaf(f[1], sa.x * factor.y, sa.y * lift1);
-                    z[2] = fmaf(f[2], sb.x * factor.x, sb.y * lift0);
-                    z[3] = fmaf(f[3], sb.x * factor.y, sb.y * lift1);
-                    va = ua.x; la = ua.y; vb = ub.x; lb = ub.y;
+                    const float ka = no_inf(fmaf(sa.y, 0.f, sa.x)), kb = no_inf(fmaf(sb.y, 0.f, sb.x));
+                    z[0] = fmaf(f[0], ka * factor.x, sa.y * lift0);
+                    z[1] = fmaf(f[1], ka * factor.y, sa.y * lift1);
+                    z[2] = fmaf(f[2], kb * factor.x, sb.y * lift0);
+                    z[3] = fmaf(f[3], kb * factor.y, sb.y * lift1);
+                    va = fmaf(ua.y, 0.f, ua.x); la = ua.y; vb = fmaf(ub.y, 0.f, ub.x); lb = ub.y;
                 } else {
-                    const float sa = *reinterpret_cast<const float*>(X.ks + 4 * tg), sb = *reinterpret_cast<const float*>(X.ks + 4 * (tg + 8));
+                    const float sa = no_inf(*reinterpret_cast<const float*>(X.ks + 4 * tg)), sb = no_inf(*reinterpret_cast<const float*>(X.ks + 4 * (tg + 8)));
                     va = *reinterpret_cast<const float*>(X.vs + 4 * tg);
                     vb = *reinterpret_cast<const float*>(X.vs + 4 * (tg + 8));
                     z[0] = f[0] * (sa * factor.x);

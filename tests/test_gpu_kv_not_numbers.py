@@ -56,3 +56,52 @@ def test_a_row_with_a_nan(count, which, asym):
             assert check_seen(cache, at, q, count, *refs[0]) > 0
             seen = check_seen(cache, at, q, count, *refs[1], window=176)
             assert count > 1 or (seen == 0) == (at == 20)
+
+
+@pytest.mark.parametrize("asym", [False, True])
+@pytest.mark.parametrize("count", [1, 3, 60, 150])
+def test_a_scale_that_is_no_number(count, asym):
+    """In the pool itself: Delta (and lo) of a key or a value, in a unit that every row sees whole and in ones that they see in part."""
+    gbs_build.build()
+    with Plan(128, 128, 1, 4, 128, 0.9, asymmetric=asym) as plan:
+        sf = 2 if asym else 1
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(count)
+        cache = filled(plan, [200], 2, 32, seed=2)
+        q = torch.randn((count, 4, 128), generator=gen, device=DEV).to(torch.bfloat16)
+        refs = [kv_util.attention(cache, q, [0], [0, count], few=2 * count <= 16, window=w) for w in (0, 176)]
+        for at in (20, 40, 199):
+            block = cache.pages[cache.page_table[0, at // 32].long()].view(2, -1)[1]
+            floats = block[32 * 128:].view(torch.float32)
+            for which in range(2):
+                for part in range(sf):
+                    i = (which * 32 + at % 32) * sf + part
+                    was = floats[i].clone()
+                    for bad in (NAN, INF, -INF):
+                        floats[i] = bad
+                        assert check_seen(cache, at, q, count, *refs[0]) > 0
+                        check_seen(cache, at, q, count, *refs[1], window=176)
+                    floats[i] = was
+
+
+@pytest.mark.parametrize("asym", [False, True])
+@pytest.mark.parametrize("count", [1, 40])
+def test_a_row_with_an_infinity(count, asym):
+    """Appended: its scale is infinite or a NaN, and the rows that see it are NaN."""
+    gbs_build.build()
+    with Plan(128, 128, 1, 4, 128, 0.9, asymmetric=asym) as plan:
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(count)
+        q = torch.randn((count, 4, 128), generator=gen, device=DEV).to(torch.bfloat16)
+        for which in range(2):
+            for at, where in ((20, (0,)), (70, (64,)), (199, (3, 77))):
+                cache = filled(plan, [200], 2, 32, seed=at)
+                x = [torch.randn((200, 2, 128), generator=gen, device=DEV).to(torch.bfloat16) for _ in range(2)]
+                cache.append(*x, ints(0), ints(0, 200))
+                ref = kv_util.attention(cache, q, [0], [0, count], few=2 * count <= 16)
+                for sign in (INF, -INF):
+                    for i in where:
+                        x[which][at, 1, i] = sign
+                    cache.append(*x, ints(0), ints(0, 200))
+                    assert not torch.isfinite(cache.read(ints(0), ints(0, 200), 200)[which][at, 1]).any()
+                    assert check_seen(cache, at, q, count, *ref) > 0
