@@ -31,7 +31,10 @@ namespace {
 
 constexpr int ROWS = 8, UNIT = 32;
 constexpr int WARPS = 4, THREADS = 32 * WARPS + 32;  // warps that compute, and the one that fetches
-constexpr int STAGES = 11;                           // unit i of a block's is worked on by warp i % WARPS, from stage i % STAGES
+constexpr int STAGES = 12;                           // unit i of a block's is worked on by warp i % WARPS, from stage i % STAGES
+// A stage is always the same warp's.  A wait for a phase goes by its parity, so it is one only for who has seen the phase before end; another warp, ahead
+// of the one whose copy is late, would read the stage at once.
+static_assert(STAGES % WARPS == 0, "a stage has one warp");
 constexpr int PART = KV_PART<ROWS>;
 static_assert(2 * WARPS == ROWS, "each warp finishes two rows");
 constexpr int BLOCKS_PER_SM = 3;
@@ -49,7 +52,6 @@ template <bool ASYM>
 struct Smem {
     Stage<ASYM> ring[STAGES];
     float part[WARPS][ROWS * 128];                   // 16-byte pieces c of each 64 bytes of rows 2 t, 2 t + 1 at c ^ t
-    float m[WARPS][ROWS], l[WARPS][ROWS], add[WARPS][ROWS], mw[WARPS][ROWS];
     // of two segments in turn: the rows' integers (upper and lower byte; of 8 coordinates the even ones first), their factors and sums, what
     // each row sees and what all of them see, the segment and the block's piece of it
     struct alignas(16) Query {
@@ -60,7 +62,10 @@ struct Smem {
         KvSeg seg;
         KvPiece piece;
         bool last;
+        // where the integers were, at the segment's end: the warps' maxima m, totals, sums of p lo, and maxima M
+        __device__ __forceinline__ float* stat(int which, int warp) { return reinterpret_cast<float*>(h) + (which * WARPS + warp) * ROWS; }
     } query[2];
+    static_assert(4 * WARPS * ROWS * sizeof(float) <= sizeof(Query::h), "room for the warps' statistics");
     unsigned long long full[STAGES], empty[STAGES], qfull[2], qempty[2];
     unsigned valid[STAGES];                          // bit h: tokens 16 h .. of the unit have a page
     KvSeg seg;                                       // the block's first segment
@@ -256,7 +261,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
     unsigned phase = 0;
     bool dead = false;
     for (int round = 0;; ++round) {
-        const auto& Q = S.query[round & 1];
+        auto& Q = S.query[round & 1];
         if (!dead && !mbar_wait_warp(&S.abort, &S.qfull[round & 1], (unsigned)(round / 2) & 1u, P.status, 64)) dead = true;
         unsigned qh[4][2], ql[4][2];
 #pragma unroll
@@ -418,13 +423,12 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
         const KvSeg seg = Q.seg;
         const KvPiece piece = Q.piece;
         const bool last = Q.last;
-        meet();                                              // the sums before these have been read
-        if (lane == 0) mbar_arrive(&S.qempty[round & 1]);
+        meet();                                              // the sums before these have been read, and the integers of this segment's rows
         if (g == 0) {
-            *reinterpret_cast<float2*>(&S.m[w][2 * t]) = make_float2(m0, m1);
-            *reinterpret_cast<float2*>(&S.l[w][2 * t]) = make_float2(l0, l1);
-            *reinterpret_cast<float2*>(&S.add[w][2 * t]) = make_float2(add0, add1);
-            *reinterpret_cast<float2*>(&S.mw[w][2 * t]) = make_float2(mw0, mw1);
+            *reinterpret_cast<float2*>(Q.stat(0, w) + 2 * t) = make_float2(m0, m1);
+            *reinterpret_cast<float2*>(Q.stat(1, w) + 2 * t) = make_float2(l0, l1);
+            *reinterpret_cast<float2*>(Q.stat(2, w) + 2 * t) = make_float2(add0, add1);
+            *reinterpret_cast<float2*>(Q.stat(3, w) + 2 * t) = make_float2(mw0, mw1);
         }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -440,17 +444,17 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             float top = NONE, top_w = NONE;
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) {
-                top = fmaxf(top, S.m[i][row]);
-                top_w = fmaxf(top_w, S.mw[i][row]);
+                top = fmaxf(top, Q.stat(0, i)[row]);
+                top_w = fmaxf(top_w, Q.stat(3, i)[row]);
             }
             float y[16], total = 0.f, extra = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) y[i] = 0.f;
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) {
-                const float keep = kv_ex2(S.m[i][row] - top), keep_w = kv_ex2(S.mw[i][row] - top_w);
-                total = fmaf(S.l[i][row], keep, total);
-                extra = fmaf(S.add[i][row], keep, extra);
+                const float keep = kv_ex2(Q.stat(0, i)[row] - top), keep_w = kv_ex2(Q.stat(3, i)[row] - top_w);
+                total = fmaf(Q.stat(1, i)[row], keep, total);
+                extra = fmaf(Q.stat(2, i)[row], keep, extra);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {            // coordinates 64 (q >> 1) + 8 l8 + 4 (q & 1) ..
                     const int at = 64 * (q >> 1) + 8 * l8 + 4 * (q & 1);
@@ -484,6 +488,8 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 if (threadIdx.x == 0 && piece.starts) P.joins[blockIdx.x] = kv_join(P.line, seg, places);
             }
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S.qempty[round & 1]);
         // a wait that ran out ends all of them together
         bool bad = false;
 #pragma unroll
