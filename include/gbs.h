@@ -464,6 +464,19 @@ int gbs_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const 
                      void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Self-test of what gbs_kv_attention does when one of its bounded waits runs out (a diagnostic, as gbs_selftest_wait_expiry): the same call,
+ * in which the waits of this code in every block's segment of this number (0, 1, ..) count as run out without being made.  The kernel ends, the code
+ * stands in the plan's status word, and rows of out may be any numbers; nothing else is written.  A block that has no such wait there
+ * ends as always.
+ *   code              61 .. 64: up to 16 rows a KV head and item (a unit's copies, a free stage, a free slot for query rows, the query rows)
+ */
+int gbs_selftest_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens,
+                              int n_items, int64_t n_tokens, int max_tokens, int max_len, const void* q, int64_t q_token_stride,
+                              int64_t q_head_stride, int n_heads, float scale, int window, int flags, void* out,
+                              int64_t out_token_stride, int64_t out_head_stride, void* workspace, int64_t workspace_bytes, int code,
+                              int segment, void* cuda_stream);
+
+/*
  * State of one projection's search (Algorithm 1), a handful of numbers: plain data that may be copied, stored
  * and handed back later to resume the search where it stopped (gbs_search_state_init gives the algorithm's
  * start a = 0, b = 1, m = 1/2).

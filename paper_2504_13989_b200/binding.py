@@ -40,7 +40,8 @@ EXPORTS = ("gbs_plan_create", "gbs_plan_create_ex", "gbs_plan_destroy", "gbs_pla
            "gbs_search_clip_ratio", "gbs_search_state_init", "gbs_search_clip_ratio_fn", "gbs_search_clip_ratio_batch",
            "gbs_hadamard_m", "gbs_status_string", "gbs_selftest_wait_expiry", "gbs_weight_rotate_quantize",
            "gbs_quantized_matmul", "gbs_kv_page_bytes", "gbs_kv_extend", "gbs_kv_fork", "gbs_kv_free", "gbs_kv_compact",
-           "gbs_kv_append", "gbs_kv_append_extended", "gbs_kv_read", "gbs_kv_attention_workspace", "gbs_kv_attention")
+           "gbs_kv_append", "gbs_kv_append_extended", "gbs_kv_read", "gbs_kv_attention_workspace", "gbs_kv_attention",
+           "gbs_selftest_kv_attention")
 GBS_STATIC_MAX_D_PAD = 4096
 
 
@@ -146,7 +147,8 @@ def lib() -> ctypes.CDLL:
         L.gbs_kv_attention_workspace.argtypes = [vp, kv, i32, i64, i32, ctypes.POINTER(i64)]
         L.gbs_kv_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, i32, vp, i64, i64,
                                        vp, i64, vp]
-        for name in EXPORTS[-10:]:
+        L.gbs_selftest_kv_attention.argtypes = L.gbs_kv_attention.argtypes[:-1] + [i32, i32, vp]
+        for name in EXPORTS[-11:]:
             getattr(L, name).restype = i32
         L.gbs_hadamard_m.argtypes = [i32, vp]
         L.gbs_hadamard_m.restype = i32

@@ -217,6 +217,7 @@ struct gbs_kv_attn {
     const void* q;
     void* out;
     long long q_token, q_head, out_token, out_head;
+    int lost_code, lost_segment;        // of the self-test: waits that count as run out (0: none)
 };
 // gbs_kv_attn.cu : up to GBS_KV_FEW_ROWS query rows of an item and KV head
 #define GBS_KV_FEW_ROWS 16

@@ -70,7 +70,6 @@ struct Smem {
     unsigned valid[STAGES];                          // bit h: tokens 16 h .. of the unit have a page
     KvSeg seg;                                       // the block's first segment
     long long share[WARPS + 1];
-    bool bad[WARPS];
     int abort;
 };
 
@@ -173,8 +172,16 @@ __device__ __forceinline__ float no_inf(float x) { return fmaf(x, 0.f, x); }
 
 // the warps that compute
 __device__ __forceinline__ void meet() { asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory"); }
+// The same, and whether any of their threads says so (a barrier of its own: one that is waited for in both ways has to be at rest between them).
+__device__ __forceinline__ bool meet_any(bool x)
+{
+    int any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbar.red.or.pred q, 2, %2, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any) : "r"((int)x), "n"(32 * WARPS) : "memory");
+    return any != 0;
+}
 
-template <bool ASYM>
+template <bool ASYM, bool TEST>
 __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __grid_constant__ KvAttnArgs P)
 {
     extern __shared__ __align__(128) unsigned char smem_raw[];
@@ -210,7 +217,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
         const int in_slot = piece < 2 ? KV_ROW : (ASYM ? 8 : 4);
         const int in_stage = (piece < 2 ? piece * UNIT * KV_ROW : 2 * UNIT * KV_ROW + (piece - 2) * Stage<ASYM>::SCALE) + half * (int)piece_bytes;
         bool dead = false, more = true;
-        int at = 0;                                          // units of the block so far
+        int at = 0, armed = 0;                               // units of the segments so far, and of all that have been sent for
         KvSeg seg = S.seg;
         for (int round = 0; more && !dead; ++round) {
             const KvPiece part = kv_piece(P.line, seg, places);
@@ -223,7 +230,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 const int u = at + i + mine, st = u % STAGES, use = u / STAGES;
                 const bool have = i + mine < part.n;
                 const int next_tok = tok + 4 * UNIT, next = copies && i + 4 + mine < part.n && next_tok < seg.e.hi ? row[next_tok >> ps_log] : -1;
-                if (have && use > 0 && !mbar_wait(&S.abort, &S.empty[st], (unsigned)(use - 1) & 1u, P.status, 62)) dead = true;
+                if (have && use > 0 && (kv_lost<TEST>(P, &S.abort, 62, round) || !mbar_wait(&S.abort, &S.empty[st], (unsigned)(use - 1) & 1u, P.status, 62))) dead = true;
                 if (__any_sync(0xffffffffu, dead)) { dead = true; break; }
                 const bool ok = have && (unsigned)page < (unsigned)A.c.n_pages;
                 const unsigned who = __ballot_sync(0xffffffffu, ok) >> (8 * mine), first = who & 1, second = (who >> 4) & 1;
@@ -235,11 +242,15 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 if (ok)
                     bulk_load(reinterpret_cast<unsigned char*>(&S.ring[st]) + in_stage,
                               A.c.pages + ((long long)page * A.c.page_bytes + off + (tok & ((1 << ps_log) - 1)) * in_slot), piece_bytes, &S.full[st]);
+                armed = at + max(min(i + 4, part.n), 0);
                 tok = next_tok;
                 page = next;
                 if (i > 0) continue;
                 // with the first units under way: the segment's query rows, eight lanes a row, rotated and made integers
-                if (round > 1 && !mbar_wait_warp(&S.abort, &S.qempty[round & 1], (unsigned)(round / 2 - 1) & 1u, P.status, 63)) { dead = true; break; }
+                if (round > 1 && (kv_lost<TEST>(P, &S.abort, 63, round) || !mbar_wait_warp(&S.abort, &S.qempty[round & 1], (unsigned)(round / 2 - 1) & 1u, P.status, 63))) {
+                    dead = true;
+                    break;
+                }
                 prepare<ASYM>(A, seg, S.query[round & 1], lane);
                 if (lane == 0) {
                     S.query[round & 1].seg = seg;
@@ -252,17 +263,17 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             at += max(part.n, 0);
             if (more) kv_next(A, P.line, seg);
         }
-        if (dead) drain_copies(S.full, STAGES, at);
+        drain_copies(S.full, STAGES, armed);                 // the others may have given up on copies that are still on their way
         return;
     }
 
     // ---- the segments ----
     int mine = w, st = w, done = 0;                          // this warp's next unit of the block's, and its stage; units of the segments before
     unsigned phase = 0;
-    bool dead = false;
     for (int round = 0;; ++round) {
         auto& Q = S.query[round & 1];
-        if (!dead && !mbar_wait_warp(&S.abort, &S.qfull[round & 1], (unsigned)(round / 2) & 1u, P.status, 64)) dead = true;
+        // a warp whose wait ran out goes on to where the warps meet, and there all of them leave: what Q holds then counts for nothing
+        bool dead = kv_lost<TEST>(P, &S.abort, 64, round) || !mbar_wait_warp(&S.abort, &S.qfull[round & 1], (unsigned)(round / 2) & 1u, P.status, 64);
         unsigned qh[4][2], ql[4][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -280,9 +291,12 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
         for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
         float m0 = NONE, m1 = NONE, mw0 = NONE, mw1 = NONE, up0 = 0.f, up1 = 0.f, l0 = 0.f, l1 = 0.f, add0 = 0.f, add1 = 0.f;     // up = 64 2^(m - M)
 
-        const int stop = done + max(Q.piece.n, 0), tok_at = ((Q.seg.e.lo >> 5) + Q.piece.skip - done) * UNIT;
+        const int stop = dead ? done : done + max(Q.piece.n, 0), tok_at = ((Q.seg.e.lo >> 5) + Q.piece.skip - done) * UNIT;
         for (; mine < stop; mine += WARPS) {
-            if (!dead && !mbar_wait_warp(&S.abort, &S.full[st], phase, P.status, 61)) dead = true;
+            if (kv_lost<TEST>(P, &S.abort, 61, round) || !mbar_wait_warp(&S.abort, &S.full[st], phase, P.status, 61)) {
+                dead = true;
+                break;
+            }
             const Stage<ASYM>& X = S.ring[st];
             const unsigned valid = S.valid[st];
             const int tok0 = tok_at + mine * UNIT;
@@ -436,8 +450,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
             *reinterpret_cast<float4*>(to) = make_float4(o[2 * c][0], o[2 * c][2], o[2 * c + 1][0], o[2 * c + 1][2]);
             *reinterpret_cast<float4*>(to + 128) = make_float4(o[2 * c][1], o[2 * c][3], o[2 * c + 1][1], o[2 * c + 1][3]);
         }
-        if (lane == 0) S.bad[w] = dead;
-        meet();
+        if (meet_any(dead)) break;
         // two rows a warp, eight lanes a row (the upper half of the warp does the same and writes nothing)
         if (piece.n > 0) {
             const int row = 2 * w + ((lane >> 3) & 1), l8 = lane & 7;
@@ -490,11 +503,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&S.qempty[round & 1]);
-        // a wait that ran out ends all of them together
-        bool bad = false;
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) bad |= S.bad[i];
-        if (last || bad) break;
+        if (last) break;
     }
 }
 
@@ -524,10 +533,11 @@ int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, 
     P.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + blocks * sizeof(KvJoin));
     P.status = p->d_status;
     const size_t smem = p->asym ? sizeof(Smem<true>) : sizeof(Smem<false>);
-    const void* f = p->asym ? (const void*)k_kv_attn_few<true> : (const void*)k_kv_attn_few<false>;
-    const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const auto f = A.lost_code ? (p->asym ? k_kv_attn_few<true, true> : k_kv_attn_few<false, true>)
+                               : (p->asym ? k_kv_attn_few<true, false> : k_kv_attn_few<false, false>);
+    const cudaError_t e = cudaFuncSetAttribute((const void*)f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return (int)e;
-    const int rc = gbs_kv_launch(p, p->asym ? k_kv_attn_few<true> : k_kv_attn_few<false>, dim3((unsigned)blocks), THREADS, smem, stream, P);
+    const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
     if (rc != 0 || P.line.pad < 0) return rc;
     return gbs_kv_launch(p, k_kv_attn_join<ROWS>, dim3((unsigned)blocks), 256, 0, stream, P);
 }

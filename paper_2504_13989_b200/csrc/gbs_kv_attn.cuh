@@ -22,6 +22,16 @@ struct KvAttnArgs {
     int* status;
 };
 
+// Whether a wait counts as one that ran out: in the self-test's instances, those with the given code in a block's segment of the given number.
+template <bool TEST>
+__device__ __forceinline__ bool kv_lost(const KvAttnArgs& P, volatile int* abort_flag, int code, int segment)
+{
+    if (!TEST || code != P.a.lost_code || segment != P.a.lost_segment) return false;
+    *abort_flag = 1;
+    atomicCAS(P.status, 0, code);
+    return true;
+}
+
 __device__ __forceinline__ unsigned as_u(__half2 x) { return *reinterpret_cast<unsigned*>(&x); }
 __device__ __forceinline__ __half2 as_h(unsigned x) { return *reinterpret_cast<__half2*>(&x); }
 

@@ -207,10 +207,12 @@ extern "C" int gbs_kv_attention_workspace(const gbs_plan_t* p, const gbs_kv_cach
     return GBS_OK;
 }
 
-extern "C" int gbs_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
-                                int64_t n_tokens, int max_tokens, int max_len, const void* q, int64_t q_token_stride, int64_t q_head_stride,
-                                int n_heads, float scale, int window, int flags, void* out, int64_t out_token_stride,
-                                int64_t out_head_stride, void* workspace, int64_t workspace_bytes, void* stream)
+namespace {
+
+// code, segment: of the waits that count as run out in the self-test (0: none)
+int attention(const gbs_plan* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items, int64_t n_tokens, int max_tokens,
+              int max_len, const void* q, int64_t q_token_stride, int64_t q_head_stride, int n_heads, float scale, int window, int flags, void* out,
+              int64_t out_token_stride, int64_t out_head_stride, void* workspace, int64_t workspace_bytes, int code, int segment, void* stream)
 {
     gbs_kv_attn A = {};
     bool empty = false;
@@ -227,6 +229,8 @@ extern "C" int gbs_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache
     if (rc != GBS_OK) return rc;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16)) return GBS_ERR_ALIGNMENT;
     if (q == out) return GBS_ERR_INVALID_ARG;                        // rows are read after others have been written
+    A.lost_code = code;
+    A.lost_segment = segment;
     A.seqs = seqs;
     A.cu = cu_tokens;
     A.n_items = n_items;
@@ -250,4 +254,25 @@ extern "C" int gbs_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache
         return few_rows(A.group, max_tokens) ? gbs_kv_few_launch(p, A, workspace, static_cast<cudaStream_t>(stream))
                                              : gbs_tc_kvattn_launch(p, A, workspace, static_cast<cudaStream_t>(stream));
     });
+}
+
+}  // namespace
+
+extern "C" int gbs_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                                int64_t n_tokens, int max_tokens, int max_len, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                                int n_heads, float scale, int window, int flags, void* out, int64_t out_token_stride,
+                                int64_t out_head_stride, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    return attention(p, cache, seqs, cu_tokens, n_items, n_tokens, max_tokens, max_len, q, q_token_stride, q_head_stride, n_heads,
+                     scale, window, flags, out, out_token_stride, out_head_stride, workspace, workspace_bytes, 0, 0, stream);
+}
+
+extern "C" int gbs_selftest_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                                         int64_t n_tokens, int max_tokens, int max_len, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                                         int n_heads, float scale, int window, int flags, void* out, int64_t out_token_stride,
+                                         int64_t out_head_stride, void* workspace, int64_t workspace_bytes, int code, int segment, void* stream)
+{
+    if (code < 61 || code > 64 || segment < 0) return GBS_ERR_INVALID_ARG;
+    return attention(p, cache, seqs, cu_tokens, n_items, n_tokens, max_tokens, max_len, q, q_token_stride, q_head_stride, n_heads,
+                     scale, window, flags, out, out_token_stride, out_head_stride, workspace, workspace_bytes, code, segment, stream);
 }

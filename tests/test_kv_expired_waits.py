@@ -1,0 +1,92 @@
+"""What attention over the paged KV cache does when one of its bounded waits runs out: the kernel ends, the code stands in the plan's status word, and
+nothing is written but rows of the result and the workspace.  gbs_selftest_kv_attention makes the waits run out; nothing faults or hangs."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import kv_norms
+from kv_util import DEV, filled
+from paper_2504_13989_b200 import Plan, binding
+from paper_2504_13989_b200 import build as gbs_build
+from test_kv_host import INVALID, OK, P, plan, pool
+
+GUARD = 1 << 20
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    gbs_build.build()
+
+
+def test_refusals():
+    lib, c = binding.lib(), pool()
+
+    def f(code, segment, n=2, flags=1, q=P):
+        return lib.gbs_selftest_kv_attention(plan(), ctypes.byref(c), P, P, n, 3, 2, 0, q, 1024, 128, 8, 0.0, 0, flags, P + 4096, 1024, 128, P, 1 << 40, code, segment, None)
+    for code in (0, 1, -1, 60, 65, 1 << 20):
+        assert f(code, 0) == INVALID
+    assert f(61, -1) == INVALID and f(61, 0, flags=2) == INVALID and f(61, 0, q=None) == INVALID and f(64, 3, n=0) == OK
+
+
+class Call:
+    """One call on a pool of many sequences, its result and workspace between guards."""
+
+    def __init__(self, lengths, counts, heads, kv_heads, max_len, asym):
+        self.plan = Plan(128, 128, 1, 4, 128, 0.9, asymmetric=asym)
+        self.cache = filled(self.plan, lengths, kv_heads, 32, seed=1)
+        self.counts, self.heads, self.max_len = counts, heads, max_len
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(2)
+        n = sum(counts)
+        self.q = torch.randn((n, heads, 128), generator=gen, device=DEV).to(torch.bfloat16)
+        self.cu = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device=DEV)
+        self.out = torch.full((2 * GUARD + n * heads * 128,), 7.0, dtype=torch.bfloat16, device=DEV)
+        need = ctypes.c_int64(0)
+        args = self.plan.handle, ctypes.byref(self.cache._c), heads, n, max(counts)
+        assert binding.lib().gbs_kv_attention_workspace(*args, ctypes.byref(need)) == OK
+        self.need = need.value
+        self.work = torch.full((2 * GUARD + (self.need + 15) // 16 * 16,), 77, dtype=torch.uint8, device=DEV)
+        self.kept = [t.clone() for t in self.cache._kept + (self.q, self.cu)]
+
+    def run(self, code=None, segment=0):
+        h = self.heads
+        args = [self.plan.handle, ctypes.byref(self.cache._c), None, self.cu.data_ptr(), len(self.counts), sum(self.counts), max(self.counts), self.max_len,
+                self.q.data_ptr(), 128 * h, 128, h, 0.0, 0, 1, self.out.data_ptr() + 2 * GUARD, 128 * h, 128, self.work.data_ptr() + GUARD, self.need]
+        if code is None:
+            assert binding.lib().gbs_kv_attention(*args, None) == OK
+        else:
+            assert binding.lib().gbs_selftest_kv_attention(*args, code, segment, None) == OK
+        torch.cuda.synchronize()
+        inner = self.out[GUARD:-GUARD].clone()
+        self.out[GUARD:-GUARD] = 7.0
+        assert bool((self.out == 7.0).all())
+        assert bool((self.work[:GUARD] == 77).all()) and bool((self.work[GUARD + self.need:] == 77).all())
+        same = zip((t.view(torch.uint8) for t in self.cache._kept + (self.q, self.cu)), (t.view(torch.uint8) for t in self.kept))
+        assert all(torch.equal(a, b) for a, b in same)
+        return inner.view(-1, h, 128)
+
+
+FEW = [([70] * 900 + [500, 3], 2, 512), ([3000, 70, 20000] * 60, 2, 0), ([1200] * 40, 4, 0)]     # undivided, divided, few long segments
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("asym", [False, True])
+@pytest.mark.parametrize("lengths,heads,max_len", FEW)
+@pytest.mark.parametrize("code", [61, 62, 63, 64])
+def test_few_rows(code, lengths, heads, max_len, asym):
+    c = Call(lengths, [1] * len(lengths), heads, 2, max_len, asym)
+    right = c.run()
+    kv_norms.check(c.cache, right, c.q, range(len(lengths)), c.counts)
+    assert c.plan.device_status() == 0
+    seen = []
+    for segment in range(4):
+        c.run(code, segment)
+        seen.append(c.plan.device_status())
+        assert seen[-1] in (0, code)                           # 0: no block makes such a wait there
+        again = c.run()
+        assert torch.equal(again, right)                       # the next call is as always
+    # reading the word clears it; a free slot and a free stage are waited for where a block has three segments, or twelve units
+    assert code in seen or (code in (62, 63) and len(lengths) < 100)
+    c.plan.close()
