@@ -468,7 +468,8 @@ int gbs_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const 
  * in which the waits of this code in every block's segment of this number (0, 1, ..) count as run out without being made.  The kernel ends, the code
  * stands in the plan's status word, and rows of out may be any numbers; nothing else is written.  A block that has no such wait there
  * ends as always.
- *   code              61 .. 64: up to 16 rows a KV head and item (a unit's copies, a free stage, a free slot for query rows, the query rows)
+ *   code              61 .. 64: up to 16 rows a KV head and item (a unit's copies, a free stage, a free slot for query rows, the query rows);
+ *                     71 .. 77: more rows (keys, values, weights, room for keys, room for values, scores, the results)
  */
 int gbs_selftest_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens,
                               int n_items, int64_t n_tokens, int max_tokens, int max_len, const void* q, int64_t q_token_stride,

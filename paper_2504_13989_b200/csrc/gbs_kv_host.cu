@@ -272,7 +272,7 @@ extern "C" int gbs_selftest_kv_attention(const gbs_plan_t* p, const gbs_kv_cache
                                          int n_heads, float scale, int window, int flags, void* out, int64_t out_token_stride,
                                          int64_t out_head_stride, void* workspace, int64_t workspace_bytes, int code, int segment, void* stream)
 {
-    if (code < 61 || code > 64 || segment < 0) return GBS_ERR_INVALID_ARG;
+    if (!((code >= 61 && code <= 64) || (code >= 71 && code <= 77)) || segment < 0) return GBS_ERR_INVALID_ARG;
     return attention(p, cache, seqs, cu_tokens, n_items, n_tokens, max_tokens, max_len, q, q_token_stride, q_head_stride, n_heads,
                      scale, window, flags, out, out_token_stride, out_head_stride, workspace, workspace_bytes, code, segment, stream);
 }

@@ -56,6 +56,14 @@ struct Is { static constexpr int value = N; };
 __device__ __forceinline__ unsigned uniform(unsigned x) { return __shfl_sync(0xffffffffu, x, 0); }
 // the block's warps meet, wherever in the code they are
 __device__ __forceinline__ void meet_all() { asm volatile("bar.sync 0, %0;" ::"n"(THREADS) : "memory"); }
+// The same, and whether any of their threads says so: all of them leave, or none.  (The flag of the waits may be raised between two reads of it.)
+__device__ __forceinline__ bool meet_any(bool x)
+{
+    int any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbar.red.or.pred q, 1, %2, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any) : "r"((int)x), "n"(THREADS) : "memory");
+    return any != 0;
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st32(unsigned taddr, const unsigned r[32])
 {
@@ -127,7 +135,7 @@ __device__ __forceinline__ void shrink(unsigned scores, unsigned sums, float kee
     }
 }
 
-template <bool ASYM>
+template <bool ASYM, bool TEST>
 __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant__ KvAttnArgs P)
 {
     extern __shared__ unsigned char smem_raw[];
@@ -236,7 +244,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 const unsigned now = it + i;
                 const int nb = now & 3, tok = tok0 + i * UNIT;
                 const bool plain = tok >= all_lo && tok + UNIT <= all_hi;
-                if (!(ok = mbar_wait_warp(&S.abort, &S.sfull[t], (t == 0 ? now : phase_b + i) & 1u, P.status, 76))) break;
+                if (!(ok = !kv_lost<TEST>(P, &S.abort, 76, round) && mbar_wait_warp(&S.abort, &S.sfull[t], (t == 0 ? now : phase_b + i) & 1u, P.status, 76))) break;
                 tc_fence_after();
 #pragma unroll 1
                 for (int c = 0; c < 2; ++c) {                // 64 tokens at a time
@@ -297,7 +305,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 if (lane == 0) mbar_arrive(&S.pfull[t]);
             }
             // ---- the rows' sums, by way of shared memory ----
-            if (ok && (t == 0 || two) && mbar_wait_warp(&S.abort, &S.ofull, round & 1u, P.status, 77)) {
+            if (ok && (t == 0 || two) && (ok = !kv_lost<TEST>(P, &S.abort, 77, round) && mbar_wait_warp(&S.abort, &S.ofull, round & 1u, P.status, 77))) {
                 tc_fence_after();
                 unsigned char* to = t == 0 ? S.k[0] : S.v[0];
 #pragma unroll 1
@@ -315,9 +323,8 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 S.m[row] = M;
             }
             tc_fence_before();
-            meet_all();
+            if (meet_any(!ok)) break;
             tc_fence_after();
-            if (S.abort) break;
             float* parts = P.parts + ((long long)blockIdx.x * 2 + (piece.starts ? 1 : 0)) * PART;
 #pragma unroll 1
             for (int q0 = 0; q0 < (two ? ROWS : TILE); q0 += 32) {
@@ -389,7 +396,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             for (int i = 0; i < n; ++i) {
                 const unsigned now = it + i, use = now >> 1;
                 const int b = now & 1, nb = now & 3;
-                if (now > 1 && !(ok = mbar_wait_warp(&S.abort, &S.kfree[b], (use + 1) & 1u, P.status, 74))) break;
+                if (now > 1 && !(ok = !kv_lost<TEST>(P, &S.abort, 74, round) && mbar_wait_warp(&S.abort, &S.kfree[b], (use + 1) & 1u, P.status, 74))) break;
                 // tokens that are not there become 0, those whose scales are no numbers NaN keys: the scores of rows that see them are none
                 const bool wrong = !(fabsf(ks) + fabsf(vs) + fabsf(kl) + fabsf(vl) < INFINITY);
                 if (!there || wrong) ks = kl = vs = vl = 0.f;
@@ -405,7 +412,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&S.kfull[b]);
-                if (now > 1 && !(ok = mbar_wait_warp(&S.abort, &S.vfree[b], (use + 1) & 1u, P.status, 75))) break;
+                if (now > 1 && !(ok = !kv_lost<TEST>(P, &S.abort, 75, round) && mbar_wait_warp(&S.abort, &S.vfree[b], (use + 1) & 1u, P.status, 75))) break;
                 store_codes<ASYM>(S.v[b], me, v, __float2half2_rn(vs * up_v), __float2half2_rn(vm * up_v));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -417,8 +424,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                     load();
                 }
             }
-            meet_all();                                 // the sums are there
-            if (S.abort) break;
+            if (meet_any(!ok)) break;                   // the sums are there
         } else {
             // ---- MMAs: weights times values of a unit, then the next one's scores, for one tile and the other in turn ----
             // Everything that an MMA takes is made uniform, and what changes between them is known when this is compiled: see umma_f16.
@@ -461,15 +467,15 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 constexpr int t = decltype(tile)::value;
                 const unsigned now = at0 + i, next = now + 1;
                 if (i >= 0) {
-                    if (t == 0 && !mbar_wait_warp(&S.abort, &S.vfull[now & 1], (now >> 1) & 1u, P.status, 72)) return false;
-                    if (!mbar_wait_warp(&S.abort, &S.pfull[t], (t == 0 ? now : at0_b + i) & 1u, P.status, 73)) return false;
+                    if (t == 0 && (kv_lost<TEST>(P, &S.abort, 72, round) || !mbar_wait_warp(&S.abort, &S.vfull[now & 1], (now >> 1) & 1u, P.status, 72))) return false;
+                    if (kv_lost<TEST>(P, &S.abort, 73, round) || !mbar_wait_warp(&S.abort, &S.pfull[t], (t == 0 ? now : at0_b + i) & 1u, P.status, 73)) return false;
                     tc_fence_after();
                     values(tile, adds, now & 1);
                     if (t + 1 == tiles) umma_commit(&S.vfree[now & 1]);
                 }
                 if (i + 1 < units) {
                     if (t == 0) {
-                        if (!mbar_wait_warp(&S.abort, &S.kfull[next & 1], (next >> 1) & 1u, P.status, 71)) return false;
+                        if (kv_lost<TEST>(P, &S.abort, 71, round) || !mbar_wait_warp(&S.abort, &S.kfull[next & 1], (next >> 1) & 1u, P.status, 71)) return false;
                         tc_fence_after();
                     }
                     scores(tile, next & 1);
@@ -491,8 +497,10 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 kv_next(A, P.line, next);
                 S.seg[(round + 1) & 1] = next;
             }
-            meet_all();
-            if (S.abort) break;
+            if (meet_any(!ok)) {
+                if (ok) drain_copies(&S.ofull, 1, (int)round + 1);       // the products are given time to end, as above
+                break;
+            }
         }
         it += n;
         more = kv_more(P.line, seg, places);
@@ -530,10 +538,11 @@ int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspac
     P.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + blocks * sizeof(KvJoin));
     P.status = p->d_status;
     const size_t smem = sizeof(Smem) + 1024;
-    const void* f = p->asym ? (const void*)k_tc_kvattn<true> : (const void*)k_tc_kvattn<false>;
-    const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const auto f = A.lost_code ? (p->asym ? k_tc_kvattn<true, true> : k_tc_kvattn<false, true>)
+                               : (p->asym ? k_tc_kvattn<true, false> : k_tc_kvattn<false, false>);
+    const cudaError_t e = cudaFuncSetAttribute((const void*)f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return (int)e;
-    const int rc = gbs_kv_launch(p, p->asym ? k_tc_kvattn<true> : k_tc_kvattn<false>, dim3((unsigned)blocks), THREADS, smem, stream, P);
+    const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
     if (rc != 0) return rc;
     return gbs_kv_launch(p, k_kv_attn_join<ROWS>, dim3((unsigned)blocks, ROWS / 8), 256, 0, stream, P);
 }

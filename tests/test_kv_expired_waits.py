@@ -25,7 +25,7 @@ def test_refusals():
 
     def f(code, segment, n=2, flags=1, q=P):
         return lib.gbs_selftest_kv_attention(plan(), ctypes.byref(c), P, P, n, 3, 2, 0, q, 1024, 128, 8, 0.0, 0, flags, P + 4096, 1024, 128, P, 1 << 40, code, segment, None)
-    for code in (0, 1, -1, 60, 65, 1 << 20):
+    for code in (0, 1, -1, 60, 65, 70, 78, 1 << 20):
         assert f(code, 0) == INVALID
     assert f(61, -1) == INVALID and f(61, 0, flags=2) == INVALID and f(61, 0, q=None) == INVALID and f(64, 3, n=0) == OK
 
@@ -76,9 +76,23 @@ FEW = [([70] * 900 + [500, 3], 2, 512), ([3000, 70, 20000] * 60, 2, 0), ([1200] 
 @pytest.mark.parametrize("lengths,heads,max_len", FEW)
 @pytest.mark.parametrize("code", [61, 62, 63, 64])
 def test_few_rows(code, lengths, heads, max_len, asym):
-    c = Call(lengths, [1] * len(lengths), heads, 2, max_len, asym)
+    check_expiry(Call(lengths, [1] * len(lengths), heads, 2, max_len, asym), code, code in (62, 63) and len(lengths) < 100)
+
+
+MANY = [([300] * 400, [100] * 400, 4), ([5000, 300, 9000] * 20, [150, 60, 40] * 20, 2), ([2000] * 4, [2000] * 4, 4)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("asym", [False, True])
+@pytest.mark.parametrize("lengths,counts,heads", MANY)
+@pytest.mark.parametrize("code", [71, 72, 73, 74, 75, 76, 77])
+def test_many_rows(code, lengths, counts, heads, asym):
+    check_expiry(Call(lengths, counts, heads, 2, 0, asym), code, False)
+
+
+def check_expiry(c, code, may_not_occur):
     right = c.run()
-    kv_norms.check(c.cache, right, c.q, range(len(lengths)), c.counts)
+    kv_norms.check(c.cache, right, c.q, range(len(c.counts)), c.counts)
     assert c.plan.device_status() == 0
     seen = []
     for segment in range(4):
@@ -87,6 +101,6 @@ def test_few_rows(code, lengths, heads, max_len, asym):
         assert seen[-1] in (0, code)                           # 0: no block makes such a wait there
         again = c.run()
         assert torch.equal(again, right)                       # the next call is as always
-    # reading the word clears it; a free slot and a free stage are waited for where a block has three segments, or twelve units
-    assert code in seen or (code in (62, 63) and len(lengths) < 100)
+    # reading the word clears it; a free slot and a free stage are waited for where a block has three segments, or more units than stages
+    assert code in seen or may_not_occur
     c.plan.close()
