@@ -444,8 +444,8 @@ int gbs_kv_read(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32
  *   max_tokens        no item has more tokens (1 where cu_tokens is NULL); what is beyond it is left as it is.  It chooses the
  *                     kernel and bounds what is looked through for work, so the closer the better.
  *                     n_items * max_tokens * query heads of a KV head: at most 2^28
- *   max_len           no sequence of the call is longer (0: the table's width); one that is longer is read up to max_len only.
- *                     It bounds how far the work is split, not what is read.
+ *   max_len           about how long the longest sequence of the call is at most (0: the table's width).  It chooses how far the work is
+ *                     split, never what is read: a longer sequence is read whole, if more slowly.
  *   scale             0: 1 / sqrt(d)
  *   workspace         device, gbs_kv_attention_workspace bytes, 16-byte aligned; overwritten, needs no preparation, and one call at
  *                     a time may use it

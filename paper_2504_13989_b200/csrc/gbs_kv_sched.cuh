@@ -65,7 +65,7 @@ __device__ __forceinline__ KvEntry kv_entry(const gbs_kv_attn& A, const KvLine& 
     e.before = e.length = e.lo = e.hi = e.units = 0;
     if (e.row0 >= e.rows) return e;
     e.before = length - count;
-    e.length = min(length, A.max_len);
+    e.length = length;
     const int last = min(e.rows, e.row0 + L.tile_rows) - 1;
     e.hi = kv_row_hi(A, e, A.by_group(last));
     e.lo = kv_row_lo(A, e, A.by_group(e.row0));
