@@ -342,15 +342,24 @@ __global__ __launch_bounds__(COPY) void k_kv_move(const __grid_constant__ Compac
     }
 }
 
+constexpr unsigned table_mask(unsigned n_items)
+{
+    unsigned mask = 63;
+    while (mask + 1 < 2 * n_items) mask = 2 * mask + 1;
+    return mask;
+}
+constexpr size_t table_bytes(unsigned n_items) { return (2 * ((size_t)table_mask(n_items) + 1) + 3 * (size_t)n_items) * sizeof(int); }
+static_assert(table_bytes(GBS_KV_MAX_ITEMS) + 1024 <= 227 * 1024, "one block's shared memory");
+
 int allocate(const gbs_plan* p, bool fork, const AllocArgs& A0, cudaStream_t stream)
 {
     AllocArgs A = A0;
-    A.mask = 63;
-    while (A.mask + 1 < 2u * (unsigned)A.n_items) A.mask = 2 * A.mask + 1;
-    const size_t smem = (2 * ((size_t)A.mask + 1) + 3 * (size_t)A.n_items) * sizeof(int);
+    A.mask = table_mask((unsigned)A.n_items);
+    const size_t smem = table_bytes((unsigned)A.n_items);
     const void* f = fork ? (const void*)k_kv_allocate<true> : (const void*)k_kv_allocate<false>;
     if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        // the limit is the function's, for all threads of the process: always the same one, since a smaller call's may come between another's and its launch
+        const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)table_bytes(GBS_KV_MAX_ITEMS));
         if (e != cudaSuccess) return (int)e;
     }
     return gbs_kv_launch(p, fork ? k_kv_allocate<true> : k_kv_allocate<false>, dim3(1), ONE, smem, stream, A);
