@@ -1,7 +1,7 @@
 // Attention over the paged KV cache for few query rows (gbs_kv_attention: decoding).
 //
-// With khat = Delta c (+ lo) in the rotated basis, scores are Delta_k (H q . c) (+ lo sum H q) and the result is H sum_j (p_j Delta_v) c_j
-// (+ sum_j p_j lo_j): the codes go into the matrix unit as they are, exactly, and the rotation is applied to eight query rows and
+// With khat = Delta c (+ lo) in the rotated basis, scores are Delta_k (H q . c) (+ lo sum H q) and the result is H sum_j (p_j Delta_v) c_j, or
+// H (sum_j (p_j Delta_v) (c_j - 8) + sum_j p_j mid_j) with mid = lo + 8 Delta: the codes go into the matrix unit as they are, exactly, and the rotation is applied to eight query rows and
 // eight results instead of to every cached row.
 //
 // What bounds it is the cache, 136 or 144 bytes a token and KV head, read once, and next to it the conversion of 256 codes a token.
@@ -62,7 +62,7 @@ struct Smem {
         KvSeg seg;
         KvPiece piece;
         bool last;
-        // where the integers were, at the segment's end: the warps' maxima m, totals, sums of p lo, and maxima M
+        // where the integers were, at the segment's end: the warps' maxima m, totals, sums of p mid, and maxima M
         __device__ __forceinline__ float* stat(int which, int warp) { return reinterpret_cast<float*>(h) + (which * WARPS + warp) * ROWS; }
     } query[2];
     static_assert(4 * WARPS * ROWS * sizeof(float) <= sizeof(Query::h), "room for the warps' statistics");
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 float f[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) f[i] = (float)(256 * s[i] + r[i]);
-                float va, vb, la = 0.f, lb = 0.f, z[4];  // (token, row 2 t), (token, row 2 t + 1), (token + 8, the same)
+                float va, vb, la = 0.f, lb = 0.f, z[4];  // Delta and mid; (token, row 2 t), (token, row 2 t + 1), (token + 8, the same)
                 if (ASYM) {
                     const float2 sa = *reinterpret_cast<const float2*>(X.ks + 8 * tg), sb = *reinterpret_cast<const float2*>(X.ks + 8 * (tg + 8));
                     const float2 ua = *reinterpret_cast<const float2*>(X.vs + 8 * tg), ub = *reinterpret_cast<const float2*>(X.vs + 8 * (tg + 8));
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                     z[1] = fmaf(f[1], ka * factor.y, sa.y * lift1);
                     z[2] = fmaf(f[2], kb * factor.x, sb.y * lift0);
                     z[3] = fmaf(f[3], kb * factor.y, sb.y * lift1);
-                    va = fmaf(ua.y, 0.f, ua.x); la = ua.y; vb = fmaf(ub.y, 0.f, ub.x); lb = ub.y;
+                    va = fmaf(ua.y, 0.f, ua.x); la = fmaf(8.f, ua.x, ua.y); vb = fmaf(ub.y, 0.f, ub.x); lb = fmaf(8.f, ub.x, ub.y);
                 } else {
                     const float sa = no_inf(*reinterpret_cast<const float*>(X.ks + 4 * tg)), sb = no_inf(*reinterpret_cast<const float*>(X.ks + 4 * (tg + 8)));
                     va = *reinterpret_cast<const float*>(X.vs + 4 * tg);

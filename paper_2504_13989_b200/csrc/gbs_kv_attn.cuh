@@ -10,7 +10,7 @@ namespace {
 constexpr float NONE = -1e30f;                       // maximum of no scores
 constexpr float W_UP = 64.f;                         // weights are kept at 64 times their size relative to the largest
 
-// floats of a partial result: sums of w c, then for each row m, the total, the sum of p lo, and M
+// floats of a partial result: sums of w c, then for each row m, the total, the sum of p mid, and M
 template <int ROWS>
 constexpr int KV_PART = ROWS * 128 + 4 * ROWS;
 
@@ -49,12 +49,14 @@ __device__ __forceinline__ unsigned kv_and_xor(unsigned x, unsigned mask, unsign
     asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(y) : "r"(x), "r"(mask), "r"(with));
     return y;
 }
-// Nibbles (i, i + 4) of a word, i = 0 .. 3, as pairs in fp16.  A symmetric code c is taken as c ^ 8 = c + 8 of four bits.
+// Nibbles (i, i + 4) of a word, i = 0 .. 3, as pairs in fp16, -8 .. 7.  A symmetric code c is taken as c ^ 8 = c + 8 of four bits, an asymmetric one counts
+// from the middle of its range, 8: sums of products with codes that are all positive would be large next to what is left of them once lo is added,
+// and the matrix unit drops what lies below their last bit (2 x 130000 tokens in one block: a tenth of the result, with codes from 0).
 template <bool ASYM>
 __device__ __forceinline__ void kv_codes_f16(unsigned w, unsigned out[4])
 {
     constexpr unsigned LOW = ASYM ? 0x64006400u : 0x64086408u, HIGH = ASYM ? 0x64006400u : 0x64806480u;
-    const __half2 off = __float2half2_rn(ASYM ? 1024.f : 1032.f), off16 = __float2half2_rn(ASYM ? -64.f : -72.f), by = __float2half2_rn(0.0625f);
+    const __half2 off = __float2half2_rn(1032.f), off16 = __float2half2_rn(-72.f), by = __float2half2_rn(0.0625f);
     const unsigned w8 = w >> 8;
     out[0] = as_u(__hsub2(as_h(kv_and_xor(w, 0x000f000fu, LOW)), off));
     out[1] = as_u(__hfma2(as_h(kv_and_xor(w, 0x00f000f0u, HIGH)), by, off16));
@@ -62,7 +64,7 @@ __device__ __forceinline__ void kv_codes_f16(unsigned w, unsigned out[4])
     out[3] = as_u(__hfma2(as_h(kv_and_xor(w8, 0x00f000f0u, HIGH)), by, off16));
 }
 
-// sums of w c, of p and of p lo -> the result: sum / 64 2^(M - m) / total + extra / total, turned back
+// sums of w c, of p and of p mid -> the result: sum / 64 2^(M - m) / total + extra / total, turned back
 __device__ __forceinline__ void kv_finish(float y[16], int l8, float top, float top_w, float total, float extra)
 {
     const float by = total == 0.f ? 0.f : 1.f / total;

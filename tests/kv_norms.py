@@ -4,11 +4,11 @@ kv_util.attention bounds every element by the worst case, in which all roundings
 result itself.  Here roundings count as what they are, independent of one another: a number that is rounded to a type with half steps u (relative to it) is
 off by at most u and by u / sqrt(3) in the root mean square, so the result's error, a sum of such, has the variance
 
-    V = sum_j p_j^2 [ (W^2 / 3) |v_j|^2 + S_j^2 |v_j - o|^2 + R_j ]
+    V = sum_j p_j^2 [ (W^2 / 3) |u_j|^2 + S_j^2 |v_j - o|^2 + R_j ]
 
-with W = 2^-11 the half step of a weight, S_j the deviation of token j's score and R_j that of its value row:
-  few rows (up to 16)   a query coordinate is rounded to 1 / 65024 of the row's largest, m: S_j^2 = scale^2 (m / 65024)^2 / 3 |k_j|^2, R_j = 0;
-  many rows             query coordinates, Delta, the middle mid = lo + 8 Delta (0 for a symmetric plan) and the coordinates that they give are fp16:
+with W = 2^-11 the half step of a weight, u_j what it multiplies, S_j the deviation of token j's score and R_j that of its value row:
+  few rows (up to 16)   u = v - mid (the middle, mid = lo + 8 Delta, 0 for a symmetric plan, is weighted in 32 bits); a query coordinate is rounded to 1 / 65024 of the row's largest, m: S_j^2 = scale^2 (m / 65024)^2 / 3 |k_j|^2, R_j = 0;
+  many rows             u = v; query coordinates, Delta, mid and the coordinates that they give are fp16:
                         S_j^2 = scale^2 W^2 / 3 (2 sum_i q_i^2 k_i^2 + (q . (k - mid))^2 + (q . mid)^2), R_j = W^2 / 3 (|v|^2 + |v - mid|^2 + 128 mid^2).
 Sums in 24 bits and ex2 add 2^-20 of sums of absolute values.  The norm of such an error stays within six deviations (a sum of bounded independent terms is
 past them with a probability of 2 e^-18), and bf16 rounds the result by at most 2^-8 of itself:
@@ -34,14 +34,14 @@ def attend(x, k, km, v, vm, seen, scale, few):
     apart = (v2 - 2 * torch.einsum("qhgd,hkd->qhgk", o, v) + o.square().sum(-1, keepdim=True)).clamp(min=0)
     if few:
         dev = (scale / 65024) ** 2 / 3 * x.abs().amax(-1, keepdim=True).square() * k.square().sum(-1)[None, :, None]
-        rows = torch.zeros_like(v2)
+        rows, u2 = torch.zeros_like(v2), (v - vm[..., None]).square().sum(-1)[None, :, None]
     else:
         mid = x.sum(-1, keepdim=True) * km[None, :, None]
         both = torch.einsum("qhgd,hkd->qhgk", x.square(), k.square())
         dev = scale ** 2 * W ** 2 / 3 * (2 * both + (torch.einsum("qhgd,hkd->qhgk", x, k) - mid).square() + mid.square())
-        vm2 = 128 * vm.square()[None, :, None]
+        vm2, u2 = 128 * vm.square()[None, :, None], v2
         rows = W ** 2 / 3 * (v2 + (v - vm[..., None]).square().sum(-1)[None, :, None] + vm2)
-    var = (p.square() * (W ** 2 / 3 * v2 + dev * apart + rows)).sum(-1)
+    var = (p.square() * (W ** 2 / 3 * u2 + dev * apart + rows)).sum(-1)
     bound = 2.0 ** -8 * o.norm(dim=-1) + 6 * var.sqrt() + 2.0 ** -20 * (p * v2.sqrt()).sum(-1)
     return o, bound
 

@@ -40,7 +40,11 @@ def kernel_like(x, k, km, v, vm, seen, scale, few):
         v = rounded(v, vm)
     s = (s * scale).masked_fill(~seen[:, None, None], float("-inf"))
     w = torch.exp(s - s.amax(-1, keepdim=True)) * 64
-    o = torch.einsum("qhgk,hkd->qhgd", half(w), v) / w.sum(-1, keepdim=True)
+    if few:
+        o = torch.einsum("qhgk,hkd->qhgd", half(w), v - vm[..., None]) + torch.einsum("qhgk,hk->qhg", w, vm)[..., None]
+    else:
+        o = torch.einsum("qhgk,hkd->qhgd", half(w), v)
+    o = o / w.sum(-1, keepdim=True)
     return o.to(torch.bfloat16).double()
 
 
@@ -91,7 +95,7 @@ def test_the_bound(count, length, group, window, size, asym):
 HEADS = [(32, 8, 128), (8, 8, 80), (16, 1, 128), (14, 2, 64), (5, 5, 8), (40, 2, 96), (1, 1, 128)]
 
 
-def check(plan, lengths, counts, heads, kv_heads, page, seed=0, order=None, **kw):
+def check(plan, lengths, counts, heads, kv_heads, page, seed=0, order=None, max_len=0, **kw):
     """With a softmax that is broad, where every token counts, and with a narrow one."""
     order = order or list(range(len(lengths)))
     cache = kv_util.filled(plan, lengths, kv_heads, page, seed=seed)
@@ -102,7 +106,7 @@ def check(plan, lengths, counts, heads, kv_heads, page, seed=0, order=None, **kw
     ints = lambda x: torch.tensor(x, dtype=torch.int32, device=kv_util.DEV)  # noqa: E731
     for size in (0.5, 3.0):
         q = (torch.randn((sum(counts), heads, d), generator=gen, device=kv_util.DEV) * size * (128 / d) ** 0.5).to(torch.bfloat16)
-        got = cache.attention(q, ints(order), ints(np.concatenate([[0], np.cumsum(counts)]).tolist()), max(counts), **kw)
+        got = cache.attention(q, ints(order), ints(np.concatenate([[0], np.cumsum(counts)]).tolist()), max(counts), max_len=max_len, **kw)
         kv_norms.check(cache, got, q, order, counts, **kw)
 
 
@@ -149,6 +153,15 @@ def test_long_cache(counts, asym):
         lengths = [40000, 300, 20011][:len(counts)]
         for window in (0, 9000):
             check(plan, lengths, counts, 8, 2, 64, window=window)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("asym", [False, True])
+@pytest.mark.parametrize("counts", [[1, 1], [40, 2]])
+def test_long_segments_in_one_block(counts, asym):
+    """As in a large batch of long sequences, where a block goes through thousands of units of one: a small max_len has every segment undivided."""
+    with plan_of(128, asym) as plan:
+        check(plan, [60000, 130000], counts, 8, 2, 64, max_len=512)
 
 
 @pytest.mark.gpu
