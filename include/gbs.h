@@ -330,7 +330,7 @@ int gbs_quantized_matmul(const gbs_plan_t* plan_x, const void* codes_x, const fl
  * page_size tokens: key codes [page_size][64 bytes], value codes [page_size][64 bytes], key scales and value scales
  * [page_size] floats each (Delta), or [page_size][2] for an asymmetric plan (Delta, lo).  Codes are packed as everywhere.
  * page_table [n_seqs][max_pages] lists the pages of each sequence in order; only the first ceil(lengths[s] / page_size) entries
- * of a row are read, the others are left as they are.  lengths [n_seqs]: tokens of each sequence.  refs [n_pages]: how many
+ * of a row are read, the others count for nothing.  lengths [n_seqs]: tokens of each sequence.  refs [n_pages]: how many
  * sequences hold a page; 0 = free.  A page that is not full belongs to one sequence alone.  A new pool has lengths
  * and refs 0; no other preparation is needed.  All five arrays are device memory and belong to the caller.
  *

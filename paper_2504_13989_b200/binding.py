@@ -720,7 +720,8 @@ class KVCache:
     def attention(self, q: torch.Tensor, seqs=None, cu_tokens=None, max_tokens: int | None = None, causal: bool = True, window: int = 0,
                   scale: float = 0.0, max_len: int = 0, out=None, stream=None) -> torch.Tensor:
         """Attention of query tokens q [tokens, heads, d] (bf16) over the cache; the same shape comes back.  max_tokens: no item has
-        more tokens (None: as many as q has, or 1 without cu_tokens; it chooses the kernel, so the closer the better); max_len: about
+        more tokens (None: as many as q has, or 1 without cu_tokens; it chooses the kernel and bounds what is looked through, so the closer
+        the better, and items x max_tokens x heads / n_kv_heads may be 2^28 at most); max_len: about
         how long the longest sequence is (0: the table's width), by which the work is split; scale 0: 1 / sqrt(d).  Rows behind the last item's, and an item's beyond
         max_tokens, are left as they are in `out`, and undefined without one."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:

@@ -219,7 +219,10 @@ struct gbs_kv_attn {
     long long q_token, q_head, out_token, out_head;
     int lost_code, lost_segment;        // of the self-test: waits that count as run out (0: none)
 };
-// gbs_kv_attn.cu : up to GBS_KV_FEW_ROWS query rows of an item and KV head
+// gbs_kv_attn.cu : up to GBS_KV_FEW_ROWS query rows of an item and KV head, eight to a tile, each tile reading its part of the cache; gbs_tc_kvattn.cu : more,
+// 256 to a tile.  us of the two, 8 KV heads, at 16 rows: 64 sequences of 300 tokens 25 and 68, one of 8000 19 and 29, 16 of 4096 41 and 100, 2 of 60000 64 and
+// 130, 64 of 4096 126 and 294.  At 32 rows 39 and 69, 21 and 29, 69 and 100, 110 and 130, 243 and 295; at 48 rows 53 and 69, 23 and 30, 96 and 100, 157 and
+// 130, 367 and 295.  So they meet between 32 and 48 rows, and up to the line the first is never the slower one.  What the header says of precision goes by it.
 #define GBS_KV_FEW_ROWS 16
 int64_t gbs_kv_few_workspace(const gbs_plan* p);
 int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, cudaStream_t stream);

@@ -9,8 +9,9 @@
 // Scores are integers: key codes are bytes after a mask and a shift (3 operations for 8 codes), and a query row is an integer of 16 bits
 // per coordinate, in two pieces of 8; sums are exact, and the offset 8 of symmetric codes is the value that they start from.  Weights span too many binary places for that:
 // values become fp16 (a nibble in the mantissa of 1024, which is subtracted again, exactly; 9 operations for 8 codes).  In fp16 for both products, with
-// the weights in two pieces as well, a unit took 797 instructions instead of 568, and 16 sequences x 32 KV heads x 4096 tokens of one query row 107 us instead of 71: 4.2 TB/s of
-// the cache.  That is two thirds of a plain copy's rate; both the issue slots and the copies in flight are then about 60% used.
+// the weights in two pieces as well, a unit took 797 instructions instead of 576, and 16 sequences x 32 KV heads x 4096 tokens of one query row 107 us instead of 72: 4.2 TB/s of
+// the cache, two thirds of a plain copy's rate.  What bounds it then is latency: issue slots are 54 % used, the integer pipe 47 %, DRAM 52 %; 128 registers and
+// 160 threads leave 15 warps an SM, each a chain of loads, integer products, scores, weights and products again.
 // Layouts are chosen so that codes go from shared memory to the operand registers without being moved between threads: the order of the 128
 // coordinates of a score, of a group's 16 tokens and of the 128 rows of the result is free, as long as both operands have the same.
 // Only the weights are transposed on the way (movmatrix).

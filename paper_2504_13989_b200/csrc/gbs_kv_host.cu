@@ -178,7 +178,7 @@ extern "C" int gbs_kv_read(const gbs_plan_t* p, const gbs_kv_cache_t* cache, con
 
 namespace {
 
-// tiles of 8 rows up to here, of 128 beyond
+// tiles of 8 rows up to here, of 256 beyond
 bool few_rows(int group, int max_tokens) { return (int64_t)max_tokens * group <= GBS_KV_FEW_ROWS; }
 
 int64_t workspace_bytes_of(const gbs_plan* p, int group, int max_tokens)

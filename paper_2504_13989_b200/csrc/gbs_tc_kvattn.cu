@@ -14,6 +14,7 @@
 // The MMAs take 1024 cycles of a tile, ex2 as many; two tiles of a unit take 5600, most of it the chain of a tile (scores, softmax, weights, second
 // product, next scores), which the other tile's overlaps but in part.  The last 2048 of 8048 tokens, 32 query heads over 8 KV heads: 318 us, 740
 // TFLOP/s.  Blocks of 128 rows, two on an SM, every warp doing all of it in turn: 433 us.  32 tokens at a time in the softmax: 348.
+// 13 warps leave a thread 128 registers, and 74 bytes of one spill.
 // Weights reach 2^-30 of the row's largest, below what a bf16 result shows; l is of fp32 weights, which go under when value
 // scales that one row sees differ by more than 2^100: the share of the small ones in l is then lost.
 #include "gbs_kv_attn.cuh"
