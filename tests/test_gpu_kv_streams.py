@@ -56,3 +56,33 @@ def test_two_divided_calls_at_the_same_time():
                 torch.cuda.synchronize()
                 assert all(torch.equal(g, want[i & 1]) for i, g in enumerate(got))
         assert plan.device_status() == 0
+
+
+def test_captured_calls_that_are_given_a_stream():
+    """The capturing stream itself, and one that forks from it and joins it again."""
+    gbs_build.build()
+    with Plan(128, 128, 1, 4, 128, 0.9) as plan:
+        cache = filled(plan, [3000, 700, 40], 4, 64, seed=6)
+        seqs, cu = ints(2, 0, 1), ints(0, 1, 41, 42)
+        q = torch.randn((42, 16, 128), device=DEV).to(torch.bfloat16)
+        side = torch.cuda.Stream()
+        one, none = ints(2), ints(0)
+        cache.attention(q, seqs, cu, 40), cache.read(seqs, cu, 42), cache.extend(one, none)
+        torch.cuda.synchronize()
+        for fork in (False, True):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                s = torch.cuda.current_stream()
+                if fork:
+                    side.wait_stream(s)
+                    s = side
+                got = cache.attention(q, seqs, cu, 40, stream=s)
+                rows = cache.read(seqs, cu, 42, stream=s)
+                status = cache.extend(one, none, stream=s)
+                if fork:
+                    torch.cuda.current_stream().wait_stream(side)
+            for _ in range(3):
+                q.copy_(torch.randn_like(q))
+                g.replay()
+                assert status.tolist() == [0] and torch.equal(got, cache.attention(q, seqs, cu, 40))
+                assert all(torch.equal(a, b) for a, b in zip(rows, cache.read(seqs, cu, 42)))
