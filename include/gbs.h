@@ -338,7 +338,8 @@ int gbs_quantized_matmul(const gbs_plan_t* plan_x, const void* codes_x, const fl
  * cu_tokens[i] .. cu_tokens[i + 1] - 1 of the call's row tensors (device int32, n_items + 1 values that do not fall, from 0), or row i
  * alone where cu_tokens is NULL.  They are the LAST tokens of the sequence as lengths[] has it: a step extends the
  * sequences first, then appends and attends.  So an item that gbs_kv_extend refused must not be appended: its rows would replace the
- * sequence's last ones, which other sequences may share; gbs_kv_append_extended leaves such items out.  Rows behind cu_tokens[n_items] count for nothing and are not written.
+ * sequence's last ones, which other sequences may share; gbs_kv_append_extended leaves such items out.  Rows behind
+ * cu_tokens[n_items] count for nothing and are not written.
  * Numbers that only the device knows are checked there: an item whose sequence is out of range, a token whose position is
  * below 0 or whose page is not one of the pool's is left out (a row that would be written from it becomes 0).
  *
@@ -444,8 +445,8 @@ int gbs_kv_read(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32
  *   max_tokens        no item has more tokens (1 where cu_tokens is NULL); what is beyond it is left as it is.  It chooses the
  *                     kernel and bounds what is looked through for work, so the closer the better.
  *                     n_items * max_tokens * query heads of a KV head: at most 2^28
- *   max_len           about how long the longest sequence of the call is at most (0: the table's width).  It chooses how far the work is
- *                     split, never what is read: a longer sequence is read whole, if more slowly.
+ *   max_len           about the length of the call's longest sequence (0: the table's width).  It chooses how far the work is split, never
+ *                     what is read: a longer sequence is read whole, if more slowly.
  *   scale             0: 1 / sqrt(d)
  *   workspace         device, gbs_kv_attention_workspace bytes, 16-byte aligned; overwritten, needs no preparation, and one call at
  *                     a time may use it

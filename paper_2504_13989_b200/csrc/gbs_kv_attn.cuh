@@ -51,7 +51,7 @@ __device__ __forceinline__ unsigned kv_and_xor(unsigned x, unsigned mask, unsign
 }
 // Nibbles (i, i + 4) of a word, i = 0 .. 3, as pairs in fp16, -8 .. 7.  A symmetric code c is taken as c ^ 8 = c + 8 of four bits, an asymmetric one counts
 // from the middle of its range, 8: sums of products with codes that are all positive would be large next to what is left of them once lo is added,
-// and the matrix unit drops what lies below their last bit (2 x 130000 tokens in one block: a tenth of the result, with codes from 0).
+// and the matrix unit drops what lies below their last bit (130000 tokens in one block, a broad softmax: a tenth of the result, with codes from 0).
 template <bool ASYM>
 __device__ __forceinline__ void kv_codes_f16(unsigned w, unsigned out[4])
 {
