@@ -41,7 +41,7 @@ EXPORTS = ("gbs_plan_create", "gbs_plan_create_ex", "gbs_plan_destroy", "gbs_pla
            "gbs_hadamard_m", "gbs_status_string", "gbs_selftest_wait_expiry", "gbs_weight_rotate_quantize",
            "gbs_quantized_matmul", "gbs_kv_page_bytes", "gbs_kv_extend", "gbs_kv_fork", "gbs_kv_free", "gbs_kv_compact",
            "gbs_kv_append", "gbs_kv_append_extended", "gbs_kv_read", "gbs_kv_attention_workspace", "gbs_kv_attention",
-           "gbs_selftest_kv_attention")
+           "gbs_selftest_kv_attention", "gbs_kv_shared_attention_workspace", "gbs_kv_shared_attention")
 GBS_STATIC_MAX_D_PAD = 4096
 
 
@@ -148,7 +148,10 @@ def lib() -> ctypes.CDLL:
         L.gbs_kv_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, i32, vp, i64, i64,
                                        vp, i64, vp]
         L.gbs_selftest_kv_attention.argtypes = L.gbs_kv_attention.argtypes[:-1] + [i32, i32, vp]
-        for name in EXPORTS[-11:]:
+        L.gbs_kv_shared_attention_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i32, ctypes.POINTER(i64)]
+        L.gbs_kv_shared_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, vp, i64, i64,
+                                              vp, i64, vp]
+        for name in EXPORTS[EXPORTS.index("gbs_kv_page_bytes"):]:
             getattr(L, name).restype = i32
         L.gbs_hadamard_m.argtypes = [i32, vp]
         L.gbs_hadamard_m.restype = i32
@@ -747,9 +750,40 @@ class KVCache:
                "gbs_kv_attention")
         return out
 
+    def shared_attention(self, q: torch.Tensor, seqs=None, cu_tokens=None, groups=None, max_tokens: int | None = None, causal: bool = True,
+                         scale: float = 0.0, max_own: int = 0, out=None, stream=None) -> torch.Tensor:
+        """attention (without a window) for items whose sequences begin alike, as forks of one prompt do: the pages that all items of a group begin with are
+        read once for the group.  groups: int32 [groups + 1], the first item of each group and the end (None: all items are one group); which pages
+        are common is found in the page table.  max_own: about how many tokens the longest sequence has behind what its group shares."""
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            raise ValueError("gbs: q must be [tokens, heads, d]")
+        self._rows("q", q, q.shape[1])
+        if max_tokens is None:
+            max_tokens = max(1, q.shape[0]) if cu_tokens is not None else 1
+        for what, v in (("max_tokens", max_tokens), ("max_own", max_own)):
+            _int32(what, v)
+        if out is None:
+            out = self._empty(stream, q.shape, torch.bfloat16)
+        self._rows("out", out, q.shape[1])
+        if out.shape[0] != q.shape[0]:
+            raise ValueError("gbs: q has %d tokens, out %d" % (q.shape[0], out.shape[0]))
+        s, cu, n = self._items(seqs, cu_tokens, q.shape[0])
+        if groups is not None and (groups.dim() != 1 or groups.shape[0] < 2):
+            raise ValueError("gbs: groups must be one row of the groups' first items and the end")
+        n_groups = groups.shape[0] - 1 if groups is not None else 1
+        need = ctypes.c_int64(0)
+        _check(lib().gbs_kv_shared_attention_workspace(self.plan.handle, ctypes.byref(self._c), n, q.shape[0], max_tokens, n_groups, q.shape[1],
+                                                       ctypes.byref(need)), "gbs_kv_shared_attention_workspace")
+        work = self._empty(stream, need.value, torch.uint8, False)
+        _check(lib().gbs_kv_shared_attention(self.plan.handle, ctypes.byref(self._c), s, cu, n, q.shape[0], max_tokens,
+                                             self._ints("groups", groups, n_groups + 1), n_groups, max_own, q.data_ptr(), *self._strides(q), q.shape[1],
+                                             float(scale), GBS_KV_CAUSAL if causal else 0, out.data_ptr(), *self._strides(out), work.data_ptr(),
+                                             need.value, self._stream(stream, q, out, seqs, cu_tokens, groups)), "gbs_kv_shared_attention")
+        return out
+
 
 # the methods that _native.so has a regular call for
-_PYTHON_KV_METHODS = {name: KVCache.__dict__[name] for name in ("extend", "fork", "free", "compact", "append", "read", "attention")}
+_PYTHON_KV_METHODS = {name: KVCache.__dict__[name] for name in ("extend", "fork", "free", "compact", "append", "read", "attention", "shared_attention")}
 _PYTHON_METHODS = {name: Plan.__dict__[name] for name in ("rotate_quantize", "dequantize", "quantized_matmul", "clip_error")}
 
 

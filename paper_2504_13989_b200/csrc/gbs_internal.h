@@ -218,6 +218,11 @@ struct gbs_kv_attn {
     void* out;
     long long q_token, q_head, out_token, out_head;
     int lost_code, lost_segment;        // of the self-test: waits that count as run out (0: none)
+    // of gbs_kv_shared_attention: tokens that each item shares with its group, the groups' tiles, and what the rows got from the shared tokens
+    const int* shared;
+    const void* entries;
+    float* prefix;
+    int n_entries;
 };
 // gbs_kv_attn.cu : up to GBS_KV_FEW_ROWS query rows of an item and KV head, eight to a tile, each tile reading its part of the cache; gbs_tc_kvattn.cu : more,
 // 256 to a tile.  us of the two, 8 KV heads, at 16 rows: 64 sequences of 300 tokens 25 and 68, one of 8000 19 and 29, 16 of 4096 41 and 100, 2 of 60000 64 and
@@ -229,6 +234,11 @@ int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, 
 // gbs_tc_kvattn.cu : more rows
 int64_t gbs_tc_kvattn_workspace(const gbs_plan* p);
 int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, cudaStream_t stream);
+
+// gbs_kv_shared.cu : the same for groups of items whose sequences begin with the same pages
+#define GBS_KV_PREFIX_ROW 132           // floats that a row's sums over the common prefix take
+int64_t gbs_kv_shared_workspace(const gbs_plan* p, const gbs_kv_attn& A, int n_groups);
+int gbs_kv_shared_launch(const gbs_plan* p, const gbs_kv_attn& A, const int* groups, int n_groups, void* workspace, cudaStream_t stream);
 
 #ifdef __CUDACC__
 // Launch on `stream`, its set-up overlapping the end of the launch before it (kernels wait before they touch memory).

@@ -36,7 +36,7 @@ constexpr int STAGES = 12;                           // unit i of a block's is w
 // A stage is always the same warp's.  A wait for a phase goes by its parity, so it is one only for who has seen the phase before end; another warp, ahead
 // of the one whose copy is late, would read the stage at once.
 static_assert(STAGES % WARPS == 0, "a stage has one warp");
-constexpr int PART = KV_PART<ROWS>;
+constexpr int PIECE = KV_PART<ROWS>;
 static_assert(2 * WARPS == ROWS, "each warp finishes two rows");
 constexpr int BLOCKS_PER_SM = 3;
 constexpr float MOVE = 8.f;                          // m moves when a score is so much (log2) above it
@@ -97,7 +97,7 @@ __device__ __forceinline__ unsigned transposed(unsigned x)
 }
 
 // The query rows of a segment by one warp, eight lanes a row: rotated, and made integers.
-template <bool ASYM>
+template <bool ASYM, int PART>
 __device__ __forceinline__ void prepare(const gbs_kv_attn& A, const KvSeg& seg, typename Smem<ASYM>::Query& Q, int lane)
 {
     const int l8 = lane & 7;
@@ -158,10 +158,10 @@ __device__ __forceinline__ void prepare(const gbs_kv_attn& A, const KvSeg& seg, 
             Q.factor[row] = m * (A.scale * (KV_NORM * 1.4426950408889634f / 32512.f)) + wrong;
             Q.sum[row] = sum;
             const int token = A.by_group(min(seg.e.row0 + row, seg.e.rows - 1));
-            Q.lo[row] = kv_row_lo(A, seg.e, token);
+            Q.lo[row] = kv_row_lo<PART>(A, seg.e, token);
             Q.hi[row] = kv_row_hi(A, seg.e, token);
             if (row == 0) {                          // the last row sees the latest window, the first the shortest past
-                Q.all_lo = kv_row_lo(A, seg.e, A.by_group(min(seg.e.rows, seg.e.row0 + ROWS) - 1));
+                Q.all_lo = kv_row_lo<PART>(A, seg.e, A.by_group(min(seg.e.rows, seg.e.row0 + ROWS) - 1));
                 Q.all_hi = Q.hi[0];
             }
         }
@@ -182,7 +182,7 @@ __device__ __forceinline__ bool meet_any(bool x)
     return any != 0;
 }
 
-template <bool ASYM, bool TEST>
+template <bool ASYM, bool TEST, int PART>
 __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __grid_constant__ KvAttnArgs P)
 {
     extern __shared__ __align__(128) unsigned char smem_raw[];
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
     kv_wait_before();
     kv_let_next();
 
-    const int places = kv_share<THREADS>(A, P.line, &S.seg, S.share);
+    const int places = kv_share<THREADS, PART>(A, P.line, &S.seg, S.share);
     if (threadIdx.x == 0 && P.line.pad >= 0) P.joins[blockIdx.x] = KvJoin{0, 0, 0, 0};
     if (places == 0) return;
 
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                     dead = true;
                     break;
                 }
-                prepare<ASYM>(A, seg, S.query[round & 1], lane);
+                prepare<ASYM, PART>(A, seg, S.query[round & 1], lane);
                 if (lane == 0) {
                     S.query[round & 1].seg = seg;
                     S.query[round & 1].piece = part;
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 if (lane == 0) mbar_arrive(&S.qfull[round & 1]);
             }
             at += max(part.n, 0);
-            if (more) kv_next(A, P.line, seg);
+            if (more) kv_next<PART>(A, P.line, seg);
         }
         // The others may have given up on copies that are still on their way: in the self-test, where they leave at once.  A wait that ran out by itself
         // began two seconds ago; what had been sent for by then is not on its way any more.  (Always: 64 ragged sequences 37.9 us -> 38.4.)
@@ -482,16 +482,23 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_attn_few(const __
                 }
             }
             if (piece.starts && piece.ends) {
-                kv_finish(y, l8, top, top_w, total, extra);
-                if (seg.e.row0 + row < seg.e.rows && lane < 16) {
-                    int token, head;
-                    kv_row_of(A, seg, row, token, head);
+                const bool there = seg.e.row0 + row < seg.e.rows;
+                int token, head;
+                kv_row_of(A, seg, row, token, head);
+                if (PART == KV_PREFIX) {
+                    if (there && lane < 16) kv_leave_prefix(kv_prefix_row(A, seg, token, head), y, l8, top, top_w, total, extra);
+                } else {
+                    if (PART == KV_OWN && there && seg.e.lo > 0) kv_add_prefix(kv_prefix_row(A, seg, token, head), y, l8, top, top_w, total, extra);
+                    __syncwarp();
+                    kv_finish(y, l8, top, top_w, total, extra);
+                }
+                if (PART != KV_PREFIX && there && lane < 16) {
                     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (seg.e.first + token) * A.out_token + head * A.out_head;
                     if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
                     if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
                 }
             } else if (lane < 16) {
-                float* part = P.parts + ((long long)blockIdx.x * 2 + (piece.starts ? 1 : 0)) * PART;
+                float* part = P.parts + ((long long)blockIdx.x * 2 + (piece.starts ? 1 : 0)) * PIECE;
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     *reinterpret_cast<float4*>(part + row * 128 + 64 * (q >> 1) + 8 * l8 + 4 * (q & 1)) = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
@@ -516,8 +523,26 @@ int blocks_of(const gbs_plan* p) { return p->sm_count * BLOCKS_PER_SM; }
 
 int64_t gbs_kv_few_workspace(const gbs_plan* p)
 {
-    return (int64_t)blocks_of(p) * (2 * PART * sizeof(float) + sizeof(KvJoin)) + 16;
+    return (int64_t)blocks_of(p) * (2 * PIECE * sizeof(float) + sizeof(KvJoin)) + 16;
 }
+
+namespace {
+
+template <int PART>
+int launch(const gbs_plan* p, const KvAttnArgs& P, int blocks, cudaStream_t stream)
+{
+    const size_t smem = p->asym ? sizeof(Smem<true>) : sizeof(Smem<false>);
+    const bool test = PART == KV_WHOLE && P.a.lost_code;
+    const auto f = test ? (p->asym ? k_kv_attn_few<true, PART == KV_WHOLE, PART> : k_kv_attn_few<false, PART == KV_WHOLE, PART>)
+                        : (p->asym ? k_kv_attn_few<true, false, PART> : k_kv_attn_few<false, false, PART>);
+    const cudaError_t e = cudaFuncSetAttribute((const void*)f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return (int)e;
+    const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
+    if (rc != 0 || P.line.pad < 0) return rc;
+    return gbs_kv_launch(p, k_kv_attn_join<ROWS, PART>, dim3((unsigned)blocks), 256, 0, stream, P);
+}
+
+}  // namespace
 
 int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, cudaStream_t stream)
 {
@@ -527,7 +552,7 @@ int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, 
     P.line.unit_log = 5;
     P.line.tiles = (int)(((int64_t)A.max_tokens * A.group + ROWS - 1) / ROWS);
     P.line.by_tiles.set((unsigned)P.line.tiles);
-    P.line.entries = A.n_items * P.line.tiles;
+    P.line.entries = A.entries ? A.n_entries : A.n_items * P.line.tiles;
     // a short sequence is not worth dividing: the join's launch takes as long as a block needs for 16 units
     P.line.pad = A.max_len <= 16 * UNIT ? -1 : 7;
     P.line.least = P.line.pad < 0 ? 1 : 12;
@@ -535,12 +560,5 @@ int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, 
     P.joins = static_cast<KvJoin*>(workspace);
     P.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + blocks * sizeof(KvJoin));
     P.status = p->d_status;
-    const size_t smem = p->asym ? sizeof(Smem<true>) : sizeof(Smem<false>);
-    const auto f = A.lost_code ? (p->asym ? k_kv_attn_few<true, true> : k_kv_attn_few<false, true>)
-                               : (p->asym ? k_kv_attn_few<true, false> : k_kv_attn_few<false, false>);
-    const cudaError_t e = cudaFuncSetAttribute((const void*)f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return (int)e;
-    const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
-    if (rc != 0 || P.line.pad < 0) return rc;
-    return gbs_kv_launch(p, k_kv_attn_join<ROWS>, dim3((unsigned)blocks), 256, 0, stream, P);
+    return A.entries ? launch<KV_PREFIX>(p, P, blocks, stream) : A.shared ? launch<KV_OWN>(p, P, blocks, stream) : launch<KV_WHOLE>(p, P, blocks, stream);
 }

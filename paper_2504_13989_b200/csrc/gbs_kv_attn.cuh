@@ -14,6 +14,10 @@ constexpr float W_UP = 64.f;                         // weights are kept at 64 t
 template <int ROWS>
 constexpr int KV_PART = ROWS * 128 + 4 * ROWS;
 
+// totals of the kernel for many rows (tiles of 256) are 64 times their size
+template <int ROWS>
+constexpr float KV_TOTAL_LOG = ROWS == 256 ? 6.f : 0.f;
+
 struct KvAttnArgs {
     gbs_kv_attn a;
     KvLine line;
@@ -75,6 +79,39 @@ __device__ __forceinline__ void kv_finish(float y[16], int l8, float top, float 
     if (l8 == 0) y[0] = fmaf(extra * by, 128.f * KV_NORM, y[0]);             // the transform of a row of ones is 128 in its first place
 }
 
+// What a row has got from the tokens that its group shares (gbs_kv_shared_attention): as in a partial result, its sums and then m, the total,
+// the sum of p mid, and M, with totals that count a token of weight 1 as 1 in both kernels.
+constexpr int KV_PREFIX_ROW = GBS_KV_PREFIX_ROW;
+__device__ __forceinline__ float* kv_prefix_row(const gbs_kv_attn& A, const KvSeg& s, int token, int head)
+{
+    return A.prefix + ((long long)(s.e.first + token) * A.n_heads + head) * KV_PREFIX_ROW;
+}
+// sums of a row in the layout of kv_hadamard
+__device__ __forceinline__ void kv_leave_prefix(float* to, const float y[16], int l8, float top, float top_w, float total, float extra)
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(to + 64 * (q >> 1) + 8 * l8 + 4 * (q & 1)) = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
+    if (l8 == 0) *reinterpret_cast<float4*>(to + 128) = make_float4(top, total, extra, top_w);
+}
+__device__ __forceinline__ void kv_add_prefix(const float* from, float y[16], int l8, float& top, float& top_w, float& total, float& extra)
+{
+    const float4 x = *reinterpret_cast<const float4*>(from + 128);
+    const float t = fmaxf(top, x.x), t_w = fmaxf(top_w, x.w);
+    const float a = kv_ex2(top - t), b = kv_ex2(x.x - t), a_w = kv_ex2(top_w - t_w), b_w = kv_ex2(x.w - t_w);
+    total = fmaf(x.y, b, total * a);
+    extra = fmaf(x.z, b, extra * a);
+    top = t;
+    top_w = t_w;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float4 v = *reinterpret_cast<const float4*>(from + 64 * (q >> 1) + 8 * l8 + 4 * (q & 1));
+        y[4 * q] = fmaf(v.x, b_w, y[4 * q] * a_w);
+        y[4 * q + 1] = fmaf(v.y, b_w, y[4 * q + 1] * a_w);
+        y[4 * q + 2] = fmaf(v.z, b_w, y[4 * q + 2] * a_w);
+        y[4 * q + 3] = fmaf(v.w, b_w, y[4 * q + 3] * a_w);
+    }
+}
+
 // row of a tile -> token of the item and query head
 __device__ __forceinline__ void kv_row_of(const gbs_kv_attn& A, const KvSeg& s, int row, int& token, int& head)
 {
@@ -86,10 +123,10 @@ __device__ __forceinline__ void kv_row_of(const gbs_kv_attn& A, const KvSeg& s, 
 // The segments that several blocks share: block b joins the one that starts in block b, a warp a row, eight
 // rows a block of this kernel.  The pieces' weights come first, a
 // lane a piece, so that their sums can be fetched many at a time: up to a few dozen pieces of a long sequence are as many trips to memory otherwise.
-template <int ROWS>
+template <int ROWS, int PART = KV_WHOLE>
 __global__ __launch_bounds__(256) void k_kv_attn_join(const __grid_constant__ KvAttnArgs P)
 {
-    constexpr int PART = KV_PART<ROWS>;
+    constexpr int PIECE = KV_PART<ROWS>;
     __shared__ float full[8][128];
     kv_wait_before();
     kv_let_next();
@@ -98,8 +135,8 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(const __grid_constant__ Kv
     const gbs_kv_attn& A = P.a;
     const int row = 8 * blockIdx.y + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     // piece b's sums: the first block's last segment, the others' first
-    const float* first = P.parts + ((long long)blockIdx.x * 2 + 1) * PART;
-    const auto piece = [&](int b) { return b == 0 ? first : first + (long long)(2 * b - 1) * PART; };
+    const float* first = P.parts + ((long long)blockIdx.x * 2 + 1) * PIECE;
+    const auto piece = [&](int b) { return b == 0 ? first : first + (long long)(2 * b - 1) * PIECE; };
     float top = NONE, top_w = NONE;
     for (int b = lane; b < j.blocks; b += 32) {
         top = fmaxf(top, piece(b)[ROWS * 128 + row]);
@@ -142,7 +179,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(const __grid_constant__ Kv
     KvSeg s;
     s.index = j.index;
     s.head = j.head;
-    s.e = kv_entry(A, P.line, j.index);
+    s.e = kv_entry<PART>(A, P.line, j.index);
     const int l8 = lane & 7;                             // the four groups of eight lanes do the same; the first one writes
     float y[16];
 #pragma unroll
@@ -150,9 +187,24 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(const __grid_constant__ Kv
         y[i] = full[row & 7][8 * l8 + i];
         y[8 + i] = full[row & 7][64 + 8 * l8 + i];
     }
+    if (PART != KV_WHOLE) {
+        top -= KV_TOTAL_LOG<ROWS>;
+        top_w -= KV_TOTAL_LOG<ROWS>;
+    }
+    int token, head;
+    if (PART == KV_PREFIX) {
+        if (s.e.row0 + row >= s.e.rows || lane >= 8) return;
+        kv_row_of(A, s, row, token, head);
+        kv_leave_prefix(kv_prefix_row(A, s, token, head), y, l8, top, top_w, total, extra);
+        return;
+    }
+    if (PART == KV_OWN && s.e.lo > 0 && s.e.row0 + row < s.e.rows) {
+        kv_row_of(A, s, row, token, head);
+        kv_add_prefix(kv_prefix_row(A, s, token, head), y, l8, top, top_w, total, extra);
+        __syncwarp();
+    }
     kv_finish(y, l8, top, top_w, total, extra);
     if (s.e.row0 + row >= s.e.rows || lane >= 8) return;
-    int token, head;
     kv_row_of(A, s, row, token, head);
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (s.e.first + token) * A.out_token + head * A.out_head;
     if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);

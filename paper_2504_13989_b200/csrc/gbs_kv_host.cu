@@ -209,50 +209,77 @@ extern "C" int gbs_kv_attention_workspace(const gbs_plan_t* p, const gbs_kv_cach
 
 namespace {
 
-// code, segment: of the waits that count as run out in the self-test (0: none)
-int attention(const gbs_plan* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items, int64_t n_tokens, int max_tokens,
-              int max_len, const void* q, int64_t q_token_stride, int64_t q_head_stride, int n_heads, float scale, int window, int flags, void* out,
-              int64_t out_token_stride, int64_t out_head_stride, void* workspace, int64_t workspace_bytes, int code, int segment, void* stream)
+struct AttnCall {
+    const int32_t *seqs, *cu_tokens;
+    int n_items;
+    int64_t n_tokens;
+    int max_tokens, max_len;
+    const void* q;
+    int64_t q_token, q_head;
+    int n_heads;
+    float scale;
+    int window, flags;
+    void* out;
+    int64_t out_token, out_head;
+};
+
+// What the calls that attend check alike, and the kernels' arguments; *empty: nothing to do.  A call without `out` has other results.
+int attn_args(const gbs_plan* p, const gbs_kv_cache_t* cache, const AttnCall& x, gbs_kv_attn* to, bool* empty)
 {
     gbs_kv_attn A = {};
-    bool empty = false;
     int rc = view_of(p, cache, &A.c);
-    if (rc == GBS_OK) rc = check_tokens(A.c, seqs, cu_tokens, n_items, n_tokens, &empty);
-    if (rc == GBS_OK) rc = check_heads(A.c, n_heads, max_tokens, cu_tokens != nullptr);
+    if (rc == GBS_OK) rc = check_tokens(A.c, x.seqs, x.cu_tokens, x.n_items, x.n_tokens, empty);
+    if (rc == GBS_OK) rc = check_heads(A.c, x.n_heads, x.max_tokens, x.cu_tokens != nullptr);
     if (rc != GBS_OK) return rc;
-    if ((flags & ~GBS_KV_CAUSAL) || window < 0 || max_len < 0 || !isfinite(scale)) return GBS_ERR_INVALID_ARG;
-    if (n_tokens * n_heads >= 1ll << 31 || (int64_t)n_items * max_tokens * (n_heads / A.c.heads) > 1ll << 28) return GBS_ERR_INVALID_ARG;
-    if (empty) return GBS_OK;
-    if (!q || !out || !workspace || workspace_bytes < workspace_bytes_of(p, n_heads / A.c.heads, max_tokens)) return GBS_ERR_INVALID_ARG;
-    rc = check_strides(p, q_token_stride, q_head_stride);
-    if (rc == GBS_OK) rc = check_strides(p, out_token_stride, out_head_stride);
-    if (rc != GBS_OK) return rc;
-    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16)) return GBS_ERR_ALIGNMENT;
-    if (q == out) return GBS_ERR_INVALID_ARG;                        // rows are read after others have been written
-    A.lost_code = code;
-    A.lost_segment = segment;
-    A.seqs = seqs;
-    A.cu = cu_tokens;
-    A.n_items = n_items;
-    A.max_tokens = (int)std::min<int64_t>(max_tokens, n_tokens);
-    A.max_len = max_len > 0 ? max_len : A.c.max_pages << A.c.page_log;
-    A.window = std::min(window, 1 << 30);                            // beyond any position: position - window stays within 32 bits
-    A.causal = flags & GBS_KV_CAUSAL;
-    A.n_heads = n_heads;
-    A.group = n_heads / A.c.heads;
+    if ((x.flags & ~GBS_KV_CAUSAL) || x.window < 0 || x.max_len < 0 || !isfinite(x.scale)) return GBS_ERR_INVALID_ARG;
+    if (x.n_tokens * x.n_heads >= 1ll << 31 || (int64_t)x.n_items * x.max_tokens * (x.n_heads / A.c.heads) > 1ll << 28) return GBS_ERR_INVALID_ARG;
+    A.seqs = x.seqs;
+    A.cu = x.cu_tokens;
+    A.n_items = x.n_items;
+    A.max_tokens = (int)std::min<int64_t>(x.max_tokens, x.n_tokens);
+    A.max_len = x.max_len > 0 ? x.max_len : A.c.max_pages << A.c.page_log;
+    A.window = std::min(x.window, 1 << 30);                          // beyond any position: position - window stays within 32 bits
+    A.causal = x.flags & GBS_KV_CAUSAL;
+    A.n_heads = x.n_heads;
+    A.group = x.n_heads / A.c.heads;
     A.by_group.set((unsigned)A.group);
     A.d = p->d;
-    A.scale = scale == 0.f ? (float)(1.0 / sqrt((double)p->d)) : scale;
-    A.n_tokens = n_tokens;
-    A.q = q;
-    A.out = out;
-    A.q_token = q_token_stride;
-    A.q_head = q_head_stride;
-    A.out_token = out_token_stride;
-    A.out_head = out_head_stride;
+    A.scale = x.scale == 0.f ? (float)(1.0 / sqrt((double)p->d)) : x.scale;
+    A.n_tokens = x.n_tokens;
+    A.q = x.q;
+    A.out = x.out;
+    A.q_token = x.q_token;
+    A.q_head = x.q_head;
+    A.out_token = x.out_token;
+    A.out_head = x.out_head;
+    *to = A;
+    return GBS_OK;
+}
+// the call's tensors
+int check_rows(const gbs_plan* p, const AttnCall& x, bool has_out, const void* workspace)
+{
+    int rc = check_strides(p, x.q_token, x.q_head);
+    if (rc == GBS_OK && has_out) rc = check_strides(p, x.out_token, x.out_head);
+    if (rc != GBS_OK) return rc;
+    if (!aligned(x.q, 16) || !aligned(x.out, 16) || !aligned(workspace, 16)) return GBS_ERR_ALIGNMENT;
+    return x.q == x.out ? GBS_ERR_INVALID_ARG : GBS_OK;              // rows are read after others have been written
+}
+
+// code, segment: of the waits that count as run out in the self-test (0: none)
+int attention(const gbs_plan* p, const gbs_kv_cache_t* cache, const AttnCall& x, void* workspace, int64_t workspace_bytes, int code, int segment, void* stream)
+{
+    gbs_kv_attn A;
+    bool empty = false;
+    int rc = attn_args(p, cache, x, &A, &empty);
+    if (rc != GBS_OK || empty) return rc;
+    if (!x.q || !x.out || !workspace || workspace_bytes < workspace_bytes_of(p, A.group, x.max_tokens)) return GBS_ERR_INVALID_ARG;
+    rc = check_rows(p, x, true, workspace);
+    if (rc != GBS_OK) return rc;
+    A.lost_code = code;
+    A.lost_segment = segment;
     return on_device(p, [&] {
-        return few_rows(A.group, max_tokens) ? gbs_kv_few_launch(p, A, workspace, static_cast<cudaStream_t>(stream))
-                                             : gbs_tc_kvattn_launch(p, A, workspace, static_cast<cudaStream_t>(stream));
+        return few_rows(A.group, x.max_tokens) ? gbs_kv_few_launch(p, A, workspace, static_cast<cudaStream_t>(stream))
+                                               : gbs_tc_kvattn_launch(p, A, workspace, static_cast<cudaStream_t>(stream));
     });
 }
 
@@ -263,8 +290,9 @@ extern "C" int gbs_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache
                                 int n_heads, float scale, int window, int flags, void* out, int64_t out_token_stride,
                                 int64_t out_head_stride, void* workspace, int64_t workspace_bytes, void* stream)
 {
-    return attention(p, cache, seqs, cu_tokens, n_items, n_tokens, max_tokens, max_len, q, q_token_stride, q_head_stride, n_heads,
-                     scale, window, flags, out, out_token_stride, out_head_stride, workspace, workspace_bytes, 0, 0, stream);
+    const AttnCall x = {seqs, cu_tokens, n_items, n_tokens, max_tokens, max_len, q, q_token_stride, q_head_stride, n_heads,
+                        scale, window, flags, out, out_token_stride, out_head_stride};
+    return attention(p, cache, x, workspace, workspace_bytes, 0, 0, stream);
 }
 
 extern "C" int gbs_selftest_kv_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
@@ -273,6 +301,56 @@ extern "C" int gbs_selftest_kv_attention(const gbs_plan_t* p, const gbs_kv_cache
                                          int64_t out_head_stride, void* workspace, int64_t workspace_bytes, int code, int segment, void* stream)
 {
     if (!((code >= 61 && code <= 64) || (code >= 71 && code <= 77)) || segment < 0) return GBS_ERR_INVALID_ARG;
-    return attention(p, cache, seqs, cu_tokens, n_items, n_tokens, max_tokens, max_len, q, q_token_stride, q_head_stride, n_heads,
-                     scale, window, flags, out, out_token_stride, out_head_stride, workspace, workspace_bytes, code, segment, stream);
+    const AttnCall x = {seqs, cu_tokens, n_items, n_tokens, max_tokens, max_len, q, q_token_stride, q_head_stride, n_heads,
+                        scale, window, flags, out, out_token_stride, out_head_stride};
+    return attention(p, cache, x, workspace, workspace_bytes, code, segment, stream);
+}
+
+namespace {
+
+int check_groups(const int32_t* groups, int n_groups, const gbs_kv_attn& A)
+{
+    if (n_groups < 1 || n_groups > GBS_KV_MAX_ITEMS || (!groups && n_groups != 1)) return GBS_ERR_INVALID_ARG;
+    if (A.n_tokens * A.group > 1ll << 28) return GBS_ERR_INVALID_ARG;
+    return aligned(groups, 4) ? GBS_OK : GBS_ERR_ALIGNMENT;
+}
+
+}  // namespace
+
+extern "C" int gbs_kv_shared_attention_workspace(const gbs_plan_t* p, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
+                                                 int n_groups, int n_heads, int64_t* bytes_out)
+{
+    gbs_kv_attn A = {};
+    int rc = view_of(p, cache, &A.c);
+    if (rc == GBS_OK) rc = check_heads(A.c, n_heads, max_tokens, true);
+    if (rc != GBS_OK) return rc;
+    if (!bytes_out || n_items < 0 || n_items > GBS_KV_MAX_ITEMS || n_groups < 1 || n_groups > GBS_KV_MAX_ITEMS) return GBS_ERR_INVALID_ARG;
+    if (n_tokens < 0 || n_tokens >= 1ll << 30 || n_tokens * n_heads >= 1ll << 31 || n_tokens * (n_heads / A.c.heads) > 1ll << 28) return GBS_ERR_INVALID_ARG;
+    A.n_items = n_items;
+    A.n_tokens = n_tokens;
+    A.max_tokens = max_tokens;
+    A.n_heads = n_heads;
+    A.group = n_heads / A.c.heads;
+    *bytes_out = gbs_kv_shared_workspace(p, A, n_groups);
+    return GBS_OK;
+}
+
+extern "C" int gbs_kv_shared_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                                       int64_t n_tokens, int max_tokens, const int32_t* groups, int n_groups, int max_own, const void* q,
+                                       int64_t q_token_stride, int64_t q_head_stride, int n_heads, float scale, int flags, void* out,
+                                       int64_t out_token_stride, int64_t out_head_stride, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    const AttnCall x = {seqs, cu_tokens, n_items, n_tokens, max_tokens, max_own, q, q_token_stride, q_head_stride, n_heads,
+                        scale, 0, flags, out, out_token_stride, out_head_stride};
+    gbs_kv_attn A;
+    bool empty = false;
+    int rc = attn_args(p, cache, x, &A, &empty);
+    if (rc == GBS_OK) rc = check_groups(groups, n_groups, A);
+    if (rc != GBS_OK || empty) return rc;
+    gbs_kv_attn given = A;                                           // the workspace's size goes by the arguments as they are given
+    given.max_tokens = max_tokens;
+    if (!q || !out || !workspace || workspace_bytes < gbs_kv_shared_workspace(p, given, n_groups)) return GBS_ERR_INVALID_ARG;
+    rc = check_rows(p, x, true, workspace);
+    if (rc != GBS_OK) return rc;
+    return on_device(p, [&] { return gbs_kv_shared_launch(p, A, groups, n_groups, workspace, static_cast<cudaStream_t>(stream)); });
 }

@@ -14,6 +14,10 @@
 
 namespace {
 
+// What an attention kernel's entries are: tiles of the items over all that they see; tiles of groups of items over the prefix that a group's
+// sequences have in common; or tiles of the items over what they see behind that.
+enum KvPart { KV_WHOLE, KV_PREFIX, KV_OWN };
+
 // One (item, tile): where its rows and its part of the cache are.
 struct KvEntry {
     int seq;               // -1: none
@@ -30,8 +34,10 @@ __device__ __forceinline__ int kv_row_hi(const gbs_kv_attn& A, const KvEntry& e,
 {
     return A.causal ? min(e.before + token + 1, e.length) : e.length;
 }
+template <int PART = KV_WHOLE>
 __device__ __forceinline__ int kv_row_lo(const gbs_kv_attn& A, const KvEntry& e, int token)
 {
+    if (PART == KV_OWN) return e.lo;
     return A.window > 0 ? max(0, e.before + token - A.window + 1) : 0;
 }
 
@@ -44,22 +50,38 @@ struct KvLine {
     __device__ __forceinline__ int places(int units) const { return pad < 0 ? units != 0 : units != 0 ? units + pad : 0; }
 };
 
+// An item: its sequence (-1: none) and that one's length, its first row of the call's tensors, and how many it has.
+struct KvItem {
+    int seq, length, first, count;
+};
+__device__ __forceinline__ KvItem kv_item(const gbs_kv_attn& A, int item)
+{
+    KvItem x;
+    x.first = item;
+    x.seq = A.seqs ? A.seqs[item] : item;
+    x.count = 1;
+    if (A.cu) {
+        x.first = A.cu[item];
+        x.count = A.cu[item + 1] - x.first;
+    }
+    if ((unsigned)x.seq >= (unsigned)A.c.n_seqs) x.seq = -1;
+    x.length = x.seq < 0 ? 0 : kv_length(A.c, x.seq);
+    // no item has more rows than the call, nor a row outside it, whatever cu holds
+    if (x.first < 0 || x.first > (int)A.n_tokens) x.count = 0;
+    else x.count = min(x.count, (int)A.n_tokens - x.first);
+    return x;
+}
+
+template <int PART = KV_WHOLE>
 __device__ __forceinline__ KvEntry kv_entry(const gbs_kv_attn& A, const KvLine& L, int index)
 {
+    if (PART == KV_PREFIX) return static_cast<const KvEntry*>(A.entries)[index];
     KvEntry e;
     const int item = L.by_tiles(index), tile = index - item * L.tiles;
-    e.first = item;
-    e.seq = A.seqs ? A.seqs[item] : item;
-    int count = 1;
-    if (A.cu) {
-        e.first = A.cu[item];
-        count = A.cu[item + 1] - e.first;
-    }
-    if ((unsigned)e.seq >= (unsigned)A.c.n_seqs) e.seq = -1;
-    const int length = e.seq < 0 ? 0 : kv_length(A.c, e.seq);
-    // no item has more rows than the call, nor a row outside it, whatever cu holds
-    if (e.first < 0 || e.first > (int)A.n_tokens) count = 0;
-    else count = min(count, (int)A.n_tokens - e.first);
+    const KvItem x = kv_item(A, item);
+    const int count = x.count, length = x.length;
+    e.first = x.first;
+    e.seq = x.seq;
     e.row0 = tile * L.tile_rows;
     e.rows = max(0, min(count, A.max_tokens)) * A.group;
     e.before = e.length = e.lo = e.hi = e.units = 0;
@@ -68,7 +90,7 @@ __device__ __forceinline__ KvEntry kv_entry(const gbs_kv_attn& A, const KvLine& 
     e.length = length;
     const int last = min(e.rows, e.row0 + L.tile_rows) - 1;
     e.hi = kv_row_hi(A, e, A.by_group(last));
-    e.lo = kv_row_lo(A, e, A.by_group(e.row0));
+    e.lo = PART == KV_OWN ? A.shared[item] : kv_row_lo(A, e, A.by_group(e.row0));
     // a tile that sees nothing is one unit too: its rows become 0
     e.units = 1;
     if (e.hi > e.lo) e.units = ((e.hi - 1) >> L.unit_log) - (e.lo >> L.unit_log) + 1;
@@ -96,6 +118,7 @@ __device__ __forceinline__ KvPiece kv_piece(const KvLine& L, const KvSeg& s, int
 // whether the block has places behind this segment
 __device__ __forceinline__ bool kv_more(const KvLine& L, const KvSeg& s, int places) { return s.at + L.places(s.e.units) < places; }
 
+template <int PART = KV_WHOLE>
 __device__ __forceinline__ void kv_next(const gbs_kv_attn& A, const KvLine& L, KvSeg& s)
 {
     s.at += L.places(s.e.units);
@@ -103,13 +126,13 @@ __device__ __forceinline__ void kv_next(const gbs_kv_attn& A, const KvLine& L, K
     s.head = 0;
     do {
         if (++s.index >= L.entries) { s.e.units = 0x3fffffff; return; }     // behind the last: a block has no places there
-        s.e = kv_entry(A, L, s.index);
+        s.e = kv_entry<PART>(A, L, s.index);
     } while (s.e.units == 0);
 }
 
 // The block's share: how many places, and in S the segment of the first one.  All threads of the block call it; `sh` is shared memory for
 // one number a warp.  Places are counted in 64 bits: sums over all entries and heads.
-template <int THREADS>
+template <int THREADS, int PART = KV_WHOLE>
 __device__ __forceinline__ int kv_share(const gbs_kv_attn& A, const KvLine& L, KvSeg* found, long long* sh)
 {
     constexpr int WARPS = THREADS / 32;
@@ -118,7 +141,7 @@ __device__ __forceinline__ int kv_share(const gbs_kv_attn& A, const KvLine& L, K
     long long mine = 0;
     KvEntry e = {};
     for (int i = e0; i < e1; ++i) {
-        e = kv_entry(A, L, i);
+        e = kv_entry<PART>(A, L, i);
         mine += L.places(e.units);
     }
     long long sum = mine;
@@ -143,7 +166,7 @@ __device__ __forceinline__ int kv_share(const gbs_kv_attn& A, const KvLine& L, K
     if (from < total && here <= from && from < here + mine * A.c.heads) {
         int i = e0;
         for (;; ++i) {
-            if (per > 1) e = kv_entry(A, L, i);
+            if (per > 1) e = kv_entry<PART>(A, L, i);
             const long long n = (long long)L.places(e.units) * A.c.heads;
             if (from < here + n) break;
             here += n;

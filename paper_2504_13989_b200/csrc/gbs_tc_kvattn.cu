@@ -24,7 +24,7 @@ namespace {
 
 constexpr int TILE = 128, ROWS = 2 * TILE, UNIT = 128;
 constexpr int SOFTMAX = ROWS, CODES = UNIT, THREADS = SOFTMAX + CODES + 32;
-constexpr int PART = KV_PART<ROWS>;
+constexpr int PIECE = KV_PART<ROWS>;
 constexpr float MOVE = 8.f;                          // M moves when a score is so much (log2) above it
 constexpr unsigned O_COL = 256, TMEM_COLS = 512;     // scores of tile t from column 128 t on, sums from O_COL + 128 t on
 
@@ -136,7 +136,7 @@ __device__ __forceinline__ void shrink(unsigned scores, unsigned sums, float kee
     }
 }
 
-template <bool ASYM, bool TEST>
+template <bool ASYM, bool TEST, int PART>
 __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant__ KvAttnArgs P)
 {
     extern __shared__ unsigned char smem_raw[];
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
     kv_wait_before();
     kv_let_next();
 
-    const int places = kv_share<THREADS>(A, P.line, &S.seg[0], S.share);
+    const int places = kv_share<THREADS, PART>(A, P.line, &S.seg[0], S.share);
     if (tid == 0) P.joins[blockIdx.x] = KvJoin{0, 0, 0, 0};
 
     const int ps_log = A.c.page_log, ps = 1 << ps_log;
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                     if (l8 == 0) {
                         S.factor[row] = up * (fabsf(A.scale) * (KV_NORM * 1.4426950408889634f));
                         const int token = A.by_group(min(seg.e.row0 + row, seg.e.rows - 1));
-                        S.lo[row] = kv_row_lo(A, seg.e, token);
+                        S.lo[row] = kv_row_lo<PART>(A, seg.e, token);
                         S.hi[row] = seg.e.row0 + row < seg.e.rows ? kv_row_hi(A, seg.e, token) : 0;
                     }
                 }
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             const int see_lo = S.lo[row], see_hi = S.hi[row];
             // tokens that every row of the tile sees need no mask
             const int first = seg.e.row0 + TILE * t;
-            const int all_lo = kv_row_lo(A, seg.e, A.by_group(min(seg.e.rows, first + TILE) - 1)), all_hi = kv_row_hi(A, seg.e, A.by_group(first));
+            const int all_lo = kv_row_lo<PART>(A, seg.e, A.by_group(min(seg.e.rows, first + TILE) - 1)), all_hi = kv_row_hi(A, seg.e, A.by_group(first));
             float M = NONE;
             f32x2 l = both(0.f);                             // of even and odd tokens
             for (int i = 0; i < n && ok && (t == 0 || two); ++i) {
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             tc_fence_before();
             if (meet_any(!ok)) break;
             tc_fence_after();
-            float* parts = P.parts + ((long long)blockIdx.x * 2 + (piece.starts ? 1 : 0)) * PART;
+            float* parts = P.parts + ((long long)blockIdx.x * 2 + (piece.starts ? 1 : 0)) * PIECE;
 #pragma unroll 1
             for (int q0 = 0; q0 < (two ? ROWS : TILE); q0 += 32) {
                 const int row = q0 + (tid >> 3), l8 = tid & 7;
@@ -340,10 +340,19 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 }
                 const float total = S.l[row], m = S.m[row];
                 if (piece.starts && piece.ends) {
-                    kv_finish(y, l8, 0.f, 6.f, total, 0.f);
-                    if (seg.e.row0 + row < seg.e.rows) {
-                        int token, head;
-                        kv_row_of(A, seg, row, token, head);
+                    const bool have = seg.e.row0 + row < seg.e.rows;
+                    int token, head;
+                    kv_row_of(A, seg, row, token, head);
+                    if (PART == KV_WHOLE) kv_finish(y, l8, 0.f, 6.f, total, 0.f);
+                    else if (PART == KV_PREFIX) {
+                        if (have) kv_leave_prefix(kv_prefix_row(A, seg, token, head), y, l8, m - KV_TOTAL_LOG<ROWS>, m, total, 0.f);
+                    } else {
+                        float top = m - KV_TOTAL_LOG<ROWS>, top_w = m, sum = total, extra = 0.f;
+                        if (have && seg.e.lo > 0) kv_add_prefix(kv_prefix_row(A, seg, token, head), y, l8, top, top_w, sum, extra);
+                        __syncwarp();
+                        kv_finish(y, l8, top, top_w, sum, extra);
+                    }
+                    if (PART != KV_PREFIX && have) {
                         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (seg.e.first + token) * A.out_token + head * A.out_head;
                         if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
                         if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
@@ -495,7 +504,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             if (two) phase_b += n;
             if (lane == 0 && kv_more(P.line, seg, places)) {
                 KvSeg next = seg;
-                kv_next(A, P.line, next);
+                kv_next<PART>(A, P.line, next);
                 S.seg[(round + 1) & 1] = next;
             }
             if (meet_any(!ok)) {
@@ -520,8 +529,26 @@ int blocks_of(const gbs_plan* p) { return p->sm_count; }
 
 int64_t gbs_tc_kvattn_workspace(const gbs_plan* p)
 {
-    return (int64_t)blocks_of(p) * (2 * PART * sizeof(float) + sizeof(KvJoin));
+    return (int64_t)blocks_of(p) * (2 * PIECE * sizeof(float) + sizeof(KvJoin));
 }
+
+namespace {
+
+template <int PART>
+int launch(const gbs_plan* p, const KvAttnArgs& P, int blocks, cudaStream_t stream)
+{
+    const size_t smem = sizeof(Smem) + 1024;
+    const bool test = PART == KV_WHOLE && P.a.lost_code;
+    const auto f = test ? (p->asym ? k_tc_kvattn<true, PART == KV_WHOLE, PART> : k_tc_kvattn<false, PART == KV_WHOLE, PART>)
+                        : (p->asym ? k_tc_kvattn<true, false, PART> : k_tc_kvattn<false, false, PART>);
+    const cudaError_t e = cudaFuncSetAttribute((const void*)f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return (int)e;
+    const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
+    if (rc != 0) return rc;
+    return gbs_kv_launch(p, k_kv_attn_join<ROWS, PART>, dim3((unsigned)blocks, ROWS / 8), 256, 0, stream, P);
+}
+
+}  // namespace
 
 int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, cudaStream_t stream)
 {
@@ -532,18 +559,11 @@ int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspac
     P.line.pad = 5;                                  // queries and results take as long as five units (2: 134 us for six prompts of up to 1700 tokens, 3: 117, 5: 102, 9: 106)
     P.line.tiles = (int)(((int64_t)A.max_tokens * A.group + ROWS - 1) / ROWS);
     P.line.by_tiles.set((unsigned)P.line.tiles);
-    P.line.entries = A.n_items * P.line.tiles;
+    P.line.entries = A.entries ? A.n_entries : A.n_items * P.line.tiles;
     P.line.least = 1;
     const int blocks = blocks_of(p);
     P.joins = static_cast<KvJoin*>(workspace);
     P.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + blocks * sizeof(KvJoin));
     P.status = p->d_status;
-    const size_t smem = sizeof(Smem) + 1024;
-    const auto f = A.lost_code ? (p->asym ? k_tc_kvattn<true, true> : k_tc_kvattn<false, true>)
-                               : (p->asym ? k_tc_kvattn<true, false> : k_tc_kvattn<false, false>);
-    const cudaError_t e = cudaFuncSetAttribute((const void*)f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return (int)e;
-    const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
-    if (rc != 0) return rc;
-    return gbs_kv_launch(p, k_kv_attn_join<ROWS>, dim3((unsigned)blocks, ROWS / 8), 256, 0, stream, P);
+    return A.entries ? launch<KV_PREFIX>(p, P, blocks, stream) : A.shared ? launch<KV_OWN>(p, P, blocks, stream) : launch<KV_WHOLE>(p, P, blocks, stream);
 }
