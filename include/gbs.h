@@ -359,7 +359,7 @@ typedef struct gbs_kv_cache {
     int n_seqs, max_pages;  /* n_seqs * max_pages entries; max_pages at most 2^20 */
 } gbs_kv_cache_t;
 
-/* what became of an item of gbs_kv_extend and gbs_kv_fork (device int32) */
+/* what became of an item of gbs_kv_extend, gbs_kv_fork and gbs_kv_evict (device int32) */
 #define GBS_KV_DONE 0
 #define GBS_KV_BAD_INDEX 1    /* a sequence out of range, or a negative count */
 #define GBS_KV_NOT_EMPTY 2    /* the target of a fork holds tokens */
@@ -484,6 +484,47 @@ int gbs_kv_shared_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache,
                             int64_t n_tokens, int max_tokens, const int32_t* groups, int n_groups, int max_own, const void* q,
                             int64_t q_token_stride, int64_t q_head_stride, int n_heads, float scale, int flags, void* out,
                             int64_t out_token_stride, int64_t out_head_stride, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The softmax weight that each cached token gets from the items' query tokens, by KV head: with p the probabilities of gbs_kv_attention for these
+ * arguments and j a position of item i's sequence s,
+ *     mass[s][kv head][j] = decay * base[s][kv head][j] + sum of p_j over the item's query tokens and the query heads of the KV head,
+ * where base counts as 0 for the item's own tokens, which had no weight before this call.  Written are positions 0 .. lengths[s] - 1, as far as they lie
+ * below `width`, of the sequences of items that have tokens; nothing else is.  Where two items name one sequence, either's sums may stay.
+ *   mass, base        device float [n_seqs][n_kv_heads][width]; base is mass itself or does not overlap it, and is not read (NULL will do) where decay is 0
+ *   max_tokens        no item has more tokens; what is beyond it gives no weight.  query heads of a KV head * n_tokens: at most 2^28
+ *   workspace         device, gbs_kv_attention_mass_workspace bytes for the same sizes, 16-byte aligned; overwritten, needs no preparation, and one call at a
+ *                     time may use it
+ * Weights are right to fp32: query rows are rounded to 24 bits of their largest coordinate, codes enter as they are, sums of products are exact.  Value
+ * rows count for nothing.  A token whose key scale is infinite or a NaN makes the rows that see it, and so what they see, NaN.
+ */
+int gbs_kv_attention_mass_workspace(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
+                                    int n_heads, int64_t* bytes_out);
+int gbs_kv_attention_mass(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                          int64_t n_tokens, int max_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int n_heads,
+                          float scale, int window, int flags, const float* base, float decay, float* mass, int64_t width, void* workspace,
+                          int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Sequences longer than `keep` tokens are cut down to `keep` of them, for each KV head its own: the first `first` ones, the last `recent` ones, and of those between
+ * the ones with the largest mass (of two alike the one at the lower position; a NaN counts as the largest, a position from `width` on as 0).  They move to
+ * the front of the sequence in their order, into pages of their own, taken as by gbs_kv_extend (so that room for them has to be free, and pages that other sequences
+ * share stay as they are); then refs of the pages that the sequence held fall by 1.  A sequence of at most `keep` tokens stays as it is.  Positions are from then on those in what
+ * is left: new tokens follow at position `keep`.
+ *   keep, recent, first  keep at least 1, recent + first at most keep
+ *   mass              device float [n_seqs][n_kv_heads][width], as gbs_kv_attention_mass leaves it
+ *   mass_out          the same shape: mass itself, or not overlapping it.  Positions 0 .. of each sequence and KV head receive the mass of the tokens that
+ *                     stay (below width); nothing else is written
+ *   kept              device int32 [n_items][n_kv_heads][keep], receives their former positions, which rise; -1 behind the last token of a shorter sequence, and
+ *                     in all places of an item that was refused
+ *   status_out        device int32 [n_items]; items that are refused (GBS_KV_BAD_INDEX, GBS_KV_DUPLICATE, GBS_KV_NO_PAGES) leave everything as it was
+ *   workspace         device, gbs_kv_evict_workspace bytes, 16-byte aligned; overwritten, needs no preparation, and one call at a time may use it
+ * A token that stays and whose page is not one of the pool's becomes a row of zeros.
+ */
+int gbs_kv_evict_workspace(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, int n_items, int keep, int64_t* bytes_out);
+int gbs_kv_evict(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, int n_items, int keep, int recent, int first,
+                 const float* mass, float* mass_out, int64_t width, int32_t* kept, int32_t* status_out, void* workspace,
+                 int64_t workspace_bytes, void* cuda_stream);
 
 /*
  * Self-test of what gbs_kv_attention does when one of its bounded waits runs out (a diagnostic, as gbs_selftest_wait_expiry): the same call,

@@ -41,7 +41,8 @@ EXPORTS = ("gbs_plan_create", "gbs_plan_create_ex", "gbs_plan_destroy", "gbs_pla
            "gbs_hadamard_m", "gbs_status_string", "gbs_selftest_wait_expiry", "gbs_weight_rotate_quantize",
            "gbs_quantized_matmul", "gbs_kv_page_bytes", "gbs_kv_extend", "gbs_kv_fork", "gbs_kv_free", "gbs_kv_compact",
            "gbs_kv_append", "gbs_kv_append_extended", "gbs_kv_read", "gbs_kv_attention_workspace", "gbs_kv_attention",
-           "gbs_selftest_kv_attention", "gbs_kv_shared_attention_workspace", "gbs_kv_shared_attention")
+           "gbs_selftest_kv_attention", "gbs_kv_shared_attention_workspace", "gbs_kv_shared_attention",
+           "gbs_kv_attention_mass_workspace", "gbs_kv_attention_mass", "gbs_kv_evict_workspace", "gbs_kv_evict")
 GBS_STATIC_MAX_D_PAD = 4096
 
 
@@ -151,6 +152,11 @@ def lib() -> ctypes.CDLL:
         L.gbs_kv_shared_attention_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i32, ctypes.POINTER(i64)]
         L.gbs_kv_shared_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, vp, i64, i64,
                                               vp, i64, vp]
+        L.gbs_kv_attention_mass_workspace.argtypes = [vp, kv, i32, i64, i32, i32, ctypes.POINTER(i64)]
+        L.gbs_kv_attention_mass.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i64, i64, i32, ctypes.c_float, i32, i32, vp, ctypes.c_float, vp, i64,
+                                            vp, i64, vp]
+        L.gbs_kv_evict_workspace.argtypes = [vp, kv, i32, i32, ctypes.POINTER(i64)]
+        L.gbs_kv_evict.argtypes = [vp, kv, vp, i32, i32, i32, i32, vp, vp, i64, vp, vp, vp, i64, vp]
         for name in EXPORTS[EXPORTS.index("gbs_kv_page_bytes"):]:
             getattr(L, name).restype = i32
         L.gbs_hadamard_m.argtypes = [i32, vp]
@@ -781,9 +787,67 @@ class KVCache:
                                              need.value, self._stream(stream, q, out, seqs, cu_tokens, groups)), "gbs_kv_shared_attention")
         return out
 
+    def _weights(self, what: str, t: torch.Tensor, width: int | None = None):
+        """Weights of cached tokens: [sequences, n_kv_heads, width] fp32."""
+        _check_buffer(what, t, self.pages, torch.float32, 1)
+        if t.dim() != 3 or t.shape[0] != self.page_table.shape[0] or t.shape[1] != self.n_kv_heads or (width is not None and t.shape[2] != width):
+            raise ValueError("gbs: %s must be [%d, %d, %s], got shape %s" % (what, self.page_table.shape[0], self.n_kv_heads,
+                                                                            "width" if width is None else width, tuple(t.shape)))
+
+    def attention_mass(self, q: torch.Tensor, mass: torch.Tensor, seqs=None, cu_tokens=None, max_tokens: int | None = None, decay: float = 1.0, base=None,
+                       causal: bool = True, window: int = 0, scale: float = 0.0, stream=None) -> torch.Tensor:
+        """The softmax weight that each cached token gets from query tokens q [tokens, heads, d] (bf16), summed over them and the query heads of a KV
+        head, into mass [sequences, n_kv_heads, width] (fp32) at the token's position: mass = decay * base + the sum.  base: None is mass itself, what
+        the calls before added up; the items' own tokens (the last ones of their sequences) start from 0, and with decay 0 all do.  Positions from
+        width on are left out.  Returns mass."""
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            raise ValueError("gbs: q must be [tokens, heads, d]")
+        self._rows("q", q, q.shape[1])
+        if max_tokens is None:
+            max_tokens = max(1, q.shape[0]) if cu_tokens is not None else 1
+        for what, v in (("max_tokens", max_tokens), ("window", window)):
+            _int32(what, v)
+        self._weights("mass", mass)
+        if base is None:
+            base = mass
+        self._weights("base", base, mass.shape[2])
+        s, cu, n = self._items(seqs, cu_tokens, q.shape[0])
+        need = ctypes.c_int64(0)
+        _check(lib().gbs_kv_attention_mass_workspace(self.plan.handle, ctypes.byref(self._c), n, q.shape[0], max_tokens, q.shape[1], ctypes.byref(need)),
+               "gbs_kv_attention_mass_workspace")
+        work = self._empty(stream, need.value, torch.uint8, False)
+        _check(lib().gbs_kv_attention_mass(self.plan.handle, ctypes.byref(self._c), s, cu, n, q.shape[0], max_tokens, q.data_ptr(), *self._strides(q),
+                                           q.shape[1], float(scale), window, GBS_KV_CAUSAL if causal else 0, base.data_ptr(), float(decay),
+                                           mass.data_ptr(), mass.shape[2], work.data_ptr(), need.value,
+                                           self._stream(stream, q, mass, base, seqs, cu_tokens)), "gbs_kv_attention_mass")
+        return mass
+
+    def evict(self, mass: torch.Tensor, keep: int, seqs=None, recent: int = 0, first: int = 0, into=None, stream=None):
+        """Cut sequences longer than `keep` tokens down to `keep`, for each KV head its own: the first `first`, the last `recent`, and of those between the ones with
+        the largest mass [sequences, n_kv_heads, width] (fp32, as attention_mass leaves it).  What stays moves to the front of the sequence, in order, into
+        pages of its own (which have to be free), and its mass to the front of `into` (None: of mass).  Returns the items' status (GBS_KV_*) and the
+        former positions of what stays [items, n_kv_heads, keep] (int32, -1 where there is none)."""
+        for what, v in (("keep", keep), ("recent", recent), ("first", first)):
+            _int32(what, v)
+        self._weights("mass", mass)
+        if into is None:
+            into = mass
+        self._weights("into", into, mass.shape[2])
+        n = seqs.shape[0] if seqs is not None else self.page_table.shape[0]
+        status = self._empty(stream, n, torch.int32)
+        kept = self._empty(stream, (n, self.n_kv_heads, max(keep, 0)), torch.int32)
+        need = ctypes.c_int64(0)
+        _check(lib().gbs_kv_evict_workspace(self.plan.handle, ctypes.byref(self._c), n, keep, ctypes.byref(need)), "gbs_kv_evict_workspace")
+        work = self._empty(stream, need.value, torch.uint8, False)
+        _check(lib().gbs_kv_evict(self.plan.handle, ctypes.byref(self._c), self._ints("seqs", seqs, n), n, keep, recent, first, mass.data_ptr(),
+                                  into.data_ptr(), mass.shape[2], kept.data_ptr(), status.data_ptr(), work.data_ptr(), need.value,
+                                  self._stream(stream, mass, into, seqs)), "gbs_kv_evict")
+        return status, kept
+
 
 # the methods that _native.so has a regular call for
-_PYTHON_KV_METHODS = {name: KVCache.__dict__[name] for name in ("extend", "fork", "free", "compact", "append", "read", "attention", "shared_attention")}
+_PYTHON_KV_METHODS = {name: KVCache.__dict__[name] for name in ("extend", "fork", "free", "compact", "append", "read", "attention", "shared_attention",
+                                                                   "attention_mass", "evict")}
 _PYTHON_METHODS = {name: Plan.__dict__[name] for name in ("rotate_quantize", "dequantize", "quantized_matmul", "clip_error")}
 
 

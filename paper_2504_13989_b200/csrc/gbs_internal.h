@@ -239,6 +239,23 @@ int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspac
 #define GBS_KV_PREFIX_ROW 132           // floats that a row's sums over the common prefix take
 int64_t gbs_kv_shared_workspace(const gbs_plan* p, const gbs_kv_attn& A, int n_groups);
 int gbs_kv_shared_launch(const gbs_plan* p, const gbs_kv_attn& A, const int* groups, int n_groups, void* workspace, cudaStream_t stream);
+// gbs_kv_mass.cu : the weights that cached tokens get
+int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A);
+int gbs_kv_mass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* base, float decay, float* mass, int64_t width, void* workspace,
+                       cudaStream_t stream);
+// gbs_kv_pages.cu : pages for what sequences keep; the items' status.  gbs_kv_evict.cu : what they keep, moved there
+int gbs_kv_evict_pages_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, int keep, int keep_pages, int* fresh, int* status,
+                              cudaStream_t stream);
+struct gbs_kv_eviction {
+    gbs_kv_view c;
+    const int* seqs;
+    int n_items, keep, recent, first, keep_pages;
+    const float* mass;
+    float* mass_out;
+    long long width;
+    int *status, *kept, *fresh;
+};
+int gbs_kv_evict_launch(const gbs_plan* p, const gbs_kv_eviction& E, cudaStream_t stream);
 
 #ifdef __CUDACC__
 // Launch on `stream`, its set-up overlapping the end of the launch before it (kernels wait before they touch memory).

@@ -317,20 +317,36 @@ int check_groups(const int32_t* groups, int n_groups, const gbs_kv_attn& A)
 
 }  // namespace
 
-extern "C" int gbs_kv_shared_attention_workspace(const gbs_plan_t* p, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
-                                                 int n_groups, int n_heads, int64_t* bytes_out)
+namespace {
+
+// the sizes that a workspace goes by
+int sizes_of(const gbs_plan* p, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens, int n_heads, const int64_t* bytes_out,
+             gbs_kv_attn* to)
 {
     gbs_kv_attn A = {};
     int rc = view_of(p, cache, &A.c);
     if (rc == GBS_OK) rc = check_heads(A.c, n_heads, max_tokens, true);
     if (rc != GBS_OK) return rc;
-    if (!bytes_out || n_items < 0 || n_items > GBS_KV_MAX_ITEMS || n_groups < 1 || n_groups > GBS_KV_MAX_ITEMS) return GBS_ERR_INVALID_ARG;
+    if (!bytes_out || n_items < 0 || n_items > GBS_KV_MAX_ITEMS) return GBS_ERR_INVALID_ARG;
     if (n_tokens < 0 || n_tokens >= 1ll << 30 || n_tokens * n_heads >= 1ll << 31 || n_tokens * (n_heads / A.c.heads) > 1ll << 28) return GBS_ERR_INVALID_ARG;
     A.n_items = n_items;
     A.n_tokens = n_tokens;
     A.max_tokens = max_tokens;
     A.n_heads = n_heads;
     A.group = n_heads / A.c.heads;
+    *to = A;
+    return GBS_OK;
+}
+
+}  // namespace
+
+extern "C" int gbs_kv_shared_attention_workspace(const gbs_plan_t* p, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
+                                                 int n_groups, int n_heads, int64_t* bytes_out)
+{
+    gbs_kv_attn A;
+    const int rc = sizes_of(p, cache, n_items, n_tokens, max_tokens, n_heads, bytes_out, &A);
+    if (rc != GBS_OK) return rc;
+    if (n_groups < 1 || n_groups > GBS_KV_MAX_ITEMS) return GBS_ERR_INVALID_ARG;
     *bytes_out = gbs_kv_shared_workspace(p, A, n_groups);
     return GBS_OK;
 }
@@ -353,4 +369,77 @@ extern "C" int gbs_kv_shared_attention(const gbs_plan_t* p, const gbs_kv_cache_t
     rc = check_rows(p, x, true, workspace);
     if (rc != GBS_OK) return rc;
     return on_device(p, [&] { return gbs_kv_shared_launch(p, A, groups, n_groups, workspace, static_cast<cudaStream_t>(stream)); });
+}
+
+extern "C" int gbs_kv_attention_mass_workspace(const gbs_plan_t* p, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
+                                               int n_heads, int64_t* bytes_out)
+{
+    gbs_kv_attn A;
+    const int rc = sizes_of(p, cache, n_items, n_tokens, max_tokens, n_heads, bytes_out, &A);
+    if (rc != GBS_OK) return rc;
+    *bytes_out = gbs_kv_mass_workspace(p, A);
+    return GBS_OK;
+}
+
+extern "C" int gbs_kv_attention_mass(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                                     int64_t n_tokens, int max_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int n_heads,
+                                     float scale, int window, int flags, const float* base, float decay, float* mass, int64_t width,
+                                     void* workspace, int64_t workspace_bytes, void* stream)
+{
+    const AttnCall x = {seqs, cu_tokens, n_items, n_tokens, max_tokens, 0, q, q_token_stride, q_head_stride, n_heads, scale, window, flags, nullptr, 0, 0};
+    gbs_kv_attn A;
+    bool empty = false;
+    int rc = attn_args(p, cache, x, &A, &empty);
+    if (rc != GBS_OK) return rc;
+    if (width < 1 || !isfinite(decay) || A.n_tokens * A.group > 1ll << 28) return GBS_ERR_INVALID_ARG;
+    if (empty) return GBS_OK;
+    if (!q || !mass || (!base && decay != 0.f) || !workspace || workspace_bytes < gbs_kv_mass_workspace(p, A)) return GBS_ERR_INVALID_ARG;
+    rc = check_rows(p, x, false, workspace);
+    if (rc != GBS_OK) return rc;
+    if (!aligned(mass, 4) || !aligned(base, 4)) return GBS_ERR_ALIGNMENT;
+    return on_device(p, [&] { return gbs_kv_mass_launch(p, A, base, decay, mass, width, workspace, static_cast<cudaStream_t>(stream)); });
+}
+
+namespace {
+
+// pages of the tokens that a sequence keeps
+int keep_pages_of(const gbs_kv_view& c, int keep) { return std::min((int)(((int64_t)keep + (1 << c.page_log) - 1) >> c.page_log), c.max_pages); }
+
+}  // namespace
+
+extern "C" int gbs_kv_evict_workspace(const gbs_plan_t* p, const gbs_kv_cache_t* cache, int n_items, int keep, int64_t* bytes_out)
+{
+    gbs_kv_view c;
+    const int rc = view_of(p, cache, &c);
+    if (rc != GBS_OK) return rc;
+    if (!bytes_out || n_items < 0 || n_items > GBS_KV_MAX_ITEMS || keep < 1) return GBS_ERR_INVALID_ARG;
+    *bytes_out = (int64_t)n_items * keep_pages_of(c, keep) * (int64_t)sizeof(int32_t);
+    return GBS_OK;
+}
+
+extern "C" int gbs_kv_evict(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, int n_items, int keep, int recent, int first,
+                            const float* mass, float* mass_out, int64_t width, int32_t* kept, int32_t* status_out, void* workspace,
+                            int64_t workspace_bytes, void* stream)
+{
+    gbs_kv_eviction E = {};
+    int rc = view_of(p, cache, &E.c);
+    if (rc == GBS_OK) rc = check_items(E.c, seqs, n_items);
+    if (rc != GBS_OK) return rc;
+    if (keep < 1 || recent < 0 || first < 0 || (int64_t)recent + first > keep || width < 1) return GBS_ERR_INVALID_ARG;
+    if (n_items == 0) return GBS_OK;
+    E.keep_pages = keep_pages_of(E.c, keep);
+    if (!mass || !mass_out || !kept || !status_out || !workspace || workspace_bytes < (int64_t)n_items * E.keep_pages * (int64_t)sizeof(int32_t)) return GBS_ERR_INVALID_ARG;
+    if (!aligned(mass, 4) || !aligned(mass_out, 4) || !aligned(kept, 4) || !aligned(status_out, 4) || !aligned(workspace, 16)) return GBS_ERR_ALIGNMENT;
+    E.seqs = seqs;
+    E.n_items = n_items;
+    E.keep = keep;
+    E.recent = recent;
+    E.first = first;
+    E.mass = mass;
+    E.mass_out = mass_out;
+    E.width = width;
+    E.status = status_out;
+    E.kept = kept;
+    E.fresh = static_cast<int*>(workspace);
+    return on_device(p, [&] { return gbs_kv_evict_launch(p, E, static_cast<cudaStream_t>(stream)); });
 }

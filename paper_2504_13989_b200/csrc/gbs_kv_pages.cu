@@ -71,19 +71,24 @@ struct Counters {
     }
 };
 
+enum { EXTEND, FORK, EVICT };
+
 struct AllocArgs {
     gbs_kv_view c;
     const int *seqs, *other;                     // extend: sequences and counts; fork: targets and sources
     int n_items;
     int* status;
     unsigned mask;
+    // evict: tokens that a sequence keeps, their pages, and [n_items][keep_pages] numbers of pages for them
+    int keep, keep_pages;
+    int* fresh;
 };
 
 // What an item asks for: its status, the tokens it will have, its first new page and how many.
 struct Wish {
     int status, seq, length, first, need;
 };
-template <bool FORK>
+template <int WHAT>
 __device__ __forceinline__ Wish wish_of(const AllocArgs& A, const FirstOf& f, int i)
 {
     Wish w = {GBS_KV_BAD_INDEX, -1, 0, 0, 0};
@@ -94,7 +99,7 @@ __device__ __forceinline__ Wish wish_of(const AllocArgs& A, const FirstOf& f, in
         return w;
     }
     const int ps = 1 << A.c.page_log, have = kv_length(A.c, w.seq);
-    if (FORK) {
+    if (WHAT == FORK) {
         const int src = kv_sequence(A.c, A.other, i);
         if (src < 0) return w;
         if (have != 0) {
@@ -104,6 +109,8 @@ __device__ __forceinline__ Wish wish_of(const AllocArgs& A, const FirstOf& f, in
         w.length = kv_length(A.c, src);
         w.first = w.length >> A.c.page_log;
         w.need = (w.length & (ps - 1)) != 0;
+    } else if (WHAT == EVICT) {
+        if (have > A.keep) w.need = A.keep_pages;
     } else {
         const int count = A.other ? A.other[i] : 1;
         if (count < 0) return w;
@@ -120,12 +127,14 @@ __device__ __forceinline__ Wish wish_of(const AllocArgs& A, const FirstOf& f, in
 }
 
 // Shared memory: FirstOf's two arrays of mask + 1, then for each item where in the table page number 0 of the line of taken pages would be
-// entered for it, and how many pages the items before it want (at the end, its new length).
-template <bool FORK>
+// entered for it, and how many pages the items before it want (at the end, its new length).  Evict: the table is `fresh`, and lengths stay.
+template <int WHAT>
 __global__ __launch_bounds__(ONE) void k_kv_allocate(const __grid_constant__ AllocArgs A)
 {
     extern __shared__ __align__(8) int sm[];
     __shared__ int part[32];
+    int* const table = WHAT == EVICT ? A.fresh : A.c.page_table;
+    const auto row_of = [&](const Wish& x, int i) { return WHAT == EVICT ? (long long)i * A.keep_pages : (long long)x.seq * A.c.max_pages + x.first; };
     FirstOf f = {sm, sm + A.mask + 1, A.mask};
     const int tid = threadIdx.x, n = A.n_items;
     long long* entry = reinterpret_cast<long long*>(sm + 2 * (A.mask + 1));
@@ -145,8 +154,8 @@ __global__ __launch_bounds__(ONE) void k_kv_allocate(const __grid_constant__ All
     }
     __syncthreads();
     // nothing that a wish goes by changes before the end, so a thread's first one is kept
-    const Wish mine = wish_of<FORK>(A, f, min(tid, n - 1));
-    const auto wish = [&](int i) { return i == tid ? mine : wish_of<FORK>(A, f, i); };
+    const Wish mine = wish_of<WHAT>(A, f, min(tid, n - 1));
+    const auto wish = [&](int i) { return i == tid ? mine : wish_of<WHAT>(A, f, i); };
 
     // pages wanted before each item; more than the pool has need not be told apart
     int wanted = 0;
@@ -157,7 +166,7 @@ __global__ __launch_bounds__(ONE) void k_kv_allocate(const __grid_constant__ All
         const int at = wanted + block_prefix(min(w.need, 1 << 20), part, total);
         if (i < n) {
             before[i] = at;
-            entry[i] = (long long)w.seq * A.c.max_pages + w.first - at;
+            entry[i] = row_of(w, i) - at;
         }
         wanted = min(wanted + total, 0x3fffffff);
     }
@@ -182,7 +191,7 @@ __global__ __launch_bounds__(ONE) void k_kv_allocate(const __grid_constant__ All
             for (; free_bits && r < wanted; free_bits &= free_bits - 1, ++r) {
                 while (lo + 1 < n && before[lo + 1] <= r) ++lo;
                 const int page = p + __ffs(free_bits) - 1;
-                A.c.page_table[entry[lo] + r] = page;
+                table[entry[lo] + r] = page;
                 A.c.refs[page] = 1;
             }
         }
@@ -196,11 +205,12 @@ __global__ __launch_bounds__(ONE) void k_kv_allocate(const __grid_constant__ All
         if (w.status == GBS_KV_DONE && w.need > 0 && (long long)before[i] + w.need > found) {
             w.status = GBS_KV_NO_PAGES;
             for (int j = 0; j < w.need && before[i] + j < found; ++j)
-                A.c.refs[A.c.page_table[(long long)w.seq * A.c.max_pages + w.first + j]] = 0;
+                A.c.refs[table[row_of(w, i) + j]] = 0;
         }
         A.status[i] = w.status;
         before[i] = w.status == GBS_KV_DONE ? w.length : -1;
     }
+    if (WHAT == EVICT) return;
     __syncthreads();
     for (int i = tid; i < n; i += ONE)
         if (before[i] >= 0) A.c.lengths[i == tid ? mine.seq : kv_sequence(A.c, A.seqs, i)] = before[i];
@@ -351,31 +361,31 @@ constexpr unsigned table_mask(unsigned n_items)
 constexpr size_t table_bytes(unsigned n_items) { return (2 * ((size_t)table_mask(n_items) + 1) + 3 * (size_t)n_items) * sizeof(int); }
 static_assert(table_bytes(GBS_KV_MAX_ITEMS) + 1024 <= 227 * 1024, "one block's shared memory");
 
-int allocate(const gbs_plan* p, bool fork, const AllocArgs& A0, cudaStream_t stream)
+template <int WHAT>
+int allocate(const gbs_plan* p, const AllocArgs& A0, cudaStream_t stream)
 {
     AllocArgs A = A0;
     A.mask = table_mask((unsigned)A.n_items);
     const size_t smem = table_bytes((unsigned)A.n_items);
-    const void* f = fork ? (const void*)k_kv_allocate<true> : (const void*)k_kv_allocate<false>;
     if (smem > 48 * 1024) {
         // the limit is the function's, for all threads of the process: always the same one, since a smaller call's may come between another's and its launch
-        const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)table_bytes(GBS_KV_MAX_ITEMS));
+        const cudaError_t e = cudaFuncSetAttribute((const void*)k_kv_allocate<WHAT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)table_bytes(GBS_KV_MAX_ITEMS));
         if (e != cudaSuccess) return (int)e;
     }
-    return gbs_kv_launch(p, fork ? k_kv_allocate<true> : k_kv_allocate<false>, dim3(1), ONE, smem, stream, A);
+    return gbs_kv_launch(p, k_kv_allocate<WHAT>, dim3(1), ONE, smem, stream, A);
 }
 
 }  // namespace
 
 int gbs_kv_extend_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, const int* counts, int n_items, int* status, cudaStream_t stream)
 {
-    return allocate(p, false, {c, seqs, counts, n_items, status, 0}, stream);
+    return allocate<EXTEND>(p, {c, seqs, counts, n_items, status, 0}, stream);
 }
 
 int gbs_kv_fork_launch(const gbs_plan* p, const gbs_kv_view& c, const int* src, const int* dst, int n_items, int* status, cudaStream_t stream)
 {
     const AllocArgs A = {c, dst, src, n_items, status, 0};
-    const int e = allocate(p, true, A, stream);
+    const int e = allocate<FORK>(p, A, stream);
     if (e != 0) return e;
     return gbs_kv_launch(p, k_kv_share, dim3((unsigned)n_items, (unsigned)c.heads), PART, 0, stream, A);
 }
@@ -392,4 +402,14 @@ int gbs_kv_compact_launch(const gbs_plan* p, const gbs_kv_view& c, const gbs_kv_
     const int e = gbs_kv_launch(p, k_kv_number, dim3(1), ONE, 0, stream, A);
     if (e != 0) return e;
     return gbs_kv_launch(p, k_kv_move, dim3((unsigned)(p->sm_count * 8)), COPY, 0, stream, A);
+}
+
+int gbs_kv_evict_pages_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, int keep, int keep_pages, int* fresh, int* status,
+                              cudaStream_t stream)
+{
+    AllocArgs A = {c, seqs, nullptr, n_items, status, 0};
+    A.keep = keep;
+    A.keep_pages = keep_pages;
+    A.fresh = fresh;
+    return allocate<EVICT>(p, A, stream);
 }

@@ -15,8 +15,8 @@
 namespace {
 
 // What an attention kernel's entries are: tiles of the items over all that they see; tiles of groups of items over the prefix that a group's
-// sequences have in common; or tiles of the items over what they see behind that.
-enum KvPart { KV_WHOLE, KV_PREFIX, KV_OWN };
+// sequences have in common; or tiles of the items over what they see behind that; or the items' sequences from end to end.
+enum KvPart { KV_WHOLE, KV_PREFIX, KV_OWN, KV_ALL };
 
 // One (item, tile): where its rows and its part of the cache are.
 struct KvEntry {
@@ -91,6 +91,10 @@ __device__ __forceinline__ KvEntry kv_entry(const gbs_kv_attn& A, const KvLine& 
     const int last = min(e.rows, e.row0 + L.tile_rows) - 1;
     e.hi = kv_row_hi(A, e, A.by_group(last));
     e.lo = PART == KV_OWN ? A.shared[item] : kv_row_lo(A, e, A.by_group(e.row0));
+    if (PART == KV_ALL) {
+        e.lo = 0;
+        e.hi = length;
+    }
     // a tile that sees nothing is one unit too: its rows become 0
     e.units = 1;
     if (e.hi > e.lo) e.units = ((e.hi - 1) >> L.unit_log) - (e.lo >> L.unit_log) + 1;

@@ -564,6 +564,69 @@ PyObject* do_kv_shared_attention(const Pool& p, const PlanRef& ref, PyObject* co
     GBS_END
 }
 
+// weights of cached tokens: [sequences, KV heads, width] in fp32; *width: what it has, or has to have if it is not 0
+bool weights_of(const Pool& p, PyObject* o, float** out, int64_t* width)
+{
+    const at::Tensor* t = cuda_tensor(o);
+    if (!t || t->scalar_type() != at::kFloat || t->dim() != 3 || !t->is_contiguous() || t->device().index() != p.device) return false;
+    if (t->size(0) != p.cache.n_seqs || t->size(1) != p.cache.n_kv_heads || t->size(2) < 1 || (*width && t->size(2) != *width)) return false;
+    *width = t->size(2);
+    *out = static_cast<float*>(t->data_ptr());
+    return true;
+}
+
+// q, mass, seqs, cu_tokens, max_tokens, decay, base, causal, window, scale, stream
+PyObject* do_kv_attention_mass(const Pool& p, const PlanRef& ref, PyObject* const* g)
+{
+    GBS_BEGIN
+    Rows q;
+    Items it;
+    int most, window;
+    int64_t width = 0;
+    float *mass, *base;
+    if (!none(g[10]) || !rows3_of(p, g[0], ref.info.d, &q) || !items_of(p, g[2], g[3], q.n, &it)) Py_RETURN_NONE;
+    if (!weights_of(p, g[1], &mass, &width) || !weights_of(p, none(g[6]) ? g[1] : g[6], &base, &width)) Py_RETURN_NONE;
+    if (q.n > 0x7fffffff || !int_of(none(g[4]) ? nullptr : g[4], none(g[3]) ? 1 : static_cast<int>(std::max<int64_t>(1, q.n)), &most) || !int_of(g[8], 0, &window)) Py_RETURN_NONE;
+    const int causal = g[7] ? PyObject_IsTrue(g[7]) : 1;
+    const double decay = g[5] ? PyFloat_AsDouble(g[5]) : 1.0, scale = g[9] ? PyFloat_AsDouble(g[9]) : 0.0;
+    if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+    const int n = static_cast<int>(it.n);
+    int64_t need;
+    if (q.heads > 0x7fffffff || gbs_kv_attention_mass_workspace(ref.plan, &p.cache, n, q.n, most, static_cast<int>(q.heads), &need) != GBS_OK) Py_RETURN_NONE;
+    at::Tensor work = at::detail::empty_cuda({need}, at::kByte, device_of(p), std::nullopt);
+    if (gbs_kv_attention_mass(ref.plan, &p.cache, it.seqs, it.cu, n, q.n, most, q.ptr, q.token, q.head, static_cast<int>(q.heads), static_cast<float>(scale),
+                              window, causal ? GBS_KV_CAUSAL : 0, base, static_cast<float>(decay), mass, width, work.data_ptr(), need, stream_on(p)) != GBS_OK)
+        Py_RETURN_NONE;
+    return Py_NewRef(g[1]);
+    GBS_END
+}
+
+// mass, keep, seqs, recent, first, into, stream
+PyObject* do_kv_evict(const Pool& p, const PlanRef& ref, PyObject* const* g)
+{
+    GBS_BEGIN
+    int keep, recent, first;
+    int64_t width = 0, need;
+    float *mass, *into;
+    const int32_t* seqs;
+    const int64_t n = none(g[2]) ? p.cache.n_seqs : length_of(g[2]);
+    if (!none(g[6]) || n < 0 || n > GBS_KV_MAX_ITEMS || !ints_of(p, g[2], n, &seqs)) Py_RETURN_NONE;
+    if (!weights_of(p, g[0], &mass, &width) || !weights_of(p, none(g[5]) ? g[0] : g[5], &into, &width)) Py_RETURN_NONE;
+    if (!int_of(g[1], 0, &keep) || !int_of(g[3], 0, &recent) || !int_of(g[4], 0, &first)) Py_RETURN_NONE;
+    if (gbs_kv_evict_workspace(ref.plan, &p.cache, static_cast<int>(n), keep, &need) != GBS_OK) Py_RETURN_NONE;
+    at::Tensor status = ints(p, n), kept = at::detail::empty_cuda({n, p.cache.n_kv_heads, keep}, at::kInt, device_of(p), std::nullopt);
+    at::Tensor work = at::detail::empty_cuda({need}, at::kByte, device_of(p), std::nullopt);
+    if (gbs_kv_evict(ref.plan, &p.cache, seqs, static_cast<int>(n), keep, recent, first, mass, into, width, static_cast<int32_t*>(kept.data_ptr()),
+                     static_cast<int32_t*>(status.data_ptr()), work.data_ptr(), need, stream_on(p)) != GBS_OK)
+        Py_RETURN_NONE;
+    PyObject* t = PyTuple_New(2);
+    if (!t) return nullptr;
+    PyTuple_SET_ITEM(t, 0, THPVariable_Wrap(std::move(status)));
+    PyTuple_SET_ITEM(t, 1, THPVariable_Wrap(std::move(kept)));
+    return t;
+    GBS_END
+}
+
 PyObject* do_kv_compact(const Pool& p, const PlanRef& ref, PyObject* const* g)       // into, page_map, stream
 {
     GBS_BEGIN
@@ -585,7 +648,7 @@ PyObject* do_kv_compact(const Pool& p, const PlanRef& ref, PyObject* const* g)  
 }
 
 // A method: the names of its arguments in the class's order, how many must be given, and what to do with them; `on_pool` is for KVCache.
-constexpr int MOST_ARGS = 10;
+constexpr int MOST_ARGS = 11;
 struct Method {
     const char* name;
     int count, required;
@@ -604,6 +667,9 @@ constexpr Method KV_ATTENTION = {"attention", 10, 1, {"q", "seqs", "cu_tokens", 
                                  nullptr, do_kv_attention};
 constexpr Method KV_SHARED = {"shared_attention", 10, 1, {"q", "seqs", "cu_tokens", "groups", "max_tokens", "causal", "scale", "max_own", "out", "stream"},
                               nullptr, do_kv_shared_attention};
+constexpr Method KV_MASS = {"attention_mass", 11, 2, {"q", "mass", "seqs", "cu_tokens", "max_tokens", "decay", "base", "causal", "window", "scale", "stream"},
+                            nullptr, do_kv_attention_mass};
+constexpr Method KV_EVICT = {"evict", 7, 2, {"mass", "keep", "seqs", "recent", "first", "into", "stream"}, nullptr, do_kv_evict};
 
 PyObject* or_none(PyObject* o) { return o ? o : Py_None; }
 
@@ -718,7 +784,7 @@ void method_dealloc(PyObject* self)
     Py_DECREF(type);
 }
 PyTypeObject* method_type = nullptr;
-const Method* const METHODS[] = {&ROTATE, &DEQUANTIZE, &MATMUL, &CLIP, &KV_EXTEND, &KV_FORK, &KV_FREE, &KV_COMPACT, &KV_APPEND, &KV_READ, &KV_ATTENTION, &KV_SHARED};
+const Method* const METHODS[] = {&ROTATE, &DEQUANTIZE, &MATMUL, &CLIP, &KV_EXTEND, &KV_FORK, &KV_FREE, &KV_COMPACT, &KV_APPEND, &KV_READ, &KV_ATTENTION, &KV_SHARED, &KV_MASS, &KV_EVICT};
 
 PyObject* make_method(PyObject*, PyObject* args)
 {
