@@ -467,11 +467,18 @@ int launch(const gbs_plan* p, const MassArgs& P, cudaStream_t stream)
 
 }  // namespace
 
-int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A) { return layout_of(p, A).bytes; }
+namespace {
+
+bool many(const gbs_kv_attn& A) { return std::min<int64_t>(A.max_tokens, A.n_tokens) * A.group > GBS_KV_MASS_FEW_ROWS; }
+
+}  // namespace
+
+int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A) { return many(A) ? gbs_tc_kvmass_workspace(p, A) : layout_of(p, A).bytes; }
 
 int gbs_kv_mass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* base, float decay, float* mass, int64_t width, void* workspace,
                        cudaStream_t stream)
 {
+    if (many(A)) return gbs_tc_kvmass_launch(p, A, base, decay, mass, width, workspace, stream);
     const Layout l = layout_of(p, A);
     unsigned char* w = static_cast<unsigned char*>(workspace);
     MassArgs P = {};
