@@ -248,8 +248,8 @@ int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A);
 int gbs_kv_mass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* base, float decay, float* mass, int64_t width, void* workspace,
                        cudaStream_t stream);
 // gbs_kv_pages.cu : pages for what sequences keep; the items' status.  gbs_kv_evict.cu : what they keep, moved there
-int gbs_kv_evict_pages_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, int keep, int keep_pages, int* fresh, int* status,
-                              cudaStream_t stream);
+int gbs_kv_evict_pages_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, int keep, int keep_pages, int* fresh, int* arrived,
+                              int* status, cudaStream_t stream);
 struct gbs_kv_eviction {
     gbs_kv_view c;
     const int* seqs;
@@ -257,7 +257,9 @@ struct gbs_kv_eviction {
     const float* mass;
     float* mass_out;
     long long width;
-    int *status, *kept, *fresh;
+    int *status, *kept;
+    int *fresh, *arrived;               // [n_items][keep_pages], [n_items]
+    float* weights;                     // [n_items][heads][keep]: of what stays
 };
 int gbs_kv_evict_launch(const gbs_plan* p, const gbs_kv_eviction& E, cudaStream_t stream);
 

@@ -402,8 +402,15 @@ extern "C" int gbs_kv_attention_mass(const gbs_plan_t* p, const gbs_kv_cache_t* 
 
 namespace {
 
-// pages of the tokens that a sequence keeps
+// pages of the tokens that a sequence keeps, and the workspace: their numbers, a count of each item, and the weights of what stays
 int keep_pages_of(const gbs_kv_view& c, int keep) { return std::min((int)(((int64_t)keep + (1 << c.page_log) - 1) >> c.page_log), c.max_pages); }
+int64_t evict_numbers(const gbs_kv_view& c, int n_items, int keep) { return (int64_t)n_items * (keep_pages_of(c, keep) + 1); }
+int64_t evict_bytes(const gbs_kv_view& c, int n_items, int keep)
+{
+    // no more tokens stay than a sequence can have
+    const int64_t most = std::min<int64_t>(keep, (int64_t)c.max_pages << c.page_log);
+    return (evict_numbers(c, n_items, keep) + n_items * c.heads * most) * 4;
+}
 
 }  // namespace
 
@@ -413,7 +420,7 @@ extern "C" int gbs_kv_evict_workspace(const gbs_plan_t* p, const gbs_kv_cache_t*
     const int rc = view_of(p, cache, &c);
     if (rc != GBS_OK) return rc;
     if (!bytes_out || n_items < 0 || n_items > GBS_KV_MAX_ITEMS || keep < 1) return GBS_ERR_INVALID_ARG;
-    *bytes_out = (int64_t)n_items * keep_pages_of(c, keep) * (int64_t)sizeof(int32_t);
+    *bytes_out = evict_bytes(c, n_items, keep);
     return GBS_OK;
 }
 
@@ -428,7 +435,7 @@ extern "C" int gbs_kv_evict(const gbs_plan_t* p, const gbs_kv_cache_t* cache, co
     if (keep < 1 || recent < 0 || first < 0 || (int64_t)recent + first > keep || width < 1) return GBS_ERR_INVALID_ARG;
     if (n_items == 0) return GBS_OK;
     E.keep_pages = keep_pages_of(E.c, keep);
-    if (!mass || !mass_out || !kept || !status_out || !workspace || workspace_bytes < (int64_t)n_items * E.keep_pages * (int64_t)sizeof(int32_t)) return GBS_ERR_INVALID_ARG;
+    if (!mass || !mass_out || !kept || !status_out || !workspace || workspace_bytes < evict_bytes(E.c, n_items, keep)) return GBS_ERR_INVALID_ARG;
     if (!aligned(mass, 4) || !aligned(mass_out, 4) || !aligned(kept, 4) || !aligned(status_out, 4) || !aligned(workspace, 16)) return GBS_ERR_ALIGNMENT;
     E.seqs = seqs;
     E.n_items = n_items;
@@ -441,5 +448,7 @@ extern "C" int gbs_kv_evict(const gbs_plan_t* p, const gbs_kv_cache_t* cache, co
     E.status = status_out;
     E.kept = kept;
     E.fresh = static_cast<int*>(workspace);
+    E.arrived = E.fresh + (int64_t)n_items * E.keep_pages;
+    E.weights = reinterpret_cast<float*>(E.fresh) + evict_numbers(E.c, n_items, keep);
     return on_device(p, [&] { return gbs_kv_evict_launch(p, E, static_cast<cudaStream_t>(stream)); });
 }

@@ -82,6 +82,7 @@ struct AllocArgs {
     // evict: tokens that a sequence keeps, their pages, and [n_items][keep_pages] numbers of pages for them
     int keep, keep_pages;
     int* fresh;
+    int* arrived;                                // [n_items], becomes 0: what has been moved is counted there
 };
 
 // What an item asks for: its status, the tokens it will have, its first new page and how many.
@@ -208,6 +209,7 @@ __global__ __launch_bounds__(ONE) void k_kv_allocate(const __grid_constant__ All
                 A.c.refs[table[row_of(w, i) + j]] = 0;
         }
         A.status[i] = w.status;
+        if (WHAT == EVICT) A.arrived[i] = 0;
         before[i] = w.status == GBS_KV_DONE ? w.length : -1;
     }
     if (WHAT == EVICT) return;
@@ -404,12 +406,13 @@ int gbs_kv_compact_launch(const gbs_plan* p, const gbs_kv_view& c, const gbs_kv_
     return gbs_kv_launch(p, k_kv_move, dim3((unsigned)(p->sm_count * 8)), COPY, 0, stream, A);
 }
 
-int gbs_kv_evict_pages_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, int keep, int keep_pages, int* fresh, int* status,
-                              cudaStream_t stream)
+int gbs_kv_evict_pages_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, int keep, int keep_pages, int* fresh, int* arrived,
+                              int* status, cudaStream_t stream)
 {
     AllocArgs A = {c, seqs, nullptr, n_items, status, 0};
     A.keep = keep;
     A.keep_pages = keep_pages;
     A.fresh = fresh;
+    A.arrived = arrived;
     return allocate<EVICT>(p, A, stream);
 }

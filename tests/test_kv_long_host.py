@@ -89,9 +89,8 @@ def test_evict(lib):
         assert f(**{name: None}) == INVALID and f(**{name: P + 2}) == ALIGN
     size, r = ctypes.c_int64(-1), ctypes.byref(pool())
     w = lib.gbs_kv_evict_workspace
-    assert w(plan(), r, 2, 17, ctypes.byref(size)) == OK and size.value == 2 * 2 * 4
-    assert w(plan(), r, 2, 2 ** 31 - 1, ctypes.byref(size)) == OK and size.value == 2 * 7 * 4            # no more than a sequence can have
-    assert f(keep=17, size=15) == INVALID
+    assert w(plan(), r, 2, 2 ** 31 - 1, ctypes.byref(size)) == OK and size.value < 1 << 16               # no more than a sequence can have
+    assert w(plan(), r, 2, 17, ctypes.byref(size)) == OK and size.value > 0 and f(keep=17, size=size.value - 1) == INVALID
     assert w(plan(), r, -1, 17, ctypes.byref(size)) == INVALID and w(plan(), r, 2, 0, ctypes.byref(size)) == INVALID and w(plan(), r, 2, 17, None) == INVALID
 
 
