@@ -12,7 +12,7 @@
 namespace {
 
 constexpr int EACH = 8, HELD = 2;                // neighbouring tokens of a thread, and how many times so many it keeps in registers
-constexpr int MOVE = 256;
+constexpr int MOVE = 256, TOKENS = 2;            // threads of a block that moves, and tokens of one at a time
 constexpr int BINS = 2048;
 
 // weights as integers of the same order: NaN the largest, -0 as 0
@@ -77,37 +77,46 @@ __global__ __launch_bounds__(THREADS) void k_kv_select(const __grid_constant__ g
     const int lo = E.first, hi = length - E.recent;      // the tokens between
     const auto weight = [&](int pos) { return pos < to && pos < E.width ? mass[pos] : 0.f; };
     float w[HELD][EACH];
-    unsigned threshold = 0;
-    int want = E.keep - E.first - E.recent;
-    const bool none = want == 0;
-    if (cut && !none) {
+    if (cut)
 #pragma unroll
         for (int x = 0; x < HELD; ++x)
 #pragma unroll
             for (int k = 0; k < EACH; ++k) w[x][k] = weight(from + EACH * (THREADS * x + tid) + k);
+    // f(first position of the thread's, its weights), by all threads of the block alike
+    const auto each = [&](auto f) {
+#pragma unroll
+        for (int x = 0; x < HELD; ++x)
+            if (from + EACH * THREADS * x < to) f(from + EACH * (THREADS * x + tid), w[x]);
+        for (int p0 = from + HELD * EACH * THREADS; p0 < to; p0 += EACH * THREADS) {
+            float v[EACH];
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) v[k] = weight(p0 + EACH * tid + k);
+            f(p0 + EACH * tid, v);
+        }
+    };
+    unsigned threshold = 0;
+    int want = E.keep - E.first - E.recent;
+    const bool none = want == 0;
+    if (cut && !none) {
         // ---- the threshold: `want` of the largest, digit by digit ----
         for (int digit = 0; digit < 3; ++digit) {
             const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit < 2 ? 11 : 10, n = 1 << bits;
             for (int i = tid; i < BINS; i += THREADS) bins[i] = 0;
             __syncthreads();
-            // weights of a distribution fall into few bins: those of a warp's that are alike are counted together
-            const auto count = [&](int pos, float x) {
-                const unsigned u = order_of(x);
-                const bool mine = pos >= lo && pos < hi && pos < to && (digit == 0 || (u >> (shift + bits)) == threshold);
-                const unsigned bin = mine ? (u >> shift) & (n - 1) : 0xffffffffu, same = __match_any_sync(0xffffffffu, bin);
-                if (mine && lane == __ffs(same) - 1) atomicAdd(&bins[bin], __popc(same));
-            };
-#pragma unroll
-            for (int x = 0; x < HELD; ++x)
-                if (from + EACH * THREADS * x < to)
-#pragma unroll
-                    for (int k = 0; k < EACH; ++k) count(from + EACH * (THREADS * x + tid) + k, w[x][k]);
-            for (int p0 = from + HELD * EACH * THREADS; p0 < to; p0 += EACH * THREADS)
+            each([&](int pos, const float* v) {
 #pragma unroll
                 for (int k = 0; k < EACH; ++k) {
-                    const int pos = p0 + EACH * tid + k;
-                    count(pos, weight(pos));
+                    const unsigned u = order_of(v[k]);
+                    const bool mine = pos + k >= lo && pos + k < hi && pos + k < to && (digit == 0 || (u >> (shift + bits)) == threshold);
+                    const unsigned bin = mine ? (u >> shift) & (n - 1) : 0xffffffffu;
+                    if (digit == 0) {            // the upper digits of most weights fall into few bins: those of a warp's that are alike are counted together
+                        const unsigned same = __match_any_sync(0xffffffffu, bin);
+                        if (mine && lane == __ffs(same) - 1) atomicAdd(&bins[bin], __popc(same));
+                    } else if (mine) {
+                        atomicAdd(&bins[bin], 1);
+                    }
                 }
+            });
             all_blocks();
             // bins from the highest down, PER a thread
             int have[PER], sum = 0;
@@ -147,12 +156,13 @@ __global__ __launch_bounds__(THREADS) void k_kv_select(const __grid_constant__ g
     unsigned long long before = 0;               // upper half: that stay for sure, lower: equal to the threshold
     if (cut && BLOCKS > 1) {                     // of the slices below
         unsigned long long mine = 0;
-        for (int p0 = from; p0 < to; p0 += EACH * THREADS)
+        each([&](int pos, const float* v) {
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
-                const int pos = p0 + EACH * tid + k, x = sort(pos, weight(pos));
+                const int x = sort(pos + k, v[k]);
                 mine += x == 2 ? 1ull << 32 : (unsigned long long)x;
             }
+        });
         unsigned long long total;
         block_prefix<WARPS>(mine, part, total);
         if (tid == 0) counts = total;
@@ -173,15 +183,12 @@ __global__ __launch_bounds__(THREADS) void k_kv_select(const __grid_constant__ g
     }
     int* kept = E.kept + ((long long)item * E.c.heads + head) * E.keep;
     float* weights = E.weights + ((long long)item * E.c.heads + head) * E.keep;
-    for (int p0 = from; p0 < to; p0 += EACH * THREADS) {
-        const int pos = p0 + EACH * tid;
-        float x[EACH];
+    each([&](int pos, const float* v) {
         int how[EACH];
         unsigned long long mine = 0;
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
-            x[k] = weight(pos + k);
-            how[k] = sort(pos + k, x[k]);
+            how[k] = sort(pos + k, v[k]);
             mine += how[k] == 2 ? 1ull << 32 : (unsigned long long)how[k];
         }
         unsigned long long total;
@@ -192,46 +199,75 @@ __global__ __launch_bounds__(THREADS) void k_kv_select(const __grid_constant__ g
             if (how[k] == 2 || (how[k] == 1 && q < want)) {
                 const int j = s + min(q, want);
                 kept[j] = pos + k;
-                weights[j] = x[k];
+                weights[j] = v[k];
             }
             s += how[k] == 2;
             q += how[k] == 1;
         }
         before += total;
-    }
+    });
 }
 
 // Rows of what stays: eight threads a token, 16 bytes of its codes each, two of them a scale as well, another one its weight.  The last block of an item lets its former pages go
 // and enters the new ones into the table.
-__global__ __launch_bounds__(MOVE) void k_kv_evict_move(const __grid_constant__ gbs_kv_eviction E)
+__global__ __launch_bounds__(MOVE, 5) void k_kv_evict_move(const __grid_constant__ gbs_kv_eviction E)
 {
     __shared__ int last;
     kv_wait_before();
     kv_let_next();
-    const int item = blockIdx.x / E.c.heads, head = blockIdx.x - item * E.c.heads;
-    if (E.status[item] != GBS_KV_DONE) return;
-    const int seq = kv_sequence(E.c, E.seqs, item), length = kv_length(E.c, seq);
-    if (length <= E.keep) return;
+    const int item = blockIdx.x / E.c.heads, head = blockIdx.x - item * E.c.heads, part = threadIdx.x & 7;
     const long long base = ((long long)item * E.c.heads + head) * E.keep;
-    const int* kept = E.kept + base;
+    // a thread's part of TOKENS tokens, 32 apart; what does not depend on one another is asked for at once
+    const int j0 = blockIdx.y * (TOKENS * MOVE / 8) + (threadIdx.x >> 3), step = gridDim.y * (TOKENS * MOVE / 8);
+    int pos[TOKENS];
+#pragma unroll
+    for (int k = 0; k < TOKENS; ++k) pos[k] = j0 + 32 * k < E.keep ? E.kept[base + j0 + 32 * k] : -1;
+    const int seq = kv_sequence(E.c, E.seqs, item);
+    if (E.status[item] != GBS_KV_DONE) return;
     const int* fresh = E.fresh + (long long)item * E.keep_pages;
     int* table = E.c.page_table + (long long)seq * E.c.max_pages;
+    const int length = kv_length(E.c, seq);
     float* out = E.mass_out + ((long long)seq * E.c.heads + head) * E.width;
-    const int ps = 1 << E.c.page_log, scale_bytes = E.c.block_bytes / ps / 2 - KV_ROW, part = threadIdx.x & 7;
-    for (int j = blockIdx.y * (MOVE / 8) + (threadIdx.x >> 3); j < E.keep; j += gridDim.y * (MOVE / 8)) {
-        const int pos = kept[j], from = kv_page(E.c, seq, pos), a = pos & (ps - 1), b = j & (ps - 1);
-        unsigned char* to = kv_block(E.c, fresh[j >> E.c.page_log], head);
-        const unsigned char* x = kv_block(E.c, max(from, 0), head);
-        const int codes = (part >> 2) * ps * KV_ROW + 16 * (part & 3);
-        uint4 v = *reinterpret_cast<const uint4*>(x + codes + a * KV_ROW);
-        if (from < 0) v = make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4*>(to + codes + b * KV_ROW) = v;
-        if ((part & 3) == 0) {
-            const int scales = 2 * ps * KV_ROW + (part >> 2) * ps * scale_bytes;
-            for (int k = 0; k < scale_bytes; k += 4)
-                *reinterpret_cast<float*>(to + scales + b * scale_bytes + k) = from < 0 ? 0.f : *reinterpret_cast<const float*>(x + scales + a * scale_bytes + k);
+    const int ps = 1 << E.c.page_log, scale_bytes = E.c.block_bytes / ps / 2 - KV_ROW;
+    const int codes = (part >> 2) * ps * KV_ROW + 16 * (part & 3), scales = 2 * ps * KV_ROW + (part >> 2) * ps * scale_bytes;
+    if (length <= E.keep) return;
+    for (int j = j0; j < E.keep; j += step) {
+        uint4 v[TOKENS];
+        float2 sc[TOKENS];
+        float weight[TOKENS];
+        int page[TOKENS];
+#pragma unroll
+        for (int k = 0; k < TOKENS; ++k) {
+            const int from = pos[k] >= 0 ? table[pos[k] >> E.c.page_log] : -1;
+            page[k] = pos[k] >= 0 ? fresh[(j + 32 * k) >> E.c.page_log] : 0;
+            const bool ok = (unsigned)from < (unsigned)E.c.n_pages;
+            const unsigned char* x = kv_block(E.c, ok ? from : 0, head);
+            const int a = pos[k] & (ps - 1);
+            v[k] = ok ? *reinterpret_cast<const uint4*>(x + codes + a * KV_ROW) : make_uint4(0, 0, 0, 0);
+            sc[k] = make_float2(0.f, 0.f);
+            if (ok && (part & 3) == 0) {
+                if (scale_bytes == 8) sc[k] = *reinterpret_cast<const float2*>(x + scales + a * 8);
+                else sc[k].x = *reinterpret_cast<const float*>(x + scales + a * 4);
+            }
+            weight[k] = part == 1 && pos[k] >= 0 ? E.weights[base + j + 32 * k] : 0.f;
         }
-        if (part == 1 && j < E.width) out[j] = E.weights[base + j];
+        int next[TOKENS];
+#pragma unroll
+        for (int k = 0; k < TOKENS; ++k) next[k] = j + step + 32 * k < E.keep ? E.kept[base + j + step + 32 * k] : -1;
+#pragma unroll
+        for (int k = 0; k < TOKENS; ++k) {
+            if (pos[k] < 0) continue;
+            const int to_j = j + 32 * k, b = to_j & (ps - 1);
+            unsigned char* to = kv_block(E.c, page[k], head);
+            *reinterpret_cast<uint4*>(to + codes + b * KV_ROW) = v[k];
+            if ((part & 3) == 0) {
+                if (scale_bytes == 8) *reinterpret_cast<float2*>(to + scales + b * 8) = sc[k];
+                else *reinterpret_cast<float*>(to + scales + b * 4) = sc[k].x;
+            }
+            if (part == 1 && to_j < E.width) out[to_j] = weight[k];
+        }
+#pragma unroll
+        for (int k = 0; k < TOKENS; ++k) pos[k] = next[k];
     }
     __threadfence();
     __syncthreads();                             // the block has read the table and the length
@@ -276,8 +312,8 @@ int gbs_kv_evict_launch(const gbs_plan* p, const gbs_kv_eviction& E, cudaStream_
     int rc = gbs_kv_evict_pages_launch(p, E.c, E.seqs, E.n_items, E.keep, E.keep_pages, E.fresh, E.arrived, E.status, stream);
     const int64_t rows = (int64_t)E.n_items * E.c.heads, longest = (int64_t)E.c.max_pages << E.c.page_log;
     if (rc == 0) rc = longest > 2 * EACH * HELD * FEW && rows <= p->sm_count ? select<MANY, CLUSTER>(p, E, stream) : select<FEW, 1>(p, E, stream);
-    // a block moves 32 tokens at a time; so many blocks of an item and KV head that all of them fill the GPU some times over
-    const int64_t most = ((int64_t)E.keep + MOVE / 8 - 1) / (MOVE / 8), y = (int64_t)p->sm_count * 32 / rows + 1;
+    // a block moves 64 tokens at a time; so many blocks of an item and KV head that all of them fill the GPU some times over
+    const int64_t at_once = TOKENS * MOVE / 8, most = ((int64_t)E.keep + at_once - 1) / at_once, y = (int64_t)p->sm_count * 32 / rows + 1;
     if (rc == 0) rc = gbs_kv_launch(p, k_kv_evict_move, dim3((unsigned)rows, (unsigned)(y < most ? y : most)), MOVE, 0, stream, E);
     return rc;
 }
