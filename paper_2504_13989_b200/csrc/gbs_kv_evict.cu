@@ -12,7 +12,7 @@
 namespace {
 
 constexpr int EACH = 8, HELD = 2;                // neighbouring tokens of a thread, and how many times so many it keeps in registers
-constexpr int MOVE = 256, TOKENS = 2;            // threads of a block that moves, and tokens of one at a time
+constexpr int MOVE = 256;                        // tokens that a block moves, and its threads
 constexpr int BINS = 2048;
 
 // weights as integers of the same order: NaN the largest, -0 as 0
@@ -50,23 +50,22 @@ __device__ __forceinline__ unsigned long long block_prefix(unsigned long long v,
 // A block, or a cluster of eight, per item and KV head.  A thread has EACH neighbouring tokens of every EACH * THREADS of its block's slice.  What it reads
 // was written by launches that had ended before the one before it, which looks for pages, let it begin; only that one's status is waited for.
 template <int THREADS, int BLOCKS>
-__global__ __launch_bounds__(THREADS) void k_kv_select(const __grid_constant__ gbs_kv_eviction E)
+__global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(const __grid_constant__ gbs_kv_eviction E)
 {
     namespace cg = cooperative_groups;
     constexpr int PER = BINS / THREADS, WARPS = THREADS / 32;
-    __shared__ int bins[BINS];
+    static_assert(HELD == 2 && EACH * THREADS < 1 << 16, "four counts in 64 bits");
+    __shared__ int bins[BINS], all[BLOCKS > 1 ? 2 : 1][BLOCKS > 1 ? BINS : 1];       // of the block; of the cluster, digit by digit in turn
     __shared__ unsigned long long part[WARPS];
     __shared__ int found[2];                     // the bin, and how many of it stay
-    __shared__ unsigned long long counts;        // of the slice: tokens that stay for sure, and those equal to the threshold
+    __shared__ int above_threshold, at_threshold;        // of the slice's tokens between
+    __shared__ long long slices[BLOCKS];         // of each block: tokens that stay for sure (upper half), and that are equal to the threshold
     const int tid = threadIdx.x, lane = tid & 31, rank = BLOCKS > 1 ? (int)cg::this_cluster().block_rank() : 0;
     const int row_of = blockIdx.x / BLOCKS, item = row_of / E.c.heads, head = row_of - item * E.c.heads;
     const auto all_blocks = [&] {
         if (BLOCKS > 1) cg::this_cluster().sync();
         else __syncthreads();
     };
-    // of a block of the cluster
-    const auto bins_of = [&](int r) { return BLOCKS > 1 ? cg::this_cluster().map_shared_rank(bins, r) : bins; };
-    const auto counts_of = [&](int r) { return BLOCKS > 1 ? *cg::this_cluster().map_shared_rank(&counts, r) : counts; };
 
     const int seq = kv_sequence(E.c, E.seqs, item), length = seq < 0 ? 0 : kv_length(E.c, seq);
     const bool cut = length > E.keep;
@@ -76,70 +75,92 @@ __global__ __launch_bounds__(THREADS) void k_kv_select(const __grid_constant__ g
     const int per = ((length + BLOCKS - 1) / BLOCKS + EACH - 1) / EACH * EACH, from = min(rank * per, length), to = min(from + per, length);
     const int lo = E.first, hi = length - E.recent;      // the tokens between
     const auto weight = [&](int pos) { return pos < to && pos < E.width ? mass[pos] : 0.f; };
-    float w[HELD][EACH];
-    if (cut)
+    // a token between as a number above 0; 0: one that is not
+    const auto key_of = [&](int pos, float x) { return pos >= lo && pos < hi && pos < to ? order_of(x) : 0u; };
+    unsigned u[HELD][EACH];
+    if (cut) {
+        float w[HELD][EACH];
 #pragma unroll
         for (int x = 0; x < HELD; ++x)
 #pragma unroll
             for (int k = 0; k < EACH; ++k) w[x][k] = weight(from + EACH * (THREADS * x + tid) + k);
-    // f(first position of the thread's, its weights), by all threads of the block alike
-    const auto each = [&](auto f) {
 #pragma unroll
         for (int x = 0; x < HELD; ++x)
-            if (from + EACH * THREADS * x < to) f(from + EACH * (THREADS * x + tid), w[x]);
-        for (int p0 = from + HELD * EACH * THREADS; p0 < to; p0 += EACH * THREADS) {
-            float v[EACH];
 #pragma unroll
-            for (int k = 0; k < EACH; ++k) v[k] = weight(p0 + EACH * tid + k);
-            f(p0 + EACH * tid, v);
-        }
-    };
+            for (int k = 0; k < EACH; ++k) u[x][k] = key_of(from + EACH * (THREADS * x + tid) + k, w[x][k]);
+    }
+    const int beyond = from + HELD * EACH * THREADS;     // tokens that are fetched again each time
     unsigned threshold = 0;
     int want = E.keep - E.first - E.recent;
     const bool none = want == 0;
     if (cut && !none) {
+        if (BLOCKS > 1)
+            for (int i = tid; i < BINS; i += THREADS) all[0][i] = 0;
+        if (tid == 0) above_threshold = 0;
         // ---- the threshold: `want` of the largest, digit by digit ----
         for (int digit = 0; digit < 3; ++digit) {
             const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit < 2 ? 11 : 10, n = 1 << bits;
             for (int i = tid; i < BINS; i += THREADS) bins[i] = 0;
-            __syncthreads();
-            each([&](int pos, const float* v) {
+            if (BLOCKS > 1 && digit == 0) all_blocks();          // nobody adds to what another block has not cleared yet
+            else __syncthreads();
+            const auto count = [&](unsigned v) {
+                if (digit == 0) {                // the upper digits of most weights fall into few bins: those of a warp's that are alike are counted together
+                    const unsigned same = __match_any_sync(0xffffffffu, v >> 21);
+                    if (v != 0 && lane == __ffs(same) - 1) atomicAdd(&bins[v >> 21], __popc(same));
+                } else if (v >> (shift + bits) == threshold) {
+                    atomicAdd(&bins[(v >> shift) & (n - 1)], 1);
+                }
+            };
+#pragma unroll
+            for (int x = 0; x < HELD; ++x)
+                if (from + EACH * THREADS * x < to)
+#pragma unroll
+                    for (int k = 0; k < EACH; ++k) count(u[x][k]);
+            for (int p0 = beyond; p0 < to; p0 += EACH * THREADS)
 #pragma unroll
                 for (int k = 0; k < EACH; ++k) {
-                    const unsigned u = order_of(v[k]);
-                    const bool mine = pos + k >= lo && pos + k < hi && pos + k < to && (digit == 0 || (u >> (shift + bits)) == threshold);
-                    const unsigned bin = mine ? (u >> shift) & (n - 1) : 0xffffffffu;
-                    if (digit == 0) {            // the upper digits of most weights fall into few bins: those of a warp's that are alike are counted together
-                        const unsigned same = __match_any_sync(0xffffffffu, bin);
-                        if (mine && lane == __ffs(same) - 1) atomicAdd(&bins[bin], __popc(same));
-                    } else if (mine) {
-                        atomicAdd(&bins[bin], 1);
-                    }
+                    const int pos = p0 + EACH * tid + k;
+                    count(key_of(pos, weight(pos)));
                 }
-            });
-            all_blocks();
+            __syncthreads();
             // bins from the highest down, PER a thread
-            int have[PER], sum = 0;
+            const int top = n - 1 - PER * tid;
+            int mine[PER], have[PER], sum = 0;
 #pragma unroll
-            for (int k = 0; k < PER; ++k) {
-                const int bin = n - 1 - PER * tid - k;
-                have[k] = 0;
-                if (bin >= 0)
+            for (int k = 0; k < PER; ++k) have[k] = mine[k] = top - k >= 0 ? bins[top - k] : 0;
+            if (BLOCKS > 1) {
+                const int now = digit & 1;
 #pragma unroll
-                    for (int r = 0; r < BLOCKS; ++r) have[k] += bins_of(r)[bin];
-                sum += have[k];
+                for (int k = 0; k < PER; ++k)
+                    if (mine[k] > 0)
+#pragma unroll
+                        for (int r = 0; r < BLOCKS; ++r) atomicAdd(&cg::this_cluster().map_shared_rank(all[now], r)[top - k], mine[k]);
+                for (int i = tid; i < BINS; i += THREADS) all[now ^ 1][i] = 0;       // of the digit before: all have read it
+                all_blocks();
+#pragma unroll
+                for (int k = 0; k < PER; ++k) have[k] = top - k >= 0 ? all[now][top - k] : 0;
             }
+#pragma unroll
+            for (int k = 0; k < PER; ++k) sum += have[k];
             unsigned long long total;
             int above = (int)block_prefix<WARPS>((unsigned long long)sum, part, total);
 #pragma unroll
             for (int k = 0; k < PER; ++k) {
                 if (above < want && above + have[k] >= want) {
-                    found[0] = n - 1 - PER * tid - k;
+                    found[0] = top - k;
                     found[1] = want - above;
+                    at_threshold = mine[k];
                 }
                 above += have[k];
             }
-            all_blocks();                        // all have read the bins
+            __syncthreads();
+            if (BLOCKS > 1) {                    // of the slice's, those above
+                int over = 0;
+#pragma unroll
+                for (int k = 0; k < PER; ++k) over += top - k > found[0] ? mine[k] : 0;
+                over = __reduce_add_sync(0xffffffffu, over);
+                if (lane == 0 && over > 0) atomicAdd(&above_threshold, over);
+            }
             threshold = digit == 0 ? (unsigned)found[0] : threshold << bits | (unsigned)found[0];
             want = found[1];
         }
@@ -147,127 +168,146 @@ __global__ __launch_bounds__(THREADS) void k_kv_select(const __grid_constant__ g
     // above the threshold all stay, of those equal to it `want`, the lowest positions
 
     // ---- places ----
-    const auto sort = [&](int pos, float x) -> int {     // 2: stays for sure, 1: equal to the threshold
-        if (pos >= to) return 0;
-        if (pos < lo || pos >= hi) return 2;
-        const unsigned u = order_of(x);
-        return none || u < threshold ? 0 : u > threshold ? 2 : 1;
-    };
-    unsigned long long before = 0;               // upper half: that stay for sure, lower: equal to the threshold
+    unsigned long long before = 0;               // upper half: tokens that stay for sure, lower: equal to the threshold
     if (cut && BLOCKS > 1) {                     // of the slices below
-        unsigned long long mine = 0;
-        each([&](int pos, const float* v) {
-#pragma unroll
-            for (int k = 0; k < EACH; ++k) {
-                const int x = sort(pos + k, v[k]);
-                mine += x == 2 ? 1ull << 32 : (unsigned long long)x;
-            }
-        });
-        unsigned long long total;
-        block_prefix<WARPS>(mine, part, total);
-        if (tid == 0) counts = total;
+        __syncthreads();
+        if (tid < BLOCKS) {
+            const int ends = max(0, min(to, lo) - from) + max(0, to - max(from, hi));
+            cg::this_cluster().map_shared_rank(slices, tid)[rank] = ((long long)(ends + (none ? 0 : above_threshold)) << 32) | (none ? 0 : at_threshold);
+        }
         all_blocks();
-        for (int r = 0; r < rank; ++r) before += counts_of(r);
-        all_blocks();                            // a block stays until the others have read what it has
+        for (int r = 0; r < rank; ++r) before += (unsigned long long)slices[r];
     }
     kv_wait_before();
     kv_let_next();
+    int* kept = E.kept + ((long long)item * E.c.heads + head) * E.keep;
     if (E.status[item] != GBS_KV_DONE || !cut) { // nothing was done, or all of it stays
         const int stay = E.status[item] == GBS_KV_DONE ? length : 0;
-        int* kept = E.kept + ((long long)item * E.c.heads + head) * E.keep;
         for (int j = THREADS * rank + tid; j < E.keep; j += THREADS * BLOCKS) kept[j] = j < stay ? j : -1;
         float* out = E.mass_out + row;
         if (out != mass)
             for (int j = THREADS * rank + tid; j < stay && j < E.width; j += THREADS * BLOCKS) out[j] = mass[j];
         return;
     }
-    int* kept = E.kept + ((long long)item * E.c.heads + head) * E.keep;
     float* weights = E.weights + ((long long)item * E.c.heads + head) * E.keep;
-    each([&](int pos, const float* v) {
-        int how[EACH];
-        unsigned long long mine = 0;
+    // which of a thread's EACH tokens stay for sure, and which are equal to the threshold
+    const auto masks = [&](int pos, const unsigned* v, unsigned& sure, unsigned& equal) {
+        sure = equal = 0;
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
-            how[k] = sort(pos + k, v[k]);
-            mine += how[k] == 2 ? 1ull << 32 : (unsigned long long)how[k];
+            const bool end = pos + k < to && (pos + k < lo || pos + k >= hi);
+            sure |= (unsigned)(end || (!none && v[k] > threshold)) << k;
+            equal |= (unsigned)(!none && v[k] == threshold) << k;
         }
-        unsigned long long total;
-        const unsigned long long at = before + block_prefix<WARPS>(mine, part, total);
-        int s = (int)(at >> 32), q = (int)(unsigned)at;
+    };
+    const auto write = [&](int pos, unsigned sure, unsigned equal, int s, int q) {
+        if ((sure | equal) == 0) return;
+        float w[EACH];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) w[k] = weight(pos + k);
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
-            if (how[k] == 2 || (how[k] == 1 && q < want)) {
+            const bool is = sure >> k & 1, eq = equal >> k & 1;
+            if (is || (eq && q < want)) {
                 const int j = s + min(q, want);
                 kept[j] = pos + k;
-                weights[j] = v[k];
+                weights[j] = w[k];
             }
-            s += how[k] == 2;
-            q += how[k] == 1;
+            s += is;
+            q += eq;
         }
-        before += total;
-    });
+    };
+    unsigned sure[HELD], equal[HELD];
+    unsigned long long mine = 0, total;
+#pragma unroll
+    for (int x = 0; x < HELD; ++x) {
+        masks(from + EACH * (THREADS * x + tid), u[x], sure[x], equal[x]);
+        mine |= (unsigned long long)__popc(sure[x]) << (32 * x + 16) | (unsigned long long)__popc(equal[x]) << (32 * x);
+    }
+    const unsigned long long at = block_prefix<WARPS>(mine, part, total);
+    int s = (int)(before >> 32), q = (int)(unsigned)before;
+#pragma unroll
+    for (int x = 0; x < HELD; ++x) {
+        write(from + EACH * (THREADS * x + tid), sure[x], equal[x], s + (int)(at >> (32 * x + 16) & 0xffff), q + (int)(at >> (32 * x) & 0xffff));
+        s += (int)(total >> (32 * x + 16) & 0xffff);
+        q += (int)(total >> (32 * x) & 0xffff);
+    }
+    for (int p0 = beyond; p0 < to; p0 += EACH * THREADS) {
+        const int pos = p0 + EACH * tid;
+        unsigned v[EACH], is, eq;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) v[k] = key_of(pos + k, weight(pos + k));
+        masks(pos, v, is, eq);
+        const unsigned long long here = block_prefix<WARPS>((unsigned long long)__popc(is) << 32 | (unsigned)__popc(eq), part, total);
+        write(pos, is, eq, s + (int)(here >> 32), q + (int)(unsigned)here);
+        s += (int)(total >> 32);
+        q += (int)(unsigned)total;
+    }
 }
 
-// Rows of what stays: eight threads a token, 16 bytes of its codes each, two of them a scale as well, another one its weight.  The last block of an item lets its former pages go
-// and enters the new ones into the table.
+// Rows of what stays, MOVE tokens of a KV head a block: a thread finds where a token is and where it goes, and moves its scales and its weight; then eight threads a token move
+// the codes, 16 bytes each.  The last block of an item lets its former pages go and enters the new ones into the table.  (Eight threads a token that find everything
+// themselves: 313 instructions for four tokens, and 33 us instead of 20 for 290 000 tokens.)
 __global__ __launch_bounds__(MOVE, 5) void k_kv_evict_move(const __grid_constant__ gbs_kv_eviction E)
 {
+    struct alignas(16) Way {
+        const unsigned char* from;               // null: zeros
+        unsigned char* to;                       // null: no such token
+    };
+    __shared__ Way ways[MOVE];
     __shared__ int last;
     kv_wait_before();
     kv_let_next();
-    const int item = blockIdx.x / E.c.heads, head = blockIdx.x - item * E.c.heads, part = threadIdx.x & 7;
+    const int item = blockIdx.x / E.c.heads, head = blockIdx.x - item * E.c.heads;
+    int j = blockIdx.y * MOVE + threadIdx.x;
     const long long base = ((long long)item * E.c.heads + head) * E.keep;
-    // a thread's part of TOKENS tokens, 32 apart; what does not depend on one another is asked for at once
-    const int j0 = blockIdx.y * (TOKENS * MOVE / 8) + (threadIdx.x >> 3), step = gridDim.y * (TOKENS * MOVE / 8);
-    int pos[TOKENS];
-#pragma unroll
-    for (int k = 0; k < TOKENS; ++k) pos[k] = j0 + 32 * k < E.keep ? E.kept[base + j0 + 32 * k] : -1;
+    int pos = j < E.keep ? E.kept[base + j] : -1;
     const int seq = kv_sequence(E.c, E.seqs, item);
     if (E.status[item] != GBS_KV_DONE) return;
     const int* fresh = E.fresh + (long long)item * E.keep_pages;
     int* table = E.c.page_table + (long long)seq * E.c.max_pages;
-    const int length = kv_length(E.c, seq);
-    float* out = E.mass_out + ((long long)seq * E.c.heads + head) * E.width;
-    const int ps = 1 << E.c.page_log, scale_bytes = E.c.block_bytes / ps / 2 - KV_ROW;
-    const int codes = (part >> 2) * ps * KV_ROW + 16 * (part & 3), scales = 2 * ps * KV_ROW + (part >> 2) * ps * scale_bytes;
+    const int length = kv_length(E.c, seq), ps = 1 << E.c.page_log;
+    const bool asym = E.c.block_bytes > ps * (2 * KV_ROW + 8);
     if (length <= E.keep) return;
-    for (int j = j0; j < E.keep; j += step) {
-        uint4 v[TOKENS];
-        float2 sc[TOKENS];
-        float weight[TOKENS];
-        int page[TOKENS];
-#pragma unroll
-        for (int k = 0; k < TOKENS; ++k) {
-            const int from = pos[k] >= 0 ? table[pos[k] >> E.c.page_log] : -1;
-            page[k] = pos[k] >= 0 ? fresh[(j + 32 * k) >> E.c.page_log] : 0;
-            const bool ok = (unsigned)from < (unsigned)E.c.n_pages;
-            const unsigned char* x = kv_block(E.c, ok ? from : 0, head);
-            const int a = pos[k] & (ps - 1);
-            v[k] = ok ? *reinterpret_cast<const uint4*>(x + codes + a * KV_ROW) : make_uint4(0, 0, 0, 0);
-            sc[k] = make_float2(0.f, 0.f);
-            if (ok && (part & 3) == 0) {
-                if (scale_bytes == 8) sc[k] = *reinterpret_cast<const float2*>(x + scales + a * 8);
-                else sc[k].x = *reinterpret_cast<const float*>(x + scales + a * 4);
+    for (long long first = blockIdx.y * MOVE; first < E.keep; first += gridDim.y * MOVE) {     // once, but for sequences of many millions
+        Way way = {nullptr, nullptr};
+        if (pos >= 0) {
+            const int from = kv_page(E.c, seq, pos), a = pos & (ps - 1), b = j & (ps - 1);
+            way.to = kv_block(E.c, fresh[j >> E.c.page_log], head);
+            if (from >= 0) way.from = kv_block(E.c, from, head);
+            if (asym) {
+                const float2* x = reinterpret_cast<const float2*>(way.from + 2 * ps * KV_ROW) + a;
+                const float2 k = from < 0 ? make_float2(0.f, 0.f) : x[0], v = from < 0 ? make_float2(0.f, 0.f) : x[ps];
+                float2* y = reinterpret_cast<float2*>(way.to + 2 * ps * KV_ROW) + b;
+                y[0] = k;
+                y[ps] = v;
+            } else {
+                const float* x = reinterpret_cast<const float*>(way.from + 2 * ps * KV_ROW) + a;
+                const float k = from < 0 ? 0.f : x[0], v = from < 0 ? 0.f : x[ps];
+                float* y = reinterpret_cast<float*>(way.to + 2 * ps * KV_ROW) + b;
+                y[0] = k;
+                y[ps] = v;
             }
-            weight[k] = part == 1 && pos[k] >= 0 ? E.weights[base + j + 32 * k] : 0.f;
+            if (j < E.width) E.mass_out[((long long)seq * E.c.heads + head) * E.width + j] = E.weights[base + j];
+            if (from >= 0) way.from += a * KV_ROW;
+            way.to += b * KV_ROW;
         }
-        int next[TOKENS];
+        ways[threadIdx.x] = way;
+        __syncthreads();
+        const int part = threadIdx.x & 7, off = (part >> 2) * ps * KV_ROW + 16 * (part & 3);
+        uint4 v[8];
 #pragma unroll
-        for (int k = 0; k < TOKENS; ++k) next[k] = j + step + 32 * k < E.keep ? E.kept[base + j + step + 32 * k] : -1;
-#pragma unroll
-        for (int k = 0; k < TOKENS; ++k) {
-            if (pos[k] < 0) continue;
-            const int to_j = j + 32 * k, b = to_j & (ps - 1);
-            unsigned char* to = kv_block(E.c, page[k], head);
-            *reinterpret_cast<uint4*>(to + codes + b * KV_ROW) = v[k];
-            if ((part & 3) == 0) {
-                if (scale_bytes == 8) *reinterpret_cast<float2*>(to + scales + b * 8) = sc[k];
-                else *reinterpret_cast<float*>(to + scales + b * 4) = sc[k].x;
-            }
-            if (part == 1 && to_j < E.width) out[to_j] = weight[k];
+        for (int k = 0; k < 8; ++k) {
+            const unsigned char* from = ways[32 * k + (threadIdx.x >> 3)].from;
+            v[k] = from ? *reinterpret_cast<const uint4*>(from + off) : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
-        for (int k = 0; k < TOKENS; ++k) pos[k] = next[k];
+        for (int k = 0; k < 8; ++k)
+            if (unsigned char* to = ways[32 * k + (threadIdx.x >> 3)].to) *reinterpret_cast<uint4*>(to + off) = v[k];
+        if (gridDim.y * MOVE >= E.keep) break;
+        j += gridDim.y * MOVE;               // keep is at most 2^27 where anything is cut: no overflow
+        pos = j < E.keep ? E.kept[base + j] : -1;
+        __syncthreads();                         // the ways have been read
     }
     __threadfence();
     __syncthreads();                             // the block has read the table and the length
@@ -276,10 +316,10 @@ __global__ __launch_bounds__(MOVE, 5) void k_kv_evict_move(const __grid_constant
     if (!last) return;
     __threadfence();
     const int held = (int)(((unsigned)length + (1u << E.c.page_log) - 1) >> E.c.page_log);
-    for (int j = threadIdx.x; j < held; j += MOVE) {
-        const int page = table[j];
+    for (int i = threadIdx.x; i < held; i += MOVE) {
+        const int page = table[i];
         if ((unsigned)page < (unsigned)E.c.n_pages) atomicSub(&E.c.refs[page], 1);
-        if (j < E.keep_pages) table[j] = fresh[j];
+        if (i < E.keep_pages) table[i] = fresh[i];
     }
     if (threadIdx.x == 0) E.c.lengths[seq] = E.keep;
 }
@@ -312,8 +352,7 @@ int gbs_kv_evict_launch(const gbs_plan* p, const gbs_kv_eviction& E, cudaStream_
     int rc = gbs_kv_evict_pages_launch(p, E.c, E.seqs, E.n_items, E.keep, E.keep_pages, E.fresh, E.arrived, E.status, stream);
     const int64_t rows = (int64_t)E.n_items * E.c.heads, longest = (int64_t)E.c.max_pages << E.c.page_log;
     if (rc == 0) rc = longest > 2 * EACH * HELD * FEW && rows <= p->sm_count ? select<MANY, CLUSTER>(p, E, stream) : select<FEW, 1>(p, E, stream);
-    // a block moves 64 tokens at a time; so many blocks of an item and KV head that all of them fill the GPU some times over
-    const int64_t at_once = TOKENS * MOVE / 8, most = ((int64_t)E.keep + at_once - 1) / at_once, y = (int64_t)p->sm_count * 32 / rows + 1;
-    if (rc == 0) rc = gbs_kv_launch(p, k_kv_evict_move, dim3((unsigned)rows, (unsigned)(y < most ? y : most)), MOVE, 0, stream, E);
+    const int64_t most = E.keep < longest ? E.keep : longest, y = (most + MOVE - 1) / MOVE;
+    if (rc == 0) rc = gbs_kv_launch(p, k_kv_evict_move, dim3((unsigned)rows, (unsigned)(y < 65535 ? y : 65535)), MOVE, 0, stream, E);
     return rc;
 }
