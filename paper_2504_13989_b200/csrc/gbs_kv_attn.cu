@@ -539,7 +539,10 @@ int launch(const gbs_plan* p, const KvAttnArgs& P, int blocks, cudaStream_t stre
     if (e != cudaSuccess) return (int)e;
     const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
     if (rc != 0 || P.line.pad < 0) return rc;
-    return gbs_kv_launch(p, k_kv_attn_join<ROWS, PART>, dim3((unsigned)blocks), 256, 0, stream, P);
+    // no more segments than tiles and KV heads; where they are as many as a quarter of the blocks, every block looks at its own
+    const int64_t most = (int64_t)P.line.entries * P.a.c.heads;
+    const bool few = 4 * most <= blocks;
+    return gbs_kv_launch(p, few ? k_kv_attn_join<ROWS, PART, true> : k_kv_attn_join<ROWS, PART, false>, dim3((unsigned)(few ? most : blocks)), 256, 0, stream, P);
 }
 
 }  // namespace
@@ -559,6 +562,7 @@ int gbs_kv_few_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspace, 
     const int blocks = P.line.pad < 0 ? (int)std::min<int64_t>((int64_t)P.line.entries * A.c.heads, blocks_of(p)) : blocks_of(p);
     P.joins = static_cast<KvJoin*>(workspace);
     P.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + blocks * sizeof(KvJoin));
+    P.blocks = blocks;
     P.status = p->d_status;
     return A.entries ? launch<KV_PREFIX>(p, P, blocks, stream) : A.shared ? launch<KV_OWN>(p, P, blocks, stream) : launch<KV_WHOLE>(p, P, blocks, stream);
 }

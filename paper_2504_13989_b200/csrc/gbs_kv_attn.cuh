@@ -23,6 +23,7 @@ struct KvAttnArgs {
     KvLine line;
     float* parts;                                    // [blocks][2][PART]
     KvJoin* joins;                                   // [blocks]
+    int blocks;                                      // of the kernel whose sums are joined
     int* status;
 };
 
@@ -120,23 +121,53 @@ __device__ __forceinline__ void kv_row_of(const gbs_kv_attn& A, const KvSeg& s, 
     head = s.head * A.group + (r - token * A.group);
 }
 
-// The segments that several blocks share: block b joins the one that starts in block b, a warp a row, eight
-// rows a block of this kernel.  The pieces' weights come first, a
+// The number of the block of the kernel before that started the i-th segment that several blocks share, asked by a whole warp; -1: there are fewer.
+__device__ __forceinline__ int kv_start_of(const KvAttnArgs& P, int i)
+{
+    const int lane = threadIdx.x & 31;
+    int before = 0;
+    for (int b0 = 0; b0 < P.blocks; b0 += 128) {
+        unsigned which[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) which[k] = b0 + 32 * k + lane < P.blocks ? P.joins[b0 + 32 * k + lane].blocks : 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            which[k] = __ballot_sync(0xffffffffu, which[k] != 0);
+            const bool here = (which[k] >> lane & 1) && before + __popc(which[k] & ((1u << lane) - 1)) == i;
+            const unsigned found = __ballot_sync(0xffffffffu, here);
+            if (found != 0) return b0 + 32 * k + __ffs(found) - 1;
+            before += __popc(which[k]);
+        }
+    }
+    return -1;
+}
+
+// The segments that several blocks share, a warp a row, eight rows a block of this kernel.  Block b joins the one that starts in block b of the kernel before, or, where there
+// are far fewer of them than blocks (FEW), the b-th of them: a block that only finds out that there is nothing for it still takes a place for a microsecond, of
+// the 4700 that 148 blocks with 256 rows need.  Then the first pieces' sums are also fetched while their weights are found.  17 pieces of 2048 rows: 7.5 us instead of 10.6; with many
+// segments the registers for that cost more warps than it gives (44 000 rows 15 us, 23 that way).  The pieces' weights come first, a
 // lane a piece, so that their sums can be fetched many at a time: up to a few dozen pieces of a long sequence are as many trips to memory otherwise.
-template <int ROWS, int PART = KV_WHOLE>
+template <int ROWS, int PART, bool FEW>
 __global__ __launch_bounds__(256) void k_kv_attn_join(const __grid_constant__ KvAttnArgs P)
 {
     constexpr int PIECE = KV_PART<ROWS>;
     __shared__ float full[8][128];
     kv_wait_before();
     kv_let_next();
-    const KvJoin j = P.joins[blockIdx.x];
+    const int start = FEW ? kv_start_of(P, blockIdx.x) : (int)blockIdx.x;
+    if (start < 0) return;
+    const KvJoin j = P.joins[start];
     if (j.blocks == 0) return;
     const gbs_kv_attn& A = P.a;
     const int row = 8 * blockIdx.y + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     // piece b's sums: the first block's last segment, the others' first
-    const float* first = P.parts + ((long long)blockIdx.x * 2 + 1) * PIECE;
+    const float* first = P.parts + ((long long)start * 2 + 1) * PIECE;
     const auto piece = [&](int b) { return b == 0 ? first : first + (long long)(2 * b - 1) * PIECE; };
+    constexpr int AHEAD = FEW ? 8 : 0;
+    float4 ahead[FEW ? AHEAD : 1];
+#pragma unroll
+    for (int b = 0; b < AHEAD; ++b)
+        if (b < j.blocks) ahead[b] = *reinterpret_cast<const float4*>(piece(b) + row * 128 + 4 * lane);
     float top = NONE, top_w = NONE;
     for (int b = lane; b < j.blocks; b += 32) {
         top = fmaxf(top, piece(b)[ROWS * 128 + row]);
@@ -159,15 +190,19 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(const __grid_constant__ Kv
             total = fmaf(x[ROWS], keep, total);
             extra = fmaf(x[2 * ROWS], keep, extra);
         }
-#pragma unroll 8
-        for (int b = 0; b < n; ++b) {
-            const float4 x = *reinterpret_cast<const float4*>(piece(b0 + b) + row * 128 + 4 * lane);
+        const auto add = [&](const float4& x, int b) {
             const float by = __shfl_sync(0xffffffffu, weight, b);
             sum.x = fmaf(x.x, by, sum.x);
             sum.y = fmaf(x.y, by, sum.y);
             sum.z = fmaf(x.z, by, sum.z);
             sum.w = fmaf(x.w, by, sum.w);
-        }
+        };
+        if (b0 == 0)
+#pragma unroll
+            for (int b = 0; b < AHEAD; ++b)
+                if (b < n) add(ahead[b], b);
+#pragma unroll 8
+        for (int b = b0 == 0 ? AHEAD : 0; b < n; ++b) add(*reinterpret_cast<const float4*>(piece(b0 + b) + row * 128 + 4 * lane), b);
     }
 #pragma unroll
     for (int h = 16; h; h >>= 1) {

@@ -12,121 +12,115 @@ namespace {
 
 constexpr int BLOCKS = 8, THREADS = 1024, WARPS = THREADS / 32;
 constexpr int NO_PART = -1;                      // of an item that shares nothing because it has no tokens, or no sequence
+constexpr int NONE_YET = 0x7fffffff;
 
 struct GroupArgs {
     gbs_kv_attn a;
     const int* groups;                           // null: one group of all items
     int n_groups, slices, tile_rows, unit_log, n_entries;
-    int* common;                                 // [n_items][slices]: pages in common with the group's first item, as far as the slice tells
     int* shared;                                 // [n_items]
     KvEntry* entries;                            // [n_entries]
 };
 
-struct Range {
-    int from, to;
+// What the block keeps of the items and the groups, in shared memory: every number that the call needs from elsewhere is fetched once.
+struct Tables {
+    int *seq, *before, *first;                   // [n_items]: the sequence, pages that lie wholly before the item's own tokens (NO_PART), its first row
+    int *bounds, *lead, *common, *tiles;         // [n_groups] (bounds: and the end): first item, first item that takes part, pages that all have in common, members and then tiles
 };
-__device__ __forceinline__ Range items_of(const GroupArgs& P, int g)
-{
-    if (!P.groups) return Range{0, P.a.n_items};
-    const int from = min(max(P.groups[g], 0), P.a.n_items);
-    return Range{from, min(max(P.groups[g + 1], from), P.a.n_items)};
-}
-// pages that lie wholly before an item's own tokens; NO_PART
-__device__ __forceinline__ int pages_before(const gbs_kv_attn& A, const KvItem& x)
-{
-    return x.seq < 0 || x.count <= 0 ? NO_PART : max(x.length - x.count, 0) >> A.c.page_log;
-}
-
-// Group of an item, or -1, asked by a whole warp.
-__device__ __forceinline__ int group_of(const GroupArgs& P, int item)
-{
-    if (!P.groups) return 0;
-    if (item < P.groups[0]) return -1;
-    const int g = kv_item_of(P.groups, P.n_groups, item);
-    return g < P.n_groups ? g : -1;
-}
+__host__ __device__ constexpr size_t table_ints(int n_items, int n_groups) { return 3 * (size_t)n_items + 4 * (size_t)n_groups + 1; }
+static_assert(table_ints(GBS_KV_MAX_ITEMS, GBS_KV_MAX_ITEMS) * 4 + 1024 <= 227 * 1024, "one block's shared memory");
 
 __global__ __cluster_dims__(BLOCKS, 1, 1) __launch_bounds__(THREADS) void k_kv_groups(const __grid_constant__ GroupArgs P)
 {
-    __shared__ int tiles[GBS_KV_MAX_ITEMS];      // of each group, then of those before it
+    extern __shared__ int sm[];
     __shared__ int sums[WARPS];
     const gbs_kv_attn& A = P.a;
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, rank = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, rank = blockIdx.x, n = A.n_items, ng = P.n_groups;
+    const Tables T = {sm, sm + n, sm + 2 * n, sm + 3 * n, sm + 3 * n + ng + 1, sm + 3 * n + 2 * ng + 1, sm + 3 * n + 3 * ng + 1};
     kv_wait_before();
     kv_let_next();
-    for (int i = rank * THREADS + threadIdx.x; i < A.n_items; i += BLOCKS * THREADS) P.shared[i] = 0;
 
-    // ---- an item's slice against its group's first item's ----
-    for (int job = rank * WARPS + w; job < A.n_items * P.slices; job += BLOCKS * WARPS) {
-        const int i = job / P.slices, slice = job - i * P.slices;
-        const int g = group_of(P, i);
-        int found = NO_PART;
-        if (g >= 0) {
-            const KvItem x = kv_item(A, i);
-            const int most = pages_before(A, x);
-            if (most != NO_PART) {
-                int lead = items_of(P, g).from;
-                KvItem y = kv_item(A, lead);
-                int y_most = pages_before(A, y);
-                while (y_most == NO_PART && lead < i) {      // ends at the item itself at the latest
-                    y = kv_item(A, ++lead);
-                    y_most = pages_before(A, y);
-                }
-                const int n = max(min(most, y_most), 0), per = (n + P.slices - 1) / P.slices, from = min(slice * per, n), to = min(from + per, n);
-                const int *a = A.c.page_table + (long long)x.seq * A.c.max_pages, *b = A.c.page_table + (long long)y.seq * A.c.max_pages;
-                found = n;
-                for (int j0 = from; j0 < to; j0 += 128) {
-                    int u[4], v[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int j = j0 + 32 * k + lane;
-                        u[k] = j < to ? a[j] : 0;
-                        v[k] = j < to ? b[j] : 0;
-                    }
-                    int first = 0x7fffffff;
-#pragma unroll
-                    for (int k = 3; k >= 0; --k)
-                        if (u[k] != v[k]) first = j0 + 32 * k + lane;
-                    first = __reduce_min_sync(0xffffffffu, first);
-                    if (first != 0x7fffffff) {
-                        found = first;
-                        break;
-                    }
-                }
-            }
+    // ---- the items and the groups: the same in all blocks ----
+    for (int g = tid; g <= ng; g += THREADS) {
+        T.bounds[g] = P.groups ? min(max(P.groups[g], 0), n) : g == 0 ? 0 : n;
+        if (g < ng) {
+            T.lead[g] = T.common[g] = NONE_YET;
+            T.tiles[g] = 0;
         }
-        if (lane == 0) P.common[job] = found;
     }
-    __threadfence();
-    cooperative_groups::this_cluster().sync();
-    if (rank != 0) return;
-
-    // ---- a warp a group: what all of its items share, and its rows ----
-    for (int g = w; g < P.n_groups; g += WARPS) {
-        const Range r = items_of(P, g);
-        int pages = 0x7fffffff, members = 0;
-        for (int job = r.from * P.slices + lane; job < r.to * P.slices; job += 32) {
-            const int c = __ldcg(&P.common[job]);
-            if (c != NO_PART) pages = min(pages, c);
-            members += c != NO_PART && job % P.slices == 0;
-        }
-        pages = __reduce_min_sync(0xffffffffu, pages);
-        members = __reduce_add_sync(0xffffffffu, members);
-        if (members < 2) pages = 0;              // nothing is read twice
-        if (lane == 0) {
-            const int first = r.from < r.to ? min(max(A.cu ? A.cu[r.from] : r.from, 0), (int)A.n_tokens) : 0;
-            const int end = r.from < r.to ? min(max(A.cu ? A.cu[r.to] : r.to, first), (int)A.n_tokens) : 0;
-            tiles[g] = pages == 0 ? 0 : ((end - first) * A.group + P.tile_rows - 1) / P.tile_rows;
-        }
-        for (int i = r.from + lane; i < r.to; i += 32)
-            if (__ldcg(&P.common[i * P.slices]) != NO_PART) P.shared[i] = pages << A.c.page_log;
+    for (int i = tid; i < n; i += THREADS) {
+        const KvItem x = kv_item(A, i);
+        T.seq[i] = x.seq;
+        T.first[i] = min(max(x.first, 0), (int)A.n_tokens);
+        T.before[i] = x.seq < 0 || x.count <= 0 ? NO_PART : max(x.length - x.count, 0) >> A.c.page_log;
     }
     __syncthreads();
+    // the last group that starts at an item or before it, if that reaches as far; -1
+    const auto group_of = [&](int i) {
+        if (i < T.bounds[0]) return -1;
+        int lo = 0, hi = ng - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (T.bounds[mid] <= i) lo = mid;
+            else hi = mid - 1;
+        }
+        return i < T.bounds[lo + 1] ? lo : -1;
+    };
+    for (int i = tid; i < n; i += THREADS) {
+        const int g = T.before[i] != NO_PART ? group_of(i) : -1;
+        if (g < 0) continue;
+        atomicMin(&T.lead[g], i);
+        atomicAdd(&T.tiles[g], 1);
+    }
+    // nobody adds to what the first block has not cleared yet
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    cluster.sync();
 
-    // ---- the groups' places in the list ----
-    const int per = (P.n_groups + THREADS - 1) / THREADS, g0 = min((int)threadIdx.x * per, P.n_groups), g1 = min(g0 + per, P.n_groups);
+    // ---- an item's slice against its group's first item's, a warp each ----
+    int* common = cluster.map_shared_rank(T.common, 0);
+    for (int job = rank * WARPS + w; job < n * P.slices; job += BLOCKS * WARPS) {
+        const int i = job / P.slices, slice = job - i * P.slices;
+        if (T.before[i] == NO_PART) continue;
+        const int g = group_of(i);
+        if (g < 0 || T.lead[g] == i) continue;
+        const int lead = T.lead[g], pages = min(T.before[i], T.before[lead]);
+        const int per = (pages + P.slices - 1) / P.slices, from = min(slice * per, pages), to = min(from + per, pages);
+        const int *a = A.c.page_table + (long long)T.seq[i] * A.c.max_pages, *b = A.c.page_table + (long long)T.seq[lead] * A.c.max_pages;
+        int found = pages;
+        for (int j0 = from; j0 < to; j0 += 128) {
+            int u[4], v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int j = j0 + 32 * k + lane;
+                u[k] = j < to ? a[j] : 0;
+                v[k] = j < to ? b[j] : 0;
+            }
+            int first = NONE_YET;
+#pragma unroll
+            for (int k = 3; k >= 0; --k)
+                if (u[k] != v[k]) first = j0 + 32 * k + lane;
+            first = __reduce_min_sync(0xffffffffu, first);
+            if (first != NONE_YET) {
+                found = first;
+                break;
+            }
+        }
+        if (lane == 0) atomicMin(&common[g], found);
+    }
+    cluster.sync();
+    if (rank != 0) return;
+
+    // ---- what each item shares; the tiles of each group, and their places in the list ----
+    const int per = (ng + THREADS - 1) / THREADS, g0 = min(tid * per, ng), g1 = min(g0 + per, ng);
     int mine = 0;
-    for (int g = g0; g < g1; ++g) mine += tiles[g];
+    for (int g = g0; g < g1; ++g) {
+        const int pages = T.tiles[g] < 2 || T.common[g] == NONE_YET ? 0 : T.common[g];               // alone, nothing is read twice
+        T.common[g] = pages;
+        const int end = T.bounds[g + 1] < n ? T.first[T.bounds[g + 1]] : A.cu ? min(max(A.cu[n], 0), (int)A.n_tokens) : (int)A.n_tokens;
+        const int rows = pages == 0 ? 0 : max(end - T.first[T.bounds[g]], 0) * A.group;
+        T.tiles[g] = (rows + P.tile_rows - 1) / P.tile_rows;
+        mine += T.tiles[g];
+    }
     int sum = mine;
 #pragma unroll
     for (int h = 1; h < 32; h <<= 1) {
@@ -135,44 +129,45 @@ __global__ __cluster_dims__(BLOCKS, 1, 1) __launch_bounds__(THREADS) void k_kv_g
     }
     if (lane == 31) sums[w] = sum;
     __syncthreads();
-    int below = 0, all = 0;
-    for (int i = 0; i < WARPS; ++i) {
-        if (i < w) below += sums[i];
-        all += sums[i];
+    for (int i = tid; i < n; i += THREADS) {
+        const int g = T.before[i] != NO_PART ? group_of(i) : -1;
+        P.shared[i] = g < 0 ? 0 : min(T.common[g], T.before[i]) << A.c.page_log;
+    }
+    int below = lane < w ? sums[lane] : 0, all = sums[lane];
+#pragma unroll
+    for (int h = 16; h; h >>= 1) {
+        below += __shfl_xor_sync(0xffffffffu, below, h);
+        all += __shfl_xor_sync(0xffffffffu, all, h);
     }
     int at = below + sum - mine;
     for (int g = g0; g < g1; ++g) {
-        const int n = tiles[g];
-        tiles[g] = at;
-        at += n;
+        const int tiles = T.tiles[g];
+        T.tiles[g] = at;
+        at += tiles;
     }
     __syncthreads();
     all = min(all, P.n_entries);
-    for (int e = threadIdx.x; e < P.n_entries; e += THREADS) {
+    for (int e = tid; e < P.n_entries; e += THREADS) {
         KvEntry x = {};
         x.seq = -1;
         if (e < all) {
-            int lo = 0, hi = P.n_groups - 1;     // the last group that starts at e or before
+            int lo = 0, hi = ng - 1;             // the last group whose tiles begin at e or before
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
-                if (tiles[mid] <= e) lo = mid;
+                if (T.tiles[mid] <= e) lo = mid;
                 else hi = mid - 1;
             }
-            const Range r = items_of(P, lo);
-            KvItem y = {};
-            int shared = 0;
-            for (int i = r.from; i < r.to && shared == 0; ++i) {
-                y = kv_item(A, i);
-                shared = P.shared[i];
+            const int end = T.bounds[lo + 1] < n ? T.first[T.bounds[lo + 1]] : A.cu ? min(max(A.cu[n], 0), (int)A.n_tokens) : (int)A.n_tokens;
+            const int lead = T.lead[lo], shared = T.common[lo] << A.c.page_log;
+            x.first = T.first[T.bounds[lo]];
+            x.rows = max(end - x.first, 0) * A.group;
+            x.row0 = (e - T.tiles[lo]) * P.tile_rows;
+            // groups whose numbers fall may name items twice: what does not fit together has no units
+            if (shared > 0 && lead < n && x.row0 >= 0 && x.row0 < x.rows) {
+                x.seq = T.seq[lead];
+                x.length = x.hi = min(shared, T.before[lead] << A.c.page_log);
+                x.units = ((x.hi - 1) >> P.unit_log) + 1;
             }
-            const int first = min(max(A.cu ? A.cu[r.from] : r.from, 0), (int)A.n_tokens), end = min(max(A.cu ? A.cu[r.to] : r.to, first), (int)A.n_tokens);
-            x.seq = y.seq;
-            x.first = first;
-            x.rows = (end - first) * A.group;
-            x.row0 = (e - tiles[lo]) * P.tile_rows;
-            x.length = x.hi = shared;
-            x.units = ((shared - 1) >> P.unit_log) + 1;
-            if (shared == 0 || x.seq < 0 || x.row0 >= x.rows) x.units = 0;      // groups that overlap, whose numbers disagree
         }
         P.entries[e] = x;
     }
@@ -185,8 +180,8 @@ bool few_own(const gbs_kv_attn& A) { return (int64_t)A.max_tokens * A.group <= G
 int64_t round_up(int64_t x) { return (x + 15) & ~(int64_t)15; }
 
 struct Layout {
-    int64_t attn, prefix, entries, shared, common, bytes;      // where each part starts
-    int n_entries, slices;
+    int64_t attn, prefix, entries, shared, bytes;      // where each part starts
+    int n_entries;
 };
 Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A, int n_groups)
 {
@@ -194,7 +189,6 @@ Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A, int n_groups)
     const bool few = few_prefix(A, n_groups);
     const int tile = few ? 8 : 256;
     l.n_entries = (int)((A.n_tokens * A.group + tile - 1) / tile) + n_groups;
-    l.slices = A.n_items < BLOCKS * WARPS ? BLOCKS * WARPS / (A.n_items > 0 ? A.n_items : 1) : 1;
     l.attn = 0;
     int64_t at = 0;
     if (few || few_own(A)) at = gbs_kv_few_workspace(p);
@@ -202,8 +196,7 @@ Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A, int n_groups)
     l.prefix = round_up(at);
     l.entries = l.prefix + round_up(A.n_tokens * A.n_heads * GBS_KV_PREFIX_ROW * (int64_t)sizeof(float));
     l.shared = l.entries + round_up(l.n_entries * (int64_t)sizeof(KvEntry));
-    l.common = l.shared + round_up(A.n_items * (int64_t)sizeof(int));
-    l.bytes = l.common + round_up((int64_t)A.n_items * l.slices * sizeof(int));
+    l.bytes = l.shared + round_up(A.n_items * (int64_t)sizeof(int));
     return l;
 }
 
@@ -220,14 +213,20 @@ int gbs_kv_shared_launch(const gbs_plan* p, const gbs_kv_attn& A, const int* gro
     G.a = A;
     G.groups = groups;
     G.n_groups = n_groups;
-    G.slices = l.slices;
+    G.slices = A.n_items < BLOCKS * WARPS ? BLOCKS * WARPS / A.n_items : 1;
     G.tile_rows = few ? 8 : 256;
     G.unit_log = few ? 5 : 7;
     G.n_entries = l.n_entries;
-    G.common = reinterpret_cast<int*>(w + l.common);
     G.shared = reinterpret_cast<int*>(w + l.shared);
     G.entries = reinterpret_cast<KvEntry*>(w + l.entries);
-    int rc = gbs_kv_launch(p, k_kv_groups, dim3(BLOCKS), THREADS, 0, stream, G);
+    const size_t smem = table_ints(A.n_items, n_groups) * sizeof(int);
+    if (smem > 47 * 1024) {
+        // the limit is the function's, for all threads of the process: always the same one, since a smaller call's may come between another's and its launch
+        const cudaError_t e = cudaFuncSetAttribute((const void*)k_kv_groups, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)(table_ints(GBS_KV_MAX_ITEMS, GBS_KV_MAX_ITEMS) * sizeof(int)));
+        if (e != cudaSuccess) return (int)e;
+    }
+    int rc = gbs_kv_launch(p, k_kv_groups, dim3(BLOCKS), THREADS, smem, stream, G);
     if (rc != 0) return rc;
     gbs_kv_attn X = A;
     X.shared = G.shared;

@@ -17,6 +17,8 @@
 // 13 warps leave a thread 128 registers, and 74 bytes of one spill.
 // Weights reach 2^-30 of the row's largest, below what a bf16 result shows; l is of fp32 weights, which go under when value
 // scales that one row sees differ by more than 2^100: the share of the small ones in l is then lost.
+#include <algorithm>
+
 #include "gbs_kv_attn.cuh"
 #include "gbs_tc_common.cuh"
 
@@ -551,7 +553,10 @@ int launch(const gbs_plan* p, const KvAttnArgs& P, int blocks, cudaStream_t stre
     if (e != cudaSuccess) return (int)e;
     const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
     if (rc != 0) return rc;
-    return gbs_kv_launch(p, k_kv_attn_join<ROWS, PART>, dim3((unsigned)blocks, ROWS / 8), 256, 0, stream, P);
+    // no more segments than tiles and KV heads; where they are as many as a quarter of the blocks, every block looks at its own
+    const int64_t most = (int64_t)P.line.entries * P.a.c.heads;
+    const bool few = 4 * most <= blocks;
+    return gbs_kv_launch(p, few ? k_kv_attn_join<ROWS, PART, true> : k_kv_attn_join<ROWS, PART, false>, dim3((unsigned)(few ? most : blocks), ROWS / 8), 256, 0, stream, P);
 }
 
 }  // namespace
@@ -570,6 +575,7 @@ int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspac
     const int blocks = blocks_of(p);
     P.joins = static_cast<KvJoin*>(workspace);
     P.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + blocks * sizeof(KvJoin));
+    P.blocks = blocks;
     P.status = p->d_status;
     return A.entries ? launch<KV_PREFIX>(p, P, blocks, stream) : A.shared ? launch<KV_OWN>(p, P, blocks, stream) : launch<KV_WHOLE>(p, P, blocks, stream);
 }
