@@ -12,7 +12,9 @@
 // unit of 128 tokens ahead; warp 12 issues the MMAs.  While one tile's softmax runs, the other's products do.  Scores and weights of a tile share
 // 128 columns of tensor memory (fp16 weights overwrite scores that have been read), its sums take 128 more.
 // The MMAs take 1024 cycles of a tile, ex2 as many; two tiles of a unit take 5600, most of it the chain of a tile (scores, softmax, weights, second
-// product, next scores), which the other tile's overlaps but in part.  The last 2048 of 8048 tokens, 32 query heads over 8 KV heads: 318 us, 740
+// product, next scores), which the other tile's overlaps but in part.  Where
+// rows are few (SPLIT; for gbs_kv_shared_attention), a block has one tile, and the two halves of the warps and of tensor memory take its units in turn, each with sums of its own that are added at
+// the end: 2.1 us a unit, then bound by the conversion of codes, instead of 2.5; two tiles take 2.9.  The last 2048 of 8048 tokens, 32 query heads over 8 KV heads: 318 us, 740
 // TFLOP/s.  Blocks of 128 rows, two on an SM, every warp doing all of it in turn: 433 us.  32 tokens at a time in the softmax: 348.
 // 13 warps leave a thread 128 registers, and 74 bytes of one spill.
 // Weights reach 2^-30 of the row's largest, below what a bf16 result shows; l is of fp32 weights, which go under when value
@@ -143,7 +145,8 @@ __device__ __forceinline__ void shrink(unsigned scores, unsigned sums, float kee
     }
 }
 
-template <bool ASYM, bool TEST, int PART>
+// SPLIT: a block has one tile
+template <bool ASYM, bool TEST, int PART, bool SPLIT>
 __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant__ KvAttnArgs P)
 {
     extern __shared__ unsigned char smem_raw[];
@@ -176,13 +179,14 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
     if (tid == 0) P.joins[blockIdx.x] = KvJoin{0, 0, 0, 0};
 
     const int ps_log = A.c.page_log, ps = 1 << ps_log;
-    unsigned it = 0, round = 0, phase_b = 0;                 // units, segments and the second tile's units so far, by which the barriers' phases go
+    unsigned it = 0, round = 0, used[2] = {0, 0};            // units, segments and units of each half of the softmax so far, by which the barriers' phases go
     for (bool more = places > 0; more; ++round) {
         const KvSeg& seg = S.seg[round & 1];
         const KvPiece piece = kv_piece(P.line, seg, places);
         const int n = piece.n, tok0 = (seg.e.lo / UNIT + piece.skip) * UNIT;
         if (n <= 0) break;                                   // the block's last places are in front of a segment's units
-        const bool two = seg.e.row0 + TILE < seg.e.rows;     // the second tile has rows
+        const bool two = !SPLIT && seg.e.row0 + TILE < seg.e.rows;      // the second tile has rows
+        const bool split = SPLIT && n > 1;                   // its units are taken by both halves in turn
         bool ok = true;
 
         if (w < SOFTMAX / 32) {
@@ -239,20 +243,21 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             meet_all();
 
-            const int t = w >> 2, row = tid;                 // this thread's tile and row
-            const unsigned scores = tmem + ((unsigned)(32 * (w & 3)) << 16) + 128 * t, sums = scores + O_COL;
-            const float f = S.factor[row];
-            const int see_lo = S.lo[row], see_hi = S.hi[row];
+            const int t = w >> 2, row = tid, tile = split ? 0 : t, step = split ? 2 : 1, skip = split ? t : 0;      // this thread's half, row and tile
+            const bool busy = t == 0 || two || split;
+            const unsigned scores = tmem + ((unsigned)(32 * (w & 3)) << 16) + 128 * t, sums = scores + O_COL, turn = used[t];
+            const float f = S.factor[TILE * tile + (row & 127)];
+            const int see_lo = S.lo[TILE * tile + (row & 127)], see_hi = S.hi[TILE * tile + (row & 127)];
             // tokens that every row of the tile sees need no mask
-            const int first = seg.e.row0 + TILE * t;
+            const int first = seg.e.row0 + TILE * tile;
             const int all_lo = kv_row_lo<PART>(A, seg.e, A.by_group(min(seg.e.rows, first + TILE) - 1)), all_hi = kv_row_hi(A, seg.e, A.by_group(first));
             float M = NONE;
             f32x2 l = both(0.f);                             // of even and odd tokens
-            for (int i = 0; i < n && ok && (t == 0 || two); ++i) {
+            for (int i = skip; i < n && ok && busy; i += step) {
                 const unsigned now = it + i;
                 const int nb = now & 3, tok = tok0 + i * UNIT;
                 const bool plain = tok >= all_lo && tok + UNIT <= all_hi;
-                if (!(ok = !kv_lost<TEST>(P, &S.abort, 76, round) && mbar_wait_warp(&S.abort, &S.sfull[t], (t == 0 ? now : phase_b + i) & 1u, P.status, 76))) break;
+                if (!(ok = !kv_lost<TEST>(P, &S.abort, 76, round) && mbar_wait_warp(&S.abort, &S.sfull[t], (turn + (split ? i >> 1 : i)) & 1u, P.status, 76))) break;
                 tc_fence_after();
 #pragma unroll 1
                 for (int c = 0; c < 2; ++c) {                // 64 tokens at a time
@@ -288,7 +293,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                         const float now_M = fmaxf(most[0], M), keep = kv_ex2(M - now_M);
                         M = now_M;
                         l = mul2(l, both(keep));
-                        shrink(scores, sums, keep, i > 0, 2 * c);
+                        shrink(scores, sums, keep, i >= step, 2 * c);
                     }
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -313,7 +318,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 if (lane == 0) mbar_arrive(&S.pfull[t]);
             }
             // ---- the rows' sums, by way of shared memory ----
-            if (ok && (t == 0 || two) && (ok = !kv_lost<TEST>(P, &S.abort, 77, round) && mbar_wait_warp(&S.abort, &S.ofull, round & 1u, P.status, 77))) {
+            if (ok && busy && (ok = !kv_lost<TEST>(P, &S.abort, 77, round) && mbar_wait_warp(&S.abort, &S.ofull, round & 1u, P.status, 77))) {
                 tc_fence_after();
                 unsigned char* to = t == 0 ? S.k[0] : S.v[0];
 #pragma unroll 1
@@ -345,7 +350,19 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                     const int at = 8 * (q >> 1) + 2 * (q & 1);
                     y[at] = x.x; y[at + 4] = x.y; y[at + 1] = x.z; y[at + 5] = x.w;
                 }
-                const float total = S.l[row], m = S.m[row];
+                float total = S.l[row], m = S.m[row];
+                if (split) {
+                    const float l2 = S.l[TILE + row], m2 = S.m[TILE + row], most = fmaxf(m, m2), a = kv_ex2(m - most), b = kv_ex2(m2 - most);
+                    total = fmaf(l2, b, total * a);
+                    m = most;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float4 x = *reinterpret_cast<const float4*>(S.v[0] + sum_at(row, 16 * (q >> 1) + 2 * l8 + (q & 1)));
+                        const int at = 8 * (q >> 1) + 2 * (q & 1);
+                        y[at] = fmaf(x.x, b, y[at] * a); y[at + 4] = fmaf(x.y, b, y[at + 4] * a);
+                        y[at + 1] = fmaf(x.z, b, y[at + 1] * a); y[at + 5] = fmaf(x.w, b, y[at + 5] * a);
+                    }
+                }
                 if (piece.starts && piece.ends) {
                     const bool have = seg.e.row0 + row < seg.e.rows;
                     int token, head;
@@ -377,7 +394,6 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 }
             }
             if (tid == 0 && piece.starts && !piece.ends) P.joins[blockIdx.x] = kv_join(P.line, seg, places);
-            if (t == 1 && two) phase_b += n;
         } else if (w < 12) {
             // ---- codes: keys and values of a unit, and its per-token numbers ----
             const int me = tid - SOFTMAX;                    // this thread's token of a unit
@@ -452,11 +468,11 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             const unsigned long long qd = smem_desc(smem_u32(S.q[0]), 16, 1024, 2), kd = smem_desc(smem_u32(S.k[0]), 16, 1024, 2),
                                      vd = smem_desc(smem_u32(S.v[0]), 128 * 128, 1024, 2);
             const unsigned q_lo = (unsigned)qd, k_lo = (unsigned)kd, v_lo = (unsigned)vd, hi = (unsigned)(qd >> 32);          // the same in all three
-            const unsigned at = uniform(tmem), at0 = uniform(it), at0_b = uniform(phase_b);
+            const unsigned at = uniform(tmem), at0 = uniform(it), turn_a = uniform(used[0]), turn_b = uniform(used[1]);
             const int units = (int)uniform((unsigned)n), tiles = uniform(two ? 2u : 1u);
             const auto scores = [&](auto tile, unsigned b) {
                 constexpr int t = decltype(tile)::value;
-                unsigned a_lo = q_lo + t * TILE_STEP, b_lo = k_lo + b * TILE_STEP;
+                unsigned a_lo = q_lo + (split ? 0u : t * TILE_STEP), b_lo = k_lo + b * TILE_STEP;
                 umma_f16_words<false>(at + 128 * t, a_lo, hi, b_lo, hi, ID_S);
 #pragma unroll
                 for (int k = 1; k < 8; ++k) {                // sixteen coordinates: 32 bytes, four of them in a block of 64
@@ -486,7 +502,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 const unsigned now = at0 + i, next = now + 1;
                 if (i >= 0) {
                     if (t == 0 && (kv_lost<TEST>(P, &S.abort, 72, round) || !mbar_wait_warp(&S.abort, &S.vfull[now & 1], (now >> 1) & 1u, P.status, 72))) return false;
-                    if (kv_lost<TEST>(P, &S.abort, 73, round) || !mbar_wait_warp(&S.abort, &S.pfull[t], (t == 0 ? now : at0_b + i) & 1u, P.status, 73)) return false;
+                    if (kv_lost<TEST>(P, &S.abort, 73, round) || !mbar_wait_warp(&S.abort, &S.pfull[t], ((t == 0 ? turn_a : turn_b) + i) & 1u, P.status, 73)) return false;
                     tc_fence_after();
                     values(tile, adds, now & 1);
                     if (t + 1 == tiles) umma_commit(&S.vfree[now & 1]);
@@ -502,14 +518,38 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 return true;
             };
             const auto unit = [&](auto adds, int i) { return step(A_TILE, adds, i) && (tiles == 1 || step(B_TILE, adds, i)); };
-            ok = unit(Is<0>{}, -1) && unit(Is<0>{}, 0);
-            for (int i = 1; i < units && ok; ++i) ok = unit(Is<1>{}, i);
+            // of one tile in two halves: units in turn, scores two units ahead
+            const auto ahead = [&](auto half, int i) {
+                if (i >= units) return true;
+                const unsigned now = at0 + i;
+                if (!mbar_wait_warp(&S.abort, &S.kfull[now & 1], (now >> 1) & 1u, P.status, 71)) return false;
+                tc_fence_after();
+                scores(half, now & 1);
+                umma_commit(&S.kfree[now & 1]);
+                return true;
+            };
+            const auto alternate = [&](auto half, auto adds, int i) {
+                constexpr int t = decltype(half)::value;
+                const unsigned now = at0 + i;
+                if (!mbar_wait_warp(&S.abort, &S.vfull[now & 1], (now >> 1) & 1u, P.status, 72)) return false;
+                if (!mbar_wait_warp(&S.abort, &S.pfull[t], ((t == 0 ? turn_a : turn_b) + (i >> 1)) & 1u, P.status, 73)) return false;
+                tc_fence_after();
+                values(half, adds, now & 1);
+                umma_commit(&S.vfree[now & 1]);
+                return ahead(half, i + 2);
+            };
+            if (split) {
+                ok = ahead(A_TILE, 0) && ahead(B_TILE, 1) && alternate(A_TILE, Is<0>{}, 0) && alternate(B_TILE, Is<0>{}, 1);
+                for (int i = 2; i < units && ok; i += 2) ok = alternate(A_TILE, Is<1>{}, i) && (i + 1 >= units || alternate(B_TILE, Is<1>{}, i + 1));
+            } else {
+                ok = unit(Is<0>{}, -1) && unit(Is<0>{}, 0);
+                for (int i = 1; i < units && ok; ++i) ok = unit(Is<1>{}, i);
+            }
             if (ok) umma_commit(&S.ofull);
             else {                                           // what is under way is given time to end
                 umma_commit(&S.drain);
                 drain_copies(&S.drain, 1, 1);
             }
-            if (two) phase_b += n;
             if (lane == 0 && kv_more(P.line, seg, places)) {
                 KvSeg next = seg;
                 kv_next<PART>(A, P.line, next);
@@ -521,6 +561,8 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             }
         }
         it += n;
+        used[0] += split ? (n + 1) / 2 : n;
+        used[1] += split ? n / 2 : two ? n : 0;
         more = kv_more(P.line, seg, places);
     }
     tc_fence_before();
@@ -545,10 +587,12 @@ namespace {
 template <int PART>
 int launch(const gbs_plan* p, const KvAttnArgs& P, int blocks, cudaStream_t stream)
 {
+    constexpr bool WHOLE = PART == KV_WHOLE;
     const size_t smem = sizeof(Smem) + 1024;
-    const bool test = PART == KV_WHOLE && P.a.lost_code;
-    const auto f = test ? (p->asym ? k_tc_kvattn<true, PART == KV_WHOLE, PART> : k_tc_kvattn<false, PART == KV_WHOLE, PART>)
-                        : (p->asym ? k_tc_kvattn<true, false, PART> : k_tc_kvattn<false, false, PART>);
+    const bool test = WHOLE && P.a.lost_code, split = !WHOLE && P.a.one_tile;
+    const auto f = test    ? (p->asym ? k_tc_kvattn<true, WHOLE, PART, false> : k_tc_kvattn<false, WHOLE, PART, false>)
+                   : split ? (p->asym ? k_tc_kvattn<true, false, PART, !WHOLE> : k_tc_kvattn<false, false, PART, !WHOLE>)
+                           : (p->asym ? k_tc_kvattn<true, false, PART, false> : k_tc_kvattn<false, false, PART, false>);
     const cudaError_t e = cudaFuncSetAttribute((const void*)f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return (int)e;
     const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
@@ -556,7 +600,7 @@ int launch(const gbs_plan* p, const KvAttnArgs& P, int blocks, cudaStream_t stre
     // no more segments than tiles and KV heads; where they are as many as a quarter of the blocks, every block looks at its own
     const int64_t most = (int64_t)P.line.entries * P.a.c.heads;
     const bool few = 4 * most <= blocks;
-    return gbs_kv_launch(p, few ? k_kv_attn_join<ROWS, PART, true> : k_kv_attn_join<ROWS, PART, false>, dim3((unsigned)(few ? most : blocks), ROWS / 8), 256, 0, stream, P);
+    return gbs_kv_launch(p, few ? k_kv_attn_join<ROWS, PART, true> : k_kv_attn_join<ROWS, PART, false>, dim3((unsigned)(few ? most : blocks), (unsigned)P.line.tile_rows / 8), 256, 0, stream, P);
 }
 
 }  // namespace
@@ -572,6 +616,12 @@ int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspac
     P.line.by_tiles.set((unsigned)P.line.tiles);
     P.line.entries = A.entries ? A.n_entries : A.n_items * P.line.tiles;
     P.line.least = 1;
+    if (A.one_tile) {
+        P.line.tile_rows = TILE;
+        P.line.tiles = (int)(((int64_t)A.max_tokens * A.group + TILE - 1) / TILE);
+        P.line.by_tiles.set((unsigned)P.line.tiles);
+        P.line.entries = A.entries ? A.n_entries : A.n_items * P.line.tiles;
+    }
     const int blocks = blocks_of(p);
     P.joins = static_cast<KvJoin*>(workspace);
     P.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + blocks * sizeof(KvJoin));
