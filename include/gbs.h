@@ -494,12 +494,13 @@ int gbs_kv_shared_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache,
  *   mass, base        device float [n_seqs][n_kv_heads][width]; base is mass itself or does not overlap it, and is not read (NULL will do) where decay is 0
  *   max_tokens        no item has more tokens; what is beyond it gives no weight.  query heads of a KV head * n_tokens: at most 2^28
  *   workspace         device, gbs_kv_attention_mass_workspace bytes for the same sizes, 16-byte aligned; overwritten, needs no preparation, and one call at a
- *                     time may use it
+ *                     time may use it.  With up to 32 query rows a KV head and item it has room for their scores, 4 bytes a row and position below the width,
+ *                     as long as that is 256 MB at most
  * Weights are right to fp32: query rows are rounded to 24 bits of their largest coordinate, codes enter as they are, sums of products are exact.  Value
  * rows count for nothing.  A token whose key scale is infinite or a NaN makes the rows that see it, and so what they see, NaN.
  */
 int gbs_kv_attention_mass_workspace(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
-                                    int n_heads, int64_t* bytes_out);
+                                    int n_heads, int64_t width, int64_t* bytes_out);
 int gbs_kv_attention_mass(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
                           int64_t n_tokens, int max_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int n_heads,
                           float scale, int window, int flags, const float* base, float decay, float* mass, int64_t width, void* workspace,

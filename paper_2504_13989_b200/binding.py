@@ -152,7 +152,7 @@ def lib() -> ctypes.CDLL:
         L.gbs_kv_shared_attention_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i32, ctypes.POINTER(i64)]
         L.gbs_kv_shared_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, vp, i64, i64,
                                               vp, i64, vp]
-        L.gbs_kv_attention_mass_workspace.argtypes = [vp, kv, i32, i64, i32, i32, ctypes.POINTER(i64)]
+        L.gbs_kv_attention_mass_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i64, ctypes.POINTER(i64)]
         L.gbs_kv_attention_mass.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i64, i64, i32, ctypes.c_float, i32, i32, vp, ctypes.c_float, vp, i64,
                                             vp, i64, vp]
         L.gbs_kv_evict_workspace.argtypes = [vp, kv, i32, i32, ctypes.POINTER(i64)]
@@ -813,8 +813,8 @@ class KVCache:
         self._weights("base", base, mass.shape[2])
         s, cu, n = self._items(seqs, cu_tokens, q.shape[0])
         need = ctypes.c_int64(0)
-        _check(lib().gbs_kv_attention_mass_workspace(self.plan.handle, ctypes.byref(self._c), n, q.shape[0], max_tokens, q.shape[1], ctypes.byref(need)),
-               "gbs_kv_attention_mass_workspace")
+        _check(lib().gbs_kv_attention_mass_workspace(self.plan.handle, ctypes.byref(self._c), n, q.shape[0], max_tokens, q.shape[1], mass.shape[2],
+                                                     ctypes.byref(need)), "gbs_kv_attention_mass_workspace")
         work = self._empty(stream, need.value, torch.uint8, False)
         _check(lib().gbs_kv_attention_mass(self.plan.handle, ctypes.byref(self._c), s, cu, n, q.shape[0], max_tokens, q.data_ptr(), *self._strides(q),
                                            q.shape[1], float(scale), window, GBS_KV_CAUSAL if causal else 0, base.data_ptr(), float(decay),

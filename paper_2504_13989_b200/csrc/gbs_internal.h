@@ -245,7 +245,7 @@ int gbs_kv_shared_launch(const gbs_plan* p, const gbs_kv_attn& A, const int* gro
 int64_t gbs_tc_kvmass_workspace(const gbs_plan* p, const gbs_kv_attn& A);
 int gbs_tc_kvmass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* base, float decay, float* mass, int64_t width, void* workspace,
                          cudaStream_t stream);
-int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A);
+int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A, int64_t width);
 int gbs_kv_mass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* base, float decay, float* mass, int64_t width, void* workspace,
                        cudaStream_t stream);
 // gbs_kv_pages.cu : pages for what sequences keep; the items' status.  gbs_kv_evict.cu : what they keep, moved there

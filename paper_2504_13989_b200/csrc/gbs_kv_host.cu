@@ -372,12 +372,13 @@ extern "C" int gbs_kv_shared_attention(const gbs_plan_t* p, const gbs_kv_cache_t
 }
 
 extern "C" int gbs_kv_attention_mass_workspace(const gbs_plan_t* p, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
-                                               int n_heads, int64_t* bytes_out)
+                                               int n_heads, int64_t width, int64_t* bytes_out)
 {
     gbs_kv_attn A;
     const int rc = sizes_of(p, cache, n_items, n_tokens, max_tokens, n_heads, bytes_out, &A);
     if (rc != GBS_OK) return rc;
-    *bytes_out = gbs_kv_mass_workspace(p, A);
+    if (width < 1) return GBS_ERR_INVALID_ARG;
+    *bytes_out = gbs_kv_mass_workspace(p, A, width);
     return GBS_OK;
 }
 
@@ -393,7 +394,7 @@ extern "C" int gbs_kv_attention_mass(const gbs_plan_t* p, const gbs_kv_cache_t* 
     if (rc != GBS_OK) return rc;
     if (width < 1 || !isfinite(decay) || A.n_tokens * A.group > 1ll << 28) return GBS_ERR_INVALID_ARG;
     if (empty) return GBS_OK;
-    if (!q || !mass || (!base && decay != 0.f) || !workspace || workspace_bytes < gbs_kv_mass_workspace(p, A)) return GBS_ERR_INVALID_ARG;
+    if (!q || !mass || (!base && decay != 0.f) || !workspace || workspace_bytes < gbs_kv_mass_workspace(p, A, width)) return GBS_ERR_INVALID_ARG;
     rc = check_rows(p, x, false, workspace);
     if (rc != GBS_OK) return rc;
     if (!aligned(mass, 4) || !aligned(base, 4)) return GBS_ERR_ALIGNMENT;

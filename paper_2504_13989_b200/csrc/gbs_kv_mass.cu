@@ -32,6 +32,8 @@ struct MassArgs {
     float2* parts;                               // [blocks][2][max_rows]: m and the sum, of segments that several blocks share
     KvJoin* joins;
     long long max_rows;
+    float* scores;                               // [n_items][heads][width][score_rows]; null: they are found again in the second pass
+    int score_rows;
     const float* base;
     float* mass;
     long long width;
@@ -147,8 +149,8 @@ __device__ __forceinline__ void copy_async(void* to, const void* from)
 __device__ __forceinline__ float2 norm_of(float m, float sum) { return sum == 0.f ? make_float2(0.f, 0.f) : make_float2(m, 1.f / sum); }
 __device__ __forceinline__ float no_inf(float x) { return fmaf(x, 0.f, x); }
 
-// MASS: the second pass
-template <bool ASYM, bool MASS>
+// MASS: the second pass.  KEEP: the first pass, which leaves the scores for k_kv_mass_sums.
+template <bool ASYM, bool MASS, bool KEEP>
 __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_mass(const __grid_constant__ MassArgs P)
 {
     constexpr int PART = MASS ? KV_ALL : KV_WHOLE;
@@ -173,6 +175,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_mass(const __grid
         const int see_lo = kv_row_lo(A, e, 0), see_hi = kv_row_hi(A, e, A.by_group(e.rows - 1));
         const int* pages = A.c.page_table + (long long)e.seq * A.c.max_pages;
         const long long tile0 = tile_of(P, seg.head, seg.index, e.first);
+        float* scores = KEEP ? P.scores + ((long long)seg.index * A.c.heads + seg.head) * P.width * P.score_rows : nullptr;
 
         // this thread's pieces of a unit: 16 bytes of the codes of tokens tid / 4 + 32 k, the scales of token tid
         const auto seen = [&](int tok) { return tok < see_hi && tok + UNIT > see_lo; };
@@ -344,6 +347,15 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_mass(const __grid
                                         if (pos < (j & 1 ? lo.y : lo.x) || pos >= (j & 1 ? hi.y : hi.x) || !(there >> (16 * h + 8 * (j >> 1) + g) & 1)) z[h][j] = -INFINITY;
                                     }
                                 }
+                            const int row = PASS * pass + TILE * i + 2 * t;
+                            if (KEEP && row < P.score_rows)
+#pragma unroll
+                                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                    for (int b = 0; b < 2; ++b) {
+                                        const int pos = mine + 16 * h + 8 * b + g;
+                                        if (pos < P.width) *reinterpret_cast<float2*>(scores + (long long)pos * P.score_rows + row) = make_float2(z[h][2 * b], z[h][2 * b + 1]);
+                                    }
                             if (MASS) {
 #pragma unroll
                                 for (int h = 0; h < 2; ++h)
@@ -437,13 +449,56 @@ __global__ __launch_bounds__(128) void k_kv_mass_join(const __grid_constant__ Ma
     }
 }
 
+// The second pass from scores that the first one left: a thread a position.
+__global__ __launch_bounds__(256) void k_kv_mass_sums(const __grid_constant__ MassArgs P)
+{
+    __shared__ float2 norm[GBS_KV_MASS_FEW_ROWS];
+    __shared__ int2 sees[GBS_KV_MASS_FEW_ROWS];
+    kv_wait_before();
+    kv_let_next();
+    const gbs_kv_attn& A = P.a;
+    const int item = blockIdx.x / A.c.heads, head = blockIdx.x - item * A.c.heads;
+    const KvEntry e = kv_entry<KV_ALL>(A, P.line, item);
+    if (e.units == 0 || 256ll * blockIdx.y >= e.length) return;
+    if (threadIdx.x < e.rows) {
+        const int token = A.by_group(threadIdx.x);
+        norm[threadIdx.x] = P.norms[tile_of(P, head, item, e.first) * 8 + threadIdx.x];
+        sees[threadIdx.x] = make_int2(kv_row_lo(A, e, token), kv_row_hi(A, e, token));
+    }
+    __syncthreads();
+    const long long row = ((long long)e.seq * A.c.heads + head) * P.width;
+    for (long long pos = 256ll * blockIdx.y + threadIdx.x; pos < e.length && pos < P.width; pos += 256ll * gridDim.y) {
+        const float* z = P.scores + (((long long)item * A.c.heads + head) * P.width + pos) * P.score_rows;
+        const float old = P.decay != 0.f && pos < e.before ? P.base[row + pos] : 0.f;
+        float sum = 0.f;
+        const auto add = [&](int r, float x) {
+            const float2 n = norm[r];
+            const int2 s = sees[r];
+            if (r < e.rows && pos >= s.x && pos < s.y) sum = fmaf(kv_ex2(x - n.x), n.y, sum);
+        };
+        if ((P.score_rows & 3) == 0)
+            for (int r = 0; r < e.rows; r += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(z + r);
+                add(r, x.x); add(r + 1, x.y); add(r + 2, x.z); add(r + 3, x.w);
+            }
+        else
+            for (int r = 0; r < e.rows; ++r) add(r, z[r]);
+        P.mass[row + pos] = fmaf(P.decay, old, sum);
+    }
+}
+
 int blocks_of(const gbs_plan* p) { return p->sm_count * BLOCKS_PER_SM; }
 int64_t round_up(int64_t x) { return (x + 15) & ~(int64_t)15; }
 
 struct Layout {
-    int64_t tiles, max_rows, rows, factors, norms, parts, joins, bytes;
+    int64_t tiles, max_rows, rows, factors, norms, parts, joins, scores, bytes;
+    int score_rows;                              // 0: scores are not kept
 };
-Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A)
+// Keeping scores (4 bytes a row, token and KV head, written once and read once) takes less time than finding them again from the keys, but room by the width, since the
+// lengths are not known here: up to this many bytes.
+constexpr int64_t MOST_SCORES = 256ll << 20;
+
+Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A, int64_t width)
 {
     Layout l;
     l.tiles = A.n_tokens * A.group / 8 + A.n_items + 1;
@@ -453,16 +508,19 @@ Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A)
     l.norms = l.factors + round_up(A.c.heads * l.tiles * 8 * (int64_t)sizeof(float2));
     l.parts = l.norms + round_up(A.c.heads * l.tiles * 8 * (int64_t)sizeof(float2));
     l.joins = l.parts + round_up((int64_t)blocks_of(p) * 2 * l.max_rows * sizeof(float2));
-    l.bytes = l.joins + round_up((int64_t)blocks_of(p) * sizeof(KvJoin));
+    l.scores = l.joins + round_up((int64_t)blocks_of(p) * sizeof(KvJoin));
+    const int64_t rows = (l.max_rows + 1) & ~1ll, places = (int64_t)A.n_items * A.c.heads * rows * (int64_t)sizeof(float);
+    l.score_rows = places > 0 && width <= MOST_SCORES / places ? (int)rows : 0;
+    l.bytes = l.scores + (l.score_rows ? places * width : 0);
     return l;
 }
 
-template <bool ASYM, bool MASS>
+template <bool ASYM, bool MASS, bool KEEP>
 int launch(const gbs_plan* p, const MassArgs& P, cudaStream_t stream)
 {
-    const cudaError_t e = cudaFuncSetAttribute((const void*)k_kv_mass<ASYM, MASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<ASYM>));
+    const cudaError_t e = cudaFuncSetAttribute((const void*)k_kv_mass<ASYM, MASS, KEEP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<ASYM>));
     if (e != cudaSuccess) return (int)e;
-    return gbs_kv_launch(p, k_kv_mass<ASYM, MASS>, dim3((unsigned)blocks_of(p)), THREADS, sizeof(Smem<ASYM>), stream, P);
+    return gbs_kv_launch(p, k_kv_mass<ASYM, MASS, KEEP>, dim3((unsigned)blocks_of(p)), THREADS, sizeof(Smem<ASYM>), stream, P);
 }
 
 }  // namespace
@@ -473,13 +531,13 @@ bool many(const gbs_kv_attn& A) { return std::min<int64_t>(A.max_tokens, A.n_tok
 
 }  // namespace
 
-int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A) { return many(A) ? gbs_tc_kvmass_workspace(p, A) : layout_of(p, A).bytes; }
+int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A, int64_t width) { return many(A) ? gbs_tc_kvmass_workspace(p, A) : layout_of(p, A, width).bytes; }
 
 int gbs_kv_mass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* base, float decay, float* mass, int64_t width, void* workspace,
                        cudaStream_t stream)
 {
     if (many(A)) return gbs_tc_kvmass_launch(p, A, base, decay, mass, width, workspace, stream);
-    const Layout l = layout_of(p, A);
+    const Layout l = layout_of(p, A, width);
     unsigned char* w = static_cast<unsigned char*>(workspace);
     MassArgs P = {};
     P.a = A;
@@ -497,15 +555,21 @@ int gbs_kv_mass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* bas
     P.parts = reinterpret_cast<float2*>(w + l.parts);
     P.joins = reinterpret_cast<KvJoin*>(w + l.joins);
     P.max_rows = l.max_rows;
+    P.scores = reinterpret_cast<float*>(w + l.scores);
+    P.score_rows = l.score_rows;
     P.base = base;
     P.mass = mass;
     P.width = width;
     P.decay = decay;
     const int64_t jobs = A.n_tokens * ((A.n_heads + 3) / 4);
     int rc = gbs_kv_launch(p, k_kv_mass_rows, dim3((unsigned)((jobs + 7) / 8)), 256, 0, stream, P);
-    if (rc == 0) rc = p->asym ? launch<true, false>(p, P, stream) : launch<false, false>(p, P, stream);
+    const bool keep = l.score_rows > 0;
+    if (rc == 0)
+        rc = keep ? (p->asym ? launch<true, false, true>(p, P, stream) : launch<false, false, true>(p, P, stream))
+                  : (p->asym ? launch<true, false, false>(p, P, stream) : launch<false, false, false>(p, P, stream));
     const unsigned y = (unsigned)std::min<int64_t>((l.max_rows + 127) / 128, 64);
     if (rc == 0) rc = gbs_kv_launch(p, k_kv_mass_join, dim3((unsigned)blocks_of(p), y), 128, 0, stream, P);
-    if (rc == 0) rc = p->asym ? launch<true, true>(p, P, stream) : launch<false, true>(p, P, stream);
-    return rc;
+    if (rc != 0) return rc;
+    if (!keep) return p->asym ? launch<true, true, false>(p, P, stream) : launch<false, true, false>(p, P, stream);
+    return gbs_kv_launch(p, k_kv_mass_sums, dim3((unsigned)A.n_items * (unsigned)A.c.heads, (unsigned)std::min<int64_t>((width + 255) / 256, 4096)), 256, 0, stream, P);
 }

@@ -592,7 +592,7 @@ PyObject* do_kv_attention_mass(const Pool& p, const PlanRef& ref, PyObject* cons
     if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
     const int n = static_cast<int>(it.n);
     int64_t need;
-    if (q.heads > 0x7fffffff || gbs_kv_attention_mass_workspace(ref.plan, &p.cache, n, q.n, most, static_cast<int>(q.heads), &need) != GBS_OK) Py_RETURN_NONE;
+    if (q.heads > 0x7fffffff || gbs_kv_attention_mass_workspace(ref.plan, &p.cache, n, q.n, most, static_cast<int>(q.heads), width, &need) != GBS_OK) Py_RETURN_NONE;
     at::Tensor work = at::detail::empty_cuda({need}, at::kByte, device_of(p), std::nullopt);
     if (gbs_kv_attention_mass(ref.plan, &p.cache, it.seqs, it.cu, n, q.n, most, q.ptr, q.token, q.head, static_cast<int>(q.heads), static_cast<float>(scale),
                               window, causal ? GBS_KV_CAUSAL : 0, base, static_cast<float>(decay), mass, width, work.data_ptr(), need, stream_on(p)) != GBS_OK)

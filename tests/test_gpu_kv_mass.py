@@ -133,6 +133,16 @@ def test_long_sequences_and_many_rows():
         check(cache, rows(64, 4, 128, 2, 2.0), [0], [0, 64], decay=0.0, window=5000)
 
 
+def test_scores_that_have_no_room():
+    """A width by which the scores of a call are not kept: the second pass finds them again."""
+    with Plan(128, 128, 1, 4, 128, 0.9) as plan:
+        cache = filled(plan, [700, 3000, 1, 64], 2, 64, seed=2)
+        for count, heads in ((1, 64), (4, 16), (1, 2)):
+            width = (256 << 20) // (4 * 2 * 4 * (count * heads // 2 + (count * heads // 2) % 2)) + 1
+            counts = [count, count, 1, count]
+            check(cache, rows(sum(counts), heads, 128, 1, 2.0), [0, 1, 2, 3], cu_of(counts), width=width, decay=0.9, window=2000)
+
+
 def test_tokens_beyond_max_tokens_give_no_weight():
     with Plan(128, 128, 1, 4, 128, 0.9) as plan:
         cache = filled(plan, [200, 90], 2, 16, seed=2)

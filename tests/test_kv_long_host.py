@@ -75,10 +75,12 @@ def test_attention_mass(lib):
     assert f(t=0, q=None) == OK and f(n=0, to=None) == OK
     size, r = ctypes.c_int64(-1), ctypes.byref(pool())
     w = lib.gbs_kv_attention_mass_workspace
-    assert w(plan(d=80), r, 2, 3, 2, 8, ctypes.byref(size)) == OK and f(size=size.value - 1) == INVALID
-    for bad in ((-1, 3, 2, 8), (2, -1, 2, 8), (2, 3, 0, 8), (2, 3, 2, 6)):
+    assert w(plan(d=80), r, 2, 3, 2, 8, 7, ctypes.byref(size)) == OK and f(size=size.value - 1) == INVALID
+    for bad in ((-1, 3, 2, 8, 7), (2, -1, 2, 8, 7), (2, 3, 0, 8, 7), (2, 3, 2, 6, 7), (2, 3, 2, 8, 0)):
         assert w(plan(d=80), r, *bad, ctypes.byref(size)) == INVALID
-    assert w(plan(d=80), r, 2, 3, 2, 8, None) == INVALID
+    assert w(plan(d=80), r, 2, 3, 2, 8, 7, None) == INVALID
+    for width in (1 << 20, 1 << 40, (1 << 63) - 1):                                # scores have room up to a limit
+        assert w(plan(d=80), r, 2, 3, 2, 8, width, ctypes.byref(size)) == OK and 0 < size.value < 300 << 20
 
 
 def test_evict(lib):
