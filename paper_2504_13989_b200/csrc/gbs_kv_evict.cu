@@ -104,12 +104,9 @@ __global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(cons
             if (BLOCKS > 1 && digit == 0) all_blocks();          // nobody adds to what another block has not cleared yet
             else __syncthreads();
             const auto count = [&](unsigned v) {
-                if (digit == 0) {                // the upper digits of most weights fall into few bins: those of a warp's that are alike are counted together
-                    const unsigned same = __match_any_sync(0xffffffffu, v >> 21);
-                    if (v != 0 && lane == __ffs(same) - 1) atomicAdd(&bins[v >> 21], __popc(same));
-                } else if (v >> (shift + bits) == threshold) {
-                    atomicAdd(&bins[(v >> shift) & (n - 1)], 1);
-                }
+                // (the upper digits of most weights fall into few bins; counting what is alike in a warp together first, by __match_any_sync: 37 us instead of 27 for 131 000
+                // weights by eight blocks)
+                if (digit == 0 ? v != 0 : v >> (shift + bits) == threshold) atomicAdd(&bins[(v >> shift) & (n - 1)], 1);
             };
 #pragma unroll
             for (int x = 0; x < HELD; ++x)
@@ -324,7 +321,7 @@ __global__ __launch_bounds__(MOVE, 5) void k_kv_evict_move(const __grid_constant
     if (threadIdx.x == 0) E.c.lengths[seq] = E.keep;
 }
 
-// Long sequences of few items and heads are looked through by clusters of 8 x 1024 threads, others by 256: 16 rows of 131 000 weights 168 us with a block of 1024 each.
+// Long sequences of few items and heads are looked through by clusters of 8 x 1024 threads, others by 256: 16 rows of up to 131 000 weights 27 us, 168 with a block of 1024 threads for each.
 constexpr int FEW = 256, MANY = 1024, CLUSTER = 8;
 
 template <int THREADS, int BLOCKS>
