@@ -466,13 +466,15 @@ int gbs_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const 
 
 /*
  * The same attention for items whose sequences begin alike, as forks of one prompt do: what a group's sequences have in common is read
- * once for all of the group's rows.  Common are the full pages, from a sequence's first on, that stand in the page tables of all items of the group that have
+ * once for all of the group's rows, where that is likely to take less time.  Common are the full pages, from a sequence's first on, that stand in the page tables of all items of the group that have
  * tokens and lie before the tokens of each of them; the call finds them in the tables, so a group of sequences that share nothing is attended over as well,
  * and as slowly as by gbs_kv_attention.  Results differ from that call's by rounding alone.  There is no window.
  *   groups            device int32 [n_groups + 1], values that do not fall: group g is items groups[g] .. groups[g + 1] - 1, and items of no
  *                     group share nothing.  NULL: all items are one group (n_groups is 1)
  *   n_groups          1 .. GBS_KV_MAX_ITEMS
  *   max_own           about the most tokens that a sequence has behind what its group shares (0: the table's width), as max_len of gbs_kv_attention
+ *   max_prefix        about the most tokens that a group shares (0: the table's width), by which it is judged whether sharing gains anything: finding the groups and joining
+ *                     what their rows got costs some 20 to 45 microseconds.  Where it does not, the call does what gbs_kv_attention does
  *   n_tokens          query heads of a KV head * n_tokens: at most 2^28
  *   workspace         gbs_kv_shared_attention_workspace bytes, 16-byte aligned; it holds 528 bytes a token and query head.  The same number of items, tokens and groups and
  *                     the same max_tokens as in the call
@@ -481,7 +483,7 @@ int gbs_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const 
 int gbs_kv_shared_attention_workspace(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
                                       int n_groups, int n_heads, int64_t* bytes_out);
 int gbs_kv_shared_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
-                            int64_t n_tokens, int max_tokens, const int32_t* groups, int n_groups, int max_own, const void* q,
+                            int64_t n_tokens, int max_tokens, const int32_t* groups, int n_groups, int max_own, int max_prefix, const void* q,
                             int64_t q_token_stride, int64_t q_head_stride, int n_heads, float scale, int flags, void* out,
                             int64_t out_token_stride, int64_t out_head_stride, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 

@@ -150,7 +150,7 @@ def lib() -> ctypes.CDLL:
                                        vp, i64, vp]
         L.gbs_selftest_kv_attention.argtypes = L.gbs_kv_attention.argtypes[:-1] + [i32, i32, vp]
         L.gbs_kv_shared_attention_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i32, ctypes.POINTER(i64)]
-        L.gbs_kv_shared_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, vp, i64, i64,
+        L.gbs_kv_shared_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i32, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, vp, i64, i64,
                                               vp, i64, vp]
         L.gbs_kv_attention_mass_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i64, ctypes.POINTER(i64)]
         L.gbs_kv_attention_mass.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i64, i64, i32, ctypes.c_float, i32, i32, vp, ctypes.c_float, vp, i64,
@@ -757,16 +757,17 @@ class KVCache:
         return out
 
     def shared_attention(self, q: torch.Tensor, seqs=None, cu_tokens=None, groups=None, max_tokens: int | None = None, causal: bool = True,
-                         scale: float = 0.0, max_own: int = 0, out=None, stream=None) -> torch.Tensor:
+                         scale: float = 0.0, max_own: int = 0, max_prefix: int = 0, out=None, stream=None) -> torch.Tensor:
         """attention (without a window) for items whose sequences begin alike, as forks of one prompt do: the pages that all items of a group begin with are
         read once for the group.  groups: int32 [groups + 1], the first item of each group and the end (None: all items are one group); which pages
-        are common is found in the page table.  max_own: about how many tokens the longest sequence has behind what its group shares."""
+        are common is found in the page table.  max_own: about how many tokens the longest sequence has behind what its group shares; max_prefix: about how many the longest prefix has
+        (0: the table's width), by which the call judges whether sharing gains anything; where it does not, it does what attention does."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise ValueError("gbs: q must be [tokens, heads, d]")
         self._rows("q", q, q.shape[1])
         if max_tokens is None:
             max_tokens = max(1, q.shape[0]) if cu_tokens is not None else 1
-        for what, v in (("max_tokens", max_tokens), ("max_own", max_own)):
+        for what, v in (("max_tokens", max_tokens), ("max_own", max_own), ("max_prefix", max_prefix)):
             _int32(what, v)
         if out is None:
             out = self._empty(stream, q.shape, torch.bfloat16)
@@ -782,7 +783,7 @@ class KVCache:
                                                        ctypes.byref(need)), "gbs_kv_shared_attention_workspace")
         work = self._empty(stream, need.value, torch.uint8, False)
         _check(lib().gbs_kv_shared_attention(self.plan.handle, ctypes.byref(self._c), s, cu, n, q.shape[0], max_tokens,
-                                             self._ints("groups", groups, n_groups + 1), n_groups, max_own, q.data_ptr(), *self._strides(q), q.shape[1],
+                                             self._ints("groups", groups, n_groups + 1), n_groups, max_own, max_prefix, q.data_ptr(), *self._strides(q), q.shape[1],
                                              float(scale), GBS_KV_CAUSAL if causal else 0, out.data_ptr(), *self._strides(out), work.data_ptr(),
                                              need.value, self._stream(stream, q, out, seqs, cu_tokens, groups)), "gbs_kv_shared_attention")
         return out

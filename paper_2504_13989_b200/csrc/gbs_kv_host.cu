@@ -352,7 +352,7 @@ extern "C" int gbs_kv_shared_attention_workspace(const gbs_plan_t* p, const gbs_
 }
 
 extern "C" int gbs_kv_shared_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
-                                       int64_t n_tokens, int max_tokens, const int32_t* groups, int n_groups, int max_own, const void* q,
+                                       int64_t n_tokens, int max_tokens, const int32_t* groups, int n_groups, int max_own, int max_prefix, const void* q,
                                        int64_t q_token_stride, int64_t q_head_stride, int n_heads, float scale, int flags, void* out,
                                        int64_t out_token_stride, int64_t out_head_stride, void* workspace, int64_t workspace_bytes, void* stream)
 {
@@ -361,14 +361,14 @@ extern "C" int gbs_kv_shared_attention(const gbs_plan_t* p, const gbs_kv_cache_t
     gbs_kv_attn A;
     bool empty = false;
     int rc = attn_args(p, cache, x, &A, &empty);
-    if (rc == GBS_OK) rc = check_groups(groups, n_groups, A);
+    if (rc == GBS_OK) rc = max_prefix < 0 ? GBS_ERR_INVALID_ARG : check_groups(groups, n_groups, A);
     if (rc != GBS_OK || empty) return rc;
     gbs_kv_attn given = A;                                           // the workspace's size goes by the arguments as they are given
     given.max_tokens = max_tokens;
     if (!q || !out || !workspace || workspace_bytes < gbs_kv_shared_workspace(p, given, n_groups)) return GBS_ERR_INVALID_ARG;
     rc = check_rows(p, x, true, workspace);
     if (rc != GBS_OK) return rc;
-    return on_device(p, [&] { return gbs_kv_shared_launch(p, A, groups, n_groups, workspace, static_cast<cudaStream_t>(stream)); });
+    return on_device(p, [&] { return gbs_kv_shared_launch(p, A, groups, n_groups, max_prefix, workspace, static_cast<cudaStream_t>(stream)); });
 }
 
 extern "C" int gbs_kv_attention_mass_workspace(const gbs_plan_t* p, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,

@@ -185,6 +185,21 @@ bool one_tile(const gbs_plan* p, const gbs_kv_attn& A, int n_groups)
     const int64_t rows = A.n_tokens * A.group, units = ((int64_t)A.c.max_pages << A.c.page_log) / 128;
     return rows <= 128ll * n_groups || (rows <= 256ll * n_groups && units * A.c.heads * n_groups <= 8ll * p->sm_count);
 }
+// Whether reading the prefixes once is likely to take less time than gbs_kv_attention does.  What an SM needs for 128 tokens, in microseconds: 0.63 for a tile of 8 rows, 2.5 (2.1 in one tile) up to 128
+// rows, 2.9 for 256.  The lengths are not known here; without max_prefix the table's width stands for a prefix's.  Finding the groups, two more launches and their joins cost
+// 20 to 45 us.  us with and without sharing, and the gain by this rule: 64 sequences behind 6000 tokens 54 and 98, 102; 14 behind 51 000 69 and 89, 74; 12 x 4 tokens behind 100 000 306 and 1102,
+// 1030; but 10 behind 66 000, 2 KV heads, 64 and 55, 30; 17 behind 63 000, one KV head, 64 and 48, 26; 8 prompts of 250 behind 12 000 301 and 285, 30; 40 in 7 groups behind 8000 60 and 44,
+// 19; 4 behind 300 27 and 12, 0.  Between 45 and 74 neither side was seen to lose by much.
+constexpr double LEAST_GAIN = 45;
+double gain_of(const gbs_plan* p, const gbs_kv_attn& A, int n_groups, int64_t max_prefix)
+{
+    const auto tiles = [](double rows, int tile) { return (double)(int64_t)((rows + tile - 1) / tile); };
+    const double most = (double)A.max_tokens * A.group, rows = (double)A.n_tokens * A.group / A.n_items, all = (double)A.n_tokens * A.group / n_groups;
+    const double apart = most <= GBS_KV_FEW_ROWS ? tiles(most, 8) * 0.63 : most <= 128 ? 2.5 : tiles(rows, 256) * 2.9;
+    const double once = all <= FEW_PREFIX_ROWS ? tiles(all, 8) * 0.63 : all <= 128 ? 2.1 : tiles(all, 256) * 2.9;
+    const double longest = max_prefix > 0 ? (double)max_prefix : (double)((int64_t)A.c.max_pages << A.c.page_log);
+    return (A.n_items * apart - n_groups * once) * A.c.heads / p->sm_count * longest / 128;
+}
 int64_t round_up(int64_t x) { return (x + 15) & ~(int64_t)15; }
 
 struct Layout {
@@ -212,8 +227,14 @@ Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A, int n_groups)
 
 int64_t gbs_kv_shared_workspace(const gbs_plan* p, const gbs_kv_attn& A, int n_groups) { return layout_of(p, A, n_groups).bytes; }
 
-int gbs_kv_shared_launch(const gbs_plan* p, const gbs_kv_attn& A, const int* groups, int n_groups, void* workspace, cudaStream_t stream)
+int gbs_kv_shared_launch(const gbs_plan* p, const gbs_kv_attn& A, const int* groups, int n_groups, int max_prefix, void* workspace, cudaStream_t stream)
 {
+    if (gain_of(p, A, n_groups, max_prefix) <= LEAST_GAIN) {
+        gbs_kv_attn W = A;                       // max_len of an own part becomes one of a sequence
+        const int64_t width = (int64_t)A.c.max_pages << A.c.page_log;
+        W.max_len = max_prefix > 0 && (int64_t)A.max_len + max_prefix < width ? A.max_len + max_prefix : (int)width;
+        return few_own(A) ? gbs_kv_few_launch(p, W, workspace, stream) : gbs_tc_kvattn_launch(p, W, workspace, stream);
+    }
     const Layout l = layout_of(p, A, n_groups);
     unsigned char* w = static_cast<unsigned char*>(workspace);
     const bool few = few_prefix(A, n_groups);

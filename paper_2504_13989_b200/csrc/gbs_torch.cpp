@@ -532,18 +532,18 @@ PyObject* do_kv_attention(const Pool& p, const PlanRef& ref, PyObject* const* g)
     GBS_END
 }
 
-// q, seqs, cu_tokens, groups, max_tokens, causal, scale, max_own, out, stream
+// q, seqs, cu_tokens, groups, max_tokens, causal, scale, max_own, max_prefix, out, stream
 PyObject* do_kv_shared_attention(const Pool& p, const PlanRef& ref, PyObject* const* g)
 {
     GBS_BEGIN
     Rows q, o;
     Items it;
-    int most, longest;
+    int most, longest, prefix;
     const int32_t* groups;
-    if (!none(g[9]) || !rows3_of(p, g[0], ref.info.d, &q) || !items_of(p, g[1], g[2], q.n, &it)) Py_RETURN_NONE;
+    if (!none(g[10]) || !rows3_of(p, g[0], ref.info.d, &q) || !items_of(p, g[1], g[2], q.n, &it)) Py_RETURN_NONE;
     const int64_t n_groups = none(g[3]) ? 1 : length_of(g[3]) - 1;
     if (n_groups < 1 || n_groups > GBS_KV_MAX_ITEMS || !ints_of(p, g[3], n_groups + 1, &groups)) Py_RETURN_NONE;
-    if (q.n > 0x7fffffff || !int_of(none(g[4]) ? nullptr : g[4], none(g[2]) ? 1 : static_cast<int>(std::max<int64_t>(1, q.n)), &most) || !int_of(g[7], 0, &longest)) Py_RETURN_NONE;
+    if (q.n > 0x7fffffff || !int_of(none(g[4]) ? nullptr : g[4], none(g[2]) ? 1 : static_cast<int>(std::max<int64_t>(1, q.n)), &most) || !int_of(g[7], 0, &longest) || !int_of(g[8], 0, &prefix)) Py_RETURN_NONE;
     const int causal = g[5] ? PyObject_IsTrue(g[5]) : 1;
     const double scale = g[6] ? PyFloat_AsDouble(g[6]) : 0.0;
     if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
@@ -551,15 +551,15 @@ PyObject* do_kv_shared_attention(const Pool& p, const PlanRef& ref, PyObject* co
     int64_t need;
     if (q.heads > 0x7fffffff || gbs_kv_shared_attention_workspace(ref.plan, &p.cache, n, q.n, most, ng, static_cast<int>(q.heads), &need) != GBS_OK) Py_RETURN_NONE;
     at::Tensor out;
-    if (none(g[8])) {
+    if (none(g[9])) {
         out = at::detail::empty_cuda(q.t->sizes(), at::kBFloat16, device_of(p), std::nullopt);
         o = {&out, out.data_ptr(), q.n, q.heads, q.heads * ref.info.d, ref.info.d};
-    } else if (!rows3_of(p, g[8], ref.info.d, &o) || o.n != q.n || o.heads != q.heads) Py_RETURN_NONE;
+    } else if (!rows3_of(p, g[9], ref.info.d, &o) || o.n != q.n || o.heads != q.heads) Py_RETURN_NONE;
     at::Tensor work = at::detail::empty_cuda({need}, at::kByte, device_of(p), std::nullopt);
-    if (gbs_kv_shared_attention(ref.plan, &p.cache, it.seqs, it.cu, n, q.n, most, groups, ng, longest, q.ptr, q.token, q.head, static_cast<int>(q.heads),
+    if (gbs_kv_shared_attention(ref.plan, &p.cache, it.seqs, it.cu, n, q.n, most, groups, ng, longest, prefix, q.ptr, q.token, q.head, static_cast<int>(q.heads),
                                 static_cast<float>(scale), causal ? GBS_KV_CAUSAL : 0, o.ptr, o.token, o.head, work.data_ptr(), need, stream_on(p)) != GBS_OK)
         Py_RETURN_NONE;
-    if (!none(g[8])) return Py_NewRef(g[8]);
+    if (!none(g[9])) return Py_NewRef(g[9]);
     return THPVariable_Wrap(std::move(out));
     GBS_END
 }
@@ -665,7 +665,7 @@ constexpr Method KV_APPEND = {"append", 6, 2, {"k", "v", "seqs", "cu_tokens", "s
 constexpr Method KV_READ = {"read", 5, 0, {"seqs", "cu_tokens", "n_tokens", "out", "stream"}, nullptr, do_kv_read};
 constexpr Method KV_ATTENTION = {"attention", 10, 1, {"q", "seqs", "cu_tokens", "max_tokens", "causal", "window", "scale", "max_len", "out", "stream"},
                                  nullptr, do_kv_attention};
-constexpr Method KV_SHARED = {"shared_attention", 10, 1, {"q", "seqs", "cu_tokens", "groups", "max_tokens", "causal", "scale", "max_own", "out", "stream"},
+constexpr Method KV_SHARED = {"shared_attention", 11, 1, {"q", "seqs", "cu_tokens", "groups", "max_tokens", "causal", "scale", "max_own", "max_prefix", "out", "stream"},
                               nullptr, do_kv_shared_attention};
 constexpr Method KV_MASS = {"attention_mass", 11, 2, {"q", "mass", "seqs", "cu_tokens", "max_tokens", "decay", "base", "causal", "window", "scale", "stream"},
                             nullptr, do_kv_attention_mass};

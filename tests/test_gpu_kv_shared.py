@@ -8,6 +8,7 @@ from paper_2504_13989_b200 import GbsError, Plan
 from paper_2504_13989_b200 import build as gbs_build
 
 pytestmark = pytest.mark.gpu
+LONG = 1 << 27                     # a prefix that is said to be so long is worth sharing, whatever it is
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -52,7 +53,7 @@ def forked(plan, prompts, forks, own, kvh, page, seed=0):
 
 def check(cache, q, seqs, cu, groups, causal=True, scale=0.0, **kw):
     got = cache.shared_attention(q, ints(seqs), ints(cu), None if groups is None else ints(groups), kw.pop("max_tokens", max(b - a for a, b in zip(cu, cu[1:]))),
-                                 causal=causal, scale=scale, **kw)
+                                 causal=causal, scale=scale, **{"max_prefix": LONG, **kw})
     want, tol = kv_util.attention(cache, q, seqs, cu, causal, 0, scale, few=False)
     live = ~want.isnan().all(-1).all(-1)
     assert bool(((got.double() - want).abs() <= tol)[live].all()), float(((got.double() - want).abs() / tol)[live].max())
@@ -80,6 +81,9 @@ def test_forks_of_one_prompt(d, kvh, group, page, prompt, count, asym):
             q = rows(items * count, kvh * group, d, 5, 3.0)
             check(cache, q, seqs, cu_of([count] * items), None)
             check(cache, q, seqs, cu_of([count] * items), [0, items], causal=False, scale=0.3, max_own=max(own) + page)
+            for prefix in (0, prompt):                         # as the call judges itself: prefixes as short as these are not shared
+                got = check(cache, q, seqs, cu_of([count] * items), None, max_prefix=prefix)
+                assert torch.equal(got, cache.attention(q, ints(seqs), ints(cu_of([count] * items)), count))
 
 
 @pytest.mark.parametrize("count", [1, 30])
@@ -96,7 +100,7 @@ def test_groups_of_every_kind(count):
         q = rows(sum(counts), 8, 128, 7, 2.0)
         for groups in ([0, 3, 4, 6, 11, 13], [0, 3, 3, 11], [2, 7, 11], [0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14], None):
             out = torch.full_like(q, 7.0)
-            got = cache.shared_attention(q, ints(seqs), ints(cu_of(counts)), None if groups is None else ints(groups), max(count, 1), out=out)
+            got = cache.shared_attention(q, ints(seqs), ints(cu_of(counts)), None if groups is None else ints(groups), max(count, 1), max_prefix=LONG, out=out)
             keep = [i for i in range(len(seqs)) if seqs[i] < 13]
             want, tol = kv_util.attention(cache, q, [s if s < 13 else 0 for s in seqs], cu_of(counts), few=False)
             cu = cu_of(counts)
@@ -125,7 +129,7 @@ def test_a_page_that_is_none_of_the_pools_is_left_out_of_a_prefix():
         q = rows(4, 8, 128, 2, 2.0)
         for bad in (-1, cache.pages.shape[0], 2 ** 31 - 1, -2 ** 31):
             cache.page_table[:, 3] = bad
-            assert torch.allclose(cache.shared_attention(q, ints([1, 2, 3, 4])).float(), cache.attention(q, ints([1, 2, 3, 4])).float(), atol=0.02, rtol=0.02)
+            assert torch.allclose(cache.shared_attention(q, ints([1, 2, 3, 4]), max_prefix=LONG).float(), cache.attention(q, ints([1, 2, 3, 4])).float(), atol=0.02, rtol=0.02)
 
 
 @pytest.mark.parametrize("which", [0, 1])
@@ -136,7 +140,7 @@ def test_scales_that_are_no_numbers_in_the_prefix(which):
             cache = forked(plan, [300, 300], [0] * n + [1] * n, [9] * (2 * n), 1, 16)
             cache.pages.view(torch.float32).view(cache.pages.shape[0], -1)[int(cache.page_table[0, 4]), 16 * 32 + 16 * which + 5] = float("nan")
             q = rows(2 * n, 4, 128, 2)
-            got = cache.shared_attention(q, ints(range(2, 2 + 2 * n)), None, ints([0, n, 2 * n]))
+            got = cache.shared_attention(q, ints(range(2, 2 + 2 * n)), None, ints([0, n, 2 * n]), max_prefix=LONG)
             assert got[:n].isnan().all() and got[n:].isfinite().all()
             assert plan.device_status() == 0
 
@@ -159,7 +163,7 @@ def test_strides_and_rows_that_are_left():
         q = wide[:, :, 8:104]
         room = torch.full((cu[-1] + 6, 11, 104), 5.0, dtype=torch.bfloat16, device=DEV)
         out = room[:, 2:10, :96]
-        got = cache.shared_attention(q, ints([1, 2, 3, 4, 5]), ints(cu), None, 4, out=out)
+        got = cache.shared_attention(q, ints([1, 2, 3, 4, 5]), ints(cu), None, 4, max_prefix=LONG, out=out)
         want, tol = kv_util.attention(cache, q[:cu[-1]].contiguous(), [1, 2, 3, 4, 5], cu, few=False)
         there = torch.zeros(cu[-1] + 6, dtype=torch.bool, device=DEV)
         for i, c in enumerate(counts):
@@ -180,7 +184,7 @@ def test_a_captured_step_that_grows():
         def step():
             status = cache.extend(seqs)
             cache.append(k, v, seqs, status=status)
-            return cache.shared_attention(q, seqs, max_own=32)
+            return cache.shared_attention(q, seqs, max_own=32, max_prefix=LONG)
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
             step()
@@ -206,13 +210,13 @@ def test_two_calls_at_the_same_time():
         cache = forked(plan, [6000], [0] * 20, [200] * 20, 2, 64)
         side, seqs = torch.cuda.Stream(), ints(range(1, 21))
         qs = [rows(20, 16, 128, 5), rows(20, 16, 128, 6)]
-        want = [cache.shared_attention(q, seqs) for q in qs]
+        want = [cache.shared_attention(q, seqs, max_prefix=LONG) for q in qs]
         torch.cuda.synchronize()
         for _ in range(10):
             got = []
             for _ in range(3):
-                got.append(cache.shared_attention(qs[0], seqs))
-                got.append(cache.shared_attention(qs[1], seqs, stream=side))
+                got.append(cache.shared_attention(qs[0], seqs, max_prefix=LONG))
+                got.append(cache.shared_attention(qs[1], seqs, max_prefix=LONG, stream=side))
             torch.cuda.synchronize()
             assert all(torch.equal(g, want[i & 1]) for i, g in enumerate(got))
 
@@ -224,11 +228,11 @@ def test_many_items_and_numbers_of_groups_that_fall():
         seqs = ([2, 3, 2, 3] * 2 + [4, 5] * 4) * 512
         q = rows(8192, 2, 128, 1)
         groups = sorted(list(range(0, 8192, 16)) + list(range(8, 8192, 16))) + [8192]
-        got = cache.shared_attention(q, ints(seqs), None, ints(groups))
+        got = cache.shared_attention(q, ints(seqs), None, ints(groups), max_prefix=LONG)
         assert torch.allclose(got.float(), cache.attention(q, ints(seqs)).float(), atol=0.02, rtol=0.02)
         room = torch.full((8200, 2, 128), 3.0, dtype=torch.bfloat16, device=DEV)
         for bad in ([5, 2, 9, 1, 30], [-7, 100, 50, 9000, 8192], [2 ** 31 - 1, -2 ** 31, 0, 8192]):
-            cache.shared_attention(q, ints(seqs), None, ints(bad), out=room[:8192])
+            cache.shared_attention(q, ints(seqs), None, ints(bad), max_prefix=LONG, out=room[:8192])
             assert room[8192:].eq(3).all() and plan.device_status() == 0
 
 

@@ -19,9 +19,9 @@ def lib():
     return binding.lib()
 
 
-def shared(lib, pl=None, c=None, seqs=P, cu=P, n=2, t=3, most=2, groups=P, ng=1, own=0, q=P, qt=640, qh=80, heads=8, scale=0.0, flags=1, out=P + 4096, ot=640,
+def shared(lib, pl=None, c=None, seqs=P, cu=P, n=2, t=3, most=2, groups=P, ng=1, own=0, prefix=0, q=P, qt=640, qh=80, heads=8, scale=0.0, flags=1, out=P + 4096, ot=640,
            oh=80, work=P, size=1 << 40):
-    return lib.gbs_kv_shared_attention(pl or plan(d=80), ctypes.byref(c or pool()), seqs, cu, n, t, most, groups, ng, own, q, qt, qh, heads, scale, flags, out, ot,
+    return lib.gbs_kv_shared_attention(pl or plan(d=80), ctypes.byref(c or pool()), seqs, cu, n, t, most, groups, ng, own, prefix, q, qt, qh, heads, scale, flags, out, ot,
                                        oh, work, size, None)
 
 
@@ -49,7 +49,7 @@ def test_pools_plans_and_nothing_to_do(lib, f):
 
 def test_shared_attention(lib):
     f = lambda **kw: shared(lib, **kw)  # noqa: E731
-    assert f(ng=0) == INVALID and f(ng=MOST + 1) == INVALID and f(groups=None, ng=2) == INVALID and f(groups=P + 2) == ALIGN and f(own=-1) == INVALID
+    assert f(ng=0) == INVALID and f(ng=MOST + 1) == INVALID and f(groups=None, ng=2) == INVALID and f(groups=P + 2) == ALIGN and f(own=-1) == INVALID and f(prefix=-1) == INVALID
     assert f(heads=6) == INVALID and f(heads=0) == INVALID and f(most=0) == INVALID and f(cu=None, n=3, most=2) == INVALID and f(cu=None) == INVALID
     assert f(most=1 << 30) == INVALID and f(t=-1) == INVALID and f(t=1 << 29) == INVALID and f(flags=2) == INVALID
     assert f(scale=float("inf")) == INVALID and f(scale=float("nan")) == INVALID
@@ -153,3 +153,5 @@ def test_the_methods_refuse_what_the_library_cannot_see(monkeypatch):
         f["shared_attention"](c, x[0])
     with pytest.raises(ValueError):
         f["shared_attention"](c, x, max_own=2 ** 32)
+    with pytest.raises(ValueError):
+        f["shared_attention"](c, x, max_prefix=2 ** 32)
