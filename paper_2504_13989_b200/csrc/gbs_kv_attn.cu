@@ -539,10 +539,7 @@ int launch(const gbs_plan* p, const KvAttnArgs& P, int blocks, cudaStream_t stre
     if (e != cudaSuccess) return (int)e;
     const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
     if (rc != 0 || P.line.pad < 0) return rc;
-    // no more segments than tiles and KV heads; where they are as many as a quarter of the blocks, every block looks at its own
-    const int64_t most = (int64_t)P.line.entries * P.a.c.heads;
-    const bool few = 4 * most <= blocks;
-    return gbs_kv_launch(p, few ? k_kv_attn_join<ROWS, PART, true> : k_kv_attn_join<ROWS, PART, false>, dim3((unsigned)(few ? most : blocks)), 256, 0, stream, P);
+    return gbs_kv_launch(p, k_kv_attn_join<ROWS, PART, false>, dim3((unsigned)blocks), 256, 0, stream, P);
 }
 
 }  // namespace

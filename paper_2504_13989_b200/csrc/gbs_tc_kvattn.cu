@@ -179,7 +179,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
     if (tid == 0) P.joins[blockIdx.x] = KvJoin{0, 0, 0, 0};
 
     const int ps_log = A.c.page_log, ps = 1 << ps_log;
-    unsigned it = 0, round = 0, used[2] = {0, 0};            // units, segments and units of each half of the softmax so far, by which the barriers' phases go
+    unsigned it = 0, round = 0, used_a = 0, used_b = 0;      // units, segments and units of each half of the softmax so far, by which the barriers' phases go
     for (bool more = places > 0; more; ++round) {
         const KvSeg& seg = S.seg[round & 1];
         const KvPiece piece = kv_piece(P.line, seg, places);
@@ -243,11 +243,12 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             meet_all();
 
-            const int t = w >> 2, row = tid, tile = split ? 0 : t, step = split ? 2 : 1, skip = split ? t : 0;      // this thread's half, row and tile
+            const int t = w >> 2, row = tid, tile = SPLIT && split ? 0 : t, step = SPLIT && split ? 2 : 1, skip = SPLIT && split ? t : 0;      // this thread's half, row and tile
             const bool busy = t == 0 || two || split;
-            const unsigned scores = tmem + ((unsigned)(32 * (w & 3)) << 16) + 128 * t, sums = scores + O_COL, turn = used[t];
-            const float f = S.factor[TILE * tile + (row & 127)];
-            const int see_lo = S.lo[TILE * tile + (row & 127)], see_hi = S.hi[TILE * tile + (row & 127)];
+            const unsigned scores = tmem + ((unsigned)(32 * (w & 3)) << 16) + 128 * t, sums = scores + O_COL, turn = t == 0 ? used_a : used_b;
+            const int of = split ? row & (TILE - 1) : row;
+            const float f = S.factor[of];
+            const int see_lo = S.lo[of], see_hi = S.hi[of];
             // tokens that every row of the tile sees need no mask
             const int first = seg.e.row0 + TILE * tile;
             const int all_lo = kv_row_lo<PART>(A, seg.e, A.by_group(min(seg.e.rows, first + TILE) - 1)), all_hi = kv_row_hi(A, seg.e, A.by_group(first));
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 const unsigned now = it + i;
                 const int nb = now & 3, tok = tok0 + i * UNIT;
                 const bool plain = tok >= all_lo && tok + UNIT <= all_hi;
-                if (!(ok = !kv_lost<TEST>(P, &S.abort, 76, round) && mbar_wait_warp(&S.abort, &S.sfull[t], (turn + (split ? i >> 1 : i)) & 1u, P.status, 76))) break;
+                if (!(ok = !kv_lost<TEST>(P, &S.abort, 76, round) && mbar_wait_warp(&S.abort, &S.sfull[t], (SPLIT ? turn + (split ? i >> 1 : i) : t == 0 ? now : used_b + i) & 1u, P.status, 76))) break;
                 tc_fence_after();
 #pragma unroll 1
                 for (int c = 0; c < 2; ++c) {                // 64 tokens at a time
@@ -351,7 +352,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                     y[at] = x.x; y[at + 4] = x.y; y[at + 1] = x.z; y[at + 5] = x.w;
                 }
                 float total = S.l[row], m = S.m[row];
-                if (split) {
+                if constexpr (SPLIT) if (split) {
                     const float l2 = S.l[TILE + row], m2 = S.m[TILE + row], most = fmaxf(m, m2), a = kv_ex2(m - most), b = kv_ex2(m2 - most);
                     total = fmaf(l2, b, total * a);
                     m = most;
@@ -366,17 +367,19 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 if (piece.starts && piece.ends) {
                     const bool have = seg.e.row0 + row < seg.e.rows;
                     int token, head;
-                    kv_row_of(A, seg, row, token, head);
-                    if (PART == KV_WHOLE) kv_finish(y, l8, 0.f, 6.f, total, 0.f);
-                    else if (PART == KV_PREFIX) {
+                    if constexpr (PART == KV_WHOLE) kv_finish(y, l8, 0.f, 6.f, total, 0.f);
+                    else if constexpr (PART == KV_PREFIX) {
+                        kv_row_of(A, seg, row, token, head);
                         if (have) kv_leave_prefix(kv_prefix_row(A, seg, token, head), y, l8, m - KV_TOTAL_LOG<ROWS>, m, total, 0.f);
                     } else {
                         float top = m - KV_TOTAL_LOG<ROWS>, top_w = m, sum = total, extra = 0.f;
+                        kv_row_of(A, seg, row, token, head);
                         if (have && seg.e.lo > 0) kv_add_prefix(kv_prefix_row(A, seg, token, head), y, l8, top, top_w, sum, extra);
                         __syncwarp();
                         kv_finish(y, l8, top, top_w, sum, extra);
                     }
                     if (PART != KV_PREFIX && have) {
+                        kv_row_of(A, seg, row, token, head);
                         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (seg.e.first + token) * A.out_token + head * A.out_head;
                         if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
                         if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
@@ -468,7 +471,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             const unsigned long long qd = smem_desc(smem_u32(S.q[0]), 16, 1024, 2), kd = smem_desc(smem_u32(S.k[0]), 16, 1024, 2),
                                      vd = smem_desc(smem_u32(S.v[0]), 128 * 128, 1024, 2);
             const unsigned q_lo = (unsigned)qd, k_lo = (unsigned)kd, v_lo = (unsigned)vd, hi = (unsigned)(qd >> 32);          // the same in all three
-            const unsigned at = uniform(tmem), at0 = uniform(it), turn_a = uniform(used[0]), turn_b = uniform(used[1]);
+            const unsigned at = uniform(tmem), at0 = uniform(it), turn_a = uniform(used_a), turn_b = uniform(used_b);
             const int units = (int)uniform((unsigned)n), tiles = uniform(two ? 2u : 1u);
             const auto scores = [&](auto tile, unsigned b) {
                 constexpr int t = decltype(tile)::value;
@@ -502,7 +505,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 const unsigned now = at0 + i, next = now + 1;
                 if (i >= 0) {
                     if (t == 0 && (kv_lost<TEST>(P, &S.abort, 72, round) || !mbar_wait_warp(&S.abort, &S.vfull[now & 1], (now >> 1) & 1u, P.status, 72))) return false;
-                    if (kv_lost<TEST>(P, &S.abort, 73, round) || !mbar_wait_warp(&S.abort, &S.pfull[t], ((t == 0 ? turn_a : turn_b) + i) & 1u, P.status, 73)) return false;
+                    if (kv_lost<TEST>(P, &S.abort, 73, round) || !mbar_wait_warp(&S.abort, &S.pfull[t], (t == 0 ? (SPLIT ? turn_a + i : now) : turn_b + i) & 1u, P.status, 73)) return false;
                     tc_fence_after();
                     values(tile, adds, now & 1);
                     if (t + 1 == tiles) umma_commit(&S.vfree[now & 1]);
@@ -538,7 +541,10 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 umma_commit(&S.vfree[now & 1]);
                 return ahead(half, i + 2);
             };
-            if (split) {
+            if constexpr (!SPLIT) {
+                ok = unit(Is<0>{}, -1) && unit(Is<0>{}, 0);
+                for (int i = 1; i < units && ok; ++i) ok = unit(Is<1>{}, i);
+            } else if (split) {
                 ok = ahead(A_TILE, 0) && ahead(B_TILE, 1) && alternate(A_TILE, Is<0>{}, 0) && alternate(B_TILE, Is<0>{}, 1);
                 for (int i = 2; i < units && ok; i += 2) ok = alternate(A_TILE, Is<1>{}, i) && (i + 1 >= units || alternate(B_TILE, Is<1>{}, i + 1));
             } else {
@@ -561,8 +567,8 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             }
         }
         it += n;
-        used[0] += split ? (n + 1) / 2 : n;
-        used[1] += split ? n / 2 : two ? n : 0;
+        if (SPLIT) used_a += split ? (n + 1) / 2 : n;
+        used_b += split ? n / 2 : two ? n : 0;
         more = kv_more(P.line, seg, places);
     }
     tc_fence_before();
