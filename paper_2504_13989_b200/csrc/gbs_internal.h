@@ -242,7 +242,7 @@ int64_t gbs_kv_shared_workspace(const gbs_plan* p, const gbs_kv_attn& A, int n_g
 int gbs_kv_shared_launch(const gbs_plan* p, const gbs_kv_attn& A, const int* groups, int n_groups, int max_prefix, void* workspace, cudaStream_t stream);
 // gbs_kv_mass.cu : the weights that cached tokens get from up to GBS_KV_MASS_FEW_ROWS query rows of an item and KV head; gbs_tc_kvmass.cu : from more
 #define GBS_KV_MASS_FEW_ROWS 32
-int64_t gbs_tc_kvmass_workspace(const gbs_plan* p, const gbs_kv_attn& A);
+int64_t gbs_tc_kvmass_workspace(const gbs_plan* p, const gbs_kv_attn& A, int64_t width);
 int gbs_tc_kvmass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* base, float decay, float* mass, int64_t width, void* workspace,
                          cudaStream_t stream);
 int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A, int64_t width);

@@ -561,7 +561,7 @@ bool many(const gbs_kv_attn& A) { return std::min<int64_t>(A.max_tokens, A.n_tok
 
 }  // namespace
 
-int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A, int64_t width) { return many(A) ? gbs_tc_kvmass_workspace(p, A) : layout_of(p, A, width).bytes; }
+int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A, int64_t width) { return many(A) ? gbs_tc_kvmass_workspace(p, A, width) : layout_of(p, A, width).bytes; }
 
 int gbs_kv_mass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* base, float decay, float* mass, int64_t width, void* workspace,
                        cudaStream_t stream)

@@ -36,6 +36,9 @@ struct MassArgs {
     int *lo, *hi;                                // the same: what a row sees
     float2* parts;                               // [blocks][2][128]: m and the sum
     KvJoin* joins;
+    // of the second pass: KV heads (a.c.heads counts each of them once for each share of its rows), shares, and what each of these adds up, [shares][n_items][heads][width]
+    int heads, shares;
+    float* sums;
     const float* base;
     float* mass;
     long long width;
@@ -540,7 +543,9 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
         if (piece.n <= 0) break;
         const int tok0 = piece.skip * 2 * UNIT;  // the line counts pairs of units here; the last pair of a sequence may be one unit
         const int n = min(2 * piece.n, max(1, (seg.e.length - tok0 + UNIT - 1) / UNIT));
-        const long long slot = slot_of(P, seg.head, seg.index, seg.e.first);
+        // the tiles that are this segment's share: every `stride`-th of them from `part` on
+        const int stride = STAY ? 1 : P.shares, head = STAY ? seg.head : seg.head / stride, part = STAY ? 0 : seg.head - head * stride;
+        const long long slot = slot_of(P, head, seg.index, seg.e.first);
         const int pairs = (n + 1) >> 1, tiles = (seg.e.rows + TILE - 1) / TILE;
         // whether any row of a tile sees any token of a pair; whether all of its 64 rows see all of them
         const auto sees = [&](int pair, int tile) {
@@ -566,7 +571,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
                 const bool there0 = S.there[kb][w & 3] >> lane & 1, there1 = units > 1 && (S.there[kb][4 + (w & 3)] >> lane & 1);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&S.kfree[kb]);
-                for (int tile = 0; tile < tiles && ok; ++tile) {
+                for (int tile = part; tile < tiles && ok; tile += stride) {
                     if (!sees(p, tile)) continue;
                     const unsigned b = STAY ? tile : used % TILES, filled = STAY ? (tile ? used1 : used) : used / TILES;     // fillings of the buffer before this one
                     if (!STAY) ++used;
@@ -642,8 +647,9 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
                         float sum = 0.f;
 #pragma unroll
                         for (int x = 0; x < 4; ++x) sum += S.part[now & 1][x][half * UNIT + me];
-                        const long long to = ((long long)seg.e.seq * A.c.heads + seg.head) * P.width + pos;
-                        P.mass[to] = pos < seg.e.before && P.decay != 0.f ? fmaf(P.decay, P.base[to], sum) : sum;
+                        const long long to = ((long long)seg.e.seq * P.heads + head) * P.width + pos;
+                        if (!STAY && stride > 1) P.sums[(((long long)part * A.n_items + seg.index) * P.heads + head) * P.width + pos] = sum;
+                        else P.mass[to] = pos < seg.e.before && P.decay != 0.f ? fmaf(P.decay, P.base[to], sum) : sum;
                     }
                 }
             }
@@ -657,7 +663,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
             const int* pages = A.c.page_table + (long long)seg.e.seq * A.c.max_pages;
             const auto page_of = [&](int tok) { return tok < seg.e.length ? pages[tok >> A.c.page_log] : -1; };
             Key<ASYM> key;
-            key.fetch(A.c, page_of(tok0 + me), seg.head, tok0 + me, tok0 + me < seg.e.length);
+            key.fetch(A.c, page_of(tok0 + me), head, tok0 + me, tok0 + me < seg.e.length);
             int page = page_of(tok0 + UNIT + me);
             for (int i = 0; i < n; ++i) {
                 const unsigned now = pp + (i >> 1), kb = now % PAIRS;
@@ -674,7 +680,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
                 }
                 if (i + 1 < n) {
                     const int next = tok0 + (i + 1) * UNIT + me;
-                    key.fetch(A.c, page, seg.head, next, next < seg.e.length);
+                    key.fetch(A.c, page, head, next, next < seg.e.length);
                     page = page_of(next + UNIT);
                 }
             }
@@ -685,7 +691,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
             for (int p = 0; p < all_pairs && ok; ++p) {
                 const unsigned now = uniform(pp) + p, kb = now % PAIRS;
                 if (!(ok = mbar_wait_warp(&S.abort, &S.kfull[kb], (now / PAIRS) & 1u, P.status, 95))) break;
-                for (int tile = 0; tile < all_tiles; ++tile) {
+                for (int tile = (int)uniform(part); tile < all_tiles; tile += (int)uniform(stride)) {
                     if (!uniform(sees(p, tile))) continue;
                     const unsigned u = uniform(used), u1 = uniform(used1), b = STAY ? tile : u % TILES, filled = STAY ? (tile ? u1 : u) : u / TILES, d = uniform(dt);
                     if (!(ok = mbar_wait_warp(&S.abort, &S.qfull[b], filled & 1u, P.status, 96))) break;
@@ -726,7 +732,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
                 for (int tile = 0; tile < tiles && ok; ++tile) ok = fill(tile, tile, tile ? used1 : used);
             } else {
                 for (int p = 0; p < pairs && ok; ++p)
-                    for (int tile = 0; tile < tiles && ok; ++tile)
+                    for (int tile = part; tile < tiles && ok; tile += stride)
                         if (sees(p, tile) && (ok = fill(tile, used % TILES, used / TILES))) ++used;
             }
         }
@@ -761,12 +767,51 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
     }
 }
 
+// What the shares of a KV head's rows have added up.
+__global__ __launch_bounds__(256) void k_tc_kvmass_sums(const __grid_constant__ MassArgs P)
+{
+    kv_wait_before();
+    kv_let_next();
+    const gbs_kv_attn& A = P.a;
+    const int item = blockIdx.x / P.heads, head = blockIdx.x - item * P.heads;
+    const KvEntry e = kv_entry<KV_ALL>(A, P.line, item);
+    if (e.units == 0) return;
+    const long long row = ((long long)e.seq * P.heads + head) * P.width, step = (long long)A.n_items * P.heads * P.width;
+    const float* sums = P.sums + ((long long)item * P.heads + head) * P.width;
+    for (long long pos = 256ll * blockIdx.y + threadIdx.x; pos < e.length && pos < P.width; pos += 256ll * gridDim.y) {
+        float sum = 0.f;
+        for (int i = 0; i < P.shares; ++i) sum += sums[i * step + pos];
+        P.mass[row + pos] = pos < e.before && P.decay != 0.f ? fmaf(P.decay, P.base[row + pos], sum) : sum;
+    }
+}
+
 int64_t round_up(int64_t x) { return (x + 15) & ~(int64_t)15; }
+// In the second pass a block has a pair of units and all rows that see them, of which a few thousand tokens have too few to go round (6000 tokens, 4 KV heads: 96 pairs for 148 SMs).  So the
+// tiles of rows are shared among segments where that is likely to be done sooner, by the pairs that the width has: the most that a block has to do counts, and a segment's start takes as long as one
+// and a half tiles.  1000 tokens of 4 query heads a KV head: 94 us undivided, 69 in three shares, 85 in eight.  The shares' sums need room by the width.
+constexpr int MOST_SHARES = 8;
+constexpr int64_t MOST_SUMS = 64ll << 20;
+int shares_of(const gbs_plan* p, const gbs_kv_attn& A, int64_t width)
+{
+    const int64_t tiles = ((int64_t)std::min<int64_t>(A.max_tokens, A.n_tokens) * A.group + TILE - 1) / TILE, segments = (int64_t)A.n_items * A.c.heads;
+    const int64_t pairs = std::min<int64_t>(width, (int64_t)A.c.max_pages << A.c.page_log) / (2 * UNIT) + 1;
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= MOST_SHARES && (s == 1 || 4 * s <= tiles); ++s) {
+        if (s > 1 && (segments == 0 || width > MOST_SUMS / (segments * s * (int64_t)sizeof(float)))) break;
+        const double cost = (double)((segments * pairs * s + p->sm_count - 1) / p->sm_count) * ((double)tiles / s + 1.5);
+        if (s == 1 || cost < least) {
+            best = s;
+            least = cost;
+        }
+    }
+    return best;
+}
 
 struct Layout {
-    int64_t slots, rows, factor, lift, norm, lo, hi, parts, joins, bytes;
+    int64_t slots, rows, factor, lift, norm, lo, hi, parts, joins, sums, bytes;
 };
-Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A)
+Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A, int64_t width)
 {
     Layout l;
     l.slots = A.n_tokens * A.group / TILE + A.n_items + 2;
@@ -779,7 +824,9 @@ Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A)
     l.hi = l.lo + all * TILE * (int64_t)sizeof(int);
     l.parts = l.hi + all * TILE * (int64_t)sizeof(int);
     l.joins = l.parts + (int64_t)p->sm_count * 2 * UNIT * sizeof(float2);
-    l.bytes = l.joins + round_up((int64_t)p->sm_count * sizeof(KvJoin));
+    l.sums = l.joins + round_up((int64_t)p->sm_count * sizeof(KvJoin));
+    const int shares = shares_of(p, A, width);
+    l.bytes = l.sums + (shares > 1 ? (int64_t)shares * A.n_items * A.c.heads * width * (int64_t)sizeof(float) : 0);
     return l;
 }
 
@@ -792,12 +839,12 @@ int launch(const gbs_plan* p, K kernel, size_t smem, const MassArgs& P, cudaStre
 
 }  // namespace
 
-int64_t gbs_tc_kvmass_workspace(const gbs_plan* p, const gbs_kv_attn& A) { return layout_of(p, A).bytes; }
+int64_t gbs_tc_kvmass_workspace(const gbs_plan* p, const gbs_kv_attn& A, int64_t width) { return layout_of(p, A, width).bytes; }
 
 int gbs_tc_kvmass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* base, float decay, float* mass, int64_t width, void* workspace,
                          cudaStream_t stream)
 {
-    const Layout l = layout_of(p, A);
+    const Layout l = layout_of(p, A, width);
     unsigned char* w = static_cast<unsigned char*>(workspace);
     MassArgs P = {};
     P.a = A;
@@ -838,5 +885,11 @@ int gbs_tc_kvmass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* b
     const size_t smem = (stay ? sizeof(TokensSmem<true>) : sizeof(TokensSmem<false>)) + 1024;
     const auto f = p->asym ? (stay ? k_tc_kvmass_tokens<true, true> : k_tc_kvmass_tokens<true, false>)
                            : (stay ? k_tc_kvmass_tokens<false, true> : k_tc_kvmass_tokens<false, false>);
-    return launch(p, f, smem, P, stream);
+    P.heads = A.c.heads;
+    P.shares = stay ? 1 : shares_of(p, A, width);
+    P.a.c.heads *= P.shares;
+    P.sums = reinterpret_cast<float*>(w + l.sums);
+    rc = launch(p, f, smem, P, stream);
+    if (rc != 0 || P.shares == 1) return rc;
+    return gbs_kv_launch(p, k_tc_kvmass_sums, dim3((unsigned)A.n_items * (unsigned)A.c.heads, (unsigned)std::min<int64_t>((width + 255) / 256, 1024)), 256, 0, stream, P);
 }
