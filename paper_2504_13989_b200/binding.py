@@ -149,7 +149,7 @@ def lib() -> ctypes.CDLL:
         L.gbs_kv_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, i32, vp, i64, i64,
                                        vp, i64, vp]
         L.gbs_selftest_kv_attention.argtypes = L.gbs_kv_attention.argtypes[:-1] + [i32, i32, vp]
-        L.gbs_kv_shared_attention_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i32, ctypes.POINTER(i64)]
+        L.gbs_kv_shared_attention_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i32, i32, ctypes.POINTER(i64)]
         L.gbs_kv_shared_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i32, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, vp, i64, i64,
                                               vp, i64, vp]
         L.gbs_kv_attention_mass_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i64, ctypes.POINTER(i64)]
@@ -775,11 +775,11 @@ class KVCache:
         if out.shape[0] != q.shape[0]:
             raise ValueError("gbs: q has %d tokens, out %d" % (q.shape[0], out.shape[0]))
         s, cu, n = self._items(seqs, cu_tokens, q.shape[0])
-        if groups is not None and (groups.dim() != 1 or groups.shape[0] < 2):
+        if groups is not None and (not isinstance(groups, torch.Tensor) or groups.dim() != 1 or groups.shape[0] < 2):
             raise ValueError("gbs: groups must be one row of the groups' first items and the end")
         n_groups = groups.shape[0] - 1 if groups is not None else 1
         need = ctypes.c_int64(0)
-        _check(lib().gbs_kv_shared_attention_workspace(self.plan.handle, ctypes.byref(self._c), n, q.shape[0], max_tokens, n_groups, q.shape[1],
+        _check(lib().gbs_kv_shared_attention_workspace(self.plan.handle, ctypes.byref(self._c), n, q.shape[0], max_tokens, n_groups, max_prefix, q.shape[1],
                                                        ctypes.byref(need)), "gbs_kv_shared_attention_workspace")
         work = self._empty(stream, need.value, torch.uint8, False)
         _check(lib().gbs_kv_shared_attention(self.plan.handle, ctypes.byref(self._c), s, cu, n, q.shape[0], max_tokens,

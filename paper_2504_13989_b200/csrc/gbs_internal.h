@@ -238,7 +238,7 @@ int gbs_tc_kvattn_launch(const gbs_plan* p, const gbs_kv_attn& A, void* workspac
 
 // gbs_kv_shared.cu : the same for groups of items whose sequences begin with the same pages
 #define GBS_KV_PREFIX_ROW 132           // floats that a row's sums over the common prefix take
-int64_t gbs_kv_shared_workspace(const gbs_plan* p, const gbs_kv_attn& A, int n_groups);
+int64_t gbs_kv_shared_workspace(const gbs_plan* p, const gbs_kv_attn& A, int n_groups, int max_prefix);
 int gbs_kv_shared_launch(const gbs_plan* p, const gbs_kv_attn& A, const int* groups, int n_groups, int max_prefix, void* workspace, cudaStream_t stream);
 // gbs_kv_mass.cu : the weights that cached tokens get from up to GBS_KV_MASS_FEW_ROWS query rows of an item and KV head; gbs_tc_kvmass.cu : from more
 #define GBS_KV_MASS_FEW_ROWS 32

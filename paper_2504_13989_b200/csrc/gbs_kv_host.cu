@@ -331,7 +331,7 @@ int sizes_of(const gbs_plan* p, const gbs_kv_cache_t* cache, int n_items, int64_
     if (n_tokens < 0 || n_tokens >= 1ll << 30 || n_tokens * n_heads >= 1ll << 31 || n_tokens * (n_heads / A.c.heads) > 1ll << 28) return GBS_ERR_INVALID_ARG;
     A.n_items = n_items;
     A.n_tokens = n_tokens;
-    A.max_tokens = max_tokens;
+    A.max_tokens = (int)std::min<int64_t>(max_tokens, n_tokens);     // as in the call
     A.n_heads = n_heads;
     A.group = n_heads / A.c.heads;
     *to = A;
@@ -341,13 +341,13 @@ int sizes_of(const gbs_plan* p, const gbs_kv_cache_t* cache, int n_items, int64_
 }  // namespace
 
 extern "C" int gbs_kv_shared_attention_workspace(const gbs_plan_t* p, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
-                                                 int n_groups, int n_heads, int64_t* bytes_out)
+                                                 int n_groups, int max_prefix, int n_heads, int64_t* bytes_out)
 {
     gbs_kv_attn A;
     const int rc = sizes_of(p, cache, n_items, n_tokens, max_tokens, n_heads, bytes_out, &A);
     if (rc != GBS_OK) return rc;
-    if (n_groups < 1 || n_groups > GBS_KV_MAX_ITEMS) return GBS_ERR_INVALID_ARG;
-    *bytes_out = gbs_kv_shared_workspace(p, A, n_groups);
+    if (n_groups < 1 || n_groups > GBS_KV_MAX_ITEMS || max_prefix < 0) return GBS_ERR_INVALID_ARG;
+    *bytes_out = gbs_kv_shared_workspace(p, A, n_groups, max_prefix);
     return GBS_OK;
 }
 
@@ -363,9 +363,7 @@ extern "C" int gbs_kv_shared_attention(const gbs_plan_t* p, const gbs_kv_cache_t
     int rc = attn_args(p, cache, x, &A, &empty);
     if (rc == GBS_OK) rc = max_prefix < 0 ? GBS_ERR_INVALID_ARG : check_groups(groups, n_groups, A);
     if (rc != GBS_OK || empty) return rc;
-    gbs_kv_attn given = A;                                           // the workspace's size goes by the arguments as they are given
-    given.max_tokens = max_tokens;
-    if (!q || !out || !workspace || workspace_bytes < gbs_kv_shared_workspace(p, given, n_groups)) return GBS_ERR_INVALID_ARG;
+    if (!q || !out || !workspace || workspace_bytes < gbs_kv_shared_workspace(p, A, n_groups, max_prefix)) return GBS_ERR_INVALID_ARG;
     rc = check_rows(p, x, true, workspace);
     if (rc != GBS_OK) return rc;
     return on_device(p, [&] { return gbs_kv_shared_launch(p, A, groups, n_groups, max_prefix, workspace, static_cast<cudaStream_t>(stream)); });

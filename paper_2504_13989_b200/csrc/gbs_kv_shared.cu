@@ -191,14 +191,15 @@ bool one_tile(const gbs_plan* p, const gbs_kv_attn& A, int n_groups)
 // 1030; but 10 behind 66 000, 2 KV heads, 64 and 55, 30; 17 behind 63 000, one KV head, 64 and 48, 26; 8 prompts of 250 behind 12 000 301 and 285, 30; 40 in 7 groups behind 8000 60 and 44,
 // 19; 4 behind 300 27 and 12, 0.  Between 45 and 74 neither side was seen to lose by much.
 constexpr double LEAST_GAIN = 45;
-double gain_of(const gbs_plan* p, const gbs_kv_attn& A, int n_groups, int64_t max_prefix)
+bool shares(const gbs_plan* p, const gbs_kv_attn& A, int n_groups, int64_t max_prefix)
 {
+    if (A.n_items == 0) return false;
     const auto tiles = [](double rows, int tile) { return (double)(int64_t)((rows + tile - 1) / tile); };
     const double most = (double)A.max_tokens * A.group, rows = (double)A.n_tokens * A.group / A.n_items, all = (double)A.n_tokens * A.group / n_groups;
     const double apart = most <= GBS_KV_FEW_ROWS ? tiles(most, 8) * 0.63 : most <= 128 ? 2.5 : tiles(rows, 256) * 2.9;
     const double once = all <= FEW_PREFIX_ROWS ? tiles(all, 8) * 0.63 : all <= 128 ? 2.1 : tiles(all, 256) * 2.9;
     const double longest = max_prefix > 0 ? (double)max_prefix : (double)((int64_t)A.c.max_pages << A.c.page_log);
-    return (A.n_items * apart - n_groups * once) * A.c.heads / p->sm_count * longest / 128;
+    return (A.n_items * apart - n_groups * once) * A.c.heads / p->sm_count * longest / 128 > LEAST_GAIN;
 }
 int64_t round_up(int64_t x) { return (x + 15) & ~(int64_t)15; }
 
@@ -225,11 +226,15 @@ Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A, int n_groups)
 
 }  // namespace
 
-int64_t gbs_kv_shared_workspace(const gbs_plan* p, const gbs_kv_attn& A, int n_groups) { return layout_of(p, A, n_groups).bytes; }
+int64_t gbs_kv_shared_workspace(const gbs_plan* p, const gbs_kv_attn& A, int n_groups, int max_prefix)
+{
+    if (shares(p, A, n_groups, max_prefix)) return layout_of(p, A, n_groups).bytes;
+    return few_own(A) ? gbs_kv_few_workspace(p) : gbs_tc_kvattn_workspace(p);
+}
 
 int gbs_kv_shared_launch(const gbs_plan* p, const gbs_kv_attn& A, const int* groups, int n_groups, int max_prefix, void* workspace, cudaStream_t stream)
 {
-    if (gain_of(p, A, n_groups, max_prefix) <= LEAST_GAIN) {
+    if (!shares(p, A, n_groups, max_prefix)) {
         gbs_kv_attn W = A;                       // max_len of an own part becomes one of a sequence
         const int64_t width = (int64_t)A.c.max_pages << A.c.page_log;
         W.max_len = max_prefix > 0 && (int64_t)A.max_len + max_prefix < width ? A.max_len + max_prefix : (int)width;

@@ -549,7 +549,7 @@ PyObject* do_kv_shared_attention(const Pool& p, const PlanRef& ref, PyObject* co
     if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
     const int n = static_cast<int>(it.n), ng = static_cast<int>(n_groups);
     int64_t need;
-    if (q.heads > 0x7fffffff || gbs_kv_shared_attention_workspace(ref.plan, &p.cache, n, q.n, most, ng, static_cast<int>(q.heads), &need) != GBS_OK) Py_RETURN_NONE;
+    if (q.heads > 0x7fffffff || gbs_kv_shared_attention_workspace(ref.plan, &p.cache, n, q.n, most, ng, prefix, static_cast<int>(q.heads), &need) != GBS_OK) Py_RETURN_NONE;
     at::Tensor out;
     if (none(g[9])) {
         out = at::detail::empty_cuda(q.t->sizes(), at::kBFloat16, device_of(p), std::nullopt);

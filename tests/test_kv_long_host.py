@@ -59,11 +59,13 @@ def test_shared_attention(lib):
     assert f(t=0, q=None) == OK and f(n=0, q=None) == OK
     size, r = ctypes.c_int64(-1), ctypes.byref(pool())
     w = lib.gbs_kv_shared_attention_workspace
-    assert w(plan(d=80), r, 2, 3, 2, 1, 8, ctypes.byref(size)) == OK and size.value >= 3 * 8 * 528
-    assert f(size=size.value - 1) == INVALID
-    for bad in ((-1, 3, 2, 1, 8), (2, -1, 2, 1, 8), (2, 3, 0, 1, 8), (2, 3, 2, 0, 8), (2, 3, 2, MOST + 1, 8), (2, 3, 2, 1, 6), (2, 1 << 40, 2, 1, 8)):
+    for prefix in (0, 1 << 30):                                # whatever the call judges of sharing
+        assert w(plan(d=80), r, 2, 3, 2, 1, prefix, 8, ctypes.byref(size)) == OK and size.value > 0
+        assert f(size=size.value - 1, prefix=prefix) == INVALID
+    for bad in ((-1, 3, 2, 1, 0, 8), (2, -1, 2, 1, 0, 8), (2, 3, 0, 1, 0, 8), (2, 3, 2, 0, 0, 8), (2, 3, 2, MOST + 1, 0, 8), (2, 3, 2, 1, 0, 6), (2, 1 << 40, 2, 1, 0, 8),
+                (2, 3, 2, 1, -1, 8)):
         assert w(plan(d=80), r, *bad, ctypes.byref(size)) == INVALID
-    assert w(plan(d=80), r, 2, 3, 2, 1, 8, None) == INVALID
+    assert w(plan(d=80), r, 2, 3, 2, 1, 0, 8, None) == INVALID
 
 
 def test_attention_mass(lib):
