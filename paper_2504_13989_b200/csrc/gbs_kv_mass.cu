@@ -7,7 +7,10 @@
 // enter the matrix unit as they are (16 c, a byte whose upper half is the code), so the sums of products are exact integers; what is rounded is the query row (2^-24 of its largest
 // coordinate), the integer when it becomes a float, and the scale.
 //
-// What bounds it is the keys, 68 or 72 bytes a token and KV head, twice where they do not stay in L2, and with many rows the products, 768 a token, head and row.
+// For up to 32 rows of an item and KV head (gbs_tc_kvmass.cu: more) the first pass leaves the scores, 4 bytes a row, for the second, which then need not read keys. What bounds the first is
+// its instructions, 490 for 32 tokens and 8 rows by a warp, at 16 warps an SM that leave half of the issue slots empty: 48 sequences of up to 6000 tokens, 8 KV heads of 4 query heads,
+// asymmetric, 25 us (the keys at a copy's rate: 9), and 8 for the second; before that 2.7 for the rows, and 2 where sums of divided sequences are joined.  With the codes brought by bulk copies
+// instead of 16 bytes a thread it took 24.  (Where there is no room for the scores the second pass finds them again, 33 us.)
 #include <algorithm>
 
 #include "gbs_kv_attn.cuh"

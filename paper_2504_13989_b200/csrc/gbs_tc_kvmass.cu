@@ -7,7 +7,10 @@
 // First pass (k_tc_kvmass_rows): rows are lanes, tokens columns.  A block has 128 rows against units of 128 tokens; a thread has a row and a part of a unit's
 // tokens, with a maximum and a sum of its own.  Second pass (k_tc_kvmass_tokens): tokens are lanes, rows columns, so that what a token
 // gets stays in one thread.  A block has pairs of units, whose codes are converted once, and goes over all tiles of 64 rows that see them.
-// In both, sixteen warps take the scores from tensor memory (eight: half as many under way, 77 and 124 us instead of 56 and 88 for 1000 tokens behind 5000), four turn codes into fp16, one issues the MMAs, one fetches query rows.
+// In both, sixteen warps take the scores from tensor memory, four turn codes into fp16, one issues the MMAs, one fetches query rows.  (Eight readers: 77 and 124 us instead of 71 and
+// 102 for 1000 tokens of 4 query heads a KV head behind 5000, d = 80.)
+// That now takes 64 and 69 us; the MMAs would take 20 and 22, ex2 as much.  Without any work on the scores 42 and 66 were left: a product of 128 x 128 takes its operands from shared
+// memory at 128 bytes a cycle, all that there is, beside which codes and query rows are written there and factors read.  Issue slots are 46 and 49 % used, the tensor pipe 35 %.
 #include <algorithm>
 
 #include "gbs_kv_attn.cuh"
