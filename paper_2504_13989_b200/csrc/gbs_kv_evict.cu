@@ -167,7 +167,8 @@ __global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(cons
     // ---- places ----
     unsigned long long before = 0;               // upper half: tokens that stay for sure, lower: equal to the threshold
     if (cut && BLOCKS > 1) {                     // of the slices below
-        __syncthreads();
+        if (none) all_blocks();                  // nobody writes to a block that has not begun yet
+        else __syncthreads();
         if (tid < BLOCKS) {
             const int ends = max(0, min(to, lo) - from) + max(0, to - max(from, hi));
             cg::this_cluster().map_shared_rank(slices, tid)[rank] = ((long long)(ends + (none ? 0 : above_threshold)) << 32) | (none ? 0 : at_threshold);

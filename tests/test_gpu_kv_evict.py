@@ -166,6 +166,13 @@ def test_long_sequences():
             check(cache, weights(cache, 131000, 2, kind), 20000 if kind == "plain" else 9999, [1, 0], 100, 4)
 
 
+def test_long_sequences_of_which_the_ends_stay():
+    with Plan(128, 128, 1, 4, 128, 0.9) as plan:
+        for recent, first in ((9000, 999), (9999, 0), (0, 9999)):
+            cache = filled(plan, [131000, 70001, 9999], 2, 128, seed=1, spare=200)
+            check(cache, weights(cache, 131000, 2, "plain"), 9999, [1, 2, 0], recent, first)
+
+
 def test_forks_keep_what_they_share():
     """Two forks of a prompt are cut down, one after the other and in one call, and the prompt is what it was."""
     with Plan(128, 128, 1, 4, 128, 0.9) as plan:
