@@ -347,8 +347,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_rows(const __grid_cons
                     for (int j = 0; j < 16; j += 2) top = max3(z[j], z[j + 1], top);
                     if (top > MOVE || (fresh && top > -INFINITY)) {      // what has been added up changes by an exact power of two
                         const float step = ceilf(top);
-                        if (fresh) l = both(0.f);
-                        else l = mul2(l, both(kv_ex2(-step)));
+                        if (!fresh) l = mul2(l, both(kv_ex2(-step)));    // (before, it is 0, or a NaN that stays)
                         m += step;
                         fresh = false;
 #pragma unroll

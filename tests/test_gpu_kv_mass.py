@@ -199,6 +199,21 @@ def test_scales_that_are_no_numbers(count):
             assert mass.isfinite().all() and mass[0, 0, :181].eq(0).all()
 
 
+@pytest.mark.parametrize("count", [1, 5, 40])
+@pytest.mark.parametrize("asym", [False, True])
+def test_pages_without_a_number_among_their_scales(count, asym):
+    """Whole pages of NaN, the first that a thread sees among them, make what the rows see NaN as well."""
+    with Plan(128, 128, 1, 4, 128, 0.9, asymmetric=asym) as plan:
+        for pages in ((0,), (4,), (0, 1, 2, 3), (8, 9, 10, 11), (18,)):
+            cache = filled(plan, [300, 300], 1, 16, seed=2)
+            f = cache.pages.view(torch.float32).view(cache.pages.shape[0], -1)
+            for p in pages:
+                f[int(cache.page_table[0, p]), 16 * 32:16 * 32 + (32 if asym else 16)] = float("nan")
+            q = rows(2 * count, 4, 128, 2)
+            mass = cache.attention_mass(q, torch.zeros((2, 1, 300), device=DEV), None, ints([0, count, 2 * count]), count, causal=False)
+            assert mass[0].isnan().all() and mass[1].isfinite().all()
+
+
 def test_a_page_that_is_none_of_the_pools():
     with Plan(128, 128, 1, 4, 128, 0.9) as plan:
         cache = filled(plan, [300], 2, 16, seed=2)
