@@ -492,7 +492,8 @@ int gbs_kv_shared_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache,
  * arguments and j a position of item i's sequence s,
  *     mass[s][kv head][j] = decay * base[s][kv head][j] + sum of p_j over the item's query tokens and the query heads of the KV head,
  * where base counts as 0 for the item's own tokens, which had no weight before this call.  Written are positions 0 .. lengths[s] - 1, as far as they lie
- * below `width`, of the sequences of items that have tokens; nothing else is.  Where two items name one sequence, either's sums may stay.
+ * below `width`, of the sequences of items that have tokens; nothing else is.  Where two items name one sequence, either's sums may stay,
+ * where base is mass itself also with the other's as base.
  *   mass, base        device float [n_seqs][n_kv_heads][width]; base is mass itself or does not overlap it, and is not read (NULL will do) where decay is 0
  *   max_tokens        no item has more tokens; what is beyond it gives no weight.  query heads of a KV head * n_tokens: at most 2^28
  *   workspace         device, gbs_kv_attention_mass_workspace bytes for the same sizes, 16-byte aligned; overwritten, needs no preparation, and one call at a

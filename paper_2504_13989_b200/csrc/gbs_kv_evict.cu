@@ -181,7 +181,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(cons
     int* kept = E.kept + ((long long)item * E.c.heads + head) * E.keep;
     if (E.status[item] != GBS_KV_DONE || !cut) { // nothing was done, or all of it stays
         const int stay = E.status[item] == GBS_KV_DONE ? length : 0;
-        for (int j = THREADS * rank + tid; j < E.keep; j += THREADS * BLOCKS) kept[j] = j < stay ? j : -1;
+        for (long long j = THREADS * rank + tid; j < E.keep; j += THREADS * BLOCKS) kept[j] = j < stay ? (int)j : -1;      // keep may be as large as an int
         float* out = E.mass_out + row;
         if (out != mass)
             for (int j = THREADS * rank + tid; j < stay && j < E.width; j += THREADS * BLOCKS) out[j] = mass[j];
