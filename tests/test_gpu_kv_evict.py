@@ -184,6 +184,35 @@ def test_forks_keep_what_they_share():
         assert cache.refs.sum() == 34 + 4 + 4
 
 
+def test_a_document_and_its_forks_in_one_call():
+    """All read pages that the others let go."""
+    with Plan(128, 128, 1, 4, 128, 0.9, asymmetric=True) as plan:
+        cache = filled(plan, [530, 0, 0, 0], 2, 16, seed=1, spare=30)
+        cache.fork(ints([0, 0, 0]), ints([1, 2, 3]))
+        check(cache, weights(cache, 600, 3, "plain"), 64, [2, 0, 3, 1], 10, 4)
+        assert cache.refs.sum() == 16
+
+
+def test_a_page_that_is_none_of_the_pools():
+    """What would stay of it becomes rows of zeros."""
+    with Plan(128, 128, 1, 4, 128, 0.9) as plan:
+        for bad in (2 ** 31 - 1, -1, -2 ** 31):
+            cache = filled(plan, [100], 2, 16, seed=1, spare=4)
+            refs, page = cache.refs.clone(), int(cache.page_table[0, 2])
+            cache.page_table[0, 2] = bad
+            w = torch.zeros((1, 2, 100), device=DEV)
+            w[0, :, 30:50] = 1.0
+            status, kept = cache.evict(w, 20)
+            assert status.item() == 0 and kept[0].tolist() == [list(range(30, 50))] * 2
+            for x in cache.read(ints([0]), ints([0, 20]), 20):
+                assert x[2:18].eq(0).all() and x[:2].ne(0).any() and x[18:].ne(0).any()
+            refs -= refs.clamp(max=1)
+            refs[page] = 1                                     # nobody let it go
+            now = cache.refs.clone()
+            now[cache.page_table[0, :2].long()] -= 1
+            assert torch.equal(now, refs)
+
+
 def test_items_that_are_refused():
     with Plan(128, 128, 1, 4, 128, 0.9) as plan:
         cache = filled(plan, [300, 200, 100, 20], 1, 16, seed=1, spare=3)

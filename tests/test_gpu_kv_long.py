@@ -16,6 +16,39 @@ def ints(v):
     return torch.tensor(v, dtype=torch.int32, device=DEV)
 
 
+def test_offsets_beyond_32_bits():
+    """A pool of more than 4 GB whose last pages are the ones in use, and weights of more than 2^31 places: results as in a small pool."""
+    gbs_build.build()
+    with Plan(128, 128, 1, 4, 128, 0.9) as plan:
+        small = kv_util.filled(plan, [0, 0, 0, 700, 3000], 2, 64, 3, spare=20)
+        here, total, narrow, wide = small.pages.shape[0], 260000, 3100, (1 << 28) + 7
+        off = total - here
+        pages = torch.empty((total, small.pages.shape[1]), dtype=torch.uint8, device=DEV)
+        pages[off:] = small.pages
+        refs = torch.ones(total, dtype=torch.int32, device=DEV)
+        refs[off:] = small.refs
+        big = KVCache(plan, pages, torch.where(small.page_table >= 0, small.page_table + off, small.page_table), small.lengths.clone(), refs, 2, 64)
+        mass = torch.empty((5, 2, wide), device=DEV)
+        for count in (1, 12):
+            gen = torch.Generator(device=DEV)
+            gen.manual_seed(count)
+            q = torch.randn((2 * count, 8, 128), generator=gen, device=DEV).to(torch.bfloat16)
+            cu = [0, count, 2 * count]
+            outs = [c.shared_attention(q, ints([3, 4]), ints(cu), None, count, max_prefix=1 << 27) for c in (small, big)]
+            assert torch.equal(*outs)
+            start = torch.rand((5, 2, narrow), generator=gen, device=DEV)
+            mass[:, :, :narrow] = start
+            want, tol = wanted(small, q, [3, 4], cu, start, 0.5, start)
+            big.attention_mass(q, mass, ints([3, 4]), ints(cu), count, decay=0.5)
+            assert bool(((mass[:, :, :narrow].double() - want).abs() <= tol).all())
+        start = mass[:, :, :narrow].clone()
+        results = [c.evict(m, 300, ints([4, 3]), recent=20, first=4) for c, m in ((small, start), (big, mass))]
+        assert all(torch.equal(a, b) for a, b in zip(*results)) and results[0][0].eq(0).all()
+        assert torch.equal(start, mass[:, :, :narrow])
+        rows = [c.read(ints([3, 4]), ints([0, 300, 600]), 600) for c in (small, big)]
+        assert all(torch.equal(a, b) for a, b in zip(*rows))
+
+
 @pytest.mark.parametrize("asym,d,page", [(False, 128, 16), (True, 96, 64)])
 def test_answers_to_a_document(asym, d, page):
     gbs_build.build()

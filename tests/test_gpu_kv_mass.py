@@ -133,6 +133,24 @@ def test_long_sequences_and_many_rows():
         check(cache, rows(64, 4, 128, 2, 2.0), [0], [0, 64], decay=0.0, window=5000)
 
 
+@pytest.mark.parametrize("count,n", [(1, 3000), (9, 1100)])
+def test_many_items(count, n):
+    """More items than the threads that look through them; few query rows, and many."""
+    with Plan(128, 128, 1, 4, 128, 0.9) as plan:
+        cache = filled(plan, [9 + i % 140 for i in range(n)], 1, 16, seed=2)
+        counts = [count if i % 17 else 0 for i in range(n)]
+        check(cache, rows(sum(counts), 4, 128, 1, 2.0), list(range(n))[::-1], cu_of(counts), decay=0.5)
+
+
+@pytest.mark.parametrize("count,heads", [(1, 4), (7, 16), (30, 8), (90, 8)])
+def test_windows_of_queries_that_see_all_that_follows(count, heads):
+    with Plan(128, 128, 1, 4, 128, 0.9) as plan:
+        cache = filled(plan, [2000, 129, 90], 2, 64, seed=2)
+        for window in (1, 50, 129, 1 << 30):
+            check(cache, rows(3 * count, heads, 128, 1, 2.0), [0, 1, 2], cu_of([count] * 3), causal=False, window=window)
+            check(cache, rows(3 * count, heads, 128, 1, 2.0), [0, 1, 2], cu_of([count] * 3), window=window, decay=0.0)
+
+
 def test_scores_that_have_no_room():
     """A width by which the scores of a call are not kept: the second pass finds them again."""
     with Plan(128, 128, 1, 4, 128, 0.9) as plan:
