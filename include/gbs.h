@@ -474,11 +474,11 @@ int gbs_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const 
  *   n_groups          1 .. GBS_KV_MAX_ITEMS
  *   max_own           about the most tokens that a sequence has behind what its group shares (0: the table's width), as max_len of gbs_kv_attention
  *   max_prefix        about the most tokens that a group shares (0: the table's width), by which it is judged whether sharing gains anything: finding the groups and joining
- *                     what their rows got costs some 20 to 45 microseconds.  Where it does not, the call does what gbs_kv_attention does
+ *                     what their rows got costs some 20 to 45 microseconds.  Where it does not, the call reads as gbs_kv_attention does
  *   n_tokens          query heads of a KV head * n_tokens: at most 2^28
  *   workspace         gbs_kv_shared_attention_workspace bytes, 16-byte aligned, overwritten and used by one call at a time; 528 bytes a token and query head where prefixes are shared.  The same
  *                     number of items, tokens and groups and the same max_tokens and max_prefix as in the call
- * Precision is gbs_kv_attention's; rows of a prefix count as many rows (more than 16) where groups have more than 32 rows a KV head on average.
+ * Precision is gbs_kv_attention's, but that with many rows a cached coordinate is rounded once, to 11 bits; rows of a prefix count as many rows (more than 16) where groups have more than 32 rows a KV head on average.
  */
 int gbs_kv_shared_attention_workspace(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
                                       int n_groups, int max_prefix, int n_heads, int64_t* bytes_out);

@@ -761,7 +761,7 @@ class KVCache:
         """attention (without a window) for items whose sequences begin alike, as forks of one prompt do: the pages that all items of a group begin with are
         read once for the group.  groups: int32 [groups + 1], the first item of each group and the end (None: all items are one group); which pages
         are common is found in the page table.  max_own: about how many tokens the longest sequence has behind what its group shares; max_prefix: about how many the longest prefix has
-        (0: the table's width), by which the call judges whether sharing gains anything; where it does not, it does what attention does."""
+        (0: the table's width), by which the call judges whether sharing gains anything; where it does not, it reads as attention does."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise ValueError("gbs: q must be [tokens, heads, d]")
         self._rows("q", q, q.shape[1])

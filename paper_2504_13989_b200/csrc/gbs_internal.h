@@ -224,6 +224,7 @@ struct gbs_kv_attn {
     float* prefix;
     int n_entries;
     int one_tile;                       // blocks of the kernel for many rows take 128 rows instead of 256
+    int fine;                           // it rounds a cached coordinate once where nothing is shared, as where something is
 };
 // gbs_kv_attn.cu : up to GBS_KV_FEW_ROWS query rows of an item and KV head, eight to a tile, each tile reading its part of the cache; gbs_tc_kvattn.cu : more,
 // 256 to a tile.  us of the two, 8 KV heads, at 16 rows: 64 sequences of 300 tokens 25 and 68, one of 8000 19 and 29, 16 of 4096 41 and 100, 2 of 60000 64 and

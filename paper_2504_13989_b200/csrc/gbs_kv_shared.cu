@@ -188,7 +188,7 @@ bool one_tile(const gbs_plan* p, const gbs_kv_attn& A, int n_groups)
 // Whether reading the prefixes once is likely to take less time than gbs_kv_attention does.  What an SM needs for 128 tokens, in microseconds: 0.63 for a tile of 8 rows, 2.5 (2.1 in one tile) up to 128
 // rows, 2.9 for 256.  The lengths are not known here; without max_prefix the table's width stands for a prefix's.  Finding the groups, two more launches and their joins cost
 // 20 to 45 us.  us with and without sharing, and the gain by this rule: 64 sequences behind 6000 tokens 54 and 98, 102; 14 behind 51 000 69 and 89, 74; 12 x 4 tokens behind 100 000 306 and 1102,
-// 1030; but 10 behind 66 000, 2 KV heads, 64 and 55, 30; 17 behind 63 000, one KV head, 64 and 48, 26; 8 prompts of 250 behind 12 000 301 and 285, 30; 40 in 7 groups behind 8000 60 and 44,
+// 1030; but 10 behind 66 000, 2 KV heads, 64 and 55, 30; 17 behind 63 000, one KV head, 64 and 48, 26; 8 prompts of 250 behind 12 000 301 and 286, 30; 40 in 7 groups behind 8000 60 and 44,
 // 19; 4 behind 300 27 and 12, 0.  Between 45 and 74 neither side was seen to lose by much.
 constexpr double LEAST_GAIN = 45;
 bool shares(const gbs_plan* p, const gbs_kv_attn& A, int n_groups, int64_t max_prefix)
@@ -236,6 +236,7 @@ int gbs_kv_shared_launch(const gbs_plan* p, const gbs_kv_attn& A, const int* gro
 {
     if (!shares(p, A, n_groups, max_prefix)) {
         gbs_kv_attn W = A;                       // max_len of an own part becomes one of a sequence
+        W.fine = 1;                              // results are as precise whichever way they are found
         const int64_t width = (int64_t)A.c.max_pages << A.c.page_log;
         W.max_len = max_prefix > 0 && (int64_t)A.max_len + max_prefix < width ? A.max_len + max_prefix : (int)width;
         return few_own(A) ? gbs_kv_few_launch(p, W, workspace, stream) : gbs_tc_kvattn_launch(p, W, workspace, stream);

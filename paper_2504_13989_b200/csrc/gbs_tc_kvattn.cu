@@ -88,7 +88,7 @@ __device__ __forceinline__ unsigned sum_at(int row, int piece) { return (unsigne
 // queries as well; the results' columns are put back at the end.
 // FINE: the scale in two pieces, the lower one's product added to the upper one's before that is rounded, so that a number is rounded once.  Rounding a scale first puts all
 // of a token's coordinates off by the same factor, of which its score has all: behind long prefixes, where the largest of 100 000 scores count, that made the results' error 2.5e-3
-// instead of 2.0e-3 (1.7e-3 of it the results' own rounding).
+// instead of 2.0e-3 (1.7e-3 of it the results' own rounding), at 2 % more time.
 template <bool ASYM, bool FINE>
 __device__ __forceinline__ void store_codes(unsigned char* tile, int row, const uint4 codes[4], __half2 scale, __half2 rest, __half2 middle)
 {
@@ -146,7 +146,7 @@ __device__ __forceinline__ void shrink(unsigned scores, unsigned sums, float kee
 }
 
 // SPLIT: a block has one tile
-template <bool ASYM, bool TEST, int PART, bool SPLIT>
+template <bool ASYM, bool TEST, int PART, bool SPLIT, bool FINE>
 __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant__ KvAttnArgs P)
 {
     extern __shared__ unsigned char smem_raw[];
@@ -445,12 +445,12 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 const unsigned which = __ballot_sync(0xffffffffu, there);
                 if (lane == 0) S.part[nb][w - 8] = make_float4(two_to(ek), (float)ev, two_to(-ev), __uint_as_float(which));
                 const auto rest_of = [](float x) { return __float2half2_rn(x - __half2float(__float2half_rn(x))); };
-                store_codes<ASYM, PART != KV_WHOLE>(S.k[b], me, k, there && wrong ? as_h(0x7fff7fffu) : __float2half2_rn(ks * up), rest_of(ks * up), __float2half2_rn(km * up));
+                store_codes<ASYM, FINE>(S.k[b], me, k, there && wrong ? as_h(0x7fff7fffu) : __float2half2_rn(ks * up), rest_of(ks * up), __float2half2_rn(km * up));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&S.kfull[b]);
                 if (now > 1 && !(ok = !kv_lost<TEST>(P, &S.abort, 75, round) && mbar_wait_warp(&S.abort, &S.vfree[b], (use + 1) & 1u, P.status, 75))) break;
-                store_codes<ASYM, PART != KV_WHOLE>(S.v[b], me, v, __float2half2_rn(vs * up_v), rest_of(vs * up_v), __float2half2_rn(vm * up_v));
+                store_codes<ASYM, FINE>(S.v[b], me, v, __float2half2_rn(vs * up_v), rest_of(vs * up_v), __float2half2_rn(vm * up_v));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&S.vfull[b]);
@@ -596,9 +596,10 @@ int launch(const gbs_plan* p, const KvAttnArgs& P, int blocks, cudaStream_t stre
     constexpr bool WHOLE = PART == KV_WHOLE;
     const size_t smem = sizeof(Smem) + 1024;
     const bool test = WHOLE && P.a.lost_code, split = !WHOLE && P.a.one_tile;
-    const auto f = test    ? (p->asym ? k_tc_kvattn<true, WHOLE, PART, false> : k_tc_kvattn<false, WHOLE, PART, false>)
-                   : split ? (p->asym ? k_tc_kvattn<true, false, PART, !WHOLE> : k_tc_kvattn<false, false, PART, !WHOLE>)
-                           : (p->asym ? k_tc_kvattn<true, false, PART, false> : k_tc_kvattn<false, false, PART, false>);
+    const auto f = test                  ? (p->asym ? k_tc_kvattn<true, WHOLE, PART, false, !WHOLE> : k_tc_kvattn<false, WHOLE, PART, false, !WHOLE>)
+                   : split               ? (p->asym ? k_tc_kvattn<true, false, PART, !WHOLE, !WHOLE> : k_tc_kvattn<false, false, PART, !WHOLE, !WHOLE>)
+                   : !WHOLE || P.a.fine  ? (p->asym ? k_tc_kvattn<true, false, PART, false, true> : k_tc_kvattn<false, false, PART, false, true>)
+                                         : (p->asym ? k_tc_kvattn<true, false, PART, false, !WHOLE> : k_tc_kvattn<false, false, PART, false, !WHOLE>);
     const cudaError_t e = cudaFuncSetAttribute((const void*)f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return (int)e;
     const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);
