@@ -9,8 +9,8 @@
 //
 // For up to 32 rows of an item and KV head (gbs_tc_kvmass.cu: more) the first pass leaves the scores, 4 bytes a row, for the second, which then need not read keys. What bounds the first is
 // its instructions, 490 for 32 tokens and 8 rows by a warp, at 16 warps an SM that leave half of the issue slots empty: 48 sequences of up to 6000 tokens, 8 KV heads of 4 query heads,
-// asymmetric, 25 us (the keys at a copy's rate: 9), and 8 for the second; before that 2.7 for the rows, and 2 where sums of divided sequences are joined.  With the codes brought by bulk copies
-// instead of 16 bytes a thread it took 24.  (Where there is no room for the scores the second pass finds them again, 33 us.)
+// asymmetric, 23 us (the keys at a copy's rate: 9), and 8 for the second; before that 2.7 for the rows, and 2 where sums of divided sequences are joined.  With the codes brought by bulk copies
+// instead of 16 bytes a thread it took one less.  (Where there is no room for the scores the second pass finds them again, 33 us.)
 #include <algorithm>
 
 #include "gbs_kv_attn.cuh"
@@ -19,8 +19,7 @@ namespace {
 
 constexpr int UNIT = 128, THREADS = 128, WARPS = THREADS / 32, STAGES = 3;
 constexpr int TILE = 8, PIECES = 3, TILE_BYTES = PIECES * 1024;      // rows that one product takes, and their integers
-constexpr int PASS = 2 * TILE;                                       // rows at a time
-constexpr int BLOCKS_PER_SM = 4;
+constexpr int BLOCKS_PER_SM = 4;             // of one tile at a time (us, 48 sequences): 2: 32, 3: 23.9, 4: 23.2, 5: 24.2, 6: 27.4
 constexpr float MOVE = 8.f;                                          // a maximum moves when a score is so much (log2) above it
 constexpr float TOP = 127.f * 65536.f;                               // a row's largest integer
 static_assert(UNIT == WARPS * 32, "a warp has 32 tokens of a unit");
@@ -123,12 +122,13 @@ __global__ __launch_bounds__(256) void k_kv_mass_rows(const __grid_constant__ Ma
     }
 }
 
-template <bool ASYM>
+template <bool ASYM, int TILES>
 struct alignas(16) Smem {
+    static constexpr int PASS = TILES * TILE;
     unsigned char k[STAGES][UNIT * KV_ROW];
     float s[STAGES][UNIT * (ASYM ? 2 : 1)];
     unsigned there[STAGES][WARPS];               // which tokens have a page
-    unsigned char q[PASS / TILE][TILE_BYTES];
+    unsigned char q[TILES][TILE_BYTES];
     float2 factor[PASS];
     float2 norm[PASS];
     int lo[PASS], hi[PASS];
@@ -152,13 +152,14 @@ __device__ __forceinline__ void copy_async(void* to, const void* from)
 __device__ __forceinline__ float2 norm_of(float m, float sum) { return sum == 0.f ? make_float2(0.f, 0.f) : make_float2(m, 1.f / sum); }
 __device__ __forceinline__ float no_inf(float x) { return fmaf(x, 0.f, x); }
 
-// MASS: the second pass.  KEEP: the first pass, which leaves the scores for k_kv_mass_sums.
-template <bool ASYM, bool MASS, bool KEEP>
+// MASS: the second pass.  KEEP: the first pass, which leaves the scores for k_kv_mass_sums.  TILES: taken at a time; one where no item has more than 8 rows of a KV head, which
+// leaves registers enough (23.2 us instead of 25 with two).  Page numbers looked up a unit ahead: 24.1; four stages: 23.6.
+template <bool ASYM, bool MASS, bool KEEP, int TILES>
 __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_mass(const __grid_constant__ MassArgs P)
 {
-    constexpr int PART = MASS ? KV_ALL : KV_WHOLE;
+    constexpr int PART = MASS ? KV_ALL : KV_WHOLE, PASS = TILES * TILE;
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    Smem<ASYM>& S = *reinterpret_cast<Smem<ASYM>*>(smem_raw);
+    Smem<ASYM, TILES>& S = *reinterpret_cast<Smem<ASYM, TILES>*>(smem_raw);
     const gbs_kv_attn& A = P.a;
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, g = lane >> 2, t = lane & 3;
     kv_wait_before();
@@ -173,7 +174,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_mass(const __grid
         const KvPiece piece = kv_piece(P.line, seg, places);
         const KvEntry& e = seg.e;
         const int n = max(piece.n, 0), tok_at = ((e.lo >> 7) + piece.skip) * UNIT;
-        const int passes = (e.rows + PASS - 1) / PASS;
+        const int passes = TILES == 1 ? 1 : (e.rows + PASS - 1) / PASS;
         // what any row sees
         const int see_lo = kv_row_lo(A, e, 0), see_hi = kv_row_hi(A, e, A.by_group(e.rows - 1));
         const int* pages = A.c.page_table + (long long)e.seq * A.c.max_pages;
@@ -201,17 +202,17 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_mass(const __grid
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         // the rows of a pass, into registers and then into shared memory
-        uint4 qv[PASS / TILE * TILE_BYTES / 16 / THREADS];
+        constexpr int PER = TILE_BYTES / 16, LOADS = (TILES * PER + THREADS - 1) / THREADS;
+        uint4 qv[LOADS];
         float2 fv = make_float2(0.f, 0.f);
         float2 nv = make_float2(0.f, 0.f);
         int lov = 0, hiv = 0;
         const auto load_rows = [&](int pass) {
-            const uint4* from = reinterpret_cast<const uint4*>(P.rows + (tile0 + (PASS / TILE) * pass) * TILE_BYTES);
-            constexpr int PER = TILE_BYTES / 16;
+            const uint4* from = reinterpret_cast<const uint4*>(P.rows + (tile0 + TILES * pass) * TILE_BYTES);
 #pragma unroll
-            for (int k = 0; k < PASS / TILE * PER / THREADS; ++k) {
+            for (int k = 0; k < LOADS; ++k) {
                 const int i = tid + THREADS * k;
-                if (TILE * (i / PER) + PASS * pass < e.rows) qv[k] = __ldg(from + i);
+                if (i < TILES * PER && TILE * (i / PER) + PASS * pass < e.rows) qv[k] = __ldg(from + i);
             }
             const int r = PASS * pass + tid;
             fv = make_float2(0.f, 0.f);
@@ -227,7 +228,8 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_mass(const __grid
         };
         const auto store_rows = [&] {
 #pragma unroll
-            for (int k = 0; k < PASS / TILE * TILE_BYTES / 16 / THREADS; ++k) reinterpret_cast<uint4*>(S.q[0])[tid + THREADS * k] = qv[k];
+            for (int k = 0; k < LOADS; ++k)
+                if (tid + THREADS * k < TILES * PER) reinterpret_cast<uint4*>(S.q[0])[tid + THREADS * k] = qv[k];
             if (tid < PASS) {
                 S.factor[tid] = fv;
                 S.norm[tid] = nv;
@@ -241,17 +243,17 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_mass(const __grid
         for (int i = 0; i < STAGES - 1; ++i) fetch(i);
         __syncthreads();                         // the segment before is done with the rows
         store_rows();
-        float m[PASS / TILE][2], l[PASS / TILE][2];
+        float m[TILES][2], l[TILES][2];
         const auto reset = [&] {
 #pragma unroll
-            for (int i = 0; i < PASS / TILE; ++i) m[i][0] = m[i][1] = NONE, l[i][0] = l[i][1] = 0.f;
+            for (int i = 0; i < TILES; ++i) m[i][0] = m[i][1] = NONE, l[i][0] = l[i][1] = 0.f;
         };
         reset();
         // (m, sum) of the block's rows of a pass, with what was there before in `slot`
         float2* slot = P.parts + ((long long)blockIdx.x * 2 + (piece.starts ? 1 : 0)) * P.max_rows;
         const auto reduce = [&](int pass, bool first, bool last) {
 #pragma unroll
-            for (int i = 0; i < PASS / TILE; ++i)
+            for (int i = 0; i < TILES; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     float top = m[i][j];
@@ -319,7 +321,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_mass(const __grid
                         const bool plain = there == 0xffffffffu && mine >= kv_row_lo(A, e, A.by_group(last)) && mine + 32 <= kv_row_hi(A, e, A.by_group(PASS * pass));
                         float got[2][2] = {};
 #pragma unroll
-                        for (int i = 0; i < PASS / TILE; ++i) {
+                        for (int i = 0; i < TILES; ++i) {
                             if (i > 0 && PASS * pass + TILE * i >= e.rows) break;
                             int c[2][PIECES][4] = {};
 #pragma unroll
@@ -520,6 +522,7 @@ __global__ __launch_bounds__(256) void k_kv_mass_sums(const __grid_constant__ Ma
     }
 }
 
+int tiles_of(const gbs_kv_attn& A) { return std::min<int64_t>(A.max_tokens, A.n_tokens) * A.group <= TILE ? 1 : 2; }
 int blocks_of(const gbs_plan* p) { return p->sm_count * BLOCKS_PER_SM; }
 int64_t round_up(int64_t x) { return (x + 15) & ~(int64_t)15; }
 
@@ -548,12 +551,18 @@ Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A, int64_t width)
     return l;
 }
 
-template <bool ASYM, bool MASS, bool KEEP>
+template <bool MASS, bool KEEP, int TILES>
 int launch(const gbs_plan* p, const MassArgs& P, cudaStream_t stream)
 {
-    const cudaError_t e = cudaFuncSetAttribute((const void*)k_kv_mass<ASYM, MASS, KEEP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<ASYM>));
-    if (e != cudaSuccess) return (int)e;
-    return gbs_kv_launch(p, k_kv_mass<ASYM, MASS, KEEP>, dim3((unsigned)blocks_of(p)), THREADS, sizeof(Smem<ASYM>), stream, P);
+    const auto f = p->asym ? k_kv_mass<true, MASS, KEEP, TILES> : k_kv_mass<false, MASS, KEEP, TILES>;
+    const size_t smem = p->asym ? sizeof(Smem<true, TILES>) : sizeof(Smem<false, TILES>);
+    const cudaError_t e = cudaFuncSetAttribute((const void*)f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return e != cudaSuccess ? (int)e : gbs_kv_launch(p, f, dim3((unsigned)blocks_of(p)), THREADS, smem, stream, P);
+}
+template <bool MASS, bool KEEP>
+int launch(const gbs_plan* p, const MassArgs& P, cudaStream_t stream)
+{
+    return tiles_of(P.a) == 1 ? launch<MASS, KEEP, 1>(p, P, stream) : launch<MASS, KEEP, 2>(p, P, stream);
 }
 
 }  // namespace
@@ -597,12 +606,10 @@ int gbs_kv_mass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* bas
     const int64_t jobs = A.n_tokens * ((A.n_heads + 3) / 4);
     int rc = gbs_kv_launch(p, k_kv_mass_rows, dim3((unsigned)((jobs + 7) / 8)), 256, 0, stream, P);
     const bool keep = l.score_rows > 0;
-    if (rc == 0)
-        rc = keep ? (p->asym ? launch<true, false, true>(p, P, stream) : launch<false, false, true>(p, P, stream))
-                  : (p->asym ? launch<true, false, false>(p, P, stream) : launch<false, false, false>(p, P, stream));
+    if (rc == 0) rc = keep ? launch<false, true>(p, P, stream) : launch<false, false>(p, P, stream);
     const unsigned y = (unsigned)std::min<int64_t>((l.max_rows + 127) / 128, 64);
     if (rc == 0) rc = gbs_kv_launch(p, k_kv_mass_join, dim3((unsigned)blocks_of(p), y), 128, 0, stream, P);
     if (rc != 0) return rc;
-    if (!keep) return p->asym ? launch<true, true, false>(p, P, stream) : launch<false, true, false>(p, P, stream);
+    if (!keep) return launch<true, false>(p, P, stream);
     return gbs_kv_launch(p, k_kv_mass_sums, dim3((unsigned)A.n_items * (unsigned)A.c.heads, (unsigned)std::min<int64_t>((width + SUMS - 1) / SUMS, 4096)), 256, 0, stream, P);
 }
