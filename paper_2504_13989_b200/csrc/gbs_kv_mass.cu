@@ -8,7 +8,7 @@
 // coordinate), the integer when it becomes a float, and the scale.
 //
 // For up to 32 rows of an item and KV head (gbs_tc_kvmass.cu: more) the first pass leaves the scores, 4 bytes a row, for the second, which then need not read keys. What bounds the first is
-// its instructions, 490 for 32 tokens and 8 rows by a warp, at 16 warps an SM that leave half of the issue slots empty: 48 sequences of up to 6000 tokens, 8 KV heads of 4 query heads,
+// its instructions, 480 for 32 tokens and 8 rows by a warp, at 16 warps an SM that leave 45 % of the issue slots empty: 48 sequences of up to 6000 tokens, 8 KV heads of 4 query heads,
 // asymmetric, 23 us (the keys at a copy's rate: 9), and 8 for the second; before that 2.7 for the rows, and 2 where sums of divided sequences are joined.  With the codes brought by bulk copies
 // instead of 16 bytes a thread it took one less.  (Where there is no room for the scores the second pass finds them again, 33 us.)
 #include <algorithm>
