@@ -540,6 +540,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
     unsigned pp = 0, dt = 0;                     // pairs, and (pair, tile)s so far
     // STAY: segments so far, each of which fills a buffer for each of its tiles once, or the second buffer's fillings; else fillings of the ring.  Three roles keep count.
     unsigned used = 0, used1 = 0;
+    unsigned sent = 0, sent1 = 0;                // STAY: fillings of the two buffers that have been sent for: a segment's begin before, or after, another role gives up
     for (bool more = places > 0; more && ok;) {
         const KvPiece piece = kv_piece(P.line, seg, places);
         if (piece.n <= 0) break;
@@ -731,7 +732,10 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
                 return true;
             };
             if (STAY) {
-                for (int tile = 0; tile < tiles && ok; ++tile) ok = fill(tile, tile, tile ? used1 : used);
+                for (int tile = 0; tile < tiles && ok; ++tile) {
+                    ok = fill(tile, tile, tile ? used1 : used);
+                    if (ok) ++(tile ? sent1 : sent);
+                }
             } else {
                 for (int p = 0; p < pairs && ok; ++p)
                     for (int tile = part; tile < tiles && ok; tile += stride)
@@ -754,10 +758,10 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
             umma_commit(&S.drain);
             drain_copies(&S.drain, 1, 1);
         }
-        if (w == FETCH) {                           // the copies that were sent for last, or might have been
+        if (w == FETCH) {                           // the copies that were sent for last.  (A wait for one that was not would pass at once: it goes by its parity)
             if (STAY) {
-                drain_copies(&S.qfull[0], 1, (int)used + 1);
-                drain_copies(&S.qfull[1], 1, (int)used1 + 1);
+                drain_copies(&S.qfull[0], 1, (int)sent);
+                drain_copies(&S.qfull[1], 1, (int)sent1);
             } else {
                 drain_copies(S.qfull, TILES, (int)used);
             }
