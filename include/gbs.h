@@ -545,6 +545,18 @@ int gbs_selftest_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cach
                               int segment, void* cuda_stream);
 
 /*
+ * The same of gbs_kv_attention_mass, whose waits are all in its kernels for more than 32 query rows a KV head and item.  Weights may be any numbers.
+ *   code              81 .. 86: the pass for the rows' sums (scores, room for keys, query rows, keys, room for scores, room for query rows);
+ *                     91 .. 99: the pass for the tokens' (keys, query rows, scores, room for keys, keys before their product, query rows before it, room for
+ *                     scores, room for query rows, query rows of a tile that no token of a segment is seen by)
+ */
+int gbs_selftest_kv_attention_mass(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens,
+                                   int n_items, int64_t n_tokens, int max_tokens, const void* q, int64_t q_token_stride,
+                                   int64_t q_head_stride, int n_heads, float scale, int window, int flags, const float* base,
+                                   float decay, float* mass, int64_t width, void* workspace, int64_t workspace_bytes, int code,
+                                   int segment, void* cuda_stream);
+
+/*
  * State of one projection's search (Algorithm 1), a handful of numbers: plain data that may be copied, stored
  * and handed back later to resume the search where it stopped (gbs_search_state_init gives the algorithm's
  * start a = 0, b = 1, m = 1/2).

@@ -28,8 +28,8 @@ struct KvAttnArgs {
 };
 
 // Whether a wait counts as one that ran out: in the self-test's instances, those with the given code in a block's segment of the given number.
-template <bool TEST>
-__device__ __forceinline__ bool kv_lost(const KvAttnArgs& P, volatile int* abort_flag, int code, int segment)
+template <bool TEST, typename Args>
+__device__ __forceinline__ bool kv_lost(const Args& P, volatile int* abort_flag, int code, int segment)
 {
     if (!TEST || code != P.a.lost_code || segment != P.a.lost_segment) return false;
     *abort_flag = 1;

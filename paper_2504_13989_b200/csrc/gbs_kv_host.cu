@@ -380,23 +380,46 @@ extern "C" int gbs_kv_attention_mass_workspace(const gbs_plan_t* p, const gbs_kv
     return GBS_OK;
 }
 
-extern "C" int gbs_kv_attention_mass(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
-                                     int64_t n_tokens, int max_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int n_heads,
-                                     float scale, int window, int flags, const float* base, float decay, float* mass, int64_t width,
-                                     void* workspace, int64_t workspace_bytes, void* stream)
+namespace {
+
+// code, segment: as for attention
+int attention_mass(const gbs_plan* p, const gbs_kv_cache_t* cache, const AttnCall& x, const float* base, float decay, float* mass, int64_t width,
+                   void* workspace, int64_t workspace_bytes, int code, int segment, void* stream)
 {
-    const AttnCall x = {seqs, cu_tokens, n_items, n_tokens, max_tokens, 0, q, q_token_stride, q_head_stride, n_heads, scale, window, flags, nullptr, 0, 0};
     gbs_kv_attn A;
     bool empty = false;
     int rc = attn_args(p, cache, x, &A, &empty);
     if (rc != GBS_OK) return rc;
     if (width < 1 || !isfinite(decay) || A.n_tokens * A.group > 1ll << 28) return GBS_ERR_INVALID_ARG;
     if (empty) return GBS_OK;
-    if (!q || !mass || (!base && decay != 0.f) || !workspace || workspace_bytes < gbs_kv_mass_workspace(p, A, width)) return GBS_ERR_INVALID_ARG;
+    if (!x.q || !mass || (!base && decay != 0.f) || !workspace || workspace_bytes < gbs_kv_mass_workspace(p, A, width)) return GBS_ERR_INVALID_ARG;
     rc = check_rows(p, x, false, workspace);
     if (rc != GBS_OK) return rc;
     if (!aligned(mass, 4) || !aligned(base, 4)) return GBS_ERR_ALIGNMENT;
+    A.lost_code = code;
+    A.lost_segment = segment;
     return on_device(p, [&] { return gbs_kv_mass_launch(p, A, base, decay, mass, width, workspace, static_cast<cudaStream_t>(stream)); });
+}
+
+}  // namespace
+
+extern "C" int gbs_kv_attention_mass(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                                     int64_t n_tokens, int max_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int n_heads,
+                                     float scale, int window, int flags, const float* base, float decay, float* mass, int64_t width,
+                                     void* workspace, int64_t workspace_bytes, void* stream)
+{
+    const AttnCall x = {seqs, cu_tokens, n_items, n_tokens, max_tokens, 0, q, q_token_stride, q_head_stride, n_heads, scale, window, flags, nullptr, 0, 0};
+    return attention_mass(p, cache, x, base, decay, mass, width, workspace, workspace_bytes, 0, 0, stream);
+}
+
+extern "C" int gbs_selftest_kv_attention_mass(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                                              int64_t n_tokens, int max_tokens, const void* q, int64_t q_token_stride, int64_t q_head_stride, int n_heads,
+                                              float scale, int window, int flags, const float* base, float decay, float* mass, int64_t width,
+                                              void* workspace, int64_t workspace_bytes, int code, int segment, void* stream)
+{
+    if (!((code >= 81 && code <= 86) || (code >= 91 && code <= 99)) || segment < 0) return GBS_ERR_INVALID_ARG;
+    const AttnCall x = {seqs, cu_tokens, n_items, n_tokens, max_tokens, 0, q, q_token_stride, q_head_stride, n_heads, scale, window, flags, nullptr, 0, 0};
+    return attention_mass(p, cache, x, base, decay, mass, width, workspace, workspace_bytes, code, segment, stream);
 }
 
 namespace {

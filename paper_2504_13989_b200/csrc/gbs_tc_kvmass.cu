@@ -247,7 +247,7 @@ struct RowsSmem {
 };
 static_assert(sizeof(RowsSmem) + 1024 <= 227 * 1024, "one block of an SM");
 
-template <bool ASYM>
+template <bool ASYM, bool TEST>
 __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_rows(const __grid_constant__ MassArgs P)
 {
     extern __shared__ unsigned char smem_raw[];
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_rows(const __grid_cons
             for (int i = (it + group) & 1; i < n; i += 2) {
                 const unsigned now = it + i;
                 const int tok = tok0 + i * UNIT + EACH * half;
-                if (!(ok = mbar_wait_warp(&S.abort, &S.dfull[group], (now >> 1) & 1u, P.status, 81))) break;
+                if (!(ok = !kv_lost<TEST>(P, &S.abort, 81, round) && mbar_wait_warp(&S.abort, &S.dfull[group], (now >> 1) & 1u, P.status, 81))) break;
                 tc_fence_after();
                 const uint2 there = *reinterpret_cast<const uint2*>(&S.there[now & 3][2 * half]);
                 const bool plain = tok >= all_lo && tok + EACH <= all_hi && (there.x & there.y) == 0xffffffffu;
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_rows(const __grid_cons
             for (int i = 0; i < n; ++i) {
                 const unsigned now = it + i;
                 const int b = now & 1;
-                if (now > 1 && !(ok = mbar_wait_warp(&S.abort, &S.kfree[b], ((now >> 1) + 1) & 1u, P.status, 82))) break;
+                if (now > 1 && !(ok = !kv_lost<TEST>(P, &S.abort, 82, round) && mbar_wait_warp(&S.abort, &S.kfree[b], ((now >> 1) + 1) & 1u, P.status, 82))) break;
                 key.store(S.k[b], me);
                 S.by[now & 3][me] = key.by();
                 if (ASYM) S.middle[now & 3][me] = key.middle();
@@ -408,11 +408,11 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_rows(const __grid_cons
             const unsigned long long qd = smem_desc(smem_u32(S.q[0]), 16, 1024, 2), kd = smem_desc(smem_u32(S.k[0]), 16, 1024, 2);
             const unsigned q_lo = (unsigned)qd, k_lo = (unsigned)kd, hi = (unsigned)(qd >> 32), to = uniform(tmem), at0 = uniform(it);
             const int units = (int)uniform((unsigned)n);
-            ok = mbar_wait_warp(&S.abort, &S.qfull, uniform(round) & 1u, P.status, 83);
+            ok = !kv_lost<TEST>(P, &S.abort, 83, round) && mbar_wait_warp(&S.abort, &S.qfull, uniform(round) & 1u, P.status, 83);
             for (int i = 0; i < units && ok; ++i) {
                 const unsigned now = at0 + i, b = now & 1;
-                if (!(ok = mbar_wait_warp(&S.abort, &S.kfull[b], (now >> 1) & 1u, P.status, 84))) break;
-                if (now > 1 && !(ok = mbar_wait_warp(&S.abort, &S.dfree[b], ((now >> 1) + 1) & 1u, P.status, 85))) break;
+                if (!(ok = !kv_lost<TEST>(P, &S.abort, 84, round) && mbar_wait_warp(&S.abort, &S.kfull[b], (now >> 1) & 1u, P.status, 84))) break;
+                if (now > 1 && !(ok = !kv_lost<TEST>(P, &S.abort, 85, round) && mbar_wait_warp(&S.abort, &S.dfree[b], ((now >> 1) + 1) & 1u, P.status, 85))) break;
                 tc_fence_after();
                 product(to + 256 * b, q_lo, k_lo + b * (CODES >> 4), hi);
                 product(to + 256 * b + 128, q_lo + (UNIT * 256 >> 4), k_lo + b * (CODES >> 4), hi);
@@ -422,7 +422,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_rows(const __grid_cons
             }
             if (ok) umma_commit(&S.qfree);
         } else {
-            if (round > 0) ok = mbar_wait_warp(&S.abort, &S.qfree, (round - 1) & 1u, P.status, 86);
+            if (round > 0) ok = !kv_lost<TEST>(P, &S.abort, 86, round) && mbar_wait_warp(&S.abort, &S.qfree, (round - 1) & 1u, P.status, 86);
             if (ok) ++sent;
             if (ok && lane == 0) {
                 mbar_arrive_expect_tx(&S.qfull, 2 * IMAGE);
@@ -498,7 +498,7 @@ struct TokensSmem {
 };
 static_assert(sizeof(TokensSmem<true>) + 1024 <= 227 * 1024 && sizeof(TokensSmem<false>) + 1024 <= 227 * 1024, "one block of an SM");
 
-template <bool ASYM, bool STAY>
+template <bool ASYM, bool STAY, bool TEST>
 __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_constant__ MassArgs P)
 {
     extern __shared__ unsigned char smem_raw[];
@@ -537,7 +537,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
     if (lane == 0) seg = S.seg;
     __syncwarp();
     bool ok = true;
-    unsigned pp = 0, dt = 0;                     // pairs, and (pair, tile)s so far
+    unsigned pp = 0, dt = 0, round = 0;          // pairs, (pair, tile)s and segments so far
     // STAY: segments so far, each of which fills a buffer for each of its tiles once, or the second buffer's fillings; else fillings of the ring.  Three roles keep count.
     unsigned used = 0, used1 = 0;
     unsigned sent = 0, sent1 = 0;                // STAY: fillings of the two buffers that have been sent for: a segment's begin before, or after, another role gives up
@@ -568,7 +568,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
                 const unsigned now = pp + p, kb = now % PAIRS;
                 const int units = min(2, n - 2 * p);
                 float acc[2] = {0.f, 0.f}, off[2] = {0.f, 0.f};      // sums over many rows, with what their rounding has left out
-                if (ok) ok = mbar_wait_warp(&S.abort, &S.kfull[kb], (now / PAIRS) & 1u, P.status, 91);
+                if (ok) ok = !kv_lost<TEST>(P, &S.abort, 91, round) && mbar_wait_warp(&S.abort, &S.kfull[kb], (now / PAIRS) & 1u, P.status, 91);
                 const float by0 = S.by[kb][me], by1 = S.by[kb][UNIT + me], mid0 = ASYM ? S.middle[kb][me] : 0.f, mid1 = ASYM ? S.middle[kb][UNIT + me] : 0.f;
                 const bool all_there = (S.there[kb][w & 3] & (units > 1 ? S.there[kb][4 + (w & 3)] : 0xffffffffu)) == 0xffffffffu;
                 const bool there0 = S.there[kb][w & 3] >> lane & 1, there1 = units > 1 && (S.there[kb][4 + (w & 3)] >> lane & 1);
@@ -580,8 +580,8 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
                     if (!STAY) ++used;
                     if ((dt++ & 1) != (unsigned)group) continue;
                     const unsigned turn = (dt - 1) >> 1;
-                    if (!(ok = mbar_wait_warp(&S.abort, &S.qfull[b], filled & 1u, P.status, 92))) break;
-                    if (!(ok = mbar_wait_warp(&S.abort, &S.dfull[group], turn & 1u, P.status, 93))) break;
+                    if (!(ok = !kv_lost<TEST>(P, &S.abort, 92, round) && mbar_wait_warp(&S.abort, &S.qfull[b], filled & 1u, P.status, 92))) break;
+                    if (!(ok = !kv_lost<TEST>(P, &S.abort, 93, round) && mbar_wait_warp(&S.abort, &S.dfull[group], turn & 1u, P.status, 93))) break;
                     tc_fence_after();
                     const bool plain = all_there && all(p, tile);    // what is taken for a second unit that there is not goes nowhere
                     f32x2 got0 = both(0.f), got1 = both(0.f);
@@ -670,7 +670,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
             int page = page_of(tok0 + UNIT + me);
             for (int i = 0; i < n; ++i) {
                 const unsigned now = pp + (i >> 1), kb = now % PAIRS;
-                if ((i & 1) == 0 && now >= PAIRS && !(ok = mbar_wait_warp(&S.abort, &S.kfree[kb], (now / PAIRS + 1) & 1u, P.status, 94))) break;
+                if ((i & 1) == 0 && now >= PAIRS && !(ok = !kv_lost<TEST>(P, &S.abort, 94, round) && mbar_wait_warp(&S.abort, &S.kfree[kb], (now / PAIRS + 1) & 1u, P.status, 94))) break;
                 key.store(S.k[kb][i & 1], me);
                 S.by[kb][(i & 1) * UNIT + me] = key.by();
                 if (ASYM) S.middle[kb][(i & 1) * UNIT + me] = key.middle();
@@ -693,12 +693,12 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
             const int all_units = (int)uniform((unsigned)n), all_pairs = (int)uniform((unsigned)pairs), all_tiles = (int)uniform((unsigned)tiles);
             for (int p = 0; p < all_pairs && ok; ++p) {
                 const unsigned now = uniform(pp) + p, kb = now % PAIRS;
-                if (!(ok = mbar_wait_warp(&S.abort, &S.kfull[kb], (now / PAIRS) & 1u, P.status, 95))) break;
+                if (!(ok = !kv_lost<TEST>(P, &S.abort, 95, round) && mbar_wait_warp(&S.abort, &S.kfull[kb], (now / PAIRS) & 1u, P.status, 95))) break;
                 for (int tile = (int)uniform(part); tile < all_tiles; tile += (int)uniform(stride)) {
                     if (!uniform(sees(p, tile))) continue;
                     const unsigned u = uniform(used), u1 = uniform(used1), b = STAY ? tile : u % TILES, filled = STAY ? (tile ? u1 : u) : u / TILES, d = uniform(dt);
-                    if (!(ok = mbar_wait_warp(&S.abort, &S.qfull[b], filled & 1u, P.status, 96))) break;
-                    if (d > 1 && !(ok = mbar_wait_warp(&S.abort, &S.dfree[d & 1], ((d >> 1) + 1) & 1u, P.status, 97))) break;
+                    if (!(ok = !kv_lost<TEST>(P, &S.abort, 96, round) && mbar_wait_warp(&S.abort, &S.qfull[b], filled & 1u, P.status, 96))) break;
+                    if (d > 1 && !(ok = !kv_lost<TEST>(P, &S.abort, 97, round) && mbar_wait_warp(&S.abort, &S.dfree[d & 1], ((d >> 1) + 1) & 1u, P.status, 97))) break;
                     tc_fence_after();
                     product(to + 256 * (d & 1), k_lo + 2 * kb * (CODES >> 4), q_lo + b * (IMAGE >> 4), hi);
                     if (2 * p + 1 < all_units) product(to + 256 * (d & 1) + 128, k_lo + (2 * kb + 1) * (CODES >> 4), q_lo + b * (IMAGE >> 4), hi);
@@ -711,12 +711,12 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
             }
             if (STAY)                            // a tile that no token of the segment is seen by has come all the same
                 for (int b = 0; b < all_tiles && ok; ++b) {
-                    ok = mbar_wait_warp(&S.abort, &S.qfull[b], uniform(b ? used1 : used) & 1u, P.status, 99);
+                    ok = !kv_lost<TEST>(P, &S.abort, 99, round) && mbar_wait_warp(&S.abort, &S.qfull[b], uniform(b ? used1 : used) & 1u, P.status, 99);
                     if (ok) umma_commit(&S.qfree[b]);
                 }
         } else {
             const auto fill = [&](int tile, unsigned b, unsigned filled) {
-                if (filled > 0 && !mbar_wait_warp(&S.abort, &S.qfree[b], (filled - 1) & 1u, P.status, 98)) return false;
+                if (filled > 0 && (kv_lost<TEST>(P, &S.abort, 98, round) || !mbar_wait_warp(&S.abort, &S.qfree[b], (filled - 1) & 1u, P.status, 98))) return false;
                 if (lane == 0) {
                     mbar_arrive_expect_tx(&S.qfull[b], IMAGE + 5 * TILE * 4);
 #pragma unroll
@@ -744,6 +744,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
         }
         if (!ok) break;
         pp += pairs;
+        ++round;
         if (STAY) {
             ++used;
             if (tiles > 1) ++used1;
@@ -877,9 +878,9 @@ int gbs_tc_kvmass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* b
     P.status = p->d_status;
     const int64_t jobs = A.n_tokens * ((A.n_heads + 3) / 4);
     const size_t rows_smem = sizeof(RowsSmem) + 1024;
-    const bool stay = (int64_t)A.max_tokens * A.group <= 2 * TILE;
+    const bool stay = (int64_t)A.max_tokens * A.group <= 2 * TILE, test = A.lost_code != 0;
     int rc = gbs_kv_launch(p, k_tc_kvmass_prepare, dim3((unsigned)((jobs + 7) / 8)), 256, 0, stream, P);
-    if (rc == 0) rc = p->asym ? launch(p, k_tc_kvmass_rows<true>, rows_smem, P, stream) : launch(p, k_tc_kvmass_rows<false>, rows_smem, P, stream);
+    if (rc == 0) rc = launch(p, test ? (p->asym ? k_tc_kvmass_rows<true, true> : k_tc_kvmass_rows<false, true>) : (p->asym ? k_tc_kvmass_rows<true, false> : k_tc_kvmass_rows<false, false>), rows_smem, P, stream);
     if (rc == 0) rc = gbs_kv_launch(p, k_tc_kvmass_join, dim3((unsigned)p->sm_count), UNIT, 0, stream, P);
     P.line.unit_log = 8;
     P.line.tile_rows = 1 << 29;                  // a sequence is one tile from here on
@@ -889,8 +890,10 @@ int gbs_tc_kvmass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* b
     P.line.pad = 0;
     if (rc != 0) return rc;
     const size_t smem = (stay ? sizeof(TokensSmem<true>) : sizeof(TokensSmem<false>)) + 1024;
-    const auto f = p->asym ? (stay ? k_tc_kvmass_tokens<true, true> : k_tc_kvmass_tokens<true, false>)
-                           : (stay ? k_tc_kvmass_tokens<false, true> : k_tc_kvmass_tokens<false, false>);
+    const auto f = test ? (p->asym ? (stay ? k_tc_kvmass_tokens<true, true, true> : k_tc_kvmass_tokens<true, false, true>)
+                                   : (stay ? k_tc_kvmass_tokens<false, true, true> : k_tc_kvmass_tokens<false, false, true>))
+                        : (p->asym ? (stay ? k_tc_kvmass_tokens<true, true, false> : k_tc_kvmass_tokens<true, false, false>)
+                                   : (stay ? k_tc_kvmass_tokens<false, true, false> : k_tc_kvmass_tokens<false, false, false>));
     P.heads = A.c.heads;
     P.shares = stay ? 1 : shares_of(p, A, width);
     P.a.c.heads *= P.shares;

@@ -1,0 +1,97 @@
+"""What the weights of cached tokens do when a bounded wait of the kernels for many query rows runs out: the kernels end, the code stands in the plan's status
+word, nothing is written but weights and the workspace, and the next call is as always.  gbs_selftest_kv_attention_mass makes the waits run out; nothing faults or hangs."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from kv_util import DEV, filled
+from paper_2504_13989_b200 import Plan, binding
+from paper_2504_13989_b200 import build as gbs_build
+from test_kv_host import INVALID, OK, P, plan, pool
+
+GUARD = 1 << 20
+ROWS, TOKENS = range(81, 87), range(91, 100)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    gbs_build.build()
+
+
+def test_refusals():
+    lib, c = binding.lib(), pool()
+
+    def f(code, segment, n=2, flags=1, q=P):
+        return lib.gbs_selftest_kv_attention_mass(plan(), ctypes.byref(c), P, P, n, 3, 2, q, 1024, 128, 8, 0.0, 0, flags, P, 1.0, P, 7, P, 1 << 40, code, segment, None)
+    for code in (0, 1, -1, 61, 77, 80, 87, 90, 100, 1 << 20):
+        assert f(code, 0) == INVALID
+    assert f(81, -1) == INVALID and f(81, 0, flags=2) == INVALID and f(81, 0, q=None) == INVALID and f(99, 3, n=0) == OK
+
+
+class Call:
+    """One call on a pool of many sequences; weights and workspace between guards."""
+
+    def __init__(self, lengths, counts, heads, kv_heads, asym, width):
+        self.plan = Plan(128, 128, 1, 4, 128, 0.9, asymmetric=asym)
+        self.cache = filled(self.plan, lengths, kv_heads, 32, seed=1)
+        self.counts, self.heads, self.width = counts, heads, width
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(2)
+        n = sum(counts)
+        self.q = torch.randn((n, heads, 128), generator=gen, device=DEV).to(torch.bfloat16)
+        self.cu = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device=DEV)
+        self.former = torch.rand((len(lengths), kv_heads, width), generator=gen, device=DEV)
+        self.mass = torch.full((2 * GUARD + self.former.numel(),), 7.0, device=DEV)
+        need = ctypes.c_int64(0)
+        args = self.plan.handle, ctypes.byref(self.cache._c), len(counts), n, max(counts), heads, width
+        assert binding.lib().gbs_kv_attention_mass_workspace(*args, ctypes.byref(need)) == OK
+        self.need = need.value
+        self.work = torch.full((2 * GUARD + (self.need + 15) // 16 * 16,), 77, dtype=torch.uint8, device=DEV)
+        self.kept = [t.clone() for t in self.cache._kept + (self.q, self.cu)]
+
+    def run(self, code=None, segment=0):
+        h, mass = self.heads, self.mass[GUARD:-GUARD].view(self.former.shape)
+        mass.copy_(self.former)
+        at = mass.data_ptr()
+        args = [self.plan.handle, ctypes.byref(self.cache._c), None, self.cu.data_ptr(), len(self.counts), sum(self.counts), max(self.counts), self.q.data_ptr(), 128 * h,
+                128, h, 0.0, 0, 1, at, 0.5, at, self.width, self.work.data_ptr() + GUARD, self.need]
+        if code is None:
+            assert binding.lib().gbs_kv_attention_mass(*args, None) == OK
+        else:
+            assert binding.lib().gbs_selftest_kv_attention_mass(*args, code, segment, None) == OK
+        torch.cuda.synchronize()
+        got = mass.clone()
+        self.mass[GUARD:-GUARD] = 7.0
+        assert bool((self.mass == 7.0).all())
+        assert bool((self.work[:GUARD] == 77).all()) and bool((self.work[GUARD + self.need:] == 77).all())
+        same = zip((t.view(torch.uint8) for t in self.cache._kept + (self.q, self.cu)), (t.view(torch.uint8) for t in self.kept))
+        assert all(torch.equal(a, b) for a, b in same)
+        return got
+
+
+# rows that stay in shared memory (one tile of 64, two, both), rows that pass through the ring, rows shared among segments
+CASES = [([300, 700, 40] * 200, [20, 30, 40] * 200, 4, 2, 700), ([3000] * 100, [128] * 100, 2, 2, 3000), ([900, 600] * 100, [200, 129] * 100, 2, 2, 900),
+         ([3000], [1500], 4, 1, 3000)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("asym", [False, True])
+@pytest.mark.parametrize("case", range(len(CASES)))
+@pytest.mark.parametrize("code", [*ROWS, *TOKENS])
+def test_expiry(code, case, asym):
+    lengths, counts, heads, kv_heads, width = CASES[case]
+    c = Call(lengths, counts, heads, kv_heads, asym, width)
+    right = c.run()
+    assert c.plan.device_status() == 0
+    seen = []
+    for segment in range(4):
+        c.run(code, segment)
+        seen.append(c.plan.device_status())
+        assert seen[-1] in (0, code)                           # 0: no block makes such a wait there
+        assert torch.equal(c.run(), right)                     # the next call is as always
+    # The last case has 12 pairs of units, in at most eight shares: 96 segments for 148 blocks, and 24 tiles of 128 rows over 24 units in the first pass: a block has one segment (no room
+    # for query rows to be waited for in the first pass) of one pair (no room for keys in the second).  Only rows that stay are waited for behind a segment's tokens
+    assert code in seen or (case == 3 and code in (86, 94, 98)) or (case > 1 and code == 99)
+    c.plan.close()
