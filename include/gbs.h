@@ -501,6 +501,8 @@ int gbs_kv_shared_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache,
  *                     as long as that is 256 MB at most
  * Weights are right to fp32: query rows are rounded to 24 bits of their largest coordinate, codes enter as they are, sums of products are exact.  Value
  * rows count for nothing.  A token whose key scale is infinite or a NaN makes the rows that see it, and so what they see, NaN.
+ * Where a bounded wait runs out (gbs_plan_device_status), a weight is what it was or what it was to become, nothing else; all are what they were if that
+ * is before all rows' sums are known.
  */
 int gbs_kv_attention_mass_workspace(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,
                                     int n_heads, int64_t width, int64_t* bytes_out);
@@ -545,7 +547,7 @@ int gbs_selftest_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cach
                               int segment, void* cuda_stream);
 
 /*
- * The same of gbs_kv_attention_mass, whose waits are all in its kernels for more than 32 query rows a KV head and item.  Weights may be any numbers.
+ * The same of gbs_kv_attention_mass, whose waits are all in its kernels for more than 32 query rows a KV head and item.
  *   code              81 .. 86: the pass for the rows' sums (scores, room for keys, query rows, keys, room for scores, room for query rows);
  *                     91 .. 99: the pass for the tokens' (keys, query rows, scores, room for keys, keys before their product, query rows before it, room for
  *                     scores, room for query rows, query rows of a tile that no token of a segment is seen by)

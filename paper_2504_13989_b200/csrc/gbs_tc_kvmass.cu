@@ -46,6 +46,7 @@ struct MassArgs {
     float* mass;
     long long width;
     float decay;
+    int* gave_up;                                // [2]: whether a wait ran out in the first pass, in the second: sums that are not whole are not written
     int* status;
 };
 
@@ -66,6 +67,7 @@ __global__ __launch_bounds__(256) void k_tc_kvmass_prepare(const __grid_constant
 {
     kv_wait_before();
     kv_let_next();
+    if (blockIdx.x == 0 && threadIdx.x < 2) P.gave_up[threadIdx.x] = 0;
     const gbs_kv_attn& A = P.a;
     const int lane = threadIdx.x & 31, l8 = lane & 7, fours = (A.n_heads + 3) >> 2;
     const long long job = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -443,6 +445,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_rows(const __grid_cons
     tc_fence_before();
     __syncthreads();
     if (S.abort) {                               // a wait has run out: what is under way is given time to end
+        if (tid == 0) P.gave_up[0] = 1;
         if (w == ISSUE) {
             umma_commit(&S.drain);
             drain_copies(&S.drain, 1, 1);
@@ -531,7 +534,8 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
     const unsigned tmem = S.tmem;
     kv_wait_before();
     kv_let_next();
-    const int places = kv_share<THREADS, KV_ALL>(A, P.line, &S.seg, S.share);
+    // without all rows' sums the weights stay what they are
+    const int places = P.gave_up[0] ? 0 : kv_share<THREADS, KV_ALL>(A, P.line, &S.seg, S.share);
 
     KvSeg& seg = S.own[w];
     if (lane == 0) seg = S.seg;
@@ -755,6 +759,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvmass_tokens(const __grid_co
     tc_fence_before();
     __syncthreads();
     if (S.abort) {
+        if (tid == 0) P.gave_up[1] = 1;
         if (w == ISSUE) {
             umma_commit(&S.drain);
             drain_copies(&S.drain, 1, 1);
@@ -782,7 +787,7 @@ __global__ __launch_bounds__(256) void k_tc_kvmass_sums(const __grid_constant__ 
     const gbs_kv_attn& A = P.a;
     const int item = blockIdx.x / P.heads, head = blockIdx.x - item * P.heads;
     const KvEntry e = kv_entry<KV_ALL>(A, P.line, item);
-    if (e.units == 0) return;
+    if (e.units == 0 || P.gave_up[0] || P.gave_up[1]) return;
     const long long row = ((long long)e.seq * P.heads + head) * P.width, step = (long long)A.n_items * P.heads * P.width;
     const float* sums = P.sums + ((long long)item * P.heads + head) * P.width;
     for (long long pos = 256ll * blockIdx.y + threadIdx.x; pos < e.length && pos < P.width; pos += 256ll * gridDim.y) {
@@ -816,7 +821,7 @@ int shares_of(const gbs_plan* p, const gbs_kv_attn& A, int64_t width)
 }
 
 struct Layout {
-    int64_t slots, rows, factor, lift, norm, lo, hi, parts, joins, sums, bytes;
+    int64_t slots, rows, factor, lift, norm, lo, hi, parts, joins, gave_up, sums, bytes;
 };
 Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A, int64_t width)
 {
@@ -831,7 +836,8 @@ Layout layout_of(const gbs_plan* p, const gbs_kv_attn& A, int64_t width)
     l.hi = l.lo + all * TILE * (int64_t)sizeof(int);
     l.parts = l.hi + all * TILE * (int64_t)sizeof(int);
     l.joins = l.parts + (int64_t)p->sm_count * 2 * UNIT * sizeof(float2);
-    l.sums = l.joins + round_up((int64_t)p->sm_count * sizeof(KvJoin));
+    l.gave_up = l.joins + round_up((int64_t)p->sm_count * sizeof(KvJoin));
+    l.sums = l.gave_up + 16;
     const int shares = shares_of(p, A, width);
     l.bytes = l.sums + (shares > 1 ? (int64_t)shares * A.n_items * A.c.heads * width * (int64_t)sizeof(float) : 0);
     return l;
@@ -871,6 +877,7 @@ int gbs_tc_kvmass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* b
     P.hi = reinterpret_cast<int*>(w + l.hi);
     P.parts = reinterpret_cast<float2*>(w + l.parts);
     P.joins = reinterpret_cast<KvJoin*>(w + l.joins);
+    P.gave_up = reinterpret_cast<int*>(w + l.gave_up);
     P.base = base;
     P.mass = mass;
     P.width = width;
