@@ -547,6 +547,15 @@ int gbs_selftest_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cach
                               int segment, void* cuda_stream);
 
 /*
+ * The same of gbs_kv_shared_attention: in both of its passes, over what groups share and over what is an item's own, where the call has them.
+ */
+int gbs_selftest_kv_shared_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens,
+                                     int n_items, int64_t n_tokens, int max_tokens, const int32_t* groups, int n_groups, int max_own,
+                                     int max_prefix, const void* q, int64_t q_token_stride, int64_t q_head_stride, int n_heads,
+                                     float scale, int flags, void* out, int64_t out_token_stride, int64_t out_head_stride,
+                                     void* workspace, int64_t workspace_bytes, int code, int segment, void* cuda_stream);
+
+/*
  * The same of gbs_kv_attention_mass, whose waits are all in its kernels for more than 32 query rows a KV head and item.
  *   code              81 .. 86: the pass for the rows' sums (scores, room for keys, query rows, keys, room for scores, room for query rows);
  *                     91 .. 99: the pass for the tokens' (keys, query rows, scores, room for keys, keys before their product, query rows before it, room for

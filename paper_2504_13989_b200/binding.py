@@ -43,7 +43,7 @@ EXPORTS = ("gbs_plan_create", "gbs_plan_create_ex", "gbs_plan_destroy", "gbs_pla
            "gbs_kv_append", "gbs_kv_append_extended", "gbs_kv_read", "gbs_kv_attention_workspace", "gbs_kv_attention",
            "gbs_selftest_kv_attention", "gbs_kv_shared_attention_workspace", "gbs_kv_shared_attention",
            "gbs_kv_attention_mass_workspace", "gbs_kv_attention_mass", "gbs_kv_evict_workspace", "gbs_kv_evict",
-           "gbs_selftest_kv_attention_mass")
+           "gbs_selftest_kv_attention_mass", "gbs_selftest_kv_shared_attention")
 GBS_STATIC_MAX_D_PAD = 4096
 
 
@@ -153,6 +153,7 @@ def lib() -> ctypes.CDLL:
         L.gbs_kv_shared_attention_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i32, i32, ctypes.POINTER(i64)]
         L.gbs_kv_shared_attention.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i32, i32, i32, vp, i64, i64, i32, ctypes.c_float, i32, vp, i64, i64,
                                               vp, i64, vp]
+        L.gbs_selftest_kv_shared_attention.argtypes = L.gbs_kv_shared_attention.argtypes[:-1] + [i32, i32, vp]
         L.gbs_kv_attention_mass_workspace.argtypes = [vp, kv, i32, i64, i32, i32, i64, ctypes.POINTER(i64)]
         L.gbs_kv_attention_mass.argtypes = [vp, kv, vp, vp, i32, i64, i32, vp, i64, i64, i32, ctypes.c_float, i32, i32, vp, ctypes.c_float, vp, i64,
                                             vp, i64, vp]

@@ -532,9 +532,8 @@ template <int PART>
 int launch(const gbs_plan* p, const KvAttnArgs& P, int blocks, cudaStream_t stream)
 {
     const size_t smem = p->asym ? sizeof(Smem<true>) : sizeof(Smem<false>);
-    const bool test = PART == KV_WHOLE && P.a.lost_code;
-    const auto f = test ? (p->asym ? k_kv_attn_few<true, PART == KV_WHOLE, PART> : k_kv_attn_few<false, PART == KV_WHOLE, PART>)
-                        : (p->asym ? k_kv_attn_few<true, false, PART> : k_kv_attn_few<false, false, PART>);
+    const auto f = P.a.lost_code ? (p->asym ? k_kv_attn_few<true, true, PART> : k_kv_attn_few<false, true, PART>)
+                                 : (p->asym ? k_kv_attn_few<true, false, PART> : k_kv_attn_few<false, false, PART>);
     const cudaError_t e = cudaFuncSetAttribute((const void*)f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return (int)e;
     const int rc = gbs_kv_launch(p, f, dim3((unsigned)blocks), THREADS, smem, stream, P);

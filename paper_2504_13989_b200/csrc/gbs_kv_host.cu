@@ -265,6 +265,9 @@ int check_rows(const gbs_plan* p, const AttnCall& x, bool has_out, const void* w
     return x.q == x.out ? GBS_ERR_INVALID_ARG : GBS_OK;              // rows are read after others have been written
 }
 
+// waits of the attention kernels, for few rows and for many
+bool selftest_code(int code) { return (code >= 61 && code <= 64) || (code >= 71 && code <= 77); }
+
 // code, segment: of the waits that count as run out in the self-test (0: none)
 int attention(const gbs_plan* p, const gbs_kv_cache_t* cache, const AttnCall& x, void* workspace, int64_t workspace_bytes, int code, int segment, void* stream)
 {
@@ -300,7 +303,7 @@ extern "C" int gbs_selftest_kv_attention(const gbs_plan_t* p, const gbs_kv_cache
                                          int n_heads, float scale, int window, int flags, void* out, int64_t out_token_stride,
                                          int64_t out_head_stride, void* workspace, int64_t workspace_bytes, int code, int segment, void* stream)
 {
-    if (!((code >= 61 && code <= 64) || (code >= 71 && code <= 77)) || segment < 0) return GBS_ERR_INVALID_ARG;
+    if (!selftest_code(code) || segment < 0) return GBS_ERR_INVALID_ARG;
     const AttnCall x = {seqs, cu_tokens, n_items, n_tokens, max_tokens, max_len, q, q_token_stride, q_head_stride, n_heads,
                         scale, window, flags, out, out_token_stride, out_head_stride};
     return attention(p, cache, x, workspace, workspace_bytes, code, segment, stream);
@@ -314,10 +317,6 @@ int check_groups(const int32_t* groups, int n_groups, const gbs_kv_attn& A)
     if (A.n_tokens * A.group > 1ll << 28) return GBS_ERR_INVALID_ARG;
     return aligned(groups, 4) ? GBS_OK : GBS_ERR_ALIGNMENT;
 }
-
-}  // namespace
-
-namespace {
 
 // the sizes that a workspace goes by
 int sizes_of(const gbs_plan* p, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens, int n_heads, const int64_t* bytes_out,
@@ -351,6 +350,27 @@ extern "C" int gbs_kv_shared_attention_workspace(const gbs_plan_t* p, const gbs_
     return GBS_OK;
 }
 
+namespace {
+
+// code, segment: as for attention
+int shared_attention(const gbs_plan* p, const gbs_kv_cache_t* cache, const AttnCall& x, const int32_t* groups, int n_groups, int max_prefix, void* workspace,
+                     int64_t workspace_bytes, int code, int segment, void* stream)
+{
+    gbs_kv_attn A;
+    bool empty = false;
+    int rc = attn_args(p, cache, x, &A, &empty);
+    if (rc == GBS_OK) rc = max_prefix < 0 ? GBS_ERR_INVALID_ARG : check_groups(groups, n_groups, A);
+    if (rc != GBS_OK || empty) return rc;
+    if (!x.q || !x.out || !workspace || workspace_bytes < gbs_kv_shared_workspace(p, A, n_groups, max_prefix)) return GBS_ERR_INVALID_ARG;
+    rc = check_rows(p, x, true, workspace);
+    if (rc != GBS_OK) return rc;
+    A.lost_code = code;
+    A.lost_segment = segment;
+    return on_device(p, [&] { return gbs_kv_shared_launch(p, A, groups, n_groups, max_prefix, workspace, static_cast<cudaStream_t>(stream)); });
+}
+
+}  // namespace
+
 extern "C" int gbs_kv_shared_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
                                        int64_t n_tokens, int max_tokens, const int32_t* groups, int n_groups, int max_own, int max_prefix, const void* q,
                                        int64_t q_token_stride, int64_t q_head_stride, int n_heads, float scale, int flags, void* out,
@@ -358,15 +378,19 @@ extern "C" int gbs_kv_shared_attention(const gbs_plan_t* p, const gbs_kv_cache_t
 {
     const AttnCall x = {seqs, cu_tokens, n_items, n_tokens, max_tokens, max_own, q, q_token_stride, q_head_stride, n_heads,
                         scale, 0, flags, out, out_token_stride, out_head_stride};
-    gbs_kv_attn A;
-    bool empty = false;
-    int rc = attn_args(p, cache, x, &A, &empty);
-    if (rc == GBS_OK) rc = max_prefix < 0 ? GBS_ERR_INVALID_ARG : check_groups(groups, n_groups, A);
-    if (rc != GBS_OK || empty) return rc;
-    if (!q || !out || !workspace || workspace_bytes < gbs_kv_shared_workspace(p, A, n_groups, max_prefix)) return GBS_ERR_INVALID_ARG;
-    rc = check_rows(p, x, true, workspace);
-    if (rc != GBS_OK) return rc;
-    return on_device(p, [&] { return gbs_kv_shared_launch(p, A, groups, n_groups, max_prefix, workspace, static_cast<cudaStream_t>(stream)); });
+    return shared_attention(p, cache, x, groups, n_groups, max_prefix, workspace, workspace_bytes, 0, 0, stream);
+}
+
+extern "C" int gbs_selftest_kv_shared_attention(const gbs_plan_t* p, const gbs_kv_cache_t* cache, const int32_t* seqs, const int32_t* cu_tokens, int n_items,
+                                                int64_t n_tokens, int max_tokens, const int32_t* groups, int n_groups, int max_own, int max_prefix, const void* q,
+                                                int64_t q_token_stride, int64_t q_head_stride, int n_heads, float scale, int flags, void* out,
+                                                int64_t out_token_stride, int64_t out_head_stride, void* workspace, int64_t workspace_bytes, int code,
+                                                int segment, void* stream)
+{
+    if (!selftest_code(code) || segment < 0) return GBS_ERR_INVALID_ARG;
+    const AttnCall x = {seqs, cu_tokens, n_items, n_tokens, max_tokens, max_own, q, q_token_stride, q_head_stride, n_heads,
+                        scale, 0, flags, out, out_token_stride, out_head_stride};
+    return shared_attention(p, cache, x, groups, n_groups, max_prefix, workspace, workspace_bytes, code, segment, stream);
 }
 
 extern "C" int gbs_kv_attention_mass_workspace(const gbs_plan_t* p, const gbs_kv_cache_t* cache, int n_items, int64_t n_tokens, int max_tokens,

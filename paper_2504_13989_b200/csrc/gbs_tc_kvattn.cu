@@ -525,7 +525,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             const auto ahead = [&](auto half, int i) {
                 if (i >= units) return true;
                 const unsigned now = at0 + i;
-                if (!mbar_wait_warp(&S.abort, &S.kfull[now & 1], (now >> 1) & 1u, P.status, 71)) return false;
+                if (kv_lost<TEST>(P, &S.abort, 71, round) || !mbar_wait_warp(&S.abort, &S.kfull[now & 1], (now >> 1) & 1u, P.status, 71)) return false;
                 tc_fence_after();
                 scores(half, now & 1);
                 umma_commit(&S.kfree[now & 1]);
@@ -534,8 +534,8 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             const auto alternate = [&](auto half, auto adds, int i) {
                 constexpr int t = decltype(half)::value;
                 const unsigned now = at0 + i;
-                if (!mbar_wait_warp(&S.abort, &S.vfull[now & 1], (now >> 1) & 1u, P.status, 72)) return false;
-                if (!mbar_wait_warp(&S.abort, &S.pfull[t], ((t == 0 ? turn_a : turn_b) + (i >> 1)) & 1u, P.status, 73)) return false;
+                if (kv_lost<TEST>(P, &S.abort, 72, round) || !mbar_wait_warp(&S.abort, &S.vfull[now & 1], (now >> 1) & 1u, P.status, 72)) return false;
+                if (kv_lost<TEST>(P, &S.abort, 73, round) || !mbar_wait_warp(&S.abort, &S.pfull[t], ((t == 0 ? turn_a : turn_b) + (i >> 1)) & 1u, P.status, 73)) return false;
                 tc_fence_after();
                 values(half, adds, now & 1);
                 umma_commit(&S.vfree[now & 1]);
@@ -595,8 +595,10 @@ int launch(const gbs_plan* p, const KvAttnArgs& P, int blocks, cudaStream_t stre
 {
     constexpr bool WHOLE = PART == KV_WHOLE;
     const size_t smem = sizeof(Smem) + 1024;
-    const bool test = WHOLE && P.a.lost_code, split = !WHOLE && P.a.one_tile;
-    const auto f = test                  ? (p->asym ? k_tc_kvattn<true, WHOLE, PART, false, !WHOLE> : k_tc_kvattn<false, WHOLE, PART, false, !WHOLE>)
+    // whole calls have no instance of one tile, the others none that rounds twice; the self-test of a whole call has always the one that does
+    const bool split = !WHOLE && P.a.one_tile;
+    const auto f = P.a.lost_code        ? (split ? (p->asym ? k_tc_kvattn<true, true, PART, !WHOLE, !WHOLE> : k_tc_kvattn<false, true, PART, !WHOLE, !WHOLE>)
+                                                 : (p->asym ? k_tc_kvattn<true, true, PART, false, !WHOLE> : k_tc_kvattn<false, true, PART, false, !WHOLE>))
                    : split               ? (p->asym ? k_tc_kvattn<true, false, PART, !WHOLE, !WHOLE> : k_tc_kvattn<false, false, PART, !WHOLE, !WHOLE>)
                    : !WHOLE || P.a.fine  ? (p->asym ? k_tc_kvattn<true, false, PART, false, true> : k_tc_kvattn<false, false, PART, false, true>)
                                          : (p->asym ? k_tc_kvattn<true, false, PART, false, !WHOLE> : k_tc_kvattn<false, false, PART, false, !WHOLE>);
