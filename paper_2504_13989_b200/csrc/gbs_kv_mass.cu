@@ -345,8 +345,8 @@ __global__ __launch_bounds__(THREADS, BLOCKS_PER_SM) void k_kv_mass(const __grid
                                 for (int j = 0; j < 4; ++j) {
                                     const float x = fmaf((float)(256 * c[h][0][j] + c[h][1][j]), 256.f, (float)c[h][2][j]);
                                     const float fac = j & 1 ? f.z : f.x, lift = j & 1 ? f.w : f.y;
-                                    const float y = MASS ? -(j & 1 ? norm.z : norm.x) : 0.f;
-                                    z[h][j] = fmaf(x, ks[h][j >> 1] * fac, ASYM ? fmaf(km[h][j >> 1], lift, y) : y);
+                                    z[h][j] = fmaf(x, ks[h][j >> 1] * fac, ASYM ? km[h][j >> 1] * lift : 0.f);
+                                    if (MASS) z[h][j] = __fsub_rn(z[h][j], j & 1 ? norm.z : norm.x);         // from the score as the first pass had it, to the last bit
                                     if (!plain) {
                                         const int pos = mine + 16 * h + 8 * (j >> 1) + g;
                                         if (pos < (j & 1 ? lo.y : lo.x) || pos >= (j & 1 ? hi.y : hi.x) || !(there >> (16 * h + 8 * (j >> 1) + g) & 1)) z[h][j] = -INFINITY;
