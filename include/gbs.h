@@ -499,7 +499,9 @@ int gbs_kv_shared_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache,
  *   workspace         device, gbs_kv_attention_mass_workspace bytes for the same sizes, 16-byte aligned; overwritten, needs no preparation, and one call at a
  *                     time may use it.  With up to 32 query rows a KV head and item it has room for their scores, 4 bytes a row and position below the width,
  *                     as long as that is 256 MB at most
- * Weights are right to fp32: query rows are rounded to 24 bits of their largest coordinate, codes enter as they are, sums of products are exact.  Value
+ * Scores are right to fp32: query rows are rounded to 24 bits of their largest coordinate, its sign among them, codes enter as they are, sums of products are exact, and
+ * what they become is rounded as a float.  With more than 32 query rows a KV head and item it is 23 bits, and the logarithm of a row's sum is rounded as well, so that all
+ * of a row's weights may be off by 2^-24 of its largest score's size (in units of log 2).  Scores beyond 2^24 have no units in fp32: weights are finite, and no more.  Value
  * rows count for nothing.  A token whose key scale is infinite or a NaN makes the rows that see it, and so what they see, NaN.
  * Where a bounded wait runs out (gbs_plan_device_status), a weight is what it was or what it was to become, nothing else; all are what they were if that
  * is before all rows' sums are known.
