@@ -249,7 +249,7 @@ int gbs_tc_kvmass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* b
 int64_t gbs_kv_mass_workspace(const gbs_plan* p, const gbs_kv_attn& A, int64_t width);
 int gbs_kv_mass_launch(const gbs_plan* p, const gbs_kv_attn& A, const float* base, float decay, float* mass, int64_t width, void* workspace,
                        cudaStream_t stream);
-// gbs_kv_pages.cu : pages for what sequences keep; the items' status.  gbs_kv_evict.cu : what they keep, moved there
+// gbs_kv_pages.cu : pages for what sequences keep; the items' status (with many items).  gbs_kv_evict.cu : the same with few, and what they keep, moved there
 int gbs_kv_evict_pages_launch(const gbs_plan* p, const gbs_kv_view& c, const int* seqs, int n_items, int keep, int keep_pages, int* fresh, int* arrived,
                               int* status, cudaStream_t stream);
 struct gbs_kv_eviction {
@@ -262,6 +262,7 @@ struct gbs_kv_eviction {
     int *status, *kept;
     int *fresh, *arrived;               // [n_items][keep_pages], [n_items]
     float* weights;                     // [n_items][heads][keep]: of what stays
+    unsigned mask;                      // of the table of the search for pages, where it is part of the search for what stays; 0: it is a launch before
 };
 int gbs_kv_evict_launch(const gbs_plan* p, const gbs_kv_eviction& E, cudaStream_t stream);
 

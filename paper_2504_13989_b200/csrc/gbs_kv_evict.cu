@@ -7,13 +7,15 @@
 // place by prefix sums over positions: no sorting, and nothing depends on the order of threads.
 #include <cooperative_groups.h>
 
-#include "gbs_kv.cuh"
+#include "gbs_kv_alloc.cuh"
 
 namespace {
 
 constexpr int EACH = 8, HELD = 2;                // neighbouring tokens of a thread, and how many times so many it keeps in registers
 constexpr int MOVE = 256;                        // tokens that a block moves, and its threads
 constexpr int BINS = 2048;
+constexpr int FEW_ITEMS = 256;                   // up to so many, pages are looked for in the launch that looks for what stays
+static_assert(table_bytes(FEW_ITEMS) <= BINS * sizeof(int), "in the same shared memory");
 
 // weights as integers of the same order: NaN the largest, -0 as 0
 __device__ __forceinline__ unsigned order_of(float x)
@@ -47,21 +49,37 @@ __device__ __forceinline__ unsigned long long block_prefix(unsigned long long v,
     return below + s - v;
 }
 
-// A block, or a cluster of eight, per item and KV head.  A thread has EACH neighbouring tokens of every EACH * THREADS of its block's slice.  What it reads
-// was written by launches that had ended before the one before it, which looks for pages, let it begin; only that one's status is waited for.
+// (a call of its own, so that the search for what stays keeps its registers)
+template <int THREADS>
+__device__ __noinline__ void find_pages(const gbs_kv_eviction& E, int* sm, int* part)
+{
+    kv_allocate<EVICT, THREADS>(AllocArgs{E.c, E.seqs, nullptr, E.n_items, E.status, E.mask, E.keep, E.keep_pages, E.fresh, E.arrived}, sm, part);
+}
+
+// A block, or a cluster of eight, per item and KV head.  A thread has EACH neighbouring tokens of every EACH * THREADS of its block's slice.  Neither what stays nor the pages for it need the other,
+// so that one more block, the first one, looks for pages meanwhile; what this leaves of an item that is refused, the moving launch takes back.  (The two as launches of their own, each waiting for
+// the one before, as with many items: 4 us more.)
 template <int THREADS, int BLOCKS>
 __global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(const __grid_constant__ gbs_kv_eviction E)
 {
     namespace cg = cooperative_groups;
     constexpr int PER = BINS / THREADS, WARPS = THREADS / 32;
     static_assert(HELD == 2 && EACH * THREADS < 1 << 16, "four counts in 64 bits");
-    __shared__ int bins[BINS], all[BLOCKS > 1 ? 2 : 1][BLOCKS > 1 ? BINS : 1];       // of the block; of the cluster, digit by digit in turn
+    __shared__ __align__(8) int bins[BINS];      // (and what the search for pages needs)
+    __shared__ int all[BLOCKS > 1 ? 2 : 1][BLOCKS > 1 ? BINS : 1];       // of the block; of the cluster, digit by digit in turn
     __shared__ unsigned long long part[WARPS];
     __shared__ int found[2];                     // the bin, and how many of it stay
     __shared__ int above_threshold, at_threshold;        // of the slice's tokens between
     __shared__ long long slices[BLOCKS];         // of each block: tokens that stay for sure (upper half), and that are equal to the threshold
     const int tid = threadIdx.x, lane = tid & 31, rank = BLOCKS > 1 ? (int)cg::this_cluster().block_rank() : 0;
-    const int row_of = blockIdx.x / BLOCKS, item = row_of / E.c.heads, head = row_of - item * E.c.heads;
+    if (E.mask != 0 && blockIdx.x == 0) kv_allocate_begin<THREADS>(E.mask, bins);
+    kv_wait_before();
+    kv_let_next();
+    if (E.mask != 0 && blockIdx.x < BLOCKS) {
+        if (blockIdx.x == 0) find_pages<THREADS>(E, bins, reinterpret_cast<int*>(part));
+        return;
+    }
+    const int row_of = blockIdx.x / BLOCKS - (E.mask != 0), item = row_of / E.c.heads, head = row_of - item * E.c.heads;
     const auto all_blocks = [&] {
         if (BLOCKS > 1) cg::this_cluster().sync();
         else __syncthreads();
@@ -176,15 +194,12 @@ __global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(cons
         all_blocks();
         for (int r = 0; r < rank; ++r) before += (unsigned long long)slices[r];
     }
-    kv_wait_before();
-    kv_let_next();
     int* kept = E.kept + ((long long)item * E.c.heads + head) * E.keep;
-    if (E.status[item] != GBS_KV_DONE || !cut) { // nothing was done, or all of it stays
-        const int stay = E.status[item] == GBS_KV_DONE ? length : 0;
-        for (long long j = THREADS * rank + tid; j < E.keep; j += THREADS * BLOCKS) kept[j] = j < stay ? (int)j : -1;      // keep may be as large as an int
+    if (!cut) {                                  // all of it stays
+        for (long long j = THREADS * rank + tid; j < E.keep; j += THREADS * BLOCKS) kept[j] = j < length ? (int)j : -1;    // keep may be as large as an int
         float* out = E.mass_out + row;
-        if (out != mass)
-            for (int j = THREADS * rank + tid; j < stay && j < E.width; j += THREADS * BLOCKS) out[j] = mass[j];
+        if (out != mass)                         // (of an item that is refused because an earlier one names its sequence, the same)
+            for (int j = THREADS * rank + tid; j < length && j < E.width; j += THREADS * BLOCKS) out[j] = mass[j];
         return;
     }
     float* weights = E.weights + ((long long)item * E.c.heads + head) * E.keep;
@@ -261,7 +276,11 @@ __global__ __launch_bounds__(MOVE, 5) void k_kv_evict_move(const __grid_constant
     const long long base = ((long long)item * E.c.heads + head) * E.keep;
     int pos = j < E.keep ? E.kept[base + j] : -1;
     const int seq = kv_sequence(E.c, E.seqs, item);
-    if (E.status[item] != GBS_KV_DONE) return;
+    if (E.status[item] != GBS_KV_DONE) {         // nothing is done, and nothing stays (places that no sequence has are -1 already)
+        const int most = min(E.keep, E.c.max_pages << E.c.page_log);
+        for (; j < most; j += gridDim.y * MOVE) E.kept[base + j] = -1;
+        return;
+    }
     const int* fresh = E.fresh + (long long)item * E.keep_pages;
     int* table = E.c.page_table + (long long)seq * E.c.max_pages;
     const int length = kv_length(E.c, seq), ps = 1 << E.c.page_log;
@@ -329,12 +348,13 @@ template <int THREADS, int BLOCKS>
 int select(const gbs_plan* p, const gbs_kv_eviction& E, cudaStream_t stream)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)E.n_items * (unsigned)E.c.heads * BLOCKS);
+    cfg.gridDim = dim3(((unsigned)E.n_items * (unsigned)E.c.heads + (E.mask != 0)) * BLOCKS);
     cfg.blockDim = dim3(THREADS);
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = p->pdl ? 1 : 0;
+    // single blocks that began while the launch before still has most SMs would share the others: 32 us for 27 sequences of up to 7700 tokens behind a fork, 20 when they begin at its end
+    attr[0].val.programmaticStreamSerializationAllowed = p->pdl && BLOCKS > 1 ? 1 : 0;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = BLOCKS;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
@@ -345,9 +365,11 @@ int select(const gbs_plan* p, const gbs_kv_eviction& E, cudaStream_t stream)
 
 }  // namespace
 
-int gbs_kv_evict_launch(const gbs_plan* p, const gbs_kv_eviction& E, cudaStream_t stream)
+int gbs_kv_evict_launch(const gbs_plan* p, const gbs_kv_eviction& E0, cudaStream_t stream)
 {
-    int rc = gbs_kv_evict_pages_launch(p, E.c, E.seqs, E.n_items, E.keep, E.keep_pages, E.fresh, E.arrived, E.status, stream);
+    gbs_kv_eviction E = E0;
+    E.mask = E.n_items <= FEW_ITEMS ? table_mask((unsigned)E.n_items) : 0;
+    int rc = E.mask != 0 ? 0 : gbs_kv_evict_pages_launch(p, E.c, E.seqs, E.n_items, E.keep, E.keep_pages, E.fresh, E.arrived, E.status, stream);
     const int64_t rows = (int64_t)E.n_items * E.c.heads, longest = (int64_t)E.c.max_pages << E.c.page_log;
     if (rc == 0) rc = longest > 2 * EACH * HELD * FEW && rows <= p->sm_count ? select<MANY, CLUSTER>(p, E, stream) : select<FEW, 1>(p, E, stream);
     const int64_t most = E.keep < longest ? E.keep : longest, y = (most + MOVE - 1) / MOVE;
