@@ -56,11 +56,12 @@ __device__ __noinline__ void find_pages(const gbs_kv_eviction& E, int* sm, int* 
     kv_allocate<EVICT, THREADS>(AllocArgs{E.c, E.seqs, nullptr, E.n_items, E.status, E.mask, E.keep, E.keep_pages, E.fresh, E.arrived}, sm, part);
 }
 
-// A block, or a cluster of eight, per item and KV head.  A thread has EACH neighbouring tokens of every EACH * THREADS of its block's slice.  Neither what stays nor the pages for it need the other,
+// A block, or a cluster of eight, per item and KV head.  A thread has EACH neighbouring tokens of every EACH * THREADS of its block's slice.  A sequence that one block can keep in registers is one
+// block's in a cluster as well: how long sequences are is known here alone.  Neither what stays nor the pages for it need the other,
 // so that one more block, the first one, looks for pages meanwhile; what this leaves of an item that is refused, the moving launch takes back.  (The two as launches of their own, each waiting for
 // the one before, as with many items: 4 us more.)
 template <int THREADS, int BLOCKS>
-__global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(const __grid_constant__ gbs_kv_eviction E)
+__global__ __launch_bounds__(THREADS, THREADS == 256 ? 6 : 1) void k_kv_select(const __grid_constant__ gbs_kv_eviction E)
 {
     namespace cg = cooperative_groups;
     constexpr int PER = BINS / THREADS, WARPS = THREADS / 32;
@@ -80,17 +81,18 @@ __global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(cons
         return;
     }
     const int row_of = blockIdx.x / BLOCKS - (E.mask != 0), item = row_of / E.c.heads, head = row_of - item * E.c.heads;
-    const auto all_blocks = [&] {
-        if (BLOCKS > 1) cg::this_cluster().sync();
-        else __syncthreads();
-    };
-
     const int seq = kv_sequence(E.c, E.seqs, item), length = seq < 0 ? 0 : kv_length(E.c, seq);
     const bool cut = length > E.keep;
+    const int blocks = BLOCKS == 1 || length <= HELD * EACH * THREADS ? 1 : BLOCKS;
+    if (cut && rank >= blocks) return;
+    const auto all_blocks = [&] {
+        if (BLOCKS > 1 && blocks > 1) cg::this_cluster().sync();
+        else __syncthreads();
+    };
     const long long row = ((long long)max(seq, 0) * E.c.heads + head) * E.width;
     const float* mass = E.mass + row;
     // the block's slice, and this thread's tokens of it that are kept in registers
-    const int per = ((length + BLOCKS - 1) / BLOCKS + EACH - 1) / EACH * EACH, from = min(rank * per, length), to = min(from + per, length);
+    const int per = ((length + blocks - 1) / blocks + EACH - 1) / EACH * EACH, from = min(rank * per, length), to = min(from + per, length);
     const int lo = E.first, hi = length - E.recent;      // the tokens between
     const auto weight = [&](int pos) { return pos < to && pos < E.width ? mass[pos] : 0.f; };
     // a token between as a number above 0; 0: one that is not
@@ -112,14 +114,14 @@ __global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(cons
     int want = E.keep - E.first - E.recent;
     const bool none = want == 0;
     if (cut && !none) {
-        if (BLOCKS > 1)
+        if (blocks > 1)
             for (int i = tid; i < BINS; i += THREADS) all[0][i] = 0;
         if (tid == 0) above_threshold = 0;
         // ---- the threshold: `want` of the largest, digit by digit ----
         for (int digit = 0; digit < 3; ++digit) {
             const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit < 2 ? 11 : 10, n = 1 << bits;
             for (int i = tid; i < BINS; i += THREADS) bins[i] = 0;
-            if (BLOCKS > 1 && digit == 0) all_blocks();          // nobody adds to what another block has not cleared yet
+            if (blocks > 1 && digit == 0) all_blocks();          // nobody adds to what another block has not cleared yet
             else __syncthreads();
             const auto count = [&](unsigned v) {
                 // (the upper digits of most weights fall into few bins; counting what is alike in a warp together first, by __match_any_sync: 37 us instead of 27 for 131 000
@@ -143,7 +145,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(cons
             int mine[PER], have[PER], sum = 0;
 #pragma unroll
             for (int k = 0; k < PER; ++k) have[k] = mine[k] = top - k >= 0 ? bins[top - k] : 0;
-            if (BLOCKS > 1) {
+            if (BLOCKS > 1 && blocks > 1) {
                 const int now = digit & 1;
 #pragma unroll
                 for (int k = 0; k < PER; ++k)
@@ -169,7 +171,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(cons
                 above += have[k];
             }
             __syncthreads();
-            if (BLOCKS > 1) {                    // of the slice's, those above
+            if (blocks > 1) {                    // of the slice's, those above
                 int over = 0;
 #pragma unroll
                 for (int k = 0; k < PER; ++k) over += top - k > found[0] ? mine[k] : 0;
@@ -184,7 +186,7 @@ __global__ __launch_bounds__(THREADS, BLOCKS == 1 ? 6 : 1) void k_kv_select(cons
 
     // ---- places ----
     unsigned long long before = 0;               // upper half: tokens that stay for sure, lower: equal to the threshold
-    if (cut && BLOCKS > 1) {                     // of the slices below
+    if (BLOCKS > 1 && cut && blocks > 1) {       // of the slices below
         if (none) all_blocks();                  // nobody writes to a block that has not begun yet
         else __syncthreads();
         if (tid < BLOCKS) {
@@ -341,8 +343,29 @@ __global__ __launch_bounds__(MOVE, 5) void k_kv_evict_move(const __grid_constant
     if (threadIdx.x == 0) E.c.lengths[seq] = E.keep;
 }
 
-// Long sequences of few items and heads are looked through by clusters of 8 x 1024 threads, others by 256: 16 rows of up to 131 000 weights 27 us, 168 with a block of 1024 threads for each.
+// Rows (items x KV heads) are looked through by 256 threads each, six rows an SM; by 1024, one an SM; or by clusters of eight blocks of 1024, of which some fifteen find eight SMs of one
+// part of the GPU at a time.  The first keeps 4096 weights of a row in registers, the second 16 384; what is beyond is fetched four times.
+// Which takes least goes by the tokens that a sequence can have, the table's width: lengths are not known here.  us of a call with a free and a fork before it (19), 512 of so many tokens stay:
+//     rows      tokens 4000             9000             20 000            60 000            130 000      |  300 where 130 000 have room
+//        8      27   27   27       39   31   31       62   40   31      160   79   35      319  141   45  |  23   27   27
+//       16      27   28   29       41   33   34       63   41   45      161   80   53      320  142   67  |  25   27   27
+//       48      27   29   39       41   33   47       64   43   74      164   82   86      324  144  116  |  25   27   37
+//      144      30   33   64       43   39   81       68   49  161      174   92  192                     |  27   31   60
+//      152      33   41   64       50   49   82       82   68  175      203  151  208                     |
+//      296      36   49   98       57   62  131       93   83  308                                        |  29   43   90
+//      768      78  112  232      125  140  308      202  197  771                                        |  41   80  193
+// So where sequences are likely to be shorter than the table, the first is less of a loss than the others: they have to take a quarter less, and at most two rows an SM.
 constexpr int FEW = 256, MANY = 1024, CLUSTER = 8;
+enum Form { ROW_256, ROW_1024, ROW_CLUSTER };
+Form form_of(const gbs_plan* p, int64_t rows, int64_t longest)
+{
+    const auto waves = [&](int64_t blocks) { return (double)((blocks + p->sm_count - 1) / p->sm_count); };
+    const int64_t held = longest < HELD * EACH * FEW ? longest : HELD * EACH * FEW;
+    const double few = (5.5 + 6e-4 * held + 2.3e-3 * (longest - held)) * (0.45 + 0.55 * waves(rows));
+    const double many = waves(rows) * (4.5 + 9.2e-4 * longest), cluster = waves(10 * rows) * (12 + 1e-4 * longest);
+    if (rows > 2 * p->sm_count || few <= 1.25 * (many < cluster ? many : cluster)) return ROW_256;
+    return many <= cluster ? ROW_1024 : ROW_CLUSTER;
+}
 
 template <int THREADS, int BLOCKS>
 int select(const gbs_plan* p, const gbs_kv_eviction& E, cudaStream_t stream)
@@ -371,7 +394,8 @@ int gbs_kv_evict_launch(const gbs_plan* p, const gbs_kv_eviction& E0, cudaStream
     E.mask = E.n_items <= FEW_ITEMS ? table_mask((unsigned)E.n_items) : 0;
     int rc = E.mask != 0 ? 0 : gbs_kv_evict_pages_launch(p, E.c, E.seqs, E.n_items, E.keep, E.keep_pages, E.fresh, E.arrived, E.status, stream);
     const int64_t rows = (int64_t)E.n_items * E.c.heads, longest = (int64_t)E.c.max_pages << E.c.page_log;
-    if (rc == 0) rc = longest > 2 * EACH * HELD * FEW && rows <= p->sm_count ? select<MANY, CLUSTER>(p, E, stream) : select<FEW, 1>(p, E, stream);
+    const Form form = form_of(p, rows, longest);
+    if (rc == 0) rc = form == ROW_256 ? select<FEW, 1>(p, E, stream) : form == ROW_1024 ? select<MANY, 1>(p, E, stream) : select<MANY, CLUSTER>(p, E, stream);
     const int64_t most = E.keep < longest ? E.keep : longest, y = (most + MOVE - 1) / MOVE;
     if (rc == 0) rc = gbs_kv_launch(p, k_kv_evict_move, dim3((unsigned)rows, (unsigned)(y < 65535 ? y : 65535)), MOVE, 0, stream, E);
     return rc;
