@@ -145,7 +145,8 @@ __device__ __forceinline__ void shrink(unsigned scores, unsigned sums, float kee
     }
 }
 
-// SPLIT: a block has one tile
+// SPLIT: a block has one tile.  Where it is not set, counts, loops and the end of a segment are written as if there were no such thing: with one form for both, the compiler fetched whole calls' numbers
+// from the stack once more (the last 2048 of 8048 tokens 321.8 us instead of 319.8).
 template <bool ASYM, bool TEST, int PART, bool SPLIT, bool FINE>
 __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant__ KvAttnArgs P)
 {
@@ -244,9 +245,12 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             meet_all();
 
             const int t = w >> 2, row = tid, tile = SPLIT && split ? 0 : t, step = SPLIT && split ? 2 : 1, skip = SPLIT && split ? t : 0;      // this thread's half, row and tile
-            const bool busy = t == 0 || two || split;
-            const unsigned scores = tmem + ((unsigned)(32 * (w & 3)) << 16) + 128 * t, sums = scores + O_COL, turn = t == 0 ? used_a : used_b;
-            const int of = split ? row & (TILE - 1) : row;
+            const unsigned scores = tmem + ((unsigned)(32 * (w & 3)) << 16) + 128 * t, sums = scores + O_COL;
+            const int of = SPLIT && split ? row & (TILE - 1) : row;
+            const auto turn = [&](unsigned now, int i) {             // of the barrier of its scores
+                if constexpr (SPLIT) return (t == 0 ? used_a : used_b) + (split ? i >> 1 : i);
+                else return t == 0 ? now : used_b + i;
+            };
             const float f = S.factor[of];
             const int see_lo = S.lo[of], see_hi = S.hi[of];
             // tokens that every row of the tile sees need no mask
@@ -254,11 +258,11 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             const int all_lo = kv_row_lo<PART>(A, seg.e, A.by_group(min(seg.e.rows, first + TILE) - 1)), all_hi = kv_row_hi(A, seg.e, A.by_group(first));
             float M = NONE;
             f32x2 l = both(0.f);                             // of even and odd tokens
-            for (int i = skip; i < n && ok && busy; i += step) {
+            for (int i = skip; i < n && ok && (t == 0 || two || split); i += step) {
                 const unsigned now = it + i;
                 const int nb = now & 3, tok = tok0 + i * UNIT;
                 const bool plain = tok >= all_lo && tok + UNIT <= all_hi;
-                if (!(ok = !kv_lost<TEST>(P, &S.abort, 76, round) && mbar_wait_warp(&S.abort, &S.sfull[t], (SPLIT ? turn + (split ? i >> 1 : i) : t == 0 ? now : used_b + i) & 1u, P.status, 76))) break;
+                if (!(ok = !kv_lost<TEST>(P, &S.abort, 76, round) && mbar_wait_warp(&S.abort, &S.sfull[t], turn(now, i) & 1u, P.status, 76))) break;
                 tc_fence_after();
 #pragma unroll 1
                 for (int c = 0; c < 2; ++c) {                // 64 tokens at a time
@@ -319,7 +323,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 if (lane == 0) mbar_arrive(&S.pfull[t]);
             }
             // ---- the rows' sums, by way of shared memory ----
-            if (ok && busy && (ok = !kv_lost<TEST>(P, &S.abort, 77, round) && mbar_wait_warp(&S.abort, &S.ofull, round & 1u, P.status, 77))) {
+            if (ok && (t == 0 || two || split) && (ok = !kv_lost<TEST>(P, &S.abort, 77, round) && mbar_wait_warp(&S.abort, &S.ofull, round & 1u, P.status, 77))) {
                 tc_fence_after();
                 unsigned char* to = t == 0 ? S.k[0] : S.v[0];
 #pragma unroll 1
@@ -365,24 +369,34 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                     }
                 }
                 if (piece.starts && piece.ends) {
-                    const bool have = seg.e.row0 + row < seg.e.rows;
-                    int token, head;
-                    if constexpr (PART == KV_WHOLE) kv_finish(y, l8, 0.f, 6.f, total, 0.f);
-                    else if constexpr (PART == KV_PREFIX) {
-                        kv_row_of(A, seg, row, token, head);
-                        if (have) kv_leave_prefix(kv_prefix_row(A, seg, token, head), y, l8, m - KV_TOTAL_LOG<ROWS>, m, total, 0.f);
+                    if constexpr (PART == KV_WHOLE) {
+                        kv_finish(y, l8, 0.f, 6.f, total, 0.f);
+                        if (seg.e.row0 + row < seg.e.rows) {
+                            int token, head;
+                            kv_row_of(A, seg, row, token, head);
+                            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (seg.e.first + token) * A.out_token + head * A.out_head;
+                            if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
+                            if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
+                        }
                     } else {
-                        float top = m - KV_TOTAL_LOG<ROWS>, top_w = m, sum = total, extra = 0.f;
-                        kv_row_of(A, seg, row, token, head);
-                        if (have && seg.e.lo > 0) kv_add_prefix(kv_prefix_row(A, seg, token, head), y, l8, top, top_w, sum, extra);
-                        __syncwarp();
-                        kv_finish(y, l8, top, top_w, sum, extra);
-                    }
-                    if (PART != KV_PREFIX && have) {
-                        kv_row_of(A, seg, row, token, head);
-                        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (seg.e.first + token) * A.out_token + head * A.out_head;
-                        if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
-                        if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
+                        const bool have = seg.e.row0 + row < seg.e.rows;
+                        int token, head;
+                        if constexpr (PART == KV_PREFIX) {
+                            kv_row_of(A, seg, row, token, head);
+                            if (have) kv_leave_prefix(kv_prefix_row(A, seg, token, head), y, l8, m - KV_TOTAL_LOG<ROWS>, m, total, 0.f);
+                        } else {
+                            float top = m - KV_TOTAL_LOG<ROWS>, top_w = m, sum = total, extra = 0.f;
+                            kv_row_of(A, seg, row, token, head);
+                            if (have && seg.e.lo > 0) kv_add_prefix(kv_prefix_row(A, seg, token, head), y, l8, top, top_w, sum, extra);
+                            __syncwarp();
+                            kv_finish(y, l8, top, top_w, sum, extra);
+                        }
+                        if (PART != KV_PREFIX && have) {
+                            kv_row_of(A, seg, row, token, head);
+                            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(A.out) + (seg.e.first + token) * A.out_token + head * A.out_head;
+                            if (8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 8 * l8) = kv_pack_bf16(y);
+                            if (64 + 8 * l8 < A.d) *reinterpret_cast<uint4*>(out + 64 + 8 * l8) = kv_pack_bf16(y + 8);
+                        }
                     }
                 } else {
 #pragma unroll
@@ -397,6 +411,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 }
             }
             if (tid == 0 && piece.starts && !piece.ends) P.joins[blockIdx.x] = kv_join(P.line, seg, places);
+            if (!SPLIT && t == 1 && two) used_b += n;
         } else if (w < 12) {
             // ---- codes: keys and values of a unit, and its per-token numbers ----
             const int me = tid - SOFTMAX;                    // this thread's token of a unit
@@ -444,7 +459,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 const float up = two_to(-ek), up_v = two_to(-ev);
                 const unsigned which = __ballot_sync(0xffffffffu, there);
                 if (lane == 0) S.part[nb][w - 8] = make_float4(two_to(ek), (float)ev, two_to(-ev), __uint_as_float(which));
-                const auto rest_of = [](float x) { return __float2half2_rn(x - __half2float(__float2half_rn(x))); };
+                const auto rest_of = [](float x) { return FINE ? __float2half2_rn(x - __half2float(__float2half_rn(x))) : __half2(); };
                 store_codes<ASYM, FINE>(S.k[b], me, k, there && wrong ? as_h(0x7fff7fffu) : __float2half2_rn(ks * up), rest_of(ks * up), __float2half2_rn(km * up));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -556,6 +571,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
                 umma_commit(&S.drain);
                 drain_copies(&S.drain, 1, 1);
             }
+            if (!SPLIT && two) used_b += n;
             if (lane == 0 && kv_more(P.line, seg, places)) {
                 KvSeg next = seg;
                 kv_next<PART>(A, P.line, next);
@@ -567,8 +583,10 @@ __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant_
             }
         }
         it += n;
-        if (SPLIT) used_a += split ? (n + 1) / 2 : n;
-        used_b += split ? n / 2 : two ? n : 0;
+        if (SPLIT) {
+            used_a += split ? (n + 1) / 2 : n;
+            used_b += split ? n / 2 : 0;
+        }
         more = kv_more(P.line, seg, places);
     }
     tc_fence_before();
