@@ -466,16 +466,18 @@ int gbs_kv_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, const 
 
 /*
  * The same attention for items whose sequences begin alike, as forks of one prompt do: what a group's sequences have in common is read
- * once for all of the group's rows, where that is likely to take less time.  Common are the full pages, from a sequence's first on, that stand in the page tables of all items of the group that have
- * tokens and lie before the tokens of each of them; the call finds them in the tables, so a group of sequences that share nothing is attended over as well,
- * and as slowly as by gbs_kv_attention.  Results differ from that call's by rounding alone.  There is no window.
+ * once for all of the group's rows, where that is likely to take less time.  Common are the full pages, from a sequence's first on, that stand in the page
+ * tables of all items of the group that have tokens and lie before the tokens of each of them; the call finds them in the tables, so a group of
+ * sequences that share nothing is attended over as well.  Results differ from gbs_kv_attention's by rounding alone.  There is no window: what a window leaves of a
+ * common prefix differs from item to item.
  *   groups            device int32 [n_groups + 1], values that do not fall: group g is items groups[g] .. groups[g + 1] - 1, and items of no
  *                     group share nothing.  NULL: all items are one group (n_groups is 1)
  *   n_groups          1 .. GBS_KV_MAX_ITEMS
  *   max_own           about the most tokens that a sequence has behind what its group shares (0: the table's width), as max_len of gbs_kv_attention
- *   max_prefix        about the most tokens that a group shares (0: the table's width), by which it is judged whether sharing gains anything: finding the groups and joining
- *                     what their rows got costs some 20 to 45 microseconds.  Where it does not, the call reads as gbs_kv_attention does
- *   n_tokens          query heads of a KV head * n_tokens: at most 2^28
+ *   max_prefix        about the most tokens that a group shares (0: the table's width, which a table with room to spare makes too much).  By it and the sizes it is
+ *                     judged whether sharing gains anything: finding the groups and joining what their rows got costs some 20 to 45 microseconds, also where they turn
+ *                     out to share little or nothing.  Where it is not likely to gain more, the call reads as gbs_kv_attention does
+ *   n_tokens          query heads of a KV head * n_tokens: at most 2^28, and so query heads of a KV head * n_items * max_tokens, as in gbs_kv_attention
  *   workspace         gbs_kv_shared_attention_workspace bytes, 16-byte aligned, overwritten and used by one call at a time; 528 bytes a token and query head where prefixes are shared.  The same
  *                     number of items, tokens and groups and the same max_tokens and max_prefix as in the call
  * Precision is gbs_kv_attention's, but that with many rows a cached coordinate is rounded once, to 11 bits; rows of a prefix count as many rows (more than 16) where groups have more than 32 rows a KV head on average.
@@ -495,10 +497,13 @@ int gbs_kv_shared_attention(const gbs_plan_t* plan, const gbs_kv_cache_t* cache,
  * below `width`, of the sequences of items that have tokens; nothing else is.  Where two items name one sequence, either's sums may stay,
  * where base is mass itself also with the other's as base.
  *   mass, base        device float [n_seqs][n_kv_heads][width]; base is mass itself or does not overlap it, and is not read (NULL will do) where decay is 0
- *   max_tokens        no item has more tokens; what is beyond it gives no weight.  query heads of a KV head * n_tokens: at most 2^28
+ *   max_tokens        no item has more tokens; what is beyond it gives no weight.  query heads of a KV head * n_tokens: at most 2^28,
+ *                     and so query heads of a KV head * n_items * max_tokens
  *   workspace         device, gbs_kv_attention_mass_workspace bytes for the same sizes, 16-byte aligned; overwritten, needs no preparation, and one call at a
  *                     time may use it.  With up to 32 query rows a KV head and item it has room for their scores, 4 bytes a row and position below the width,
- *                     as long as that is 256 MB at most
+ *                     as long as that is 256 MB at most; with more, 532 bytes a token and query head and at most 64 MB for sums
+ * Weights belong to positions.  The caller clears those of a sequence that begins anew and copies them for a fork: only the items' own tokens start from 0, and tokens that never
+ * were an item's own (those of a prompt before the last ones that a call was made for) start from what stands in base.
  * Scores are right to fp32: query rows are rounded to 24 bits of their largest coordinate, its sign among them, codes enter as they are, sums of products are exact, and
  * what they become is rounded as a float.  With more than 32 query rows a KV head and item it is 23 bits, and the logarithm of a row's sum is rounded as well, so that all
  * of a row's weights may be off by 2^-24 of its largest score's size (in units of log 2).  Scores beyond 2^24 have no units in fp32: weights are finite, and no more.  Value
@@ -522,7 +527,7 @@ int gbs_kv_attention_mass(const gbs_plan_t* plan, const gbs_kv_cache_t* cache, c
  *   keep, recent, first  keep at least 1, recent + first at most keep
  *   mass              device float [n_seqs][n_kv_heads][width], as gbs_kv_attention_mass leaves it
  *   mass_out          the same shape: mass itself, or not overlapping it.  Positions 0 .. of each sequence and KV head receive the mass of the tokens that
- *                     stay (below width); nothing else is written
+ *                     stay (below width); nothing else is written, so that behind them weights of tokens that are gone stand until a call gives new ones their own
  *   kept              device int32 [n_items][n_kv_heads][keep], receives their former positions, which rise; -1 behind the last token of a shorter sequence, and
  *                     in all places of an item that was refused
  *   status_out        device int32 [n_items]; items that are refused (GBS_KV_BAD_INDEX, GBS_KV_DUPLICATE, GBS_KV_NO_PAGES) leave everything as it was

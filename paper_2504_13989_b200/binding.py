@@ -764,7 +764,8 @@ class KVCache:
         """attention (without a window) for items whose sequences begin alike, as forks of one prompt do: the pages that all items of a group begin with are
         read once for the group.  groups: int32 [groups + 1], the first item of each group and the end (None: all items are one group); which pages
         are common is found in the page table.  max_own: about how many tokens the longest sequence has behind what its group shares; max_prefix: about how many the longest prefix has
-        (0: the table's width), by which the call judges whether sharing gains anything; where it does not, it reads as attention does."""
+        (0: the table's width, too much for a table with room to spare), by which the call judges whether sharing gains more than the 20 to 45 us that it costs; where that is not
+        likely, it reads as attention does."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise ValueError("gbs: q must be [tokens, heads, d]")
         self._rows("q", q, q.shape[1])
@@ -802,8 +803,8 @@ class KVCache:
                        causal: bool = True, window: int = 0, scale: float = 0.0, stream=None) -> torch.Tensor:
         """The softmax weight that each cached token gets from query tokens q [tokens, heads, d] (bf16), summed over them and the query heads of a KV
         head, into mass [sequences, n_kv_heads, width] (fp32) at the token's position: mass = decay * base + the sum.  base: None is mass itself, what
-        the calls before added up; the items' own tokens (the last ones of their sequences) start from 0, and with decay 0 all do.  Positions from
-        width on are left out.  Returns mass."""
+        the calls before added up; the items' own tokens (the last ones of their sequences) start from 0, and with decay 0 all do.  Weights belong to positions: clear
+        those of a sequence that begins anew, copy them for a fork.  Positions from width on are left out.  Returns mass."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise ValueError("gbs: q must be [tokens, heads, d]")
         self._rows("q", q, q.shape[1])
@@ -830,7 +831,7 @@ class KVCache:
         """Cut sequences longer than `keep` tokens down to `keep`, for each KV head its own: the first `first`, the last `recent`, and of those between the ones with
         the largest mass [sequences, n_kv_heads, width] (fp32, as attention_mass leaves it).  What stays moves to the front of the sequence, in order, into
         pages of its own (which have to be free), and its mass to the front of `into` (None: of mass).  Returns the items' status (GBS_KV_*) and the
-        former positions of what stays [items, n_kv_heads, keep] (int32, -1 where there is none)."""
+        former positions of what stays [items, n_kv_heads, keep] (int32, -1 where there is none).  Behind what stays, `into` is as it was."""
         for what, v in (("keep", keep), ("recent", recent), ("first", first)):
             _int32(what, v)
         self._weights("mass", mass)
