@@ -565,10 +565,6 @@ int launch(const gbs_plan* p, const MassArgs& P, cudaStream_t stream)
     return tiles_of(P.a) == 1 ? launch<MASS, KEEP, 1>(p, P, stream) : launch<MASS, KEEP, 2>(p, P, stream);
 }
 
-}  // namespace
-
-namespace {
-
 bool many(const gbs_kv_attn& A) { return std::min<int64_t>(A.max_tokens, A.n_tokens) * A.group > GBS_KV_MASS_FEW_ROWS; }
 
 }  // namespace
