@@ -1,6 +1,6 @@
 // Eviction from the paged KV cache (gbs_kv_evict): of a sequence longer than `keep` tokens each KV head keeps its first and last ones and, of those between, the ones with
-// the largest mass.  Pages for what stays are taken first (gbs_kv_pages.cu), so that nothing is written over that is still to be read, whoever shares it; then
-// a block (or a cluster of them) for each item and KV head finds what stays, all SMs move it, and last the tables change.
+// the largest mass.  What stays moves into pages of its own, so that nothing is written over that is still to be read, whoever shares it: a block (or a cluster of them)
+// for each item and KV head finds what stays, and one beside them the pages; then all SMs move it, and last the tables change.
 //
 // What stays is found by digits from the highest down: a histogram of the first 11 bits of the weights, as integers of the same order, tells in which bin the last one
 // that stays lies, then the next 11 bits of that bin's, then 10.  The threshold and how many that are equal to it stay give every token's

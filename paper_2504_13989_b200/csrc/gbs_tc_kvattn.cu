@@ -6,7 +6,7 @@
 // f is the row's factor (its power of two, the softmax scale).  With Ev inside the exponent one running maximum M (of z + Ev) serves both the weights'
 // range in fp16 and the softmax.  Delta (and the middle of an asymmetric row) is rounded to 11 bits, and the number again, 2^-12 of it each,
 // as much as a query coordinate and a weight are.  Exact codes and scales applied to scores and weights instead took three numbers a token from shared
-// memory for every row, and 400 us where this takes 320.
+// memory for every row, and 400 us where this takes 318.
 //
 // Warps 0-3 and 4-7 do the softmax of a tile each, a thread a row; warps 8-11 turn codes into fp16, a thread a token, for both tiles, a
 // unit of 128 tokens ahead; warp 12 issues the MMAs.  While one tile's softmax runs, the other's products do.  Scores and weights of a tile share
@@ -14,7 +14,7 @@
 // The MMAs take 1024 cycles of a tile, ex2 as many; two tiles of a unit take 5600, most of it the chain of a tile (scores, softmax, weights, second
 // product, next scores), which the other tile's overlaps but in part.  Where
 // rows are few (SPLIT; for gbs_kv_shared_attention), a block has one tile, and the two halves of the warps and of tensor memory take its units in turn, each with sums of its own that are added at
-// the end: 2.1 us a unit, then bound by the conversion of codes, instead of 2.5; two tiles take 2.9.  The last 2048 of 8048 tokens, 32 query heads over 8 KV heads: 320 us, 735
+// the end: 2.1 us a unit, then bound by the conversion of codes, instead of 2.5; two tiles take 2.9.  The last 2048 of 8048 tokens, 32 query heads over 8 KV heads: 318 us, 740
 // TFLOP/s.  Blocks of 128 rows, two on an SM, every warp doing all of it in turn: 433 us.  32 tokens at a time in the softmax: 348.
 // 13 warps leave a thread 128 registers, and 74 bytes of one spill.
 // Weights reach 2^-30 of the row's largest, below what a bf16 result shows; l is of fp32 weights, which go under when value
@@ -146,7 +146,7 @@ __device__ __forceinline__ void shrink(unsigned scores, unsigned sums, float kee
 }
 
 // SPLIT: a block has one tile.  Where it is not set, counts, loops and the end of a segment are written as if there were no such thing: with one form for both, the compiler fetched whole calls' numbers
-// from the stack once more (the last 2048 of 8048 tokens 321.8 us instead of 319.8).
+// from the stack once more (0.6 % of the last 2048 of 8048 tokens' time).
 template <bool ASYM, bool TEST, int PART, bool SPLIT, bool FINE>
 __global__ __launch_bounds__(THREADS, 1) void k_tc_kvattn(const __grid_constant__ KvAttnArgs P)
 {
