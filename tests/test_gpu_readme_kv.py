@@ -1,4 +1,4 @@
-"""The KV cache's examples in README.md: they run as they stand, and the one that shares a prefix has sizes by which it is shared."""
+"""The readme's examples of the KV cache: they run as they stand, and the one that shares a prefix has sizes by which it is shared."""
 import ctypes
 import os
 import re
