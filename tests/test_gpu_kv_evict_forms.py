@@ -69,3 +69,15 @@ def test_one_block_of_a_cluster_against_the_model():
             cache = wide(filled(plan, [17000, 600, 40, 16384], 1, 128, seed=2, spare=8), 200000)
             w = weights(cache, 17000, 5, kind)
             check(cache, w, 200, [1, 0, 9, 3, 0, 2], 20, 3, into=weights(cache, 17000, 6), statuses=[0, 0, 1, 0, 5, 0])
+
+
+@pytest.mark.parametrize("items", [255, 256, 257])
+def test_pages_looked_for_beside_and_before(items):
+    """Around the number of items from which the search for pages is a launch of its own; pages run out before the end, and the last item names a sequence again."""
+    with Plan(128, 128, 1, 4, 128, 0.9) as plan:
+        cache = filled(plan, [17 + i % 30 for i in range(items)], 2, 16, seed=1, spare=200)
+        seqs = list(range(items))[::-1]
+        seqs[-1] = seqs[0]
+        w = weights(cache, 50, 3, "few")
+        status = check(cache, w, 20, seqs, 3, 2, into=weights(cache, 50, 4))
+        assert status.eq(3).any() and int(status[-1]) == 5
